@@ -590,6 +590,168 @@ esb_status esb_avgpool_nhwc(const uint32_t* X, int64_t ldx, esb_format f,
                             float alpha_out, esb_format fmt_out, int32_t rounding,
                             float* y_out, uint32_t* codes_out, int64_t ldo, void* stream);
 
+/* ------------------------------------------------- language models
+ *
+ * What a decoder whose matrices are ESB codes needs around them: projection
+ * with a scale for every group of a row's values, products of few rows with
+ * such a matrix, the norm that hands coded rows to them, and the log
+ * probabilities of its answer.  No paper counterpart beyond the projection
+ * (Sec. III-C) and its DDA scale (Sec. III-D, here of each group).
+ *
+ * Rows are row-major with a stride in elements (last dimension contiguous,
+ * any alignment; rows that start on 16-byte boundaries are read and written
+ * by wide accesses).  `*_type` names an element type; sums, statistics and
+ * norms are held in fp32, and a result is rounded once, to its output type. */
+enum { ESB_F32 = 0, ESB_F16 = 1, ESB_BF16 = 2, ESB_CODES = 3 };
+
+/* A matrix of packed codes with a scale for each `group` consecutive values
+ * of a row (0, or one not below the row's length: a scale for the row):
+ * value = scale[row][column / group] * q(code).  A group is a multiple of
+ * 32 values, so it never shares a word with another. */
+typedef struct esb_coded {
+    const uint32_t* codes;     /* [device] rows of ld words */
+    int64_t ld;
+    const float* scales;       /* [device] rows of lds floats, ceil(cols / group) each */
+    int64_t lds;
+    int64_t group;
+    esb_format fmt;
+} esb_coded;
+
+/* Scale of a group: ABSMAX, alpha = fl32(max|x| / C), the smallest scale
+ * that clips nothing (max(x, 0) for unsigned sets); DDA, alpha =
+ * alpha*(b,k) (spread + 1e-7) in fp32 with the spread of the group's own
+ * values (Sec. III-D: the standard deviation about their mean, for unsigned
+ * sets the root mean square). */
+enum { ESB_SCALE_ABSMAX = 0, ESB_SCALE_DDA = 1 };
+
+/* Projection of a matrix with group scales: each group's scale by `rule`,
+ * then the codes of esb_project with that scale.  A group of zeros has scale
+ * 0 and zero codes (ABSMAX).  NaN or an infinity in a group makes its scale
+ * NaN or infinite and its codes zero codes, so the group's values are NaN.
+ *   x       [device] rows x cols values of x_type, row stride ldx
+ *   f       b = 4 or 8
+ *   group   0 or a multiple of 32
+ *   codes   [device] rows x ldc words, every word written as by esb_project
+ *   scales  [device] rows x lds floats
+ *   xq      [device] rows x cols values of xq_type (row stride ldq) or NULL:
+ *           the numbers the codes stand for, alpha q rounded to xq_type --
+ *           the fake-quantised values of a training step, whose gradient
+ *           passes to x unchanged (straight-through, as Algorithm 1)
+ * Errors: INVALID_ARG, UNSUPPORTED (b, group), CUDA. */
+esb_status esb_project_groups(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx,
+                              esb_format f, int32_t rounding, int32_t rule, int64_t group,
+                              uint32_t* codes, int64_t ldc, float* scales, int64_t lds,
+                              void* xq, int32_t xq_type, int64_t ldq, void* stream);
+
+/* Few rows times a matrix of 4-bit codes with group scales (the matrix-
+ * vector products of a decoding step):
+ *   y[m][n] = bias[n] + sum_g s[n][g] sum_{k in g} q(W[n][k]) x[m][k]
+ *   x     [device] M x K values of x_type (ESB_F32, ESB_F16, ESB_BF16), row
+ *         stride ldx; or x_type = ESB_CODES: NULL, and
+ *   xc    [host] the coded rows, b = 8 and 2 <= k <= 7, their group 0 or a
+ *         multiple of w's group
+ *   w     [host] the matrix: N rows of K codes, b = 4, rows 16-byte aligned
+ *         (ld a multiple of 4)
+ *   bias  [device] N floats or NULL
+ *   y     [device] M x N values of y_type, row stride ldy
+ * Any M; the matrix is read once for every few rows, so many rows (a prompt)
+ * belong to esb_gemm.  K < 2^19.
+ * Errors: INVALID_ARG, UNSUPPORTED (formats, groups), RANGE (K), ALIGN
+ * (w), CUDA. */
+esb_status esb_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int32_t x_type, int64_t ldx,
+                             const esb_coded* xc, const esb_coded* w, const float* bias,
+                             void* y, int32_t y_type, int64_t ldy, void* stream);
+
+/* Root-mean-square norm with the residual's addition:
+ *   z = x + residual,  rstd = 1 / sqrt(mean(z^2) + eps),  y = z rstd weight
+ * in fp32 (h is z rounded; y is computed from z itself), and y in 8-bit
+ * codes with scales max|y| / C of each group.  h, y and yq may lie on x or
+ * on the residual where their types and strides are the same. */
+typedef struct esb_norm {
+    const void* x;             /* [device] rows x cols of x_type */
+    int64_t ldx;
+    const void* residual;      /* [device] the same type, or NULL */
+    int64_t ldr;
+    const void* weight;        /* [device] cols values of w_type, or NULL: ones */
+    void* h;                   /* [device] z in x_type, or NULL */
+    int64_t ldh;
+    void* y;                   /* [device] y in y_type, or NULL */
+    int64_t ldy;
+    float* rstd;               /* [device] rows floats, or NULL */
+    uint32_t* codes;           /* [device] rows x ldc words, b = 8, or NULL; every word written */
+    int64_t ldc;
+    float* scales;             /* [device] rows x lds floats (with codes) */
+    int64_t lds;
+    void* yq;                  /* [device] the numbers the codes stand for in y_type, or NULL (with codes) */
+    int64_t ldq;
+    int64_t group;             /* 0 (a scale for the row) or a multiple of 32 */
+    esb_format fmt;
+    int32_t rounding;
+    int32_t x_type, w_type, y_type;
+    float eps;                 /* >= 0, finite */
+} esb_norm;
+/* Errors: INVALID_ARG, UNSUPPORTED (fmt, group), CUDA. */
+esb_status esb_rmsnorm(int64_t rows, int64_t cols, const esb_norm* a, void* stream);
+
+/* Its gradient, from h and rstd as the forward pass wrote them: with
+ * n = h rstd and d = dy weight,
+ *   dx = rstd (d - n mean(d n)) + dh   (of x and of the residual alike)
+ *   dweight = sum over the rows of dy n
+ * dy is the gradient of y, or of the values that the codes stand for (it
+ * passes the projection unchanged), dh that of h by way of the residual
+ * stream.  Every sum has a fixed order. */
+typedef struct esb_norm_grad {
+    const void* dy;            /* [device] rows x cols of g_type */
+    int64_t ldg;
+    const void* h;             /* [device] rows x cols of x_type */
+    int64_t ldh;
+    const void* dh;            /* [device] x_type, or NULL */
+    int64_t lddh;
+    const void* weight;        /* [device] cols of w_type, or NULL: ones */
+    const float* rstd;         /* [device] rows floats */
+    void* dx;                  /* [device] rows x cols of x_type; may lie on dy, h or dh of the same type and stride */
+    int64_t lddx;
+    float* dweight;            /* [device] cols floats, or NULL */
+    int32_t x_type, w_type, g_type;
+} esb_norm_grad;
+/*   workspace  [device] >= esb_rmsnorm_backward_workspace_bytes(rows, cols)
+ *              bytes, 16-byte aligned (with dweight; else it may be NULL)
+ * Errors: INVALID_ARG, ALIGN, CUDA. */
+size_t esb_rmsnorm_backward_workspace_bytes(int64_t rows, int64_t cols);
+esb_status esb_rmsnorm_backward(int64_t rows, int64_t cols, const esb_norm_grad* a, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* Most alternatives of esb_logprobs. */
+#define ESB_MAX_TOP 32
+
+/* Log probabilities of rows of logits x: with lse = log sum exp(x),
+ *   logp = x[id] - lse,  entropy = -sum p log p,  p = exp(x - lse)
+ * and the `top` largest logits, the lower place first among equals.
+ * A logit of -inf is a masked token (p = 0).  A row with no other logit has
+ * lse = logp = -inf and entropy 0; NaN or +inf in a row makes its numbers NaN.
+ * An id outside 0 .. cols - 1 (a negative label of a position without one)
+ * has logp 0.
+ *   ids       [device] rows int64, or NULL with logp NULL
+ *   logp, entropy, lse [device] rows floats, each may be NULL
+ *   top_logp, top_ids  [device] rows x top; where a row has fewer logits
+ *             above -inf (NaN is not one), the rest is -inf and -1
+ * cols < 2^31, 0 <= top <= ESB_MAX_TOP.
+ * Errors: INVALID_ARG, RANGE (cols, top), CUDA. */
+esb_status esb_logprobs(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids,
+                        int32_t top, float* logp, float* entropy, float* lse, float* top_logp, int64_t* top_ids,
+                        void* stream);
+
+/* Its gradient with respect to the logits:
+ *   dx[j] = dlogp ([j == id] - p_j) - dentropy p_j (log p_j + entropy)
+ * 0 for a masked logit and in a row without any other.
+ *   lse, entropy  [device] of the forward pass (entropy may be NULL without dentropy)
+ *   dlogp, dentropy [device] rows floats, each may be NULL (zeros); ids as there
+ *   dx  [device] rows x cols of x_type; may lie on x with the same stride
+ * Errors: INVALID_ARG, RANGE (cols), CUDA. */
+esb_status esb_logprobs_backward(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx,
+                                 const int64_t* ids, const float* lse, const float* entropy, const float* dlogp,
+                                 const float* dentropy, void* dx, int64_t lddx, void* stream);
+
 /* ----------------------------------------------------- peak measurement */
 
 /* Microbenchmarks of the tensor-pipe rates the contraction's roofline is

@@ -104,6 +104,23 @@ cudaError_t launch_dn_grad(const float* g, const float* x, int64_t n, const doub
                            cudaStream_t st);
 cudaError_t launch_ema(const double* batch, double* running, double gamma, cudaStream_t st);
 
+// Language-model operators: projection with group scales (esb_groups.cu),
+// few rows times a group-scaled matrix (esb_matvec.cu), RMS norm
+// (esb_norm.cu), log probabilities (esb_logprobs.cu).
+cudaError_t launch_project_groups(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ldx, const esb_format& f,
+                                  int rounding, int rule, int64_t group, double alpha_star, uint32_t* codes, int64_t ldc,
+                                  float* scales, int64_t lds, void* xq, int xq_type, int64_t ldq, cudaStream_t st);
+cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int x_type, int64_t ldx, const esb_coded* xc,
+                                 const esb_coded& w, const float* bias, void* y, int y_type, int64_t ldy, cudaStream_t st);
+cudaError_t launch_rmsnorm(int64_t rows, int64_t cols, const esb_norm& n, cudaStream_t st);
+size_t rmsnorm_grad_workspace_bytes(int64_t rows, int64_t cols);
+cudaError_t launch_rmsnorm_grad(int64_t rows, int64_t cols, const esb_norm_grad& n, void* workspace, cudaStream_t st);
+cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids, int top,
+                            float* logp, float* entropy, float* lse, float* top_logp, int64_t* top_ids, cudaStream_t st);
+cudaError_t launch_logprobs_grad(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids,
+                                 const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dx,
+                                 int64_t lddx, cudaStream_t st);
+
 // Tensor-pipe peak microbenchmarks (esb_peak.cu): kind 0 tcgen05 f8f6f4,
 // kind 1 mma.sync s8; *flops receives the operations of the launch.
 cudaError_t launch_peak(int kind, int64_t iters, int64_t* flops, cudaStream_t st);

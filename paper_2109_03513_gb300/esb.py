@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -58,6 +58,32 @@ class esb_epilogue(ctypes.Structure):
 
 class esb_conv_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n", "h", "w", "c", "cout", "r", "s", "stride", "pad", "groups")]
+
+
+class esb_coded(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scales", ctypes.c_void_p),
+                ("lds", ctypes.c_int64), ("group", ctypes.c_int64), ("fmt", esb_format)]
+
+
+class esb_norm(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64),
+        ("weight", ctypes.c_void_p), ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64),
+        ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("rstd", ctypes.c_void_p),
+        ("codes", ctypes.c_void_p), ("ldc", ctypes.c_int64), ("scales", ctypes.c_void_p), ("lds", ctypes.c_int64),
+        ("yq", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("group", ctypes.c_int64), ("fmt", esb_format),
+        ("rounding", ctypes.c_int32), ("x_type", ctypes.c_int32), ("w_type", ctypes.c_int32),
+        ("y_type", ctypes.c_int32), ("eps", ctypes.c_float),
+    ]
+
+
+class esb_norm_grad(ctypes.Structure):
+    _fields_ = [
+        ("dy", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("h", ctypes.c_void_p), ("ldh", ctypes.c_int64),
+        ("dh", ctypes.c_void_p), ("lddh", ctypes.c_int64), ("weight", ctypes.c_void_p), ("rstd", ctypes.c_void_p),
+        ("dx", ctypes.c_void_p), ("lddx", ctypes.c_int64), ("dweight", ctypes.c_void_p),
+        ("x_type", ctypes.c_int32), ("w_type", ctypes.c_int32), ("g_type", ctypes.c_int32),
+    ]
 
 
 @dataclass(frozen=True)
@@ -114,6 +140,14 @@ SIGNATURES = {
     "esb_maxpool_nhwc": (_I32, [_P, _I64, esb_format] + [_I32] * 7 + [_P, _I64, _P]),
     "esb_avgpool_nhwc": (_I32, [_P, _I64, esb_format, _I32, _I32, _I32, _F32, _F32, esb_format, _I32, _P, _P, _I64,
                                 _P]),
+    "esb_project_groups": (_I32, [_P, _I32, _I64, _I64, _I64, esb_format, _I32, _I32, _I64, _P, _I64, _P, _I64, _P,
+                                  _I32, _I64, _P]),
+    "esb_matvec_groups": (_I32, [_I64, _I64, _I64, _P, _I32, _I64, _P, _P, _P, _P, _I32, _I64, _P]),
+    "esb_rmsnorm": (_I32, [_I64, _I64, _P, _P]),
+    "esb_rmsnorm_backward_workspace_bytes": (_SZ, [_I64, _I64]),
+    "esb_rmsnorm_backward": (_I32, [_I64, _I64, _P, _P, _SZ, _P]),
+    "esb_logprobs": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I32, _P, _P, _P, _P, _P, _P]),
+    "esb_logprobs_backward": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "esb_get_status": (_I32, [_P, _P]),
     "esb_peak_launch": (_I32, [_I32, _I64, _P, _P]),
 }
@@ -573,6 +607,295 @@ def esb_avgpool_nhwc(X: torch.Tensor, f: Fmt, n: int, hw: int, c: int, scale: fl
     _check(lib().esb_avgpool_nhwc(_ptr(X), ldx, f.c(), n, hw, c, scale, alpha_out, fmt_out.c(), rounding, _ptr(y),
                                   _ptr(codes), ldo, _stream(stream)), "esb_avgpool_nhwc")
     return y, codes
+
+
+# -------------------------------------------------------- language models
+
+ESB_F32, ESB_F16, ESB_BF16, ESB_CODES = 0, 1, 2, 3
+ESB_SCALE_ABSMAX, ESB_SCALE_DDA = 0, 1
+ESB_MAX_TOP = 32
+_TYPES = {torch.float32: ESB_F32, torch.float16: ESB_F16, torch.bfloat16: ESB_BF16}
+
+
+class Coded(NamedTuple):
+    """A matrix of ESB codes with group scales: codes (rows, ld) int32, scales
+    (rows, groups) float32, `cols` values a row, `group` values a scale (0:
+    one scale for the row)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    fmt: Fmt
+    cols: int
+    group: int = 0
+
+    def c(self, name: str) -> esb_coded:
+        _codes(self.codes, f"{name}.codes", torch.int32)
+        _codes(self.scales, f"{name}.scales", torch.float32)
+        return esb_coded(self.codes.data_ptr(), _row_ld(self.codes), self.scales.data_ptr(), _row_ld(self.scales),
+                         self.group, self.fmt.c())
+
+
+def _codes(t: torch.Tensor, name: str, dtype) -> None:
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.stride(1) != 1:
+        raise ValueError(f"{name} must be a 2-D CUDA {dtype} tensor with contiguous rows")
+
+
+def _typed(t: torch.Tensor, name: str) -> int:
+    """The element type of a tensor of rows (any row stride, rows contiguous)."""
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be 2-D with contiguous rows")
+    return ty
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride in elements (a single row has none)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _like(t: torch.Tensor, name: str, shape, dtype) -> None:
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"{name} must be {tuple(shape)} {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() == 2 and t.stride(1) != 1 and t.shape[1] > 1 or t.dim() == 1 and t.stride(0) != 1 and t.shape[0] > 1:
+        raise ValueError(f"{name} must have contiguous rows")
+
+
+def _groups(cols: int, group: int) -> int:
+    return -(-cols // group) if 0 < group < cols else 1
+
+
+def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ESB_SCALE_ABSMAX,
+                       rounding: int = ESB_ROUND_HALF_AWAY, codes: Optional[torch.Tensor] = None,
+                       scales: Optional[torch.Tensor] = None, xq: Optional[torch.Tensor] = None,
+                       want_xq: bool = False, stream=None) -> tuple[Coded, Optional[torch.Tensor]]:
+    """Project a (rows, cols) matrix with a scale for every `group` values of a
+    row -> (Coded, the numbers the codes stand for (rows, cols) | None)."""
+    ty = _typed(x, "x")
+    rows, cols = x.shape
+    if codes is None:
+        codes = torch.empty((rows, esb_row_words(cols, f.b)), dtype=torch.int32, device=x.device)
+    else:
+        _codes(codes, "codes", torch.int32)
+    if scales is None:
+        scales = torch.empty((rows, _groups(cols, group)), dtype=torch.float32, device=x.device)
+    else:
+        _like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
+    if codes.shape[0] != rows:
+        raise ValueError("codes must have a row for each row of x")
+    if xq is None and want_xq:
+        xq = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    qt, ldq = (0, 0) if xq is None else (_typed(xq, "xq"), _ld(xq))
+    if xq is not None and xq.shape != x.shape:
+        raise ValueError("xq must have the shape of x")
+    _check(lib().esb_project_groups(_ptr(x), ty, rows, cols, _ld(x), f.c(), rounding, rule, group, _ptr(codes),
+                                    _row_ld(codes), _ptr(scales), _row_ld(scales), _ptr(xq), qt, ldq, _stream(stream)),
+           "esb_project_groups")
+    return Coded(codes, scales, f, cols, group), xq
+
+
+def _row_ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def esb_matvec_groups(x, w: Coded, bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                      y_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
+    """Few rows times a group-scaled 4-bit matrix: y (m, n) = x (m, k) @ w (n, k)^T + bias.
+    x: a tensor, or Coded rows with b = 8 (y is then bfloat16 unless y or y_dtype says otherwise)."""
+    wc = w.c("w")
+    n, k = w.codes.shape[0], w.cols
+    coded = isinstance(x, Coded)
+    m, xk = (x.codes.shape[0], x.cols) if coded else x.shape
+    if xk != k:
+        raise ValueError("x and w must have the same number of columns")
+    if w.scales.shape != (n, _groups(k, w.group)):
+        raise ValueError("w.scales must hold a scale for every group")
+    if coded:
+        xc, xt = x.c("x"), ESB_CODES
+        if x.scales.shape != (m, _groups(k, x.group)):
+            raise ValueError("x.scales must hold a scale for every group")
+        xp, ldx, xcp = None, 0, ctypes.byref(xc)
+    else:
+        xt = _typed(x, "x")
+        xp, ldx, xcp = x.data_ptr(), _ld(x), None
+    if y is None:
+        y = torch.empty((m, n), dtype=y_dtype or (torch.bfloat16 if coded else x.dtype), device=w.codes.device)
+    yt = _typed(y, "y")
+    if tuple(y.shape) != (m, n):
+        raise ValueError("y must be (rows of x, rows of w)")
+    if bias is not None:
+        _like(bias, "bias", (n,), torch.float32)
+    _check(lib().esb_matvec_groups(m, n, k, xp, xt, ldx, xcp, ctypes.byref(wc), _ptr(bias), _ptr(y), yt, _ld(y),
+                                   _stream(stream)), "esb_matvec_groups")
+    return y
+
+
+class NormOut(NamedTuple):
+    """What esb_rmsnorm wrote: the sum h, the norm y, 1 / rms of each row, the
+    coded norm and the numbers its codes stand for (None where not wanted)."""
+    h: Optional[torch.Tensor]
+    y: Optional[torch.Tensor]
+    rstd: Optional[torch.Tensor]
+    coded: Optional[Coded]
+    yq: Optional[torch.Tensor]
+
+
+def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6,
+                residual: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None,
+                y: Optional[torch.Tensor] = None, want_y: Optional[bool] = None,
+                rstd: Optional[torch.Tensor] = None, want_rstd: bool = False, fmt: Optional[Fmt] = None,
+                group: int = 0, rounding: int = ESB_ROUND_HALF_AWAY, codes: Optional[torch.Tensor] = None,
+                scales: Optional[torch.Tensor] = None, yq: Optional[torch.Tensor] = None,
+                y_dtype: Optional[torch.dtype] = None, stream=None) -> NormOut:
+    """RMS norm of x + residual -> NormOut.  h is written when there is a
+    residual or a tensor for it; y unless `fmt` asks for codes (or want_y says);
+    yq when there is a tensor for it."""
+    ty = _typed(x, "x")
+    rows, cols = x.shape
+    a = esb_norm()
+    a.x, a.ldx, a.x_type, a.eps = x.data_ptr(), _ld(x), ty, eps
+    if residual is not None:
+        _like(residual, "residual", x.shape, x.dtype)
+        a.residual, a.ldr = residual.data_ptr(), _ld(residual)
+    if weight is not None:
+        if weight.dtype not in _TYPES:
+            raise ValueError("weight must be float32, float16 or bfloat16")
+        _like(weight, "weight", (cols,), weight.dtype)
+        a.weight, a.w_type = weight.data_ptr(), _TYPES[weight.dtype]
+    if h is None and residual is not None:
+        h = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    if h is not None:
+        _like(h, "h", x.shape, x.dtype)
+        a.h, a.ldh = h.data_ptr(), _ld(h)
+    if y is None and (want_y if want_y is not None else fmt is None):
+        y = torch.empty((rows, cols), dtype=y_dtype or x.dtype, device=x.device)
+    if y is not None:
+        a.y_type = _typed(y, "y")
+        _like(y, "y", x.shape, y.dtype)
+        a.y, a.ldy = y.data_ptr(), _ld(y)
+    if yq is not None:
+        if y is not None and y.dtype != yq.dtype:
+            raise ValueError("y and yq must have one type")
+        a.y_type = _typed(yq, "yq")
+        _like(yq, "yq", x.shape, yq.dtype)
+        a.yq, a.ldq = yq.data_ptr(), _ld(yq)
+    if rstd is None and want_rstd:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if rstd is not None:
+        _like(rstd, "rstd", (rows,), torch.float32)
+        a.rstd = rstd.data_ptr()
+    coded = None
+    if fmt is not None:
+        if codes is None:
+            codes = torch.empty((rows, esb_row_words(cols, fmt.b)), dtype=torch.int32, device=x.device)
+        else:
+            _codes(codes, "codes", torch.int32)
+        if scales is None:
+            scales = torch.empty((rows, _groups(cols, group)), dtype=torch.float32, device=x.device)
+        else:
+            _like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
+        if codes.shape[0] != rows:
+            raise ValueError("codes must have a row for each row of x")
+        a.codes, a.ldc, a.scales, a.lds = codes.data_ptr(), _row_ld(codes), scales.data_ptr(), _row_ld(scales)
+        a.group, a.fmt, a.rounding = group, fmt.c(), rounding
+        coded = Coded(codes, scales, fmt, cols, group)
+    _check(lib().esb_rmsnorm(rows, cols, ctypes.byref(a), _stream(stream)), "esb_rmsnorm")
+    return NormOut(h, y, rstd, coded, yq)
+
+
+def esb_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor,
+                         dh: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                         dweight: Optional[torch.Tensor] = None, want_dweight: Optional[bool] = None,
+                         workspace: Optional[torch.Tensor] = None,
+                         stream=None) -> tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Gradient of esb_rmsnorm -> (dx, of x and of the residual alike; dweight
+    fp32 | None).  dweight is computed when there is a weight, unless want_dweight says."""
+    rows, cols = h.shape
+    a = esb_norm_grad()
+    a.x_type, a.g_type = _typed(h, "h"), _typed(dy, "dy")
+    _like(dy, "dy", h.shape, dy.dtype)
+    _like(rstd, "rstd", (rows,), torch.float32)
+    a.dy, a.ldg, a.h, a.ldh, a.rstd = dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h), rstd.data_ptr()
+    if dh is not None:
+        _like(dh, "dh", h.shape, h.dtype)
+        a.dh, a.lddh = dh.data_ptr(), _ld(dh)
+    if weight is not None:
+        if weight.dtype not in _TYPES:
+            raise ValueError("weight must be float32, float16 or bfloat16")
+        _like(weight, "weight", (cols,), weight.dtype)
+        a.weight, a.w_type = weight.data_ptr(), _TYPES[weight.dtype]
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
+    _like(dx, "dx", h.shape, h.dtype)
+    a.dx, a.lddx = dx.data_ptr(), _ld(dx)
+    nb = 0
+    if dweight is None and (want_dweight if want_dweight is not None else weight is not None):
+        dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
+    if dweight is not None:
+        _like(dweight, "dweight", (cols,), torch.float32)
+        a.dweight = dweight.data_ptr()
+        nb = int(lib().esb_rmsnorm_backward_workspace_bytes(rows, cols))
+        if workspace is None and nb:
+            workspace = torch.empty(nb, dtype=torch.uint8, device=h.device)
+    _check(lib().esb_rmsnorm_backward(rows, cols, ctypes.byref(a), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                      _stream(stream)), "esb_rmsnorm_backward")
+    return dx, dweight
+
+
+class LogProbs(NamedTuple):
+    """What esb_logprobs wrote: (rows,) fp32 each, and (rows, top) alternatives (None with top = 0)."""
+    logp: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_logp: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+
+
+def esb_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, top: int = 0, stream=None) -> LogProbs:
+    """Log probability of ids (rows,) int64 under each row of logits, the
+    entropy, log sum exp, and the `top` most likely tokens -> LogProbs."""
+    ty = _typed(logits, "logits")
+    rows, cols = logits.shape
+    if ids is not None:
+        _like(ids, "ids", (rows,), torch.int64)
+    if not 0 <= top <= ESB_MAX_TOP:
+        raise ValueError(f"top must be 0..{ESB_MAX_TOP}")
+    dev = logits.device
+    st = torch.empty((3, rows), dtype=torch.float32, device=dev)      # one allocation for the rows' numbers
+    logp, ent, lse = st.unbind(0)
+    tl = torch.empty((rows, top), dtype=torch.float32, device=dev) if top else None
+    ti = torch.empty((rows, top), dtype=torch.int64, device=dev) if top else None
+    if ids is None:
+        logp = None
+    _check(lib().esb_logprobs(_ptr(logits), ty, rows, cols, _ld(logits), _ptr(ids), top, _ptr(logp), _ptr(ent),
+                              _ptr(lse), _ptr(tl), _ptr(ti), _stream(stream)), "esb_logprobs")
+    return LogProbs(logp, ent, lse, tl, ti)
+
+
+def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse: torch.Tensor,
+                          entropy: Optional[torch.Tensor] = None, dlogp: Optional[torch.Tensor] = None,
+                          dentropy: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
+                          stream=None) -> torch.Tensor:
+    """Gradient of logp and entropy (dlogp, dentropy: (rows,) fp32) with respect to the logits."""
+    ty = _typed(logits, "logits")
+    rows, cols = logits.shape
+    for t, name in ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy")):
+        if t is not None:
+            _like(t, name, (rows,), torch.float32)
+    if ids is not None:
+        _like(ids, "ids", (rows,), torch.int64)
+    if dlogits is None:
+        dlogits = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
+    _like(dlogits, "dlogits", logits.shape, logits.dtype)
+    _check(lib().esb_logprobs_backward(_ptr(logits), ty, rows, cols, _ld(logits), _ptr(ids), _ptr(lse), _ptr(entropy),
+                                       _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), _ld(dlogits), _stream(stream)),
+           "esb_logprobs_backward")
+    return dlogits
 
 
 ESB_PEAK_TCGEN05_F8F6F4 = 0
