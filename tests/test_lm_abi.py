@@ -56,7 +56,7 @@ X8 = dict(ld=16, lds=1, group=0, fmt=F8)
     (INV, dict(K=0)), (INV, dict(ldx=63)), (INV, dict(ldy=7)), (INV, dict(x=None)), (INV, dict(y=None)),
     (INV, dict(w=coded(codes=None))), (INV, dict(w=coded(scales=None))), (INV, dict(w=coded(ld=4))), (INV, dict(w=coded(lds=1))),
     (UNS, dict(w=coded(fmt=F8))), (UNS, dict(w=coded(fmt=esb.esb_format(4, 4, 1)))), (UNS, dict(w=coded(group=48))),
-    (UNS, dict(w=coded(group=-32))), (RNG, dict(K=1 << 19, ldx=1 << 19, w=coded(ld=1 << 16, lds=1 << 14))),
+    (UNS, dict(w=coded(group=-32))), (RNG, dict(K=1 << 18, ldx=1 << 18, w=coded(ld=1 << 15, lds=1 << 13))),
     (ALN, dict(w=coded(codes=ctypes.c_void_p(264)))), (ALN, dict(w=coded(ld=9))), (ALN, dict(w=coded(scales=ODD))), (ALN, dict(x=ODD)),
     (ALN, dict(y=ODD)), (ALN, dict(bias=ODD)),
     (UNS, dict(xt=3, xc=coded(ld=16, lds=1, group=0, fmt=F4))), (UNS, dict(xt=3, xc=coded(ld=16, lds=1, group=0, fmt=esb.Fmt(8, 1).c()))),
