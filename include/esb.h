@@ -655,9 +655,9 @@ esb_status esb_project_groups(const void* x, int32_t x_type, int64_t rows, int64
  *   bias  [device] N floats or NULL
  *   y     [device] M x N values of y_type, row stride ldy
  * Any M; the matrix is read once for every few rows, so many rows (a prompt)
- * belong to esb_gemm.  K < 2^18.
- * Errors: INVALID_ARG, UNSUPPORTED (formats, groups), RANGE (K), ALIGN
- * (w), CUDA. */
+ * belong to esb_gemm.  K < 2^18, N < 2^31.
+ * Errors: INVALID_ARG, UNSUPPORTED (formats, groups), RANGE (K, N),
+ * ALIGN, CUDA. */
 esb_status esb_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int32_t x_type, int64_t ldx,
                              const esb_coded* xc, const esb_coded* w, const float* bias,
                              void* y, int32_t y_type, int64_t ldy, void* stream);

@@ -25,6 +25,7 @@
 // own: lane t of four holds codes 32 t .. 32 t + 31 of the step, so with x
 // zeroed in the other lanes a column sums one group (columns that a few rows
 // leave unused anyway).
+#include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -35,10 +36,13 @@ namespace esb {
 
 namespace {
 
-constexpr int kMvWarps = 8;
-constexpr int kMvThreads = kMvWarps * 32;
-constexpr int kSlice = 512;         // codes of a row in flight per warp: 16 bytes a lane, 4 steps
 constexpr int kRedLd = 20;          // floats between columns of a warp's 16 sums
+constexpr int kSlice = 512;         // codes of a row that a warp has in flight: 4 steps of 128, 16 bytes a lane and row
+
+// fp16 high bytes of the elements by the code's low 3 bits; 2^16 and 2^4.
+struct MvTable {
+    uint32_t lo, hi, by16, by4;
+};
 
 struct MvArgs {
     int64_t M, N, K;
@@ -50,12 +54,16 @@ struct MvArgs {
     const float* bias;
     void* y;
     int64_t ldy;
-    uint32_t tab_lo, tab_hi;        // fp16 high bytes of elements 0..7 of the code's low 3 bits
+    MvTable tab;
     int x_type, y_type, xvec;
+    uint32_t gmagic;                // 2^32 / (group / 32) rounded up, 0 for groups of 32
     int mt, planes;                 // rows of x in a block, planes of each
-    int kc;                         // codes of a row in a block (a multiple of kSlice)
+    int kc;                         // codes of a row in a block (a multiple of 512)
+    int zrow;                       // whether some lanes read zeros in place of x
+    int64_t wfull;                  // codes of a row that whole 16-byte words hold
     int wk;                         // warps along a row (the others take other tiles)
     int split;                      // blocks along a row (a cluster)
+    int hold;                       // tiles whose sums wait for one barrier
 };
 
 __device__ __forceinline__ uint4 ldg_stream(const uint32_t* p)
@@ -64,41 +72,64 @@ __device__ __forceinline__ uint4 ldg_stream(const uint32_t* p)
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// The warps that share a tile wait for one another.
+__device__ __forceinline__ void group_barrier(int id, int threads) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
+// c = a b, or c += a b.
+template <bool ADD>
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if constexpr (ADD)
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile(
+            "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
 // Eight codes as four fp16 pairs {0,2} {1,3} {4,6} {5,7}: the order in which
-// a word's sign bits lie at the top of alternate bytes.
-__device__ __forceinline__ void decode8(uint32_t w, uint32_t lo, uint32_t hi, uint32_t (&p)[4])
+// a word's sign bits lie at the top of alternate bytes.  The two shifts are
+// products with powers of two that the compiler does not know: the ALU pipe,
+// which the other eleven instructions take, bounds the kernel, and the
+// multiply-add pipe is free.
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
+    return r;
+}
+__device__ __forceinline__ void decode8(uint32_t w, const MvTable& tb, uint32_t (&p)[4])
 {
     const uint32_t sel = w & 0x77777777u;
-    const uint32_t m03 = __byte_perm(lo, hi, sel), m47 = __byte_perm(lo, hi, sel >> 16);
-    const uint32_t odd = __byte_perm(m03, m47, 0x7531) | (w & 0x80808080u);
-    const uint32_t even = __byte_perm(m03, m47, 0x6420) | ((w << 4) & 0x80808080u);
-    p[0] = __byte_perm(even, 0u, 0x1404);
-    p[1] = __byte_perm(odd, 0u, 0x1404);
-    p[2] = __byte_perm(even, 0u, 0x3424);
-    p[3] = __byte_perm(odd, 0u, 0x3424);
+    const uint32_t m03 = prmt(tb.lo, tb.hi, sel), m47 = prmt(tb.lo, tb.hi, __umulhi(sel, tb.by16));
+    const uint32_t odd = prmt(m03, m47, 0x7531u) | (w & 0x80808080u);
+    const uint32_t even = prmt(m03, m47, 0x6420u) | ((w * tb.by4) & 0x80808080u);
+    p[0] = prmt(even, 0u, 0x1404u);
+    p[1] = prmt(odd, 0u, 0x1404u);
+    p[2] = prmt(even, 0u, 0x3424u);
+    p[3] = prmt(odd, 0u, 0x3424u);
 }
 
 __device__ __forceinline__ uint32_t half2_of(float a, float b) { return pack2<__half>(a, b); }
 
-// Shared memory: 256 zero bytes (x of columns that are not there), then for
-// every plane of every row kc halves -- 8 at a time in the pair order above,
-// the four lanes' eights of a word next to each other -- and 64 bytes of
-// padding (lanes of neighbouring columns read other banks), the columns'
-// scales of every step, and the warps' sums, twice.
+// Shared memory: for every plane of every row kc halves -- 8 at a time in the
+// pair order above, the four lanes' eights of a word next to each other --
+// and 64 bytes of padding (lanes of neighbouring columns read other banks), a
+// row of zeros where some lanes have no x, the columns' scales of every step,
+// and the warps' sums, twice.
 __host__ __device__ inline int xs_stride(int kc) { return kc * 2 + 64; }
-__host__ inline size_t mv_smem(int rows, int kc, int nt)
-{
-    return 256 + (size_t)rows * xs_stride(kc) + (size_t)(kc / 128) * 8 * nt * 4 + 2u * kMvWarps * 8 * nt * kRedLd * 4;
-}
+__host__ inline size_t mv_x_bytes(int rows, int kc, int nt) { return (size_t)rows * xs_stride(kc) + (size_t)(kc / 128) * 8 * nt * 4; }
+__host__ inline size_t mv_sums(int cols, int warps) { return (size_t)2 * warps * cols * kRedLd * 4; }
 
 __device__ __forceinline__ void cluster_barrier()
 {
@@ -113,269 +144,328 @@ __device__ __forceinline__ float ld_cluster(const float* p, int rank)
     return v;
 }
 
-// Rows m0 .. m0 + mt - 1 of x, codes k0 .. k0 + kc - 1, into shared memory.
-template <int NT, int R>
-__device__ __forceinline__ void stage_x(const MvArgs& a, int64_t m0, int mt, int64_t k0, unsigned char* xs, float* fx, const uint16_t* xtab)
+// Eight values of x at block i of the 16 of a step: scaled, split into
+// planes, in pair order.  All 32 lanes take part.
+template <int NT, int R, int TYPE>
+__device__ __forceinline__ void put_x8(const MvArgs& a, float (&v)[8], int i, unsigned char* at, float* f)
 {
     constexpr int LANES = 16 / R;                       // lanes that share a scale
-    const int stride = xs_stride(a.kc), blocks = a.kc / 8;
-    for (int m = 0; m < mt; m++) {
-        for (int b = threadIdx.x; b < blocks; b += kMvThreads) {   // blocks is a multiple of 64: warps stay whole
-            const int64_t k = k0 + (int64_t)b * 8;
-            const int64_t n = a.K - k;
-            const int i = b & 15, step = b >> 4, r = i / LANES;
+    float back = 1.0f;
+    if constexpr (TYPE != ESB_F16) {
+        uint32_t mx = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const uint32_t u = __float_as_uint(v[j]) & 0x7fffffffu;
+            mx = max(mx, u < 0x7f800000u ? u : 0u);
+        }
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const int e = max((int)(mx >> 23), 15);         // exponent field; 2^(14 - (e - 127)) <= 2^126
+        const float s = __uint_as_float((uint32_t)(268 - e) << 23);
+        back = __uint_as_float((uint32_t)(e - 14) << 23);
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] *= s;
+    }
+    if constexpr (TYPE == ESB_F32) {
+        float lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const float hi = __half2float(__float2half_rn(v[j]));
+            lo[j] = fabsf(hi) < __int_as_float(0x7f800000) ? (v[j] - hi) * 2048.0f : 0.0f;
+            v[j] = hi;
+        }
+        *reinterpret_cast<uint4*>(at + xs_stride(a.kc)) = make_uint4(half2_of(lo[0], lo[2]), half2_of(lo[1], lo[3]),
+                                                                     half2_of(lo[4], lo[6]), half2_of(lo[5], lo[7]));
+        if (i % LANES == 0) f[R] = back * (1.0f / 2048.0f);
+    }
+    *reinterpret_cast<uint4*>(at) = make_uint4(half2_of(v[0], v[2]), half2_of(v[1], v[3]), half2_of(v[4], v[6]), half2_of(v[5], v[7]));
+    if (i % LANES == 0) *f = back;
+}
+
+// Rows m0 .. m0 + mt - 1 of x, codes k0 .. k0 + kc - 1, into shared memory: a
+// warp takes 256 values of a row at a time, several such parts in flight.
+template <int NT, int R, int WARPS, int TYPE>
+__device__ __forceinline__ void stage_x(const MvArgs& a, int64_t m0, int mt, int64_t k0, unsigned char* xs, float* fx, const uint16_t* xtab)
+{
+    constexpr int U = TYPE == ESB_F32 ? 4 : 8, WORDS = TYPE == ESB_F32 ? 8 : (TYPE == ESB_CODES ? 2 : 4);
+    const int stride = xs_stride(a.kc), parts = a.kc / 256, total = mt * parts;
+    const int lane = threadIdx.x & 31, i = lane & 15;
+    for (int q0 = threadIdx.x >> 5; q0 < total; q0 += U * WARPS) {
+        uint32_t raw[U][WORDS];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int q = q0 + u * WARPS;
+            if (q >= total) break;
+            const int m = q / parts;
+            const int64_t k = k0 + (q - m * parts) * 256 + lane * 8, n = a.K - k;
+            if constexpr (TYPE == ESB_CODES) {
+                const uint32_t* xw = a.xc.codes + (m0 + m) * a.xc.ld + k / 4;
+                raw[u][0] = n > 0 ? __ldg(xw) : 0u;
+                raw[u][1] = n > 4 ? __ldg(xw + 1) : 0u;
+            } else {
+                using T = Elem<TYPE>;
+                const T* p = static_cast<const T*>(a.x) + (m0 + m) * a.ldx + k;
+                if (a.xvec && n >= 8) {
+#pragma unroll
+                    for (int j = 0; j < WORDS; j += 4) {
+                        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + j / 4);
+                        raw[u][j] = v.x; raw[u][j + 1] = v.y; raw[u][j + 2] = v.z; raw[u][j + 3] = v.w;
+                    }
+                } else if constexpr (TYPE == ESB_F32) {
+#pragma unroll
+                    for (int j = 0; j < 8; j++) raw[u][j] = j < n ? __float_as_uint(p[j]) : 0u;
+                } else {
+                    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        raw[u][j] = (2 * j < n ? h[2 * j] : 0u) | ((2 * j + 1 < n ? (uint32_t)h[2 * j + 1] : 0u) << 16);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int q = q0 + u * WARPS;
+            if (q >= total) break;
+            const int m = q / parts, b = (q - m * parts) * 32 + lane, step = b >> 4, r = i / (16 / R);
             unsigned char* at = xs + (size_t)(m * a.planes) * stride + (size_t)(step * 128 + ((i & 3) * 4 + (i >> 2)) * 8) * 2;
             float* f = fx + step * 8 * NT + m * a.planes * R + r;
-            uint4 out;
-            if (a.x_type == ESB_CODES) {
+            if constexpr (TYPE == ESB_CODES) {
+                const int64_t k = k0 + (int64_t)b * 8, n = a.K - k;
                 uint32_t h[8];
-                const uint32_t* xw = a.xc.codes + (m0 + m) * a.xc.ld + k / 4;
-                const uint32_t w0 = n > 0 ? xw[0] : 0u, w1 = n > 4 ? xw[1] : 0u;
 #pragma unroll
-                for (int j = 0; j < 8; j++) h[j] = j < n ? xtab[((j < 4 ? w0 : w1) >> (8 * (j & 3))) & 255u] : 0u;
-                out = make_uint4(h[0] | (h[2] << 16), h[1] | (h[3] << 16), h[4] | (h[6] << 16), h[5] | (h[7] << 16));
-                if (i % LANES == 0)
+                for (int j = 0; j < 8; j++) h[j] = j < n ? xtab[(raw[u][j >> 2] >> (8 * (j & 3))) & 255u] : 0u;
+                *reinterpret_cast<uint4*>(at) = make_uint4(h[0] | (h[2] << 16), h[1] | (h[3] << 16), h[4] | (h[6] << 16), h[5] | (h[7] << 16));
+                if (i % (16 / R) == 0)
                     *f = n > 0 ? a.xc.scales[(m0 + m) * a.xc.lds + k / a.xgroup] * (a.xc.fmt.k == 2 ? 65536.0f : 1.0f) : 0.0f;
             } else {
                 float v[8];
-                load8_any(a.x, a.x_type, (m0 + m) * a.ldx + k, n, a.xvec, v);
-                float s = 1.0f, back = 1.0f;
-                if (a.x_type != ESB_F16) {
-                    uint32_t mx = 0u;
+                if constexpr (TYPE == ESB_F32) {
 #pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        const uint32_t u = __float_as_uint(v[j]) & 0x7fffffffu;
-                        mx = max(mx, u < 0x7f800000u ? u : 0u);
-                    }
+                    for (int j = 0; j < 8; j++) v[j] = __uint_as_float(raw[u][j]);
+                } else {
 #pragma unroll
-                    for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                    const int e = max((int)(mx >> 23), 15);          // exponent field; 2^(14 - (e - 127)) <= 2^126
-                    s = __uint_as_float((uint32_t)(268 - e) << 23);
-                    back = __uint_as_float((uint32_t)(e - 14) << 23);
-#pragma unroll
-                    for (int j = 0; j < 8; j++) v[j] *= s;
+                    for (int j = 0; j < 4; j++) unpack2<Elem<TYPE>>(raw[u][j], v[2 * j], v[2 * j + 1]);
                 }
-                if (a.planes == 2) {
-                    float lo[8];
-#pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        const float hi = __half2float(__float2half_rn(v[j]));
-                        lo[j] = fabsf(hi) < __int_as_float(0x7f800000) ? (v[j] - hi) * 2048.0f : 0.0f;
-                        v[j] = hi;
-                    }
-                    *reinterpret_cast<uint4*>(at + stride) = make_uint4(half2_of(lo[0], lo[2]), half2_of(lo[1], lo[3]),
-                                                                        half2_of(lo[4], lo[6]), half2_of(lo[5], lo[7]));
-                    if (i % LANES == 0) f[R] = back * (1.0f / 2048.0f);
-                }
-                out = make_uint4(half2_of(v[0], v[2]), half2_of(v[1], v[3]), half2_of(v[4], v[6]), half2_of(v[5], v[7]));
-                if (i % LANES == 0) *f = back;
+                put_x8<NT, R, TYPE>(a, v, i, at, f);
             }
-            *reinterpret_cast<uint4*>(at) = out;
         }
     }
 }
 
-template <int NT, int R>
-__global__ void __launch_bounds__(kMvThreads, 2) matvec_kernel(const MvArgs a)
+template <int NT, int R, int WARPS, int BLOCKS>
+__global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint16_t xtab[256];
+    constexpr int THREADS = WARPS * 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int64_t m0 = (int64_t)blockIdx.z * a.mt;
     const int mt = (int)min((int64_t)a.mt, a.M - m0);
     const int cols = mt * a.planes * R;
-    const int64_t k0 = (int64_t)blockIdx.y * a.kc;
-    const int slices = (int)min((int64_t)(a.kc / kSlice), (a.K - k0 + kSlice - 1) / kSlice);   // may be <= 0 in the last block of a row
-    unsigned char* xs = smem + 256;
-    float* fx = reinterpret_cast<float*>(xs + (size_t)a.mt * a.planes * xs_stride(a.kc));
+    const int k0 = (int)blockIdx.y * a.kc;
+    const int slices = min(a.kc / kSlice, ((int)a.K - k0 + kSlice - 1) / kSlice);   // may be <= 0 in the last block of a row
+    unsigned char* xs = smem;
+    unsigned char* zeros = xs + (size_t)a.mt * a.planes * xs_stride(a.kc);
+    float* fx = reinterpret_cast<float*>(zeros + (a.zrow ? xs_stride(a.kc) : 0));
     float* red = fx + (a.kc / 128) * 8 * NT;
+    const int part = a.mt * a.planes * R * kRedLd;      // floats of a warp's sums of a tile
+    const int batch = WARPS * part;
 
-    const int wn = kMvWarps / a.wk;                     // tiles of 16 rows in work at once
+    const int wn = WARPS / a.wk;                        // tiles of 16 rows in work at once
     const int wi = warp / a.wk, wj = warp % a.wk;       // this warp's tile of them, and its place along the row
-    const int64_t tiles = (a.N + 15) / 16, step = (int64_t)gridDim.x * wn;
-    const int mine = slices > wj ? (slices - wj + a.wk - 1) / a.wk : 0;
+    const int N = (int)a.N, tiles = (N + 15) / 16, stride = (int)gridDim.x * wn;
+    const int first = (int)blockIdx.x * wn;
 
     griddep_wait();
     griddep_launch_dependents();
+    // Loads of the slice after the one in work go into each step's registers as
+    // soon as that step is done.
     uint4 buf[4][2];
     float sc[2][R];                                     // scales of step t of the slice, rows g and g + 8
-    const uint32_t *pa = nullptr, *pb = nullptr;
-    const float *sa = nullptr, *sb = nullptr;
-    auto rows_of = [&](int64_t tile) {
-        const int64_t na = min(tile * 16 + g, a.N - 1), nb = min(tile * 16 + 8 + g, a.N - 1);
-        pa = a.w.codes + na * a.w.ld;
-        pb = a.w.codes + nb * a.w.ld;
-        sa = a.w.scales + na * a.w.lds;
-        sb = a.w.scales + nb * a.w.lds;
-    };
-    auto load_step = [&](int sl, int c, bool ok) {
-        const int64_t at = (k0 + (int64_t)sl * kSlice + c * 128) / 8 + t * 4;
-        ok = ok && at < a.w.ld;                         // ld is a multiple of 4: all 16 bytes are the row's
-        buf[c][0] = buf[c][1] = make_uint4(0u, 0u, 0u, 0u);
-        if (ok) {
-            buf[c][0] = ldg_stream(pa + at);
-            buf[c][1] = ldg_stream(pb + at);
+    const uint32_t* pw[2];                              // this lane's place in the slice that is loaded next
+    const float* ps[2];
+    int p_k = k0 + wj * kSlice, p_base = first;         // its first code, its tile
+    auto rows_of = [&]() {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int n = min((p_base + wi) * 16 + 8 * i + g, N - 1);
+            pw[i] = a.w.codes + n * a.w.ld + (p_k / 8 + t * 4);
+            ps[i] = a.w.scales + n * a.w.lds;
         }
     };
-    auto load_scales = [&](int sl, bool ok) {
-#pragma unroll
-        for (int i = 0; i < R; i++) {
-            const uint32_t k = (uint32_t)(k0 + (int64_t)sl * kSlice + t * 128 + i * (128 / R));
-            const uint32_t gi = k / (uint32_t)a.w.group;
-            const bool in = ok && gi < (uint32_t)a.ngroups;
-            sc[0][i] = in ? __ldg(sa + gi) : 0.0f;
-            sc[1][i] = in ? __ldg(sb + gi) : 0.0f;
+    auto load_step = [&](int c) {
+        if (p_k + kSlice <= (int)a.wfull) {
+            buf[c][0] = ldg_stream(pw[0] + c * 16);
+            buf[c][1] = ldg_stream(pw[1] + c * 16);
+        } else {
+            // past the row's end its last words will do: x is 0 there
+            const int o = min(c * 16, (int)a.wfull / 8 - 4 - (p_k / 8 + t * 4));
+            buf[c][0] = ldg_stream(pw[0] + o);
+            buf[c][1] = ldg_stream(pw[1] + o);
         }
     };
-    int64_t base = (int64_t)blockIdx.x * wn;
-    rows_of(base + wi);
+    auto load_scales = [&]() {
 #pragma unroll
-    for (int c = 0; c < 4; c++) load_step(wj, c, mine > 0);
-    load_scales(wj, mine > 0);
+        for (int j = 0; j < R; j++) {
+            const uint32_t k32 = (uint32_t)p_k / 32 + t * 4 + j * (4 / R);
+            const uint32_t gi = a.gmagic ? __umulhi(k32, a.gmagic) : k32;
+            const bool in = gi < (uint32_t)a.ngroups;
+            sc[0][j] = in ? __ldg(ps[0] + gi) : 0.0f;
+            sc[1][j] = in ? __ldg(ps[1] + gi) : 0.0f;
+        }
+    };
+    rows_of();
+    if (wj < slices) {
+#pragma unroll
+        for (int c = 0; c < 4; c++) load_step(c);
+        load_scales();
+    }
 
-    if (threadIdx.x < 16) reinterpret_cast<uint4*>(smem)[threadIdx.x] = make_uint4(0u, 0u, 0u, 0u);
-    for (int i = threadIdx.x; i < (a.kc / 128) * 8 * NT; i += kMvThreads)
+    for (int i = threadIdx.x; i < (a.kc / 128) * 8 * NT; i += THREADS)
         if (i % (8 * NT) >= cols) fx[i] = 0.0f;
+    if (a.zrow)
+        for (int i = threadIdx.x * 16; i < a.kc * 2; i += THREADS * 16) *reinterpret_cast<uint4*>(zeros + i) = make_uint4(0u, 0u, 0u, 0u);
     if (a.x_type == ESB_CODES) {
         // k = 2 reaches 1.75 * 2^30; its elements are scaled by 2^-16
-        const float v = code_value(threadIdx.x, 8, a.xc.fmt.k) * (a.xc.fmt.k == 2 ? 1.0f / 65536.0f : 1.0f);
-        const __half h = __float2half_rn(v);
-        xtab[threadIdx.x] = *reinterpret_cast<const uint16_t*>(&h);
+        for (int i = threadIdx.x; i < 256; i += THREADS) {
+            const __half h = __float2half_rn(code_value(i, 8, a.xc.fmt.k) * (a.xc.fmt.k == 2 ? 1.0f / 65536.0f : 1.0f));
+            xtab[i] = *reinterpret_cast<const uint16_t*>(&h);
+        }
         __syncthreads();
     }
-    stage_x<NT, R>(a, m0, mt, k0, xs, fx, xtab);
+    if (a.x_type == ESB_BF16) stage_x<NT, R, WARPS, ESB_BF16>(a, m0, mt, k0, xs, fx, xtab);
+    else if (a.x_type == ESB_CODES) stage_x<NT, R, WARPS, ESB_CODES>(a, m0, mt, k0, xs, fx, xtab);
+    else if (a.x_type == ESB_F16) stage_x<NT, R, WARPS, ESB_F16>(a, m0, mt, k0, xs, fx, xtab);
+    else stage_x<NT, R, WARPS, ESB_F32>(a, m0, mt, k0, xs, fx, xtab);
     __syncthreads();
 
     // where this lane reads x for column 8 i + g: its row's plane, or zeros
-    const unsigned char* xp[NT];
-    uint32_t xmask[NT];
+    uint32_t xp[NT];
 #pragma unroll
     for (int i = 0; i < NT; i++) {
         const int col = 8 * i + g;
         const bool on = col < cols && (t * R) / 4 == col % R;
-        xp[i] = on ? xs + (size_t)(col / R) * xs_stride(a.kc) + t * 16 : smem;
-        xmask[i] = on ? 0xffffffffu : 0u;
+        xp[i] = smem_u32((on ? xs + (size_t)(col / R) * xs_stride(a.kc) : zeros) + t * 16);
     }
+    const uint32_t fp = smem_u32(fx) + t * 8;
 
-    int flip = 0;
-    for (; base < tiles; base += step) {
+    auto put = [&](int n, int m, float v) {
+        if (a.bias) v += a.bias[n];
+        const int64_t at = (m0 + m) * a.ldy + n;
+        if (a.y_type == ESB_F32) static_cast<float*>(a.y)[at] = v;
+        else if (a.y_type == ESB_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(v);
+        else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+    };
+
+    int flip = 0, held = 0;                             // held: tiles whose sums wait in red's half
+    for (int base = first; base < tiles; base += stride) {
         float acc[NT][4];
 #pragma unroll
         for (int i = 0; i < NT; i++) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
-        for (int j = 0; j < mine; j++) {
-            const int sl = wj + j * a.wk;
-            const bool last = j == mine - 1;
-            const bool more = !last || base + step < tiles;
-            const int nsl = last ? wj : sl + a.wk;
-            if (last) rows_of(base + step + wi);
+#pragma unroll 1
+        for (int sl = wj; sl < slices; sl += a.wk) {
             float cur[2][R];
 #pragma unroll
-            for (int i = 0; i < R; i++) {
-                cur[0][i] = sc[0][i];
-                cur[1][i] = sc[1][i];
+            for (int j = 0; j < R; j++) {
+                cur[0][j] = sc[0][j];
+                cur[1][j] = sc[1][j];
             }
-            load_scales(nsl, more);
+            bool more = true;
+            if (sl + a.wk < slices) {
+                p_k += a.wk * kSlice;
+                pw[0] += a.wk * (kSlice / 8);
+                pw[1] += a.wk * (kSlice / 8);
+            } else {
+                p_k = k0 + wj * kSlice;
+                p_base += stride;
+                more = p_base < tiles;
+                rows_of();
+            }
+            if (more) load_scales();
+            const uint32_t xo = (uint32_t)sl * 1024u, fo = fp + (uint32_t)sl * (128u * NT);
 #pragma unroll
             for (int c = 0; c < 4; c++) {
                 const uint32_t wa[4] = {buf[c][0].x, buf[c][0].y, buf[c][0].z, buf[c][0].w};
                 const uint32_t wb[4] = {buf[c][1].x, buf[c][1].y, buf[c][1].z, buf[c][1].w};
-                load_step(nsl, c, more);
                 float sum[NT][4];
 #pragma unroll
-                for (int i = 0; i < NT; i++) sum[i][0] = sum[i][1] = sum[i][2] = sum[i][3] = 0.0f;
-                const uint32_t off = (uint32_t)(sl * 4 + c) * 256u;
-#pragma unroll
-                for (int w = 0; w < 4; w++) {
+                for (int q = 0; q < 4; q++) {
                     uint32_t da[4], db[4];
-                    decode8(wa[w], a.tab_lo, a.tab_hi, da);
-                    decode8(wb[w], a.tab_lo, a.tab_hi, db);
+                    decode8(wa[q], a.tab, da);
+                    decode8(wb[q], a.tab, db);
 #pragma unroll
                     for (int i = 0; i < NT; i++) {
-                        const uint4 b = *reinterpret_cast<const uint4*>(xp[i] + (off & xmask[i]) + w * 64);
-                        mma_16816(sum[i], da[0], db[0], da[1], db[1], b.x, b.y);
-                        mma_16816(sum[i], da[2], db[2], da[3], db[3], b.z, b.w);
+                        const uint4 b = lds16(xp[i] + xo + c * 256 + q * 64);
+                        if (q == 0) mma_16816<false>(sum[i], da[0], db[0], da[1], db[1], b.x, b.y);
+                        else mma_16816<true>(sum[i], da[0], db[0], da[1], db[1], b.x, b.y);
+                        mma_16816<true>(sum[i], da[2], db[2], da[3], db[3], b.z, b.w);
                     }
                 }
+                if (more) load_step(c);
                 // this lane's sums: rows g and g + 8, columns 2 t and 2 t + 1 of each eight
-                float s0[2], s1[2];
-                if constexpr (R == 1) {
-                    s0[0] = s0[1] = __shfl_sync(0xffffffffu, cur[0][0], (lane & 28) | c);
-                    s1[0] = s1[1] = __shfl_sync(0xffffffffu, cur[1][0], (lane & 28) | c);
-                } else {
-                    float q0[R], q1[R];
+                float s[2][2];
 #pragma unroll
-                    for (int i = 0; i < R; i++) {
-                        q0[i] = __shfl_sync(0xffffffffu, cur[0][i], (lane & 28) | c);
-                        q1[i] = __shfl_sync(0xffffffffu, cur[1][i], (lane & 28) | c);
-                    }
+                for (int h = 0; h < 2; h++) {
+                    float q[R];
+#pragma unroll
+                    for (int j = 0; j < R; j++) q[j] = __shfl_sync(0xffffffffu, cur[h][j], (lane & 28) | c);
                     const bool up = R == 4 && (t & 1);
-#pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        s0[i] = up ? q0[(i + 2) % R] : q0[i];
-                        s1[i] = up ? q1[(i + 2) % R] : q1[i];
-                    }
+                    s[h][0] = up ? q[2 % R] : q[0];
+                    s[h][1] = up ? q[3 % R] : q[1 % R];
                 }
-                const float* f = fx + (sl * 4 + c) * 8 * NT + 2 * t;
 #pragma unroll
                 for (int i = 0; i < NT; i++) {
-                    const float2 fc = *reinterpret_cast<const float2*>(f + 8 * i);
-                    acc[i][0] = fmaf(sum[i][0] * s0[0], fc.x, acc[i][0]);
-                    acc[i][1] = fmaf(sum[i][1] * s0[1], fc.y, acc[i][1]);
-                    acc[i][2] = fmaf(sum[i][2] * s1[0], fc.x, acc[i][2]);
-                    acc[i][3] = fmaf(sum[i][3] * s1[1], fc.y, acc[i][3]);
+                    float2 fc;
+                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(fc.x), "=f"(fc.y) : "r"(fo + (c * NT + i) * 32) : "memory");
+                    acc[i][0] = fmaf(sum[i][0] * s[0][0], fc.x, acc[i][0]);
+                    acc[i][1] = fmaf(sum[i][1] * s[0][1], fc.y, acc[i][1]);
+                    acc[i][2] = fmaf(sum[i][2] * s[1][0], fc.x, acc[i][2]);
+                    acc[i][3] = fmaf(sum[i][3] * s[1][1], fc.y, acc[i][3]);
                 }
             }
         }
-        // the warps' parts of each tile, in their order
-        float* rw = red + (size_t)(flip * kMvWarps + warp) * 8 * NT * kRedLd;
+        // the warps' parts wait until `hold` tiles are there; then they are
+        // added up, in their order.  A half of red is written again behind the
+        // other half's barrier.
+        float* rw = red + (flip * a.hold + held) * batch + warp * part;
 #pragma unroll
-        for (int i = 0; i < NT; i++) {
-            float* p = rw + (8 * i + 2 * t) * kRedLd + g;
-            p[0] = acc[i][0];
-            p[kRedLd] = acc[i][1];
-            p[8] = acc[i][2];
-            p[kRedLd + 8] = acc[i][3];
-        }
-        __syncthreads();
-        for (int o = threadIdx.x; o < wn * 16 * mt; o += kMvThreads) {
-            const int row = o & 15, m = (o >> 4) % mt, ti = (o >> 4) / mt;
-            float* p = red + (size_t)(flip * kMvWarps + ti * a.wk) * 8 * NT * kRedLd + row;
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+            for (int e = 0; e < 2; e++) {
+                const int col = 8 * i + 2 * t + e;
+                float* p = rw + col * kRedLd + g;
+                if (col < cols) {
+                    p[0] = acc[i][e];
+                    p[8] = acc[i][2 + e];
+                }
+            }
+        if (++held < a.hold && base + stride < tiles) continue;
+        group_barrier(wi, a.wk * 32);
+        const int each = 16 * mt;
+        for (int o = wj * 32 + lane; o < held * each; o += a.wk * 32) {
+            const int h = o / each, u = o - h * each, row = u & 15, m = u >> 4;
+            float* p = red + (flip * a.hold + h) * batch + wi * a.wk * part + m * a.planes * R * kRedLd + row;
             float v = 0.0f;
             for (int j = 0; j < a.wk; j++)
-                for (int c = 0; c < a.planes * R; c++) v += p[(size_t)j * 8 * NT * kRedLd + (m * a.planes * R + c) * kRedLd];
-            if (a.split > 1) {
-                p[m * a.planes * R * kRedLd] = v;       // this block's part, at the first of the numbers it sums
-                continue;
-            }
-            const int64_t n = (base + ti) * 16 + row;
-            if (n < a.N) {
-                if (a.bias) v += a.bias[n];
-                const int64_t at = (m0 + m) * a.ldy + n;
-                if (a.y_type == ESB_F32) static_cast<float*>(a.y)[at] = v;
-                else if (a.y_type == ESB_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(v);
-                else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-            }
+                for (int q = 0; q < a.planes * R; q++) v += p[j * part + q * kRedLd];
+            const int n = (base - (held - 1 - h) * stride + wi) * 16 + row;
+            if (a.split > 1) p[0] = v;                  // this block's part, at the first of the numbers it sums
+            else if (n < N) put(n, m, v);
         }
         if (a.split > 1) {
-            // the blocks' parts, in their order.  A part is written again two
-            // tiles on, behind the next barrier.
             cluster_barrier();
-            for (int o = threadIdx.x; o < wn * 16 * mt; o += kMvThreads) {
-                if (o % a.split != (int)blockIdx.y) continue;
-                const int row = o & 15, m = (o >> 4) % mt, ti = (o >> 4) / mt;
-                const int64_t n = (base + ti) * 16 + row;
-                if (n >= a.N) continue;
-                const float* p = red + (size_t)(flip * kMvWarps + ti * a.wk) * 8 * NT * kRedLd + row + m * a.planes * R * kRedLd;
+            for (int o = wj * 32 + lane; o < held * each; o += a.wk * 32) {
+                const int h = o / each, u = o - h * each, row = u & 15, m = u >> 4;
+                const int n = (base - (held - 1 - h) * stride + wi) * 16 + row;
+                if (m % a.split != (int)blockIdx.y || n >= N) continue;   // the blocks take the rows of x in turn
+                const float* p = red + (flip * a.hold + h) * batch + wi * a.wk * part + m * a.planes * R * kRedLd + row;
                 float v = 0.0f;
                 for (int j = 0; j < a.split; j++) v += ld_cluster(p, j);
-                if (a.bias) v += a.bias[n];
-                const int64_t at = (m0 + m) * a.ldy + n;
-                if (a.y_type == ESB_F32) static_cast<float*>(a.y)[at] = v;
-                else if (a.y_type == ESB_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(v);
-                else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+                put(n, m, v);
             }
         }
         flip ^= 1;
+        held = 0;
     }
     if (a.split > 1) cluster_barrier();                 // no block leaves while another reads its sums
 }
@@ -401,7 +491,17 @@ void element_bytes(int k, uint32_t& lo, uint32_t& hi)
 }
 
 using MvKernel = void (*)(const MvArgs);
-template <int R> MvKernel mv_kernel(int nt) { return nt == 1 ? matvec_kernel<1, R> : (nt == 2 ? matvec_kernel<2, R> : matvec_kernel<4, R>); }
+constexpr size_t kMvSmem = 225 * 1024;
+struct MvPlan {
+    MvKernel kernel;
+    int warps, blocks;
+};
+template <int R> MvPlan mv_plan(int nt)
+{
+    if (nt == 1) return {matvec_kernel<1, R, 16, 1>, 16, 1};
+    if (nt == 2) return {matvec_kernel<2, R, 16, 1>, 16, 1};
+    return {matvec_kernel<4, R, 16, 1>, 16, 1};
+}
 
 }  // namespace
 
@@ -417,43 +517,58 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
     if (a.w.group <= 0 || a.w.group >= K) a.w.group = whole;
     a.ngroups = (K + a.w.group - 1) / a.w.group;
     a.xgroup = xc && xc->group > 0 && xc->group < K ? xc->group : whole;
+    const int64_t g32 = a.w.group / 32;                 // k / group for k / 32 < 2^13: one high product
+    a.gmagic = g32 == 1 ? 0u : (uint32_t)(((1ll << 32) + g32 - 1) / g32);
     a.bias = bias; a.y = y; a.ldy = ldy;
     a.x_type = x_type; a.y_type = y_type;
     a.xvec = x && (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ldx * type_bytes(x_type) % 16 == 0;
-    element_bytes(w.fmt.k, a.tab_lo, a.tab_hi);
+    element_bytes(w.fmt.k, a.tab.lo, a.tab.hi);
+    a.tab.by16 = 1u << 16;
+    a.tab.by4 = 1u << 4;
     const int r = a.w.group % 128 == 0 ? 1 : (a.w.group % 64 == 0 ? 2 : 4);
     a.planes = x_type == ESB_F32 ? 2 : 1;
+    a.wfull = std::min<int64_t>(w.ld * 8, (int64_t)1 << 20);
 
     // Rows a block takes at once: up to 32 columns' worth, fewer where x would
     // not fit; the row's codes over up to 8 blocks (a cluster) where that
-    // makes it fit twice into an SM, or gives the SMs work.
+    // makes x fit.
     const int sms = device_sm_count();
     const int most = 32 / (a.planes * r);
-    const int64_t tiles = (N + 15) / 16, all = (K + kSlice - 1) / kSlice;
+    const int64_t tiles = (N + 15) / 16, all = (K + 511) / 512;
     int64_t passes = (M + most - 1) / most;
-    int nt;
+    MvPlan p;
     size_t smem;
     for (;; passes *= 2) {
         a.mt = (int)((M + passes - 1) / passes);
-        const int cols = a.mt * a.planes * r;
-        nt = cols <= 8 ? 1 : (cols <= 16 ? 2 : 4);
+        const int cols = a.mt * a.planes * r, nt = cols <= 8 ? 1 : (cols <= 16 ? 2 : 4);
+        p = r == 1 ? mv_plan<1>(nt) : (r == 2 ? mv_plan<2>(nt) : mv_plan<4>(nt));
+        a.zrow = r > 1 || cols < 8 * nt;
         for (a.split = 1;; a.split *= 2) {
-            a.kc = (int)((all + a.split - 1) / a.split) * kSlice;
-            smem = mv_smem(a.mt * a.planes, a.kc, nt);
-            if (a.split == 8) break;
-            if (smem <= 100 * 1024 && (tiles * a.split >= sms || a.kc <= 8 * kSlice)) break;
+            a.kc = (int)((all + a.split - 1) / a.split) * 512;
+            const size_t sums = mv_sums(cols, p.warps);
+            smem = mv_x_bytes(a.mt * a.planes + a.zrow, a.kc, nt) + sums;
+            a.hold = 1;
+            while (a.hold < 4 && (a.hold + 1) * sums <= 16 * 1024) a.hold++;
+            smem += (a.hold - 1) * sums;
+            if (a.split == 8 || smem <= kMvSmem / p.blocks) break;
         }
-        if (smem <= 200 * 1024 || a.mt == 1) break;
+        if (smem <= kMvSmem || a.mt == 1) break;
     }
     passes = (M + a.mt - 1) / a.mt;
-    const int sl = a.kc / kSlice;
-    a.wk = sl > 4 ? 8 : (sl > 2 ? 4 : sl);
-    const int64_t want = (tiles + kMvWarps / a.wk - 1) / (kMvWarps / a.wk);
-    int64_t cap = 2 * sms / (a.split * (passes < 8 ? passes : 8));
-    if (cap < 1) cap = 1;
-    const MvKernel kernel = r == 1 ? mv_kernel<1>(nt) : (r == 2 ? mv_kernel<2>(nt) : mv_kernel<4>(nt));
-    cudaError_t e = cudaSuccess;
-    if (smem > 47 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const int64_t at_once = std::max<int64_t>(1, p.blocks * sms / (a.split * std::min<int64_t>(passes, sms)));   // blocks of a pass on the SMs
+    // Warps along a row: as few rounds as possible of tiles of so many slices,
+    // each with a quarter slice's worth of work besides.
+    const int64_t slices = a.kc / kSlice;
+    double best = 0.0;
+    a.wk = 0;
+    for (int wk = 1; wk <= p.warps; wk *= 2) {
+        if (wk > slices || p.warps % wk || p.warps / wk > 16) continue;
+        const int64_t wn = p.warps / wk, rounds = (tiles + wn * at_once - 1) / (wn * at_once);
+        const double cost = (double)rounds * ((double)((slices + wk - 1) / wk) + 0.25);
+        if (!a.wk || cost < best) { best = cost; a.wk = wk; }
+    }
+    const int64_t want = (tiles + p.warps / a.wk - 1) / (p.warps / a.wk), cap = at_once;
+    cudaError_t e = cudaFuncSetAttribute(p.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
     if (e != cudaSuccess) return e;
     for (int64_t p0 = 0; p0 < passes; p0 += 65535) {    // grid.z holds 65535 passes
         const int64_t np = passes - p0 < 65535 ? passes - p0 : 65535;
@@ -468,7 +583,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(want < cap ? want : cap), (unsigned)a.split, (unsigned)np);
-        cfg.blockDim = dim3(kMvThreads);
+        cfg.blockDim = dim3((unsigned)p.warps * 32);
         cfg.dynamicSmemBytes = smem;
         cfg.stream = st;
         cudaLaunchAttribute attr[2];
@@ -480,7 +595,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = a.split > 1 ? 2 : 1;
-        e = cudaLaunchKernelEx(&cfg, kernel, b);
+        e = cudaLaunchKernelEx(&cfg, p.kernel, b);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
