@@ -743,7 +743,7 @@ esb_status esb_logprobs(const void* x, int32_t x_type, int64_t rows, int64_t col
 
 /* Its gradient with respect to the logits:
  *   dx[j] = dlogp ([j == id] - p_j) - dentropy p_j (log p_j + entropy)
- * 0 for a masked logit and in a row without any other.
+ * with p_j = 0 for a masked logit (also in a row without any other).
  *   lse, entropy  [device] of the forward pass (entropy may be NULL without dentropy)
  *   dlogp, dentropy [device] rows floats, each may be NULL (zeros); ids as there
  *   dx  [device] rows x cols of x_type; may lie on x with the same stride

@@ -1,5 +1,22 @@
 // esb_logprobs.cu -- log probabilities of given tokens, entropy and the most
 // likely alternatives of rows of logits, and the gradient.
+//
+// One pass over the row: every thread keeps the largest logit m that it has
+// met, sum e^(x-m) and sum e^(x-m) (x-m), rescaled when m grows; they are
+// joined over the block, and over the blocks of a cluster where a few rows
+// would leave SMs idle.  With M, S and D those of the row,
+//   lse = M + log S,  entropy = log S - D / S.
+// HBM-bound: 2 or 4 bytes a logit; at the measured copy rate an SM gets about
+// 11 (bf16) issue slots a logit, and the pass takes about 9.
+//
+// The alternatives come out of the same pass.  A key orders logits by value,
+// then by place.  After a row's first block of logits the best keys of the 32
+// lanes, each over all warps, are 32 logits of the row, so the top-th best of
+// them is a bound that no alternative lies below; from then on a thread puts
+// logits at or above the bound into a list, which one warp sorts and cuts to
+// the best 32 when it fills up, raising the bound.  A block of logits that
+// would overflow the list (rows that ascend) takes the row again, once for
+// each alternative.
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -10,114 +27,347 @@ namespace esb {
 
 namespace {
 
-constexpr int kLpThreads = 256;
+constexpr int kLpThreads = 512;
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpValues = 16;           // logits of a thread in a block of them
+constexpr int kLpList = 2048;
+constexpr int kLpMaxCluster = 8;
+
+using Key = unsigned long long;
 
 struct LpArgs {
     const void* x;
     int64_t rows, cols, ldx;
     const int64_t* ids;
-    int top;
+    int top, split;                     // split: blocks of a row, a cluster
     float *logp, *entropy, *lse, *top_logp;
     int64_t* top_ids;
-    int vec;
 };
 
-// Order of the alternatives: the larger logit first, the lower place among
-// equals.  Key 0 is below every number; NaN and -inf have it.
-__device__ __forceinline__ unsigned long long top_key(float v, uint32_t at)
+// Key 0 is below every number; NaN and -inf have it.
+__device__ __forceinline__ Key top_key(float v, uint32_t at)
 {
     if (!(v > __int_as_float(0xff800000))) return 0ull;
     const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v);   // -0 counts as 0
-    return ((unsigned long long)((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - at);
+    return ((Key)((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - at);
+}
+__device__ __forceinline__ uint32_t key_place(Key k) { return 0xffffffffu - (uint32_t)k; }
+
+struct LpSums {
+    float m, s, d;
+};
+// The sums of two parts of a row.  A part without a logit has m = lowest and
+// s = 0; a factor of 0 drops a part whose difference is not finite.
+__device__ __forceinline__ LpSums join(const LpSums& a, const LpSums& b)
+{
+    LpSums r;
+    r.m = fmaxf(a.m, b.m);
+    const float da = a.m - r.m, db = b.m - r.m, fa = __expf(da), fb = __expf(db);
+    r.s = a.s * fa + b.s * fb;
+    r.d = (fa == 0.0f ? 0.0f : fa * fmaf(da, a.s, a.d)) + (fb == 0.0f ? 0.0f : fb * fmaf(db, b.s, b.d));
+    if (!(a.s == a.s) || !(b.s == b.s)) r.s = r.d = __int_as_float(0x7fffffff);
+    return r;
 }
 
-template <int NW>
-__device__ __forceinline__ float lp_block(float v, float* sh, bool is_max)
+// Descending bitonic sort of one key a lane; merge keeps the best 32 of two
+// descending lists.
+__device__ __forceinline__ Key shfl_key(Key k, int o)
+{
+    return ((Key)__shfl_xor_sync(0xffffffffu, (uint32_t)(k >> 32), o) << 32) | __shfl_xor_sync(0xffffffffu, (uint32_t)k, o);
+}
+__device__ __forceinline__ Key pick(Key k, int o, bool larger)
+{
+    const Key t = shfl_key(k, o);
+    return (t > k) == larger ? t : k;
+}
+__device__ __forceinline__ Key sort32(Key k, int lane)
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float t = __shfl_xor_sync(0xffffffffu, v, o);
-        v = is_max ? fmaxf(v, t) : v + t;
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = sh[0];
+    for (int n = 2; n <= 32; n *= 2)
 #pragma unroll
-    for (int i = 1; i < NW; i++) v = is_max ? fmaxf(v, sh[i]) : v + sh[i];
-    return v;
+        for (int o = n / 2; o > 0; o /= 2) k = pick(k, o, ((lane & o) == 0) == ((lane & n) == 0 || n == 32));
+    return k;
 }
+__device__ __forceinline__ Key merge32(Key best, Key more, int lane)
+{
+    const Key r = ((Key)__shfl_sync(0xffffffffu, (uint32_t)(more >> 32), 31 - lane) << 32) | __shfl_sync(0xffffffffu, (uint32_t)more, 31 - lane);
+    Key k = best > r ? best : r;                        // a bitonic sequence
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) k = pick(k, o, (lane & o) == 0);
+    return k;
+}
+
+struct LpShared {
+    LpSums sums[kLpWarps];
+    Key lanes[kLpWarps][32];
+    Key best[32];                       // the best keys so far, descending
+    Key bound;                          // no alternative is below it
+    int count, overflow;
+    LpSums parts[kLpMaxCluster];        // of the cluster's blocks, in block 0
+    Key part_keys[kLpMaxCluster][32];
+    Key list[kLpList];
+};
+
+// Warp 0: the list's keys into the best 32; the bound is the top-th of them.
+__device__ __forceinline__ void cut_list(LpShared& sh, int top, int lane)
+{
+    const int n = min(sh.count, kLpList);
+    Key best = sh.best[lane];
+    for (int i = 0; i < n; i += 32) best = merge32(best, sort32(i + lane < n ? sh.list[i + lane] : 0ull, lane), lane);
+    sh.best[lane] = best;
+    const Key b = ((Key)__shfl_sync(0xffffffffu, (uint32_t)(best >> 32), top - 1) << 32) | __shfl_sync(0xffffffffu, (uint32_t)best, top - 1);
+    __syncwarp();
+    if (lane == 0) {
+        if (b > sh.bound) sh.bound = b;
+        sh.count = 0;
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void remote_store(T* p, int rank, const T& v)
+{
+    static_assert(sizeof(T) % 4 == 0, "words");
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 4); i++)
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a + 4 * i), "r"(w[i]) : "memory");
+}
+__device__ __forceinline__ void lp_cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// A row as 16-byte vectors: `head` values before the first 16-byte boundary,
+// then `vecs` vectors, then what is left.
+template <class T>
+struct RowParts {
+    int head, tail_at;                  // values before the vectors; the first value after them
+    int64_t vecs;
+    __device__ __forceinline__ RowParts(const T* x, int64_t cols)
+    {
+        constexpr int V = 16 / sizeof(T);
+        const int mis = (int)((reinterpret_cast<uintptr_t>(x) & 15u) / sizeof(T));
+        const int64_t h = mis ? V - mis : 0;
+        head = (int)(h < cols ? h : cols);
+        vecs = (cols - head) / V;
+        tail_at = (int)(head + vecs * V);
+    }
+};
 
 template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads) logprobs_kernel(const LpArgs a)
+__global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
 {
     using T = Elem<TYPE>;
-    constexpr int NW = kLpThreads / 32;
-    __shared__ float shf[NW];
-    __shared__ unsigned long long shk[NW];
+    constexpr int V = 16 / sizeof(T), U = kLpValues / V;   // values of a vector, vectors of a thread in a block of logits
+    extern __shared__ __align__(16) unsigned char lp_smem[];
+    LpShared& sh = *reinterpret_cast<LpShared*>(lp_smem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rank = a.split > 1 ? (int)(blockIdx.x % a.split) : 0;
+    const float ninf = __int_as_float(0xff800000), lowest = -__int_as_float(0x7f7fffff);
     griddep_wait();
-    const float ninf = __int_as_float(0xff800000);
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    if (a.split > 1) lp_cluster_barrier();              // every block of the cluster runs before its memory is written
+    for (int64_t row = blockIdx.x / a.split; row < a.rows; row += gridDim.x / a.split) {
         const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-        float v[8];
-        float m = ninf;
-        for (int64_t e = threadIdx.x * 8; e < a.cols; e += kLpThreads * 8) {
-            load8_to(x + e, a.cols - e, a.vec, v);
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-                if (e + i < a.cols) m = fmaxf(m, v[i]);
-        }
-        m = lp_block<NW>(m, shf, true);
-        const bool empty = m == ninf;            // or every value NaN
-        float s = 0.0f, sx = 0.0f;
-        for (int64_t e = threadIdx.x * 8; e < a.cols; e += kLpThreads * 8) {
-            load8_to(x + e, a.cols - e, a.vec, v);
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (e + i >= a.cols || v[i] == ninf) continue;
-                const float d = v[i] - m, p = __expf(d);
-                s += p;
-                sx = fmaf(p, p > 0.0f ? d : 0.0f, sx);
-            }
-        }
-        s = lp_block<NW>(s, shf, false);
-        sx = lp_block<NW>(sx, shf, false);
-        const float lz = logf(s);
-        const float lse = m + lz;
-        if (threadIdx.x == 0) {
-            const bool none = empty && s == 0.0f;   // every logit is -inf
-            if (a.lse) a.lse[row] = none ? ninf : lse;
-            if (a.entropy) a.entropy[row] = none ? 0.0f : lz - sx / s;
-            if (a.logp) {
-                const int64_t t = a.ids[row];
-                a.logp[row] = t < 0 || t >= a.cols ? 0.0f : (none ? ninf : (to_f32(x[t]) - m) - lz);
-            }
-        }
-        unsigned long long last = ~0ull;
-        for (int j = 0; j < a.top; j++) {
-            unsigned long long best = 0ull;
-            for (int64_t e = threadIdx.x; e < a.cols; e += kLpThreads) {
-                const unsigned long long k = top_key(to_f32(x[e]), (uint32_t)e);
-                if (k < last && k > best) best = k;
-            }
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                const unsigned long long t = __shfl_xor_sync(0xffffffffu, best, o);
-                best = t > best ? t : best;
-            }
+        const RowParts<T> rp(x, a.cols);
+        const T* xv = x + rp.head;
+        if (a.top) {
+            if (threadIdx.x < 32) sh.best[threadIdx.x] = 0ull;
+            if (threadIdx.x == 0) { sh.bound = 0ull; sh.count = 0; sh.overflow = 0; }
             __syncthreads();
-            if ((threadIdx.x & 31) == 0) shk[threadIdx.x >> 5] = best;
-            __syncthreads();
-            best = shk[0];
+        }
+        LpSums t = {lowest, 0.0f, 0.0f};
+        auto add = [&](float v) {
+            const float d = v - t.m, p = __expf(d);
+            t.s += p;
+            t.d = fmaf(p, fmaxf(d, -200.0f), t.d);      // p is 0 there
+        };
+        auto raise = [&](float m) {
+            if (m > t.m) {
+                const float d = t.m - m, f = __expf(d);
+                t.d = f == 0.0f ? 0.0f : f * fmaf(d, t.s, t.d);
+                t.s *= f;
+                t.m = m;
+            }
+        };
+        Key bound = 0ull;
+        bool full = false;              // this thread has met a list that is half full
+        auto offer = [&](float v, uint32_t at) {
+            const Key k = top_key(v, at);
+            if (k < bound || !k) return;
+            const int i = atomicAdd(&sh.count, 1);
+            if (i < kLpList) sh.list[i] = k;
+            else sh.overflow = 1;
+            full |= i >= kLpList / 2;
+        };
+        const int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
+        bool first = true;
+        for (int64_t v0 = rank * step; v0 < rp.vecs || first; v0 += a.split * step) {
+            uint4 raw[U];
 #pragma unroll
-            for (int i = 1; i < NW; i++) best = shk[i] > best ? shk[i] : best;
-            last = best;
-            if (threadIdx.x == 0) {
-                const int64_t at = best ? (int64_t)(0xffffffffu - (uint32_t)best) : -1;
-                a.top_ids[row * a.top + j] = at;
-                a.top_logp[row * a.top + j] = best ? (to_f32(x[at]) - m) - lz : ninf;
+            for (int u = 0; u < U; u++) {
+                const int64_t i = v0 + u * kLpThreads + threadIdx.x;
+                if (i < rp.vecs) raw[u] = __ldg(reinterpret_cast<const uint4*>(xv) + i);
+            }
+            // a few values before and after the vectors: the first block of
+            // the row has them, one a thread
+            float edge = ninf;
+            uint32_t edge_at = 0u;
+            if (first && rank == 0) {
+                const int64_t e = threadIdx.x < (unsigned)rp.head ? threadIdx.x : (int64_t)rp.tail_at + threadIdx.x - rp.head;
+                if (e < a.cols && threadIdx.x < 32) { edge = to_f32(x[e]); edge_at = (uint32_t)e; }
+            }
+            float v[U][V];
+            float big = fmaxf(lowest, edge);                // the thread's largest
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const int64_t i = v0 + u * kLpThreads + threadIdx.x;
+                if constexpr (V == 8) {
+                    unpack2<T>(raw[u].x, v[u][0], v[u][1]);
+                    unpack2<T>(raw[u].y, v[u][2], v[u][3]);
+                    unpack2<T>(raw[u].z, v[u][4], v[u][5]);
+                    unpack2<T>(raw[u].w, v[u][6], v[u][7]);
+                } else {
+                    v[u][0] = __uint_as_float(raw[u].x); v[u][1] = __uint_as_float(raw[u].y);
+                    v[u][2] = __uint_as_float(raw[u].z); v[u][3] = __uint_as_float(raw[u].w);
+                }
+                if (i >= rp.vecs) {
+#pragma unroll
+                    for (int j = 0; j < V; j++) v[u][j] = ninf;
+                }
+#pragma unroll
+                for (int j = 0; j < V; j++) big = fmaxf(big, v[u][j]);
+            }
+            raise(big);
+            if (edge != ninf) add(edge);
+#pragma unroll
+            for (int u = 0; u < U; u++)
+#pragma unroll
+                for (int j = 0; j < V; j++) add(v[u][j]);
+            if (a.top) {
+                auto at_of = [&](int u, int j) { return (uint32_t)(rp.head + (v0 + u * kLpThreads + threadIdx.x) * V + j); };
+                if (bound == 0ull) {                    // the same for every thread
+                    // the best key of every lane over the warps
+                    Key k = top_key(edge, edge_at);
+#pragma unroll
+                    for (int u = 0; u < U; u++)
+#pragma unroll
+                        for (int j = 0; j < V; j++)
+                            if (v[u][j] == big) {       // the block's largest is met first at its lowest place
+                                const Key c = top_key(v[u][j], at_of(u, j));
+                                k = c > k ? c : k;
+                            }
+                    sh.lanes[warp][lane] = k;
+                    __syncthreads();
+                    if (warp == 0) {
+#pragma unroll
+                        for (int w = 1; w < kLpWarps; w++) k = sh.lanes[w][lane] > k ? sh.lanes[w][lane] : k;
+                        k = sort32(k, lane);
+                        if (lane == a.top - 1) sh.bound = k;
+                    }
+                    __syncthreads();
+                    bound = sh.bound;
+                }
+                if (edge != ninf) offer(edge, edge_at);
+                // most threads have nothing at or above the bound
+                if (top_key(big, 0u) >= bound) {
+#pragma unroll
+                    for (int u = 0; u < U; u++)
+#pragma unroll
+                        for (int j = 0; j < V; j++)
+                            if (v[u][j] != ninf) offer(v[u][j], at_of(u, j));
+                }
+                if (__syncthreads_or(full)) {
+                    if (warp == 0) cut_list(sh, a.top, lane);
+                    __syncthreads();
+                    bound = sh.bound;
+                    full = false;
+                }
+            }
+            first = false;
+        }
+        // the block's sums
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const LpSums b = {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.d, o)};
+            t = join(t, b);
+        }
+        if (lane == 0) sh.sums[warp] = t;
+        __syncthreads();
+        if (warp == 0) {
+            if (lane < kLpWarps) t = sh.sums[lane];
+            else t = {lowest, 0.0f, 0.0f};
+#pragma unroll
+            for (int o = kLpWarps / 2; o > 0; o >>= 1) {
+                const LpSums b = {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.d, o)};
+                t = join(t, b);
+            }
+            if (a.top) cut_list(sh, a.top, lane);
+        }
+        if (a.top && sh.overflow) {
+            // uniform after the barrier above; rare: this block's part of the
+            // row again, for each alternative the best key below the last one
+            Key last = ~0ull;
+            for (int j = 0; j < a.top; j++) {
+                Key k = 0ull;
+                for (int64_t e = threadIdx.x; e < a.cols; e += kLpThreads) {
+                    const bool in = e < rp.head || e >= rp.tail_at ? rank == 0 : ((e - rp.head) / V / step) % a.split == rank;
+                    const Key c = in ? top_key(to_f32(x[e]), (uint32_t)e) : 0ull;
+                    if (c < last && c > k) k = c;
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) {
+                    const Key b = shfl_key(k, o);
+                    k = b > k ? b : k;
+                }
+                __syncthreads();
+                if (lane == 0) sh.lanes[0][warp] = k;
+                __syncthreads();
+                k = sh.lanes[0][0];
+#pragma unroll
+                for (int w = 1; w < kLpWarps; w++) k = sh.lanes[0][w] > k ? sh.lanes[0][w] : k;
+                last = k;
+                if (threadIdx.x == 0) sh.best[j] = k;
+            }
+            if (threadIdx.x >= a.top && threadIdx.x < 32) sh.best[threadIdx.x] = 0ull;
+            __syncthreads();
+        }
+        // the cluster's sums and keys, in block 0
+        Key best = 0ull;
+        if (warp == 0 && a.top) best = sh.best[lane];
+        if (a.split > 1) {
+            if (warp == 0 && rank) {
+                if (lane == 0) remote_store(&sh.parts[rank], 0, t);
+                if (a.top) remote_store(&sh.part_keys[rank][lane], 0, best);
+            }
+            lp_cluster_barrier();
+            if (warp == 0 && rank == 0)
+                for (int r = 1; r < a.split; r++) {
+                    t = join(t, sh.parts[r]);       // in every lane, of which lane 0 counts
+                    if (a.top) best = merge32(best, sh.part_keys[r][lane], lane);
+                }
+        }
+        if (warp == 0 && rank == 0) {
+            // lane 0 has the sums in their order
+            t = {__shfl_sync(0xffffffffu, t.m, 0), __shfl_sync(0xffffffffu, t.s, 0), __shfl_sync(0xffffffffu, t.d, 0)};
+            const bool none = t.m == lowest && t.s == 0.0f;     // every logit is -inf
+            const float lz = logf(t.s);
+            if (lane == 0) {
+                if (a.lse) a.lse[row] = none ? ninf : t.m + lz;
+                if (a.entropy) a.entropy[row] = none ? 0.0f : lz - t.d / t.s;
+                if (a.logp) {
+                    const int64_t id = a.ids[row];
+                    a.logp[row] = id < 0 || id >= a.cols ? 0.0f : (none ? ninf : (to_f32(x[id]) - t.m) - lz);
+                }
+            }
+            if (lane < a.top) {
+                a.top_ids[row * a.top + lane] = best ? (int64_t)key_place(best) : -1;
+                a.top_logp[row * a.top + lane] = best ? (to_f32(x[key_place(best)]) - t.m) - lz : ninf;
             }
         }
+        if (a.split > 1) lp_cluster_barrier();          // the parts are written again
+        else __syncthreads();                           // and so are the block's own numbers
     }
 }
 
@@ -128,35 +378,87 @@ struct LpGradArgs {
     const float *lse, *entropy, *dlogp, *dentropy;
     void* dx;
     int64_t lddx;
-    int vec, dvec;
+    int split;                          // blocks of a row
 };
 
-// dx = g (1_t - p) - gH p (log p + H), p = e^(x - lse).
+// dx = g (1_t - p) - gH p (log p + H), p = e^(x - lse): a read and a write of
+// every logit, HBM-bound.  A row's values before and after its 16-byte vectors
+// go one a thread; where x and dx lie differently within 16 bytes, all do.
 template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads) logprobs_grad_kernel(const LpGradArgs a)
+__global__ void __launch_bounds__(256) logprobs_grad_kernel(const LpGradArgs a)
 {
     using T = Elem<TYPE>;
+    constexpr int V = 16 / sizeof(T), U = 4, THREADS = 256;
     griddep_wait();
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int64_t total = a.rows * a.split;
+    for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+        const int64_t row = w / a.split;
+        const int part = (int)(w - row * a.split);
         const T* x = static_cast<const T*>(a.x) + row * a.ldx;
         T* dx = static_cast<T*>(a.dx) + row * a.lddx;
         const int64_t t = a.ids ? a.ids[row] : -1;
-        const float g = a.dlogp && t >= 0 && t < a.cols ? a.dlogp[row] : 0.0f;
-        const float gh = a.dentropy ? a.dentropy[row] : 0.0f, H = a.dentropy ? a.entropy[row] : 0.0f;
         const float lse = a.lse[row];
-        for (int64_t e = threadIdx.x * 8; e < a.cols; e += kLpThreads * 8) {
-            float v[8];
-            load8_to(x + e, a.cols - e, a.vec, v);
+        float g = a.dlogp && t >= 0 && t < a.cols ? a.dlogp[row] : 0.0f;
+        const float at_id = g;
+        const float gh = a.dentropy ? a.dentropy[row] : 0.0f;
+        // p (gH log p + gH H + g); a row whose lse is NaN has NaN gradients
+        g = a.dentropy ? fmaf(gh, a.entropy[row], g) : g;
+        if (lse != lse) g = lse;
+        auto grad = [&](float v) {
+            const float lp = fmaxf(v - lse, -200.0f);   // p is 0 there
+            return -__expf(lp) * fmaf(gh, lp, g);
+        };
+        RowParts<T> rp(x, a.cols);
+        if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15u) != 0) {
+            rp.head = 0;
+            rp.vecs = 0;
+            rp.tail_at = 0;
+        }
+        const T* xv = x + rp.head;
+        T* dv = dx + rp.head;
+        const int64_t at_vec = t >= rp.head && t < rp.tail_at ? (t - rp.head) / V : -1;
+        const int at_j = (int)((t - rp.head) % V);
+        for (int64_t i0 = (int64_t)part * THREADS * U + threadIdx.x; i0 < rp.vecs; i0 += (int64_t)a.split * THREADS * U) {
+            uint4 raw[U];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float lp = v[i] - lse;
-                const float p = __expf(lp);
-                // a masked logit has no gradient (a row of them lse = -inf)
-                const bool zero = v[i] == __int_as_float(0xff800000) || p == 0.0f;
-                v[i] = zero ? 0.0f : -p * fmaf(gh, lp + H, g);
-                if (e + i == t) v[i] += g;
+            for (int u = 0; u < U; u++)
+                if (i0 + u * THREADS < rp.vecs) raw[u] = reinterpret_cast<const uint4*>(xv)[i0 + u * THREADS];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                const int64_t i = i0 + u * THREADS;
+                if (i >= rp.vecs) break;
+                float v[V];
+                if constexpr (V == 8) {
+                    unpack2<T>(raw[u].x, v[0], v[1]);
+                    unpack2<T>(raw[u].y, v[2], v[3]);
+                    unpack2<T>(raw[u].z, v[4], v[5]);
+                    unpack2<T>(raw[u].w, v[6], v[7]);
+                } else {
+                    v[0] = __uint_as_float(raw[u].x); v[1] = __uint_as_float(raw[u].y);
+                    v[2] = __uint_as_float(raw[u].z); v[3] = __uint_as_float(raw[u].w);
+                }
+#pragma unroll
+                for (int j = 0; j < V; j++) v[j] = grad(v[j]);
+                if (i == at_vec) {
+#pragma unroll
+                    for (int j = 0; j < V; j++)
+                        if (j == at_j) v[j] += at_id;
+                }
+                if constexpr (V == 8) {
+                    reinterpret_cast<uint4*>(dv)[i] =
+                        make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+                } else {
+                    reinterpret_cast<float4*>(dv)[i] = make_float4(v[0], v[1], v[2], v[3]);
+                }
             }
-            store8_to(dx + e, a.cols - e, a.dvec, v);
+        }
+        // the rest, one by one
+        const int64_t rest = rp.head + (a.cols - rp.tail_at);
+        for (int64_t k = (int64_t)part * THREADS + threadIdx.x; k < rest; k += (int64_t)a.split * THREADS) {
+            const int64_t e = k < rp.head ? k : rp.tail_at + (k - rp.head);
+            float v = grad(to_f32(x[e]));
+            if (e == t) v += at_id;
+            dx[e] = from_f32<T>(v);
         }
     }
 }
@@ -166,25 +468,44 @@ __global__ void __launch_bounds__(kLpThreads) logprobs_grad_kernel(const LpGradA
 cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids, int top,
                             float* logp, float* entropy, float* lse, float* top_logp, int64_t* top_ids, cudaStream_t st)
 {
-    LpArgs a{x, rows, cols, ldx, ids, top, logp, entropy, lse, top_logp, top_ids, 0};
-    a.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ldx * type_bytes(type) % 16 == 0;
-    const int64_t cap = (int64_t)device_sm_count() * 8;
+    LpArgs a{x, rows, cols, ldx, ids, top, 1, logp, entropy, lse, top_logp, top_ids};
+    // Rows that do not fill the SMs are split over clusters of 2, 4 or 8
+    // blocks, as long as each has a block of logits.
+    const int64_t sms = device_sm_count();
+    while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * kLpThreads * kLpValues) a.split *= 2;
+    const int64_t cap = 4 * sms / a.split;
+    const unsigned blocks = (unsigned)((rows < cap ? rows : cap) * a.split);
     using Kernel = void (*)(const LpArgs);
     static const Kernel kernels[3] = {logprobs_kernel<ESB_F32>, logprobs_kernel<ESB_F16>, logprobs_kernel<ESB_BF16>};
-    return launch_pdl(kernels[type], dim3((unsigned)(rows < cap ? rows : cap)), dim3(kLpThreads), 0, st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(kLpThreads);
+    cfg.dynamicSmemBytes = sizeof(LpShared);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernels[type], a);
 }
 
 cudaError_t launch_logprobs_grad(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids,
                                  const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dx,
                                  int64_t lddx, cudaStream_t st)
 {
-    LpGradArgs a{x, rows, cols, ldx, ids, lse, entropy, dlogp, dentropy, dx, lddx, 0, 0};
-    a.vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && ldx * type_bytes(type) % 16 == 0;
-    a.dvec = (reinterpret_cast<uintptr_t>(dx) & 15u) == 0 && lddx * type_bytes(type) % 16 == 0;
-    const int64_t cap = (int64_t)device_sm_count() * 8;
+    LpGradArgs a{x, rows, cols, ldx, ids, lse, entropy, dlogp, dentropy, dx, lddx, 1};
+    const int64_t sms = device_sm_count(), per = 256 * 4 * (type == ESB_F32 ? 4 : 8);
+    // blocks of a row: enough of them for the SMs, none without values
+    while (rows * a.split < 16 * sms && (int64_t)a.split * 2 * per <= cols + per) a.split *= 2;
+    const int64_t total = rows * a.split, cap = 8 * sms;
     using Kernel = void (*)(const LpGradArgs);
     static const Kernel kernels[3] = {logprobs_grad_kernel<ESB_F32>, logprobs_grad_kernel<ESB_F16>, logprobs_grad_kernel<ESB_BF16>};
-    return launch_pdl(kernels[type], dim3((unsigned)(rows < cap ? rows : cap)), dim3(kLpThreads), 0, st, a);
+    return launch_pdl(kernels[type], dim3((unsigned)(total < cap ? total : cap)), dim3(256), 0, st, a);
 }
 
 }  // namespace esb

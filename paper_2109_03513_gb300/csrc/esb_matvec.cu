@@ -37,7 +37,8 @@ namespace esb {
 namespace {
 
 constexpr int kRedLd = 20;          // floats between columns of a warp's 16 sums
-constexpr int kSlice = 512;         // codes of a row that a warp has in flight: 4 steps of 128, 16 bytes a lane and row
+constexpr int kSteps = 4;           // steps of 128 codes of a row, 16 bytes a lane and row, that a warp has in flight
+constexpr int kSlice = 128 * kSteps;
 
 // fp16 high bytes of the elements by the code's low 3 bits; 2^16 and 2^4.
 struct MvTable {
@@ -133,7 +134,7 @@ __host__ inline size_t mv_sums(int cols, int warps) { return (size_t)2 * warps *
 
 __device__ __forceinline__ void cluster_barrier()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
 __device__ __forceinline__ float ld_cluster(const float* p, int rank)
 {
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     griddep_launch_dependents();
     // Loads of the slice after the one in work go into each step's registers as
     // soon as that step is done.
-    uint4 buf[4][2];
+    uint4 buf[kSteps][2];
     float sc[2][R];                                     // scales of step t of the slice, rows g and g + 8
     const uint32_t* pw[2];                              // this lane's place in the slice that is loaded next
     const float* ps[2];
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     auto load_scales = [&]() {
 #pragma unroll
         for (int j = 0; j < R; j++) {
-            const uint32_t k32 = (uint32_t)p_k / 32 + t * 4 + j * (4 / R);
+            const uint32_t k32 = (uint32_t)p_k / 32 + (t % kSteps) * 4 + j * (4 / R);
             const uint32_t gi = a.gmagic ? __umulhi(k32, a.gmagic) : k32;
             const bool in = gi < (uint32_t)a.ngroups;
             sc[0][j] = in ? __ldg(ps[0] + gi) : 0.0f;
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     rows_of();
     if (wj < slices) {
 #pragma unroll
-        for (int c = 0; c < 4; c++) load_step(c);
+        for (int c = 0; c < kSteps; c++) load_step(c);
         load_scales();
     }
 
@@ -382,9 +383,9 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
                 rows_of();
             }
             if (more) load_scales();
-            const uint32_t xo = (uint32_t)sl * 1024u, fo = fp + (uint32_t)sl * (128u * NT);
+            const uint32_t xo = (uint32_t)sl * (256u * kSteps), fo = fp + (uint32_t)sl * (32u * kSteps * NT);
 #pragma unroll
-            for (int c = 0; c < 4; c++) {
+            for (int c = 0; c < kSteps; c++) {
                 const uint32_t wa[4] = {buf[c][0].x, buf[c][0].y, buf[c][0].z, buf[c][0].w};
                 const uint32_t wb[4] = {buf[c][1].x, buf[c][1].y, buf[c][1].z, buf[c][1].w};
                 float sum[NT][4];

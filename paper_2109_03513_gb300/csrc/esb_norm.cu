@@ -16,7 +16,7 @@ struct NormArgs {
     int64_t rows, cols;
     esb_norm n;
     int64_t group, ngroups;     // columns of a group (a multiple of 32) and groups of a row; 0 without codes
-    int xvec, rvec, hvec, yvec, qvec, wvec;
+    int xvec, rvec, hvec, yvec, qvec, wvec, cvec;
     QuantFmt f;
 };
 
@@ -44,6 +44,24 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* sh)
 #pragma unroll
     for (int i = 0; i < NW; i++) t = max(t, sh[i]);
     return t;
+}
+
+// Codes (and values) of the eight values y at column e of a row.
+__device__ __forceinline__ void put_codes8(const NormArgs& a, int64_t row, int64_t e, const float (&y)[8], const GroupScale& s)
+{
+    uint32_t w[2];
+    float q[8];
+    const int64_t n = a.cols - e;
+    quantise8<8>(y, s, a.f, w, q);
+    if (n < 8) zero_past<8>(w, n, a.f);
+    uint32_t* p = a.n.codes + row * a.n.ldc + e / 4;
+    if (a.cvec && e / 4 + 1 < a.n.ldc) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    } else {
+        p[0] = w[0];
+        if (e / 4 + 1 < a.n.ldc) p[1] = w[1];
+    }
+    if (a.n.yq && n > 0) store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q);
 }
 
 // A block for each row, of any length: every pass reads the row again, and
@@ -114,26 +132,120 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
             mx = whole ? block_max<NW>(mx, shu) : __reduce_max_sync(0xffffffffu, mx);
             const float alpha = __fdiv_rn(__uint_as_float(mx), a.f.C);
             if (first == e0) a.n.scales[row * a.n.lds + g] = alpha;
-            const GroupScale s = make_scale(alpha);
+            const GroupScale s = make_scale(alpha, a.f);
             const int64_t end = g == a.ngroups - 1 ? a.n.ldc * 4 : e0 + a.group;
             for (int64_t e = first; e < end; e += step) {
-                const int64_t n = a.cols - e;
                 norm8(e);
-                if (n > 0) put8(e);
-                uint32_t c[8];
-                float q[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    c[i] = quantise(y[i], s, a.f, q[i]);
-                    q[i] = __fmul_rn(alpha, q[i]);
-                    if (i >= n) c[i] = a.f.zero_code;
-                }
-                uint32_t* cw = a.n.codes + row * a.n.ldc + e / 4;
-                cw[0] = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
-                if (e / 4 + 1 < a.n.ldc) cw[1] = c[4] | (c[5] << 8) | (c[6] << 16) | (c[7] << 24);
-                if (a.n.yq && n > 0) store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q);
+                if (e < a.cols) put8(e);
+                put_codes8(a, row, e, y, s);
             }
         }
+    }
+}
+
+// ------------------------------------------------------- rows in registers
+
+// A row of up to TPR * NV * 8 values by TPR threads, held in registers from
+// its one read to its last write; the groups of codes are 4 to 32 lanes (32 to
+// 256 values), or the row.  HBM-bound where there are many rows (8192 x 4096
+// bf16 with residual, codes and their values: 15 bytes for every 2 of x read),
+// latency-bound where there are few.
+template <int TYPE, int TPR, int NV>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rmsnorm_rows_kernel(const NormArgs a)
+{
+    using T = Elem<TYPE>;
+    constexpr int THREADS = TPR < 128 ? 128 : TPR, PER = THREADS / TPR, NW = TPR / 32;
+    __shared__ float shf[2][NW];
+    __shared__ uint32_t shu[2][NW];
+    griddep_wait();
+    const int t = threadIdx.x % TPR, lanes = (int)a.group / 8;
+    int flip = 0;
+    // a block's rows go on together, so that every thread meets every barrier
+    for (int64_t row0 = (int64_t)blockIdx.x * PER; row0 < a.rows; row0 += (int64_t)gridDim.x * PER, flip ^= 1) {
+        const int64_t row = row0 + threadIdx.x / TPR;
+        const bool on = PER == 1 || row < a.rows;
+        const T* x = static_cast<const T*>(a.n.x) + row * a.n.ldx;
+        const T* r = a.n.residual ? static_cast<const T*>(a.n.residual) + row * a.n.ldr : nullptr;
+        float z[NV][8];
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
+            load8_to(x + e, n, a.xvec, z[v]);
+        }
+        if (r) {
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
+                float u[8];
+                load8_to(r + e, n, a.rvec, u);
+#pragma unroll
+                for (int i = 0; i < 8; i++) z[v][i] = __fadd_rn(z[v][i], u[i]);
+            }
+        }
+        float ss = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) ss = fmaf(z[v][i], z[v][i], ss);
+        ss = warp_sum(ss);
+        if constexpr (NW > 1) {
+            if ((threadIdx.x & 31) == 0) shf[flip][threadIdx.x >> 5] = ss;
+            __syncthreads();
+            ss = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NW; i++) ss += shf[flip][i];
+        }
+        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)a.cols), a.n.eps)));
+        if (a.n.rstd && t == 0 && on) a.n.rstd[row] = rstd;
+        uint32_t mx = 0u;
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
+            if (a.n.h) store8_to(static_cast<T*>(a.n.h) + row * a.n.ldh + e, n, a.hvec, z[v]);
+            float w[8];
+            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, n, a.wvec, w);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                z[v][i] = __fmul_rn(z[v][i], rstd);
+                if (a.n.weight) z[v][i] = __fmul_rn(z[v][i], w[i]);
+            }
+            if (a.n.y) store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, n, a.yvec, z[v]);
+            if (a.ngroups == 1) {
+                // what lies past the row is 0 times rstd: NaN for a row that has none
+#pragma unroll
+                for (int i = 0; i < 8; i++) mx = max(mx, i < n ? magnitude_bits(z[v][i], a.f.is_signed) : 0u);
+            } else if (a.ngroups) {
+                uint32_t m = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; i++) m = max(m, i < n ? magnitude_bits(z[v][i], a.f.is_signed) : 0u);
+                for (int o = lanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const float alpha = __fdiv_rn(__uint_as_float(m), a.f.C);
+                if (on && e < a.n.ldc * 4) {
+                    if (t % lanes == 0 && n > 0) a.n.scales[row * a.n.lds + e / a.group] = alpha;
+                    put_codes8(a, row, e, z[v], make_scale(alpha, a.f));
+                }
+            }
+        }
+        if (a.ngroups == 1) {
+            mx = __reduce_max_sync(0xffffffffu, mx);
+            if constexpr (NW > 1) {
+                if ((threadIdx.x & 31) == 0) shu[flip][threadIdx.x >> 5] = mx;
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < NW; i++) mx = max(mx, shu[flip][i]);
+            }
+            const float alpha = __fdiv_rn(__uint_as_float(mx), a.f.C);
+            if (t == 0 && on) a.n.scales[row * a.n.lds] = alpha;
+            const GroupScale s = make_scale(alpha, a.f);
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int64_t e = (int64_t)(v * TPR + t) * 8;
+                if (on && e < a.n.ldc * 4) put_codes8(a, row, e, z[v], s);
+            }
+        }
+        // words past those that the threads' values reach (a long row stride)
+        if (a.ngroups && on)
+            for (int64_t w = (int64_t)TPR * NV * 2 + t; w < a.n.ldc; w += TPR) a.n.codes[row * a.n.ldc + w] = a.f.zero_code * 0x01010101u;
     }
 }
 
@@ -148,7 +260,7 @@ struct NormGradArgs {
 };
 
 // dx = rstd (d - n mean(d n)) + dh with n = h rstd, d = dy w: a block for
-// each row, which it reads twice.
+// each row of any length, which it reads twice.
 template <int TYPE>
 __global__ void __launch_bounds__(kNormThreads) rmsnorm_dx_kernel(const NormGradArgs a)
 {
@@ -190,7 +302,8 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dx_kernel(const NormGrad
     }
 }
 
-// dweight: block (x, y) adds dy n over rows y, y + parts, ... of its columns.
+// dweight of such rows: block (x, y) adds dy n over rows y, y + parts, ... of
+// its columns.
 template <int TYPE>
 __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_kernel(const NormGradArgs a)
 {
@@ -209,15 +322,120 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_kernel(const NormGrad
     store8_to(a.part + (int64_t)blockIdx.y * a.cols + e, a.cols - e, false, s);
 }
 
-// The parts' sums, in their order.
+// Both for rows in registers: a thread keeps its columns of every row of its
+// block, their weights and their part of dweight, and loads the next row while
+// it works on this one.  8192 x 4096 bf16: 268 MB of reads and writes (the
+// three kernels above read the gradient and h twice).
+template <int TYPE, int GTYPE, int TPR, int NV>
+__global__ void __launch_bounds__(TPR) rmsnorm_grad_rows_kernel(const NormGradArgs a)
+{
+    using T = Elem<TYPE>;
+    using G = Elem<GTYPE>;
+    constexpr int NW = TPR / 32;
+    __shared__ float shf[2][NW];
+    griddep_wait();
+    float w[NV][8], dw[NV][8];
+    int64_t e[NV];
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+        e[v] = (int64_t)(v * TPR + threadIdx.x) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) { w[v][i] = 1.0f; dw[v][i] = 0.0f; }
+        if (NV == 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], a.cols - e[v], a.wvec, w[v]);
+    }
+    float n[NV][8], d[NV][8], rstd = 0.0f;
+    auto load = [&](int64_t row) {
+        const bool on = row < a.rows;
+        if (on) rstd = a.n.rstd[row];
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            const int64_t left = on ? a.cols - e[v] : 0;
+            load8_to(static_cast<const T*>(a.n.h) + row * a.n.ldh + e[v], left, a.hvec, n[v]);
+            load8_to(static_cast<const G*>(a.n.dy) + row * a.n.ldg + e[v], left, a.gvec, d[v]);
+        }
+    };
+    int flip = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
+        load(row);
+        const float rs = rstd;
+        float t[8];
+        if (NV == 1 && a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[0], a.cols - e[0], a.dhvec, t);
+        float s = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            // of two vectors the weights (and dh below) are not kept: 64 registers a thread
+            if (NV > 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], a.cols - e[v], a.wvec, t);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                n[v][i] *= rs;
+                dw[v][i] = fmaf(d[v][i], n[v][i], dw[v][i]);
+                if (NV == 1) d[v][i] *= w[v][i];
+                else if (a.n.weight) d[v][i] *= t[i];
+                s = fmaf(d[v][i], n[v][i], s);
+            }
+        }
+        s = warp_sum(s);
+        if ((threadIdx.x & 31) == 0) shf[flip][threadIdx.x >> 5] = s;
+        __syncthreads();
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NW; i++) s += shf[flip][i];
+        const float m = s / (float)a.cols;
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            if (NV > 1 && a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[v], a.cols - e[v], a.dhvec, t);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                d[v][i] = rs * fmaf(-n[v][i], m, d[v][i]);
+                if (a.n.dh) d[v][i] += t[i];
+            }
+            store8_to(static_cast<T*>(a.n.dx) + row * a.n.lddx + e[v], a.cols - e[v], a.dxvec, d[v]);
+        }
+    }
+    if (a.part) {
+#pragma unroll
+        for (int v = 0; v < NV; v++) store8_to(a.part + blockIdx.x * a.cols + e[v], a.cols - e[v], (a.cols & 3) == 0, dw[v]);
+    }
+}
+
+// The parts' sums, in a fixed order: a warp's lanes take 32 columns, the
+// warps every 8th part, then the warps' sums in turn.
 __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_join_kernel(const float* part, int parts, int64_t cols, float* dw)
 {
+    __shared__ float sh[kNormThreads / 32][32];
     griddep_wait();
-    const int64_t c = (int64_t)blockIdx.x * kNormThreads + threadIdx.x;
-    if (c >= cols) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.0f;
-    for (int p = 0; p < parts; p++) s += part[p * cols + c];
-    dw[c] = s;
+    if (c < cols)
+        for (int p = warp; p < parts; p += kNormThreads / 32) s += part[p * cols + c];
+    sh[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < cols) {
+#pragma unroll
+        for (int i = 1; i < kNormThreads / 32; i++) s += sh[i][lane];
+        dw[c] = s;
+    }
+}
+
+using NormKernel = void (*)(const NormArgs);
+struct NormPlan {
+    NormKernel kernel;
+    int tpr;
+};
+// Threads for a row: few rows want all of an SM's loads at once, many rows few
+// barriers.
+template <int TYPE> NormPlan norm_plan(int64_t rows, int64_t cols, int64_t sms)
+{
+    if (cols <= 256) return {rmsnorm_rows_kernel<TYPE, 32, 1>, 32};
+    if (cols <= 512) return {rmsnorm_rows_kernel<TYPE, 32, 2>, 32};
+    if (cols <= 1024) return {rmsnorm_rows_kernel<TYPE, 128, 1>, 128};
+    if (cols <= 2048) return {rmsnorm_rows_kernel<TYPE, 256, 1>, 256};
+    if (cols <= 4096 && rows >= 4 * sms) return {rmsnorm_rows_kernel<TYPE, 256, 2>, 256};
+    if (cols <= 4096) return {rmsnorm_rows_kernel<TYPE, 512, 1>, 512};
+    if (cols <= 8192) return {rmsnorm_rows_kernel<TYPE, 512, 2>, 512};
+    if (cols <= 16384) return {rmsnorm_rows_kernel<TYPE, 1024, 2>, 1024};
+    return {rmsnorm_kernel<TYPE>, 0};
 }
 
 bool rows16(const void* p, int64_t ld, int type)
@@ -225,7 +443,31 @@ bool rows16(const void* p, int64_t ld, int type)
     return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * type_bytes(type) % 16 == 0;
 }
 
-int dw_parts(int64_t rows) { return (int)(rows < 64 ? 1 : (rows < 64 * 64 ? rows / 64 : 64)); }
+using GradKernel = void (*)(const NormGradArgs);
+struct GradPlan {
+    GradKernel kernel;
+    int tpr;
+};
+template <int TYPE, int GTYPE> GradPlan grad_plan(int64_t cols)
+{
+    if (cols <= 256) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 32, 1>, 32};
+    if (cols <= 1024) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 128, 1>, 128};
+    if (cols <= 2048) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 256, 1>, 256};
+    if (cols <= 4096) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 512, 1>, 512};
+    if (cols <= 8192) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 1024, 1>, 1024};
+    if (cols <= 16384) return {rmsnorm_grad_rows_kernel<TYPE, GTYPE, 1024, 2>, 1024};
+    return {nullptr, 0};
+}
+
+// Parts of dweight, one for each block: as many as the SMs hold (fewer where
+// a part would get less than 4 rows).
+int dw_parts(int64_t rows, int64_t cols)
+{
+    const GradPlan p = grad_plan<ESB_BF16, ESB_BF16>(cols);
+    int64_t n = p.tpr ? (int64_t)device_sm_count() * (p.tpr >= 1024 ? 1 : 1024 / p.tpr) : 64;
+    if (n > (rows + 3) / 4) n = (rows + 3) / 4;
+    return (int)(n < 1 ? 1 : n);
+}
 
 }  // namespace
 
@@ -245,14 +487,24 @@ cudaError_t launch_rmsnorm(int64_t rows, int64_t cols, const esb_norm& n, cudaSt
     a.yvec = rows16(n.y, n.ldy, n.y_type);
     a.qvec = rows16(n.yq, n.ldq, n.y_type);
     a.wvec = rows16(n.weight, 0, n.w_type);
-    const int64_t cap = (int64_t)device_sm_count() * 8;
-    const unsigned blocks = (unsigned)(rows < cap ? rows : cap);
-    using Kernel = void (*)(const NormArgs);
-    static const Kernel kernels[3] = {rmsnorm_kernel<ESB_F32>, rmsnorm_kernel<ESB_F16>, rmsnorm_kernel<ESB_BF16>};
-    return launch_pdl(kernels[n.x_type], dim3(blocks), dim3(kNormThreads), 0, st, a);
+    a.cvec = n.codes && (reinterpret_cast<uintptr_t>(n.codes) & 7u) == 0 && n.ldc % 2 == 0;
+    const int64_t sms = device_sm_count();
+    static NormPlan (*const plans[3])(int64_t, int64_t, int64_t) = {norm_plan<ESB_F32>, norm_plan<ESB_F16>, norm_plan<ESB_BF16>};
+    static const NormKernel any[3] = {rmsnorm_kernel<ESB_F32>, rmsnorm_kernel<ESB_F16>, rmsnorm_kernel<ESB_BF16>};
+    NormPlan p = plans[n.x_type](rows, cols, sms);
+    const bool lanes = a.ngroups <= 1 || a.group == 32 || a.group == 64 || a.group == 128 || a.group == 256;
+    if (!p.tpr || !lanes) {
+        const int64_t cap = sms * 8;
+        return launch_pdl(any[n.x_type], dim3((unsigned)(rows < cap ? rows : cap)), dim3(kNormThreads), 0, st, a);
+    }
+    const int threads = p.tpr < 128 ? 128 : p.tpr;
+    int64_t blocks = (rows + threads / p.tpr - 1) / (threads / p.tpr);
+    const int64_t cap = sms * (2048 / threads) * 2;
+    if (blocks > cap) blocks = cap;
+    return launch_pdl(p.kernel, dim3((unsigned)blocks), dim3((unsigned)threads), 0, st, a);
 }
 
-size_t rmsnorm_grad_workspace_bytes(int64_t rows, int64_t cols) { return sizeof(float) * (size_t)dw_parts(rows) * (size_t)cols; }
+size_t rmsnorm_grad_workspace_bytes(int64_t rows, int64_t cols) { return sizeof(float) * (size_t)dw_parts(rows, cols) * (size_t)cols; }
 
 cudaError_t launch_rmsnorm_grad(int64_t rows, int64_t cols, const esb_norm_grad& n, void* workspace, cudaStream_t st)
 {
@@ -263,22 +515,31 @@ cudaError_t launch_rmsnorm_grad(int64_t rows, int64_t cols, const esb_norm_grad&
     a.dhvec = rows16(n.dh, n.lddh, n.x_type);
     a.dxvec = rows16(n.dx, n.lddx, n.x_type);
     a.wvec = rows16(n.weight, 0, n.w_type);
-    a.part = static_cast<float*>(workspace);
-    a.parts = dw_parts(rows);
-    using Kernel = void (*)(const NormGradArgs);
-    static const Kernel dxs[3] = {rmsnorm_dx_kernel<ESB_F32>, rmsnorm_dx_kernel<ESB_F16>, rmsnorm_dx_kernel<ESB_BF16>};
-    static const Kernel dws[3] = {rmsnorm_dw_kernel<ESB_F32>, rmsnorm_dw_kernel<ESB_F16>, rmsnorm_dw_kernel<ESB_BF16>};
-    cudaError_t e = cudaSuccess;
-    if (n.dweight) {
-        const unsigned bx = (unsigned)((cols + kNormThreads * 8 - 1) / (kNormThreads * 8));
-        e = launch_pdl(dws[n.x_type], dim3(bx, (unsigned)a.parts), dim3(kNormThreads), 0, st, a);
-        if (e != cudaSuccess) return e;
-        e = launch_pdl(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + kNormThreads - 1) / kNormThreads)), dim3(kNormThreads), 0, st,
-                       (const float*)a.part, a.parts, cols, n.dweight);
-        if (e != cudaSuccess) return e;
+    a.part = n.dweight ? static_cast<float*>(workspace) : nullptr;
+    a.parts = dw_parts(rows, cols);
+    GradPlan p{nullptr, 0};
+    if (n.g_type == n.x_type) {
+        static GradPlan (*const same[3])(int64_t) = {grad_plan<ESB_F32, ESB_F32>, grad_plan<ESB_F16, ESB_F16>, grad_plan<ESB_BF16, ESB_BF16>};
+        p = same[n.x_type](cols);
     }
-    const int64_t cap = (int64_t)device_sm_count() * 8;
-    return launch_pdl(dxs[n.x_type], dim3((unsigned)(rows < cap ? rows : cap)), dim3(kNormThreads), 0, st, a);
+    cudaError_t e = cudaSuccess;
+    if (p.kernel) {
+        e = launch_pdl(p.kernel, dim3((unsigned)a.parts), dim3((unsigned)p.tpr), 0, st, a);
+    } else {
+        static const GradKernel dxs[3] = {rmsnorm_dx_kernel<ESB_F32>, rmsnorm_dx_kernel<ESB_F16>, rmsnorm_dx_kernel<ESB_BF16>};
+        static const GradKernel dws[3] = {rmsnorm_dw_kernel<ESB_F32>, rmsnorm_dw_kernel<ESB_F16>, rmsnorm_dw_kernel<ESB_BF16>};
+        if (n.dweight) {
+            // before dx, which may lie on the gradient or on h
+            const unsigned bx = (unsigned)((cols + kNormThreads * 8 - 1) / (kNormThreads * 8));
+            e = launch_pdl(dws[n.x_type], dim3(bx, (unsigned)a.parts), dim3(kNormThreads), 0, st, a);
+            if (e != cudaSuccess) return e;
+        }
+        const int64_t cap = (int64_t)device_sm_count() * 8;
+        e = launch_pdl(dxs[n.x_type], dim3((unsigned)(rows < cap ? rows : cap)), dim3(kNormThreads), 0, st, a);
+    }
+    if (e != cudaSuccess || !n.dweight) return e;
+    return launch_pdl(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(kNormThreads), 0, st, (const float*)a.part, a.parts,
+                      cols, n.dweight);
 }
 
 }  // namespace esb

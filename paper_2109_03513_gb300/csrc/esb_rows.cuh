@@ -135,94 +135,125 @@ __device__ __forceinline__ float warp_sum(float v)
 
 // Projection constants of a format with b = 4 or 8.
 struct QuantFmt {
-    int b, k, is_signed, even;
-    uint32_t zero_code, max_code, C_bits;
-    float C, pk, ipk;       // largest value; 2^k and 2^-k
+    int k, is_signed, even, linear;   // linear: the set has one spacing
+    uint32_t zero_code, rotate;       // added to places, it gives codes (modulo the sign bit)
+    float C, Ck, pk, ipk;             // largest value, 2^k times it, 2^k and 2^-k
 };
 
 __host__ inline QuantFmt make_quant_fmt(const esb_format& f, int rounding)
 {
     const ProjParams p = make_proj_params(f.b, f.k, f.is_signed, rounding);
     QuantFmt q;
-    q.b = f.b; q.k = f.k; q.is_signed = f.is_signed; q.even = rounding;
-    q.zero_code = p.zero_code; q.max_code = p.max_code; q.C_bits = p.C_bits;
+    q.k = f.k; q.is_signed = f.is_signed; q.even = rounding;
+    q.linear = p.N <= 1;
+    q.zero_code = p.zero_code;
+    q.rotate = p.zero_code * (f.b == 4 ? 0x11111111u : 0x01010101u);
     q.C = fmt_C(f.b, f.k);
     q.pk = (float)(1 << f.k);
+    q.Ck = q.C * q.pk;
     q.ipk = 1.0f / q.pk;
     return q;
 }
 
 // A group's scale with what its divisions need.
 struct GroupScale {
-    float alpha, rcp;
+    float alpha, step, rcp; // step = alpha 2^-k, rcp = 1 / step
     bool fast;              // alpha far from the ends of fp32
 };
 
-__device__ __forceinline__ GroupScale make_scale(float alpha)
+__device__ __forceinline__ GroupScale make_scale(float alpha, const QuantFmt& f)
 {
     GroupScale s;
     s.alpha = alpha;
     s.fast = alpha > 0x1p-60f && alpha < 0x1p60f;
-    s.rcp = s.fast ? __frcp_rn(alpha) : 0.0f;
+    s.step = alpha * f.ipk;
+    s.rcp = s.fast ? __frcp_rn(s.step) : 0.0f;
     return s;
 }
 
-// |x| / alpha, rounded to nearest as IEEE division.  Many values share alpha,
-// so its correctly rounded reciprocal y is found once; q = a y is then within
-// two units of a / alpha, one step with the exact remainder makes it faithful,
-// and by Markstein's theorem (Computation of elementary functions on the IBM
-// RISC System/6000 processor, 1990) a second one rounds it correctly.  A scale
-// at the ends of fp32, where a remainder could underflow, takes the division.
-__device__ __forceinline__ float scaled_abs(float x, const GroupScale& s)
+// |x| / alpha (max(x, 0) / alpha for the unsigned set) times 2^k, rounded to
+// nearest as IEEE division (the power of two is exact).  Many values share
+// alpha, so its correctly rounded reciprocal y is found once; q = a y is then
+// within two units of a / alpha, one step with the exact remainder makes it
+// faithful, and by Markstein's theorem (Computation of elementary functions on
+// the IBM RISC System/6000 processor, 1990) a second one rounds it correctly.
+// A scale at the ends of fp32, where a remainder could underflow, takes the
+// division.
+__device__ __forceinline__ float scaled_value(float x, const GroupScale& s, const QuantFmt& f)
 {
-    const float a = fabsf(x);
-    if (!s.fast) return __fdiv_rn(a, s.alpha);
+    const float a = f.is_signed ? fabsf(x) : fmaxf(x, 0.0f);
+    if (!s.fast) return __fdiv_rn(a, s.alpha) * f.pk;
     float q = __fmul_rn(a, s.rcp);
-    q = __fmaf_rn(__fmaf_rn(-q, s.alpha, a), s.rcp, q);
-    return __fmaf_rn(__fmaf_rn(-q, s.alpha, a), s.rcp, q);
+    q = __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
+    return __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
 }
 
-// The code of x and the set element it stands for (in units of alpha), as
-// project_scaled.  At and above 1 the k leading fraction bits are kept, and a
-// carry into the next binade is the next code; below 1 the spacing is 2^-k,
-// and elements 0 .. 2^k take the codes N 2^k + r modulo 2^(b-1), so r = 2^k is
-// the code of 1.  An alpha of 0 (a group of zeros) or one that is not finite
-// gives zero codes.
-__device__ __forceinline__ uint32_t quantise(float x, const GroupScale& s, const QuantFmt& f, float& q)
+// Eight values to codes: their places in the ascending non-negative set (and
+// the sign bits), then the words.  Place j has the code (j - 2^k) mod 2^(b-1),
+// so the words take one add and a mask; zero keeps sign 0.  Places are found
+// with t = 2^k |x| / alpha: below 2^k (values below 1) the place is t rounded;
+// above, the k leading fraction bits are kept, and a carry into the next
+// binade is the next place.  q receives the numbers that the codes stand for.
+// An alpha of 0 (a group of zeros) or one that is not finite gives zero codes;
+// otherwise no value of the group is NaN.
+template <int B>
+__device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&q)[8])
 {
-    const float v = scaled_abs(x, s);
-    const uint32_t u = __float_as_uint(v);
-    uint32_t code;
-    if (u >= 0x3f800000u) {
-        const int sh = 23 - f.k;
-        const uint32_t half = 1u << (sh - 1);
-        const uint32_t odd = f.k ? (u >> sh) & 1u : 1u;       // k = 0: the one significant bit
-        const uint32_t r = (u + (f.even ? half - 1u + odd : half)) >> sh;
-        code = r - (127u << f.k);
-        q = __uint_as_float(r << sh);
-    } else {
-        // round to nearest by the addition of 2^23; half away from zero as
+    constexpr int PER = 32 / B;
+    constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
+    constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
+    uint32_t S[B / 4];
+#pragma unroll
+    for (int i = 0; i < B / 4; i++) w[i] = S[i] = 0u;
+    const bool dead = !(s.alpha > 0.0f && s.alpha < __int_as_float(0x7f800000));
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float t = fminf(scaled_value(x[i], s, f), f.Ck);
+        uint32_t j;
+        float r;
+        // rounded to nearest by the addition of 2^23; half away from zero as
         // the floor of t + 1/2, both sums truncated
-        const float t = v * f.pk;
         const float big = f.even ? __fadd_rn(t, 8388608.0f) : __fadd_rz(__fadd_rz(t, 0.5f), 8388608.0f);
-        const uint32_t r = __float_as_uint(big) - 0x4B000000u;
-        code = (f.zero_code + r) & ((1u << (f.b - 1)) - 1u);
-        q = (big - 8388608.0f) * f.ipk;
+        j = __float_as_uint(big) - 0x4B000000u;
+        r = big - 8388608.0f;
+        if (!f.linear) {
+            const uint32_t u = __float_as_uint(t);
+            const int sh = 23 - f.k;
+            const uint32_t odd = f.k ? (u >> sh) & 1u : 1u;          // k = 0: the one significant bit
+            const uint32_t h = (u + (f.even ? (1u << (sh - 1)) - 1u + odd : 1u << (sh - 1))) >> sh;
+            const bool above = t >= f.pk;
+            // place 2^k is t = 2^k, whose leading bits are (127 + k) 2^k
+            j = above ? h - (((126u + (uint32_t)f.k) << f.k)) : j;
+            r = above ? __uint_as_float(h << sh) : r;
+        }
+        w[i / PER] += j << (B * (i % PER));
+        S[i / PER] |= ((__float_as_uint(x[i]) >> 31) & (uint32_t)f.is_signed) << (B * (i % PER) + B - 1);
+        r = dead ? 0.0f : r;
+        r = s.fast ? __fmul_rn(s.step, r) : __fmul_rn(s.alpha, r * f.ipk);
+        q[i] = x[i] < 0.0f ? -r : r;
     }
-    if (u >= f.C_bits) {
-        code = f.max_code;
-        q = f.C;
+#pragma unroll
+    for (int i = 0; i < B / 4; i++) {
+        if (dead) w[i] = 0u;
+        const uint32_t nz = (w[i] + (TOP - ONES)) & TOP;
+        w[i] = ((w[i] + f.rotate) & ~TOP) | (S[i] & nz);
     }
-    if (u > 0x7f800000u || !(s.alpha > 0.0f) || (x < 0.0f && !f.is_signed) || q == 0.0f) {
-        code = f.zero_code;
-        q = 0.0f;
-        return code;
+}
+
+// The words of eight codes of which only the first n are a row's: the rest
+// become the zero code.
+template <int B>
+__device__ __forceinline__ void zero_past(uint32_t (&w)[B / 4], int64_t n, const QuantFmt& f)
+{
+    constexpr int PER = 32 / B;
+    constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
+#pragma unroll
+    for (int i = 0; i < B / 4; i++) {
+        const int64_t k = n - i * PER;
+        if (k >= PER) continue;
+        const uint32_t keep = k <= 0 ? 0u : (1u << (B * (int)k)) - 1u;
+        w[i] = (w[i] & keep) | ((f.zero_code * ONES) & ~keep);
     }
-    if (x < 0.0f) {
-        code |= 1u << (f.b - 1);
-        q = -q;
-    }
-    return code;
 }
 
 // Magnitude of x that a group's largest value is taken over, as bits: those
