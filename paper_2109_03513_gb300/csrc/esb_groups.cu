@@ -45,13 +45,10 @@ __device__ __forceinline__ void project8(const GroupArgs& a, int64_t row, int64_
         for (int i = 0; i < B / 4; i++)
             if (vec * (B / 4) + i < a.ldc) p[i] = w[i];
     }
-    if (a.xq && n > 0) store8_any(a.xq, a.xq_type, row * a.ldq + vec * 8, n, a.qvec, q);
+    if (!a.xq || n <= 0) return;
+    element_values(v, s, a.f, q);
+    store8_any(a.xq, a.xq_type, row * a.ldq + vec * 8, n, a.qvec, q);
 }
-
-// alpha of a group of n values from its sums: the largest magnitude over C,
-// or alpha* (spread + 1e-7) in fp32, spread the standard deviation about the
-// group's own mean (signed) or the root mean square (unsigned).
-__device__ __forceinline__ float absmax_scale(uint32_t mx, const QuantFmt& f) { return __fdiv_rn(__uint_as_float(mx), f.C); }
 
 // A warp for each group, of any length: the values are read twice or, for
 // the DDA scale, three times.
@@ -111,81 +108,133 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
     }
 }
 
-// Groups of 32, 64, 128 or 256 values: 8 a lane, LANES lanes to a group, the
-// values in registers from the scale to the codes, kVecs vectors of 8 in
-// flight.  Rows are padded to whole groups (`vecs` vectors); a thread goes on
-// by dr rows and dv vectors.  16384 x 4096 bf16 with values: 302 MB of reads
-// and writes; two passes by a warp for each group took 422 us.
-constexpr int kVecs = 4;
+// Groups of 32, 64, 128 or 256 values: 16 a lane, LANES lanes to a group, the
+// values in registers from the scale to the codes, kChunks times 16 of them in
+// flight.  Rows are padded to whole groups (`chunks` sixteens); a thread goes
+// on by dr rows and dc sixteens.  Instructions bound it (16384 x 4096 bf16 to
+// (4,2) with values, 302 MB of reads and writes): a value may cost 24 at the
+// copy rate, and the quotient, its rounding and sign, the element's value and
+// a sixteenth of the group's scale take about as many.
+constexpr int kChunks = 2;
 template <int TYPE, int B, int LANES>
-__global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(const GroupArgs a, int64_t vecs, int64_t dr, int64_t dv)
+__global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(const GroupArgs a, int chunks, int dr, int dc)
 {
     using T = Elem<TYPE>;
     griddep_wait();
-    const int64_t at = (int64_t)blockIdx.x * kGroupThreads + threadIdx.x;
-    int64_t row = at / vecs, vec = at - row * vecs;
-    const int part = threadIdx.x % LANES;               // vecs and a block are whole groups
+    const int at = (int)blockIdx.x * kGroupThreads + (int)threadIdx.x;
+    int row = at / chunks, chunk = at - row * chunks;
+    const int part = threadIdx.x % LANES;               // chunks and a block are whole groups
+    const int rows = (int)a.rows;
     auto total = [&](float v) {
 #pragma unroll
         for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     };
-    while (__any_sync(0xffffffffu, row < a.rows)) {
-        float v[kVecs][8];
-        int64_t rows[kVecs], at_vec[kVecs];
+    while (__any_sync(0xffffffffu, row < rows)) {
+        Raw8<T> raw[kChunks][2];
+        int in_row[kChunks], in_chunk[kChunks];
 #pragma unroll
-        for (int u = 0; u < kVecs; u++) {
-            rows[u] = row;
-            at_vec[u] = vec;
-            const int64_t n = row < a.rows ? a.cols - vec * 8 : 0;
-            load8_to(static_cast<const T*>(a.x) + row * a.ldx + vec * 8, n, a.xvec, v[u]);
+        for (int u = 0; u < kChunks; u++) {
+            in_row[u] = row;
+            in_chunk[u] = chunk;
+            const int64_t e = (int64_t)chunk * 16, n = row < rows ? a.cols - e : 0;
+            const T* x = static_cast<const T*>(a.x) + row * a.ldx + e;
+            raw[u][0].load(x, n, a.xvec);
+            raw[u][1].load(x + 8, n - 8, a.xvec);
             row += dr;
-            vec += dv;
-            if (vec >= vecs) { vec -= vecs; row++; }
+            chunk += dc;
+            if (chunk >= chunks) { chunk -= chunks; row++; }
         }
 #pragma unroll
-        for (int u = 0; u < kVecs; u++) {
+        for (int u = 0; u < kChunks; u++) {
+            const int64_t e = (int64_t)in_chunk[u] * 16;
+            float v[2][8];
+            raw[u][0].values(v[0]);
+            raw[u][1].values(v[1]);
             float alpha;
             if (a.rule == ESB_SCALE_ABSMAX) {
                 uint32_t mx = 0u;
+                if (TYPE != ESB_F32 && a.f.is_signed) {
+                    // magnitudes in pairs of 16 bits, which order as the numbers do
 #pragma unroll
-                for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(v[u][i], a.f.is_signed));
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int i = 0; i < 4; i++) mx = __vmaxu2(mx, raw[u][h].w[i] & 0x7fff7fffu);
+                    mx = max(mx & 0xffffu, mx >> 16);
+                    const uint16_t m16 = (uint16_t)mx;
+                    mx = __float_as_uint(to_f32(*reinterpret_cast<const T*>(&m16)));
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(v[h][i], a.f.is_signed));
+                }
 #pragma unroll
                 for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 alpha = absmax_scale(mx, a.f);
             } else {
-                const int64_t left = a.cols - (at_vec[u] - part) * 8;
-                const float n = (float)(left < 8 * LANES ? left : 8 * LANES);
+                const int64_t left = a.cols - (e - part * 16);
+                const float n = (float)(left < 16 * LANES ? left : 16 * LANES);
                 float mean = 0.0f, s2 = 0.0f;
                 if (a.f.is_signed) {
 #pragma unroll
-                    for (int i = 0; i < 8; i++) mean += v[u][i];
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int i = 0; i < 8; i++) mean += v[h][i];
                     mean = total(mean) / n;
                 }
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float d = at_vec[u] * 8 + i < a.cols ? v[u][i] - mean : 0.0f;
-                    s2 = fmaf(d, d, s2);
-                }
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        const float d = e + 8 * h + i < a.cols ? v[h][i] - mean : 0.0f;
+                        s2 = fmaf(d, d, s2);
+                    }
                 alpha = __fmul_rn(a.astar, __fadd_rn(__fsqrt_rn(total(s2) / n), 1e-7f));
             }
-            if (rows[u] >= a.rows) continue;
-            const int64_t gi = at_vec[u] / LANES;
-            if (part == 0 && gi < a.ngroups) a.scales[rows[u] * a.lds + gi] = alpha;
-            project8<B>(a, rows[u], at_vec[u], v[u], make_scale(alpha, a.f));
+            if (in_row[u] >= rows) continue;
+            const int64_t gi = in_chunk[u] / LANES;
+            if (part == 0 && gi < a.ngroups) a.scales[in_row[u] * a.lds + gi] = alpha;
+            const GroupScale s = make_scale(alpha, a.f);
+            uint32_t w[2][B / 4];
+            float r[2][8];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                quantise8<B>(v[h], s, a.f, w[h], r[h]);
+                const int64_t n = a.cols - e - 8 * h;
+                if (n < 8) zero_past<B>(w[h], n, a.f);
+            }
+            constexpr int WORDS = B / 2;                // of 16 codes
+            uint32_t* p = a.codes + in_row[u] * a.ldc + (int64_t)in_chunk[u] * WORDS;
+            if (a.cvec && (int64_t)(in_chunk[u] + 1) * WORDS <= a.ldc) {
+                if constexpr (B == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0][0], w[1][0]);
+                else *reinterpret_cast<uint4*>(p) = make_uint4(w[0][0], w[0][B / 4 - 1], w[1][0], w[1][B / 4 - 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < WORDS; i++)
+                    if ((int64_t)in_chunk[u] * WORDS + i < a.ldc) p[i] = w[i / (B / 4)][i % (B / 4)];
+            }
+            if (!a.xq) continue;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const int64_t n = a.cols - e - 8 * h;
+                if (n <= 0) break;
+                element_values(v[h], s, a.f, r[h]);
+                store8_any(a.xq, a.xq_type, in_row[u] * a.ldq + e + 8 * h, n, a.qvec, r[h]);
+            }
         }
     }
 }
 
 using GroupKernel = void (*)(const GroupArgs);
-using SmallKernel = void (*)(const GroupArgs, int64_t, int64_t, int64_t);
+using SmallKernel = void (*)(const GroupArgs, int, int, int);
 template <int TYPE, int B> SmallKernel small_kernel(int lanes)
 {
     switch (lanes) {
+    case 2: return project_small_groups_kernel<TYPE, B, 2>;
     case 4: return project_small_groups_kernel<TYPE, B, 4>;
     case 8: return project_small_groups_kernel<TYPE, B, 8>;
-    case 16: return project_small_groups_kernel<TYPE, B, 16>;
-    default: return project_small_groups_kernel<TYPE, B, 32>;
+    default: return project_small_groups_kernel<TYPE, B, 16>;
     }
 }
 
@@ -208,23 +257,24 @@ cudaError_t launch_project_groups(const void* x, int x_type, int64_t rows, int64
     a.xvec = rows16(x, ldx, x_type);
     a.qvec = xq && rows16(xq, ldq, xq_type);
     a.f = make_quant_fmt(f, rounding);
-    a.cvec = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 2 == 0;
+    const int words = f.b / 2;                          // of 16 codes
+    a.cvec = (reinterpret_cast<uintptr_t>(codes) & (4u * words - 1u)) == 0 && ldc % words == 0;
     const int64_t sms = device_sm_count();
-    if (a.group == 32 || a.group == 64 || a.group == 128 || a.group == 256) {
-        const int lanes = (int)a.group / 8;
+    const int lanes = (int)(a.group / 16);
+    // sixteens of a row up to its last code word, in whole groups
+    const int64_t chunks = lanes ? ((ldc + words - 1) / words + lanes - 1) / lanes * lanes : 0;
+    if ((a.group == 32 || a.group == 64 || a.group == 128 || a.group == 256) && rows < (1 << 30) && chunks < (1 << 30)) {
         static SmallKernel (*const pick[3][2])(int) = {{small_kernel<ESB_F32, 4>, small_kernel<ESB_F32, 8>},
                                                        {small_kernel<ESB_F16, 4>, small_kernel<ESB_F16, 8>},
                                                        {small_kernel<ESB_BF16, 4>, small_kernel<ESB_BF16, 8>}};
-        // vectors of a row up to its last code word, in whole groups
-        const int64_t vecs0 = f.b == 4 ? ldc : (ldc + 1) / 2;
-        const int64_t vecs = (vecs0 + lanes - 1) / lanes * lanes, total = rows * vecs;
-        int64_t blocks = (total + kGroupThreads - 1) / kGroupThreads;
-        const int64_t cap = sms * 6;
+        int64_t blocks = (rows * chunks + kGroupThreads - 1) / kGroupThreads;
+        const int64_t cap = sms * 8;
         if (blocks > cap) blocks = cap;
         const int64_t threads = blocks * kGroupThreads;
-        return launch_pdl(pick[x_type][f.b == 8](lanes), dim3((unsigned)blocks), dim3(kGroupThreads), 0, st, a, vecs, threads / vecs,
-                          threads % vecs);
+        return launch_pdl(pick[x_type][f.b == 8](lanes), dim3((unsigned)blocks), dim3(kGroupThreads), 0, st, a, (int)chunks,
+                          (int)(threads / chunks), (int)(threads % chunks));
     }
+    a.cvec = (reinterpret_cast<uintptr_t>(codes) & 7u) == 0 && ldc % 2 == 0;
     const int64_t total = rows * a.ngroups;
     const int64_t per = kGroupThreads / 32;
     int64_t blocks = (total + per - 1) / per;

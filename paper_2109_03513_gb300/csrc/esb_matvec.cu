@@ -569,7 +569,8 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         if (!a.wk || cost < best) { best = cost; a.wk = wk; }
     }
     const int64_t want = (tiles + p.warps / a.wk - 1) / (p.warps / a.wk), cap = at_once;
-    cudaError_t e = cudaFuncSetAttribute(p.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
+    cudaError_t e = cudaSuccess;
+    if (smem > 47 * 1024) e = cudaFuncSetAttribute(p.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
     if (e != cudaSuccess) return e;
     for (int64_t p0 = 0; p0 < passes; p0 += 65535) {    // grid.z holds 65535 passes
         const int64_t np = passes - p0 < 65535 ? passes - p0 : 65535;

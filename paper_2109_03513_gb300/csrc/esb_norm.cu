@@ -61,7 +61,9 @@ __device__ __forceinline__ void put_codes8(const NormArgs& a, int64_t row, int64
         p[0] = w[0];
         if (e / 4 + 1 < a.n.ldc) p[1] = w[1];
     }
-    if (a.n.yq && n > 0) store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q);
+    if (!a.n.yq || n <= 0) return;
+    element_values(y, s, a.f, q);
+    store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q);
 }
 
 // A block for each row, of any length: every pass reads the row again, and
@@ -130,7 +132,7 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
                 for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(y[i], a.f.is_signed));
             }
             mx = whole ? block_max<NW>(mx, shu) : __reduce_max_sync(0xffffffffu, mx);
-            const float alpha = __fdiv_rn(__uint_as_float(mx), a.f.C);
+            const float alpha = absmax_scale(mx, a.f);
             if (first == e0) a.n.scales[row * a.n.lds + g] = alpha;
             const GroupScale s = make_scale(alpha, a.f);
             const int64_t end = g == a.ngroups - 1 ? a.n.ldc * 4 : e0 + a.group;
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rmsnorm_rows_kernel(con
 #pragma unroll
                 for (int i = 0; i < 8; i++) m = max(m, i < n ? magnitude_bits(z[v][i], a.f.is_signed) : 0u);
                 for (int o = lanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const float alpha = __fdiv_rn(__uint_as_float(m), a.f.C);
+                const float alpha = absmax_scale(m, a.f);
                 if (on && e < a.n.ldc * 4) {
                     if (t % lanes == 0 && n > 0) a.n.scales[row * a.n.lds + e / a.group] = alpha;
                     put_codes8(a, row, e, z[v], make_scale(alpha, a.f));
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rmsnorm_rows_kernel(con
 #pragma unroll
                 for (int i = 0; i < NW; i++) mx = max(mx, shu[flip][i]);
             }
-            const float alpha = __fdiv_rn(__uint_as_float(mx), a.f.C);
+            const float alpha = absmax_scale(mx, a.f);
             if (t == 0 && on) a.n.scales[row * a.n.lds] = alpha;
             const GroupScale s = make_scale(alpha, a.f);
 #pragma unroll

@@ -110,6 +110,40 @@ __device__ __forceinline__ void store8_to(T* p, int64_t n, bool vec, const float
         if (i < n) p[i] = from_f32<T>(v[i]);
 }
 
+// Eight consecutive values as they lie in memory: loads that are waiting take
+// half the registers of fp32 values.
+template <class T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ void load(const T* p, int64_t n, bool vec)
+    {
+        if (vec && n >= 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; i++) {
+                const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+                w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+            }
+        } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) w[i] = i < n ? __float_as_uint(p[i]) : 0u;
+        } else {
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = (2 * i < n ? h[2 * i] : 0u) | ((2 * i + 1 < n ? (uint32_t)h[2 * i + 1] : 0u) << 16);
+        }
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = __uint_as_float(w[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) unpack2<T>(w[i], v[2 * i], v[2 * i + 1]);
+        }
+    }
+};
+
 // Values of a type that the kernel learns at run time (uniform branches).
 __device__ __forceinline__ void load8_any(const void* p, int type, int64_t at, int64_t n, bool vec, float (&v)[8])
 {
@@ -135,9 +169,10 @@ __device__ __forceinline__ float warp_sum(float v)
 
 // Projection constants of a format with b = 4 or 8.
 struct QuantFmt {
-    int k, is_signed, even, linear;   // linear: the set has one spacing
+    int k, is_signed, even;
+    int linear, plain;                // the set has one spacing; signed with ties away from zero
     uint32_t zero_code, rotate;       // added to places, it gives codes (modulo the sign bit)
-    float C, Ck, pk, ipk;             // largest value, 2^k times it, 2^k and 2^-k
+    float C, rC, Ck, pk, ipk;         // largest value, its rounded reciprocal, 2^k times it, 2^k and 2^-k
 };
 
 __host__ inline QuantFmt make_quant_fmt(const esb_format& f, int rounding)
@@ -146,9 +181,11 @@ __host__ inline QuantFmt make_quant_fmt(const esb_format& f, int rounding)
     QuantFmt q;
     q.k = f.k; q.is_signed = f.is_signed; q.even = rounding;
     q.linear = p.N <= 1;
+    q.plain = f.is_signed && rounding == ESB_ROUND_HALF_AWAY;
     q.zero_code = p.zero_code;
     q.rotate = p.zero_code * (f.b == 4 ? 0x11111111u : 0x01010101u);
     q.C = fmt_C(f.b, f.k);
+    q.rC = 1.0f / q.C;
     q.pk = (float)(1 << f.k);
     q.Ck = q.C * q.pk;
     q.ipk = 1.0f / q.pk;
@@ -171,73 +208,155 @@ __device__ __forceinline__ GroupScale make_scale(float alpha, const QuantFmt& f)
     return s;
 }
 
-// |x| / alpha (max(x, 0) / alpha for the unsigned set) times 2^k, rounded to
-// nearest as IEEE division (the power of two is exact).  Many values share
-// alpha, so its correctly rounded reciprocal y is found once; q = a y is then
-// within two units of a / alpha, one step with the exact remainder makes it
-// faithful, and by Markstein's theorem (Computation of elementary functions on
-// the IBM RISC System/6000 processor, 1990) a second one rounds it correctly.
-// A scale at the ends of fp32, where a remainder could underflow, takes the
-// division.
-__device__ __forceinline__ float scaled_value(float x, const GroupScale& s, const QuantFmt& f)
+// The scale of a group with this largest magnitude: it over C, rounded to
+// nearest (in the middle of fp32's range as fast_quotient below).
+__device__ __forceinline__ float absmax_scale(uint32_t mx, const QuantFmt& f)
 {
-    const float a = f.is_signed ? fabsf(x) : fmaxf(x, 0.0f);
-    if (!s.fast) return __fdiv_rn(a, s.alpha) * f.pk;
+    const float a = __uint_as_float(mx);
+    if (!(a > 0x1p-60f && a < 0x1p60f) || f.C > 0x1p60f) return __fdiv_rn(a, f.C);
+    float q = __fmul_rn(a, f.rC);
+    q = __fmaf_rn(__fmaf_rn(-q, f.C, a), f.rC, q);
+    return __fmaf_rn(__fmaf_rn(-q, f.C, a), f.rC, q);
+}
+
+// 2^k |x| / alpha, rounded to nearest as IEEE division of |x| by alpha (the
+// power of two is exact).  Many values share alpha, so the correctly rounded
+// reciprocal y of the step is found once; q = a y is then within two units of
+// the quotient, one step with the exact remainder makes it faithful, and by
+// Markstein's theorem (Computation of elementary functions on the IBM RISC
+// System/6000 processor, 1990) a second one rounds it correctly.
+__device__ __forceinline__ float fast_quotient(float a, const GroupScale& s)
+{
     float q = __fmul_rn(a, s.rcp);
     q = __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
     return __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
 }
 
-// Eight values to codes: their places in the ascending non-negative set (and
-// the sign bits), then the words.  Place j has the code (j - 2^k) mod 2^(b-1),
-// so the words take one add and a mask; zero keeps sign 0.  Places are found
-// with t = 2^k |x| / alpha: below 2^k (values below 1) the place is t rounded;
-// above, the k leading fraction bits are kept, and a carry into the next
-// binade is the next place.  q receives the numbers that the codes stand for.
-// An alpha of 0 (a group of zeros) or one that is not finite gives zero codes;
-// otherwise no value of the group is NaN.
+// t = 2^k |x| / alpha on the set: r receives the element (times 2^k), the
+// return value its place among the non-negative elements.  Places are t
+// rounded below 2^k (values below 1); above, the k leading fraction bits are
+// kept, and a carry into the next binade is the next place.
+__device__ __forceinline__ uint32_t round_away(float t, bool linear, int k, float pk, float& r)
+{
+    // half away from zero as the floor of t + 1/2, both sums truncated
+    const float big = __fadd_rz(__fadd_rz(t, 0.5f), 8388608.0f);
+    uint32_t j = __float_as_uint(big) - 0x4B000000u;
+    r = big - 8388608.0f;
+    if (!linear) {
+        const int sh = 23 - k;
+        const uint32_t h = (__float_as_uint(t) + (1u << (sh - 1))) >> sh;
+        const bool above = t >= pk;
+        // place 2^k is t = 2^k, whose leading bits are (127 + k) 2^k
+        j = above ? h - ((126u + (uint32_t)k) << k) : j;
+        r = above ? __uint_as_float(h << sh) : r;
+    }
+    return j;
+}
+
+// The general case of one value: unsigned sets, the other tie rule, scales at
+// the ends of fp32 (where a remainder could underflow) by division, and groups
+// whose scale is 0 or not finite, which have zero codes.
+static __device__ __noinline__ uint2 place_any(float x, float alpha, const QuantFmt& f)
+{
+    float r = 0.0f;
+    if (!(alpha > 0.0f && alpha < __int_as_float(0x7f800000))) return make_uint2(0u, 0u);
+    const float a = f.is_signed ? fabsf(x) : fmaxf(x, 0.0f);
+    const float t = fminf(__fdiv_rn(a, alpha) * f.pk, f.Ck);
+    if (!f.even) {
+        const uint32_t j = round_away(t, f.linear, f.k, f.pk, r);
+        return make_uint2(j, __float_as_uint(r));
+    }
+    if (f.linear || t < f.pk) {
+        const float big = __fadd_rn(t, 8388608.0f);
+        return make_uint2(__float_as_uint(big) - 0x4B000000u, __float_as_uint(big - 8388608.0f));
+    }
+    const int sh = 23 - f.k;
+    const uint32_t u = __float_as_uint(t), odd = f.k ? (u >> sh) & 1u : 1u;   // k = 0: the one significant bit
+    const uint32_t h = (u + (1u << (sh - 1)) - 1u + odd) >> sh;
+    return make_uint2(h - ((126u + (uint32_t)f.k) << f.k), h << sh);
+}
+
+// Eight values to codes: their places (a nibble or byte each) and sign bits,
+// then the words.  Place j has the code (j - 2^k) mod 2^(b-1), so a word takes
+// one add and a mask; zero keeps sign 0.  r receives the elements' magnitudes
+// times 2^k (element_values turns them into numbers).  In a group with a
+// finite scale no value is NaN.
+template <int B, bool LINEAR>
+__device__ __forceinline__ void places8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
+{
+    constexpr int PER = 32 / B;
+    constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
+#pragma unroll
+    for (int i = 0; i < B / 4; i++) w[i] = LINEAR ? 0u - 0x4B000000u * ONES : 0u;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float t = fminf(fast_quotient(fabsf(x[i]), s), f.Ck);
+        if constexpr (LINEAR) {
+            // the place is the low bits of the sum; what lies above them is
+            // taken off the word at once
+            const float big = __fadd_rz(__fadd_rz(t, 0.5f), 8388608.0f);
+            r[i] = big - 8388608.0f;
+            w[i / PER] += __float_as_uint(big) * (1u << (B * (i % PER)));
+        } else {
+            w[i / PER] += round_away(t, false, f.k, f.pk, r[i]) << (B * (i % PER));
+        }
+    }
+}
+// The sign bits of eight values at the tops of their codes.
 template <int B>
-__device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&q)[8])
+__device__ __forceinline__ void signs8(const float (&x)[8], uint32_t (&S)[B / 4])
+{
+    uint32_t u[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) u[i] = __float_as_uint(x[i]);
+    auto tops = [&](int a, int b, int c, int d) {       // the values' top bytes
+        return __byte_perm(__byte_perm(u[a], u[b], 0x0073), __byte_perm(u[c], u[d], 0x0073), 0x5410) & 0x80808080u;
+    };
+    if constexpr (B == 8) {
+        S[0] = tops(0, 1, 2, 3);
+        S[1] = tops(4, 5, 6, 7);
+    } else {
+        S[0] = tops(1, 3, 5, 7) | (tops(0, 2, 4, 6) >> 4);
+    }
+}
+template <int B>
+__device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
 {
     constexpr int PER = 32 / B;
     constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
     constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
-    uint32_t S[B / 4];
+    if (s.fast && f.plain) {
+        if (f.linear) places8<B, true>(x, s, f, w, r);
+        else places8<B, false>(x, s, f, w, r);
+    } else {
 #pragma unroll
-    for (int i = 0; i < B / 4; i++) w[i] = S[i] = 0u;
-    const bool dead = !(s.alpha > 0.0f && s.alpha < __int_as_float(0x7f800000));
+        for (int i = 0; i < B / 4; i++) w[i] = 0u;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float t = fminf(scaled_value(x[i], s, f), f.Ck);
-        uint32_t j;
-        float r;
-        // rounded to nearest by the addition of 2^23; half away from zero as
-        // the floor of t + 1/2, both sums truncated
-        const float big = f.even ? __fadd_rn(t, 8388608.0f) : __fadd_rz(__fadd_rz(t, 0.5f), 8388608.0f);
-        j = __float_as_uint(big) - 0x4B000000u;
-        r = big - 8388608.0f;
-        if (!f.linear) {
-            const uint32_t u = __float_as_uint(t);
-            const int sh = 23 - f.k;
-            const uint32_t odd = f.k ? (u >> sh) & 1u : 1u;          // k = 0: the one significant bit
-            const uint32_t h = (u + (f.even ? (1u << (sh - 1)) - 1u + odd : 1u << (sh - 1))) >> sh;
-            const bool above = t >= f.pk;
-            // place 2^k is t = 2^k, whose leading bits are (127 + k) 2^k
-            j = above ? h - (((126u + (uint32_t)f.k) << f.k)) : j;
-            r = above ? __uint_as_float(h << sh) : r;
+        for (int i = 0; i < 8; i++) {
+            const uint2 p = place_any(x[i], s.alpha, f);
+            w[i / PER] += p.x << (B * (i % PER));
+            r[i] = __uint_as_float(p.y);
         }
-        w[i / PER] += j << (B * (i % PER));
-        S[i / PER] |= ((__float_as_uint(x[i]) >> 31) & (uint32_t)f.is_signed) << (B * (i % PER) + B - 1);
-        r = dead ? 0.0f : r;
-        r = s.fast ? __fmul_rn(s.step, r) : __fmul_rn(s.alpha, r * f.ipk);
-        q[i] = x[i] < 0.0f ? -r : r;
     }
+    uint32_t S[B / 4];
+    signs8<B>(x, S);
 #pragma unroll
     for (int i = 0; i < B / 4; i++) {
-        if (dead) w[i] = 0u;
         const uint32_t nz = (w[i] + (TOP - ONES)) & TOP;
         w[i] = ((w[i] + f.rotate) & ~TOP) | (S[i] & nz);
     }
+}
+
+// The numbers that the codes of x stand for, alpha q, from r.
+__device__ __forceinline__ void element_values(const float (&x)[8], const GroupScale& s, const QuantFmt& f, float (&r)[8])
+{
+    const float by = s.fast ? s.step : s.alpha;
+    if (!s.fast) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) r[i] *= f.ipk;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) r[i] = __uint_as_float(__float_as_uint(__fmul_rn(by, r[i])) ^ (__float_as_uint(x[i]) & 0x80000000u));
 }
 
 // The words of eight codes of which only the first n are a row's: the rest

@@ -628,45 +628,84 @@ class Coded(NamedTuple):
     group: int = 0
 
     def c(self, name: str) -> esb_coded:
-        _codes(self.codes, f"{name}.codes", torch.int32)
-        _codes(self.scales, f"{name}.scales", torch.float32)
-        return esb_coded(self.codes.data_ptr(), _row_ld(self.codes), self.scales.data_ptr(), _row_ld(self.scales),
+        n = self.codes.shape[0]
+        lds = _rows_like(self.scales, name + ".scales", (n, _groups(self.cols, self.group)), torch.float32)
+        return esb_coded(self.codes.data_ptr(), _words(self.codes, name + ".codes", n), self.scales.data_ptr(), lds,
                          self.group, self.fmt.c())
 
 
-def _codes(t: torch.Tensor, name: str, dtype) -> None:
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.stride(1) != 1:
-        raise ValueError(f"{name} must be a 2-D CUDA {dtype} tensor with contiguous rows")
+# The checks below are short on purpose: at a decoding step's sizes they cost
+# more than the kernels.
 
-
-def _typed(t: torch.Tensor, name: str) -> int:
-    """The element type of a tensor of rows (any row stride, rows contiguous)."""
+def _rows(t: torch.Tensor, name: str) -> tuple[int, int]:
+    """(element type, row stride) of a matrix of rows (any row stride, rows contiguous)."""
     ty = _TYPES.get(t.dtype)
     if ty is None:
         raise ValueError(f"{name} must be float32, float16 or bfloat16")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] > 1):
         raise ValueError(f"{name} must be 2-D with contiguous rows")
-    return ty
+    # a single row has no stride
+    return ty, st[0] if t.shape[0] != 1 else max(t.shape[1], 1)
 
 
-def _ld(t: torch.Tensor) -> int:
-    """Row stride in elements (a single row has none)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _like(t: torch.Tensor, name: str, shape, dtype) -> None:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+def _rows_like(t: torch.Tensor, name: str, shape, dtype) -> int:
+    """Row stride of a matrix that has to have this shape and type."""
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be {tuple(shape)} {dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() == 2 and t.stride(1) != 1 and t.shape[1] > 1 or t.dim() == 1 and t.stride(0) != 1 and t.shape[0] > 1:
+    st = t.stride()
+    if st[1] != 1 and shape[1] > 1:
         raise ValueError(f"{name} must have contiguous rows")
+    return st[0] if shape[0] != 1 else max(shape[1], 1)
+
+
+def _vector(t: torch.Tensor, name: str, n: int, dtype) -> int:
+    """Address of a contiguous vector of n values of this type."""
+    if t.dtype != dtype or t.shape != (n,):
+        raise ValueError(f"{name} must be ({n},) {dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _weight(t: torch.Tensor, n: int) -> tuple[int, int]:
+    """(address, element type) of a norm's weight."""
+    ty = _TYPES.get(t.dtype)
+    if ty is None:
+        raise ValueError("weight must be float32, float16 or bfloat16")
+    return _vector(t, "weight", n, t.dtype), ty
+
+
+def _words(t: torch.Tensor, name: str, rows: int) -> int:
+    """Row stride of a matrix of code words with this many rows."""
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.stride(1) != 1 or t.shape[0] != rows:
+        raise ValueError(f"{name} must be a 2-D CUDA int32 tensor with {rows} contiguous rows")
+    return t.stride(0) if rows != 1 else t.shape[1]
 
 
 def _groups(cols: int, group: int) -> int:
     return -(-cols // group) if 0 < group < cols else 1
+
+
+def _coded_out(x: torch.Tensor, rows: int, cols: int, f: Fmt, group: int, codes, scales):
+    """Code words and scales of a (rows, cols) result, made where not given -> (codes, ldc, scales, lds)."""
+    if codes is None:
+        ldc = (-(-cols // (32 // f.b)) + 3) & -4 if 2 <= f.b <= 8 else 4
+        codes = torch.empty((rows, ldc), dtype=torch.int32, device=x.device)
+    else:
+        ldc = _words(codes, "codes", rows)
+    if scales is None:
+        lds = _groups(cols, group)
+        scales = torch.empty((rows, lds), dtype=torch.float32, device=x.device)
+    else:
+        lds = _rows_like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
+    return codes, ldc, scales, lds
 
 
 def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ESB_SCALE_ABSMAX,
@@ -675,31 +714,20 @@ def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ES
                        want_xq: bool = False, stream=None) -> tuple[Coded, Optional[torch.Tensor]]:
     """Project a (rows, cols) matrix with a scale for every `group` values of a
     row -> (Coded, the numbers the codes stand for (rows, cols) | None)."""
-    ty = _typed(x, "x")
+    ty, ldx = _rows(x, "x")
     rows, cols = x.shape
-    if codes is None:
-        codes = torch.empty((rows, esb_row_words(cols, f.b)), dtype=torch.int32, device=x.device)
-    else:
-        _codes(codes, "codes", torch.int32)
-    if scales is None:
-        scales = torch.empty((rows, _groups(cols, group)), dtype=torch.float32, device=x.device)
-    else:
-        _like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
-    if codes.shape[0] != rows:
-        raise ValueError("codes must have a row for each row of x")
+    codes, ldc, scales, lds = _coded_out(x, rows, cols, f, group, codes, scales)
     if xq is None and want_xq:
         xq = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    qt, ldq = (0, 0) if xq is None else (_typed(xq, "xq"), _ld(xq))
-    if xq is not None and xq.shape != x.shape:
-        raise ValueError("xq must have the shape of x")
-    _check(lib().esb_project_groups(_ptr(x), ty, rows, cols, _ld(x), f.c(), rounding, rule, group, _ptr(codes),
-                                    _row_ld(codes), _ptr(scales), _row_ld(scales), _ptr(xq), qt, ldq, _stream(stream)),
-           "esb_project_groups")
+    qp, qt, ldq = None, 0, 0
+    if xq is not None:
+        qt, ldq = _rows(xq, "xq")
+        qp = xq.data_ptr()
+        if xq.shape != x.shape:
+            raise ValueError("xq must have the shape of x")
+    _check(lib().esb_project_groups(x.data_ptr(), ty, rows, cols, ldx, f.c(), rounding, rule, group, codes.data_ptr(),
+                                    ldc, scales.data_ptr(), lds, qp, qt, ldq, _stream(stream)), "esb_project_groups")
     return Coded(codes, scales, f, cols, group), xq
-
-
-def _row_ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def esb_matvec_groups(x, w: Coded, bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
@@ -709,28 +737,24 @@ def esb_matvec_groups(x, w: Coded, bias: Optional[torch.Tensor] = None, y: Optio
     wc = w.c("w")
     n, k = w.codes.shape[0], w.cols
     coded = isinstance(x, Coded)
-    m, xk = (x.codes.shape[0], x.cols) if coded else x.shape
-    if xk != k:
-        raise ValueError("x and w must have the same number of columns")
-    if w.scales.shape != (n, _groups(k, w.group)):
-        raise ValueError("w.scales must hold a scale for every group")
     if coded:
+        m, xk = x.codes.shape[0], x.cols
         xc, xt = x.c("x"), ESB_CODES
-        if x.scales.shape != (m, _groups(k, x.group)):
-            raise ValueError("x.scales must hold a scale for every group")
         xp, ldx, xcp = None, 0, ctypes.byref(xc)
     else:
-        xt = _typed(x, "x")
-        xp, ldx, xcp = x.data_ptr(), _ld(x), None
+        xt, ldx = _rows(x, "x")
+        m, xk = x.shape
+        xp, xcp = x.data_ptr(), None
+    if xk != k:
+        raise ValueError("x and w must have the same number of columns")
     if y is None:
         y = torch.empty((m, n), dtype=y_dtype or (torch.bfloat16 if coded else x.dtype), device=w.codes.device)
-    yt = _typed(y, "y")
-    if tuple(y.shape) != (m, n):
+    yt, ldy = _rows(y, "y")
+    if y.shape != (m, n):
         raise ValueError("y must be (rows of x, rows of w)")
-    if bias is not None:
-        _like(bias, "bias", (n,), torch.float32)
-    _check(lib().esb_matvec_groups(m, n, k, xp, xt, ldx, xcp, ctypes.byref(wc), _ptr(bias), _ptr(y), yt, _ld(y),
-                                   _stream(stream)), "esb_matvec_groups")
+    _check(lib().esb_matvec_groups(m, n, k, xp, xt, ldx, xcp, ctypes.byref(wc),
+                                   None if bias is None else _vector(bias, "bias", n, torch.float32), y.data_ptr(), yt,
+                                   ldy, _stream(stream)), "esb_matvec_groups")
     return y
 
 
@@ -754,54 +778,43 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
     """RMS norm of x + residual -> NormOut.  h is written when there is a
     residual or a tensor for it; y unless `fmt` asks for codes (or want_y says);
     yq when there is a tensor for it."""
-    ty = _typed(x, "x")
-    rows, cols = x.shape
     a = esb_norm()
-    a.x, a.ldx, a.x_type, a.eps = x.data_ptr(), _ld(x), ty, eps
+    a.x_type, a.ldx = _rows(x, "x")
+    a.x, a.eps = x.data_ptr(), eps
+    shape, dtype = x.shape, x.dtype
+    rows, cols = shape
     if residual is not None:
-        _like(residual, "residual", x.shape, x.dtype)
-        a.residual, a.ldr = residual.data_ptr(), _ld(residual)
+        a.ldr = _rows_like(residual, "residual", shape, dtype)
+        a.residual = residual.data_ptr()
+        if h is None:
+            h = torch.empty(shape, dtype=dtype, device=x.device)
     if weight is not None:
-        if weight.dtype not in _TYPES:
-            raise ValueError("weight must be float32, float16 or bfloat16")
-        _like(weight, "weight", (cols,), weight.dtype)
-        a.weight, a.w_type = weight.data_ptr(), _TYPES[weight.dtype]
-    if h is None and residual is not None:
-        h = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        a.weight, a.w_type = _weight(weight, cols)
     if h is not None:
-        _like(h, "h", x.shape, x.dtype)
-        a.h, a.ldh = h.data_ptr(), _ld(h)
-    if y is None and (want_y if want_y is not None else fmt is None):
-        y = torch.empty((rows, cols), dtype=y_dtype or x.dtype, device=x.device)
+        a.ldh = _rows_like(h, "h", shape, dtype)
+        a.h = h.data_ptr()
+    if y is None and (fmt is None if want_y is None else want_y):
+        y = torch.empty(shape, dtype=y_dtype or dtype, device=x.device)
     if y is not None:
-        a.y_type = _typed(y, "y")
-        _like(y, "y", x.shape, y.dtype)
-        a.y, a.ldy = y.data_ptr(), _ld(y)
+        a.y_type, a.ldy = _rows(y, "y")
+        a.y = y.data_ptr()
+        if y.shape != shape:
+            raise ValueError("y must have the shape of x")
     if yq is not None:
         if y is not None and y.dtype != yq.dtype:
             raise ValueError("y and yq must have one type")
-        a.y_type = _typed(yq, "yq")
-        _like(yq, "yq", x.shape, yq.dtype)
-        a.yq, a.ldq = yq.data_ptr(), _ld(yq)
+        a.y_type, a.ldq = _rows(yq, "yq")
+        a.yq = yq.data_ptr()
+        if yq.shape != shape:
+            raise ValueError("yq must have the shape of x")
     if rstd is None and want_rstd:
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     if rstd is not None:
-        _like(rstd, "rstd", (rows,), torch.float32)
-        a.rstd = rstd.data_ptr()
+        a.rstd = _vector(rstd, "rstd", rows, torch.float32)
     coded = None
     if fmt is not None:
-        if codes is None:
-            codes = torch.empty((rows, esb_row_words(cols, fmt.b)), dtype=torch.int32, device=x.device)
-        else:
-            _codes(codes, "codes", torch.int32)
-        if scales is None:
-            scales = torch.empty((rows, _groups(cols, group)), dtype=torch.float32, device=x.device)
-        else:
-            _like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
-        if codes.shape[0] != rows:
-            raise ValueError("codes must have a row for each row of x")
-        a.codes, a.ldc, a.scales, a.lds = codes.data_ptr(), _row_ld(codes), scales.data_ptr(), _row_ld(scales)
-        a.group, a.fmt, a.rounding = group, fmt.c(), rounding
+        codes, a.ldc, scales, a.lds = _coded_out(x, rows, cols, fmt, group, codes, scales)
+        a.codes, a.scales, a.group, a.fmt, a.rounding = codes.data_ptr(), scales.data_ptr(), group, fmt.c(), rounding
         coded = Coded(codes, scales, fmt, cols, group)
     _check(lib().esb_rmsnorm(rows, cols, ctypes.byref(a), _stream(stream)), "esb_rmsnorm")
     return NormOut(h, y, rstd, coded, yq)
@@ -814,36 +827,36 @@ def esb_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[tor
                          stream=None) -> tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Gradient of esb_rmsnorm -> (dx, of x and of the residual alike; dweight
     fp32 | None).  dweight is computed when there is a weight, unless want_dweight says."""
-    rows, cols = h.shape
     a = esb_norm_grad()
-    a.x_type, a.g_type = _typed(h, "h"), _typed(dy, "dy")
-    _like(dy, "dy", h.shape, dy.dtype)
-    _like(rstd, "rstd", (rows,), torch.float32)
-    a.dy, a.ldg, a.h, a.ldh, a.rstd = dy.data_ptr(), _ld(dy), h.data_ptr(), _ld(h), rstd.data_ptr()
+    a.x_type, a.ldh = _rows(h, "h")
+    a.g_type, a.ldg = _rows(dy, "dy")
+    shape, dtype = h.shape, h.dtype
+    rows, cols = shape
+    if dy.shape != shape:
+        raise ValueError("dy must have the shape of h")
+    a.dy, a.h, a.rstd = dy.data_ptr(), h.data_ptr(), _vector(rstd, "rstd", rows, torch.float32)
     if dh is not None:
-        _like(dh, "dh", h.shape, h.dtype)
-        a.dh, a.lddh = dh.data_ptr(), _ld(dh)
+        a.lddh = _rows_like(dh, "dh", shape, dtype)
+        a.dh = dh.data_ptr()
     if weight is not None:
-        if weight.dtype not in _TYPES:
-            raise ValueError("weight must be float32, float16 or bfloat16")
-        _like(weight, "weight", (cols,), weight.dtype)
-        a.weight, a.w_type = weight.data_ptr(), _TYPES[weight.dtype]
+        a.weight, a.w_type = _weight(weight, cols)
     if dx is None:
-        dx = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
-    _like(dx, "dx", h.shape, h.dtype)
-    a.dx, a.lddx = dx.data_ptr(), _ld(dx)
-    nb = 0
-    if dweight is None and (want_dweight if want_dweight is not None else weight is not None):
+        dx = torch.empty(shape, dtype=dtype, device=h.device)
+    a.lddx = _rows_like(dx, "dx", shape, dtype)
+    a.dx = dx.data_ptr()
+    wp, nb = None, 0
+    if dweight is None and (weight is not None if want_dweight is None else want_dweight):
         dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
     if dweight is not None:
-        _like(dweight, "dweight", (cols,), torch.float32)
-        a.dweight = dweight.data_ptr()
-        nb = int(lib().esb_rmsnorm_backward_workspace_bytes(rows, cols))
-        if workspace is None and nb:
+        a.dweight = _vector(dweight, "dweight", cols, torch.float32)
+        if workspace is None:
+            nb = int(lib().esb_rmsnorm_backward_workspace_bytes(rows, cols))
             workspace = torch.empty(nb, dtype=torch.uint8, device=h.device)
-    _check(lib().esb_rmsnorm_backward(rows, cols, ctypes.byref(a), _ptr(workspace),
-                                      0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                      _stream(stream)), "esb_rmsnorm_backward")
+        else:
+            _dev(workspace, "workspace")
+            nb = workspace.numel() * workspace.element_size()
+        wp = workspace.data_ptr()
+    _check(lib().esb_rmsnorm_backward(rows, cols, ctypes.byref(a), wp, nb, _stream(stream)), "esb_rmsnorm_backward")
     return dx, dweight
 
 
@@ -859,22 +872,23 @@ class LogProbs(NamedTuple):
 def esb_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, top: int = 0, stream=None) -> LogProbs:
     """Log probability of ids (rows,) int64 under each row of logits, the
     entropy, log sum exp, and the `top` most likely tokens -> LogProbs."""
-    ty = _typed(logits, "logits")
+    ty, ldx = _rows(logits, "logits")
     rows, cols = logits.shape
-    if ids is not None:
-        _like(ids, "ids", (rows,), torch.int64)
+    ip = None if ids is None else _vector(ids, "ids", rows, torch.int64)
     if not 0 <= top <= ESB_MAX_TOP:
         raise ValueError(f"top must be 0..{ESB_MAX_TOP}")
     dev = logits.device
-    st = torch.empty((3, rows), dtype=torch.float32, device=dev)      # one allocation for the rows' numbers
-    logp, ent, lse = st.unbind(0)
-    tl = torch.empty((rows, top), dtype=torch.float32, device=dev) if top else None
-    ti = torch.empty((rows, top), dtype=torch.int64, device=dev) if top else None
-    if ids is None:
-        logp = None
-    _check(lib().esb_logprobs(_ptr(logits), ty, rows, cols, _ld(logits), _ptr(ids), top, _ptr(logp), _ptr(ent),
-                              _ptr(lse), _ptr(tl), _ptr(ti), _stream(stream)), "esb_logprobs")
-    return LogProbs(logp, ent, lse, tl, ti)
+    st = torch.empty((3 + top, rows), dtype=torch.float32, device=dev)   # one allocation for the rows' numbers
+    p = st.data_ptr()
+    ent, lse = st[1], st[2]
+    tl = ti = None
+    if top:
+        tl = st[3:].view(rows, top)
+        ti = torch.empty((rows, top), dtype=torch.int64, device=dev)
+    _check(lib().esb_logprobs(logits.data_ptr(), ty, rows, cols, ldx, ip, top, p if ip else None, p + 4 * rows,
+                              p + 8 * rows, p + 12 * rows if top else None, ti.data_ptr() if top else None,
+                              _stream(stream)), "esb_logprobs")
+    return LogProbs(st[0] if ip else None, ent, lse, tl, ti)
 
 
 def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse: torch.Tensor,
@@ -882,19 +896,19 @@ def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse
                           dentropy: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None,
                           stream=None) -> torch.Tensor:
     """Gradient of logp and entropy (dlogp, dentropy: (rows,) fp32) with respect to the logits."""
-    ty = _typed(logits, "logits")
-    rows, cols = logits.shape
-    for t, name in ((lse, "lse"), (entropy, "entropy"), (dlogp, "dlogp"), (dentropy, "dentropy")):
-        if t is not None:
-            _like(t, name, (rows,), torch.float32)
-    if ids is not None:
-        _like(ids, "ids", (rows,), torch.int64)
+    ty, ldx = _rows(logits, "logits")
+    rows, cols = shape = logits.shape
+    f32 = torch.float32
+    lp = _vector(lse, "lse", rows, f32)
+    ep = None if entropy is None else _vector(entropy, "entropy", rows, f32)
+    gp = None if dlogp is None else _vector(dlogp, "dlogp", rows, f32)
+    hp = None if dentropy is None else _vector(dentropy, "dentropy", rows, f32)
+    ip = None if ids is None else _vector(ids, "ids", rows, torch.int64)
     if dlogits is None:
-        dlogits = torch.empty((rows, cols), dtype=logits.dtype, device=logits.device)
-    _like(dlogits, "dlogits", logits.shape, logits.dtype)
-    _check(lib().esb_logprobs_backward(_ptr(logits), ty, rows, cols, _ld(logits), _ptr(ids), _ptr(lse), _ptr(entropy),
-                                       _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), _ld(dlogits), _stream(stream)),
-           "esb_logprobs_backward")
+        dlogits = torch.empty(shape, dtype=logits.dtype, device=logits.device)
+    ldd = _rows_like(dlogits, "dlogits", shape, logits.dtype)
+    _check(lib().esb_logprobs_backward(logits.data_ptr(), ty, rows, cols, ldx, ip, lp, ep, gp, hp, dlogits.data_ptr(),
+                                       ldd, _stream(stream)), "esb_logprobs_backward")
     return dlogits
 
 
