@@ -27,8 +27,7 @@ namespace esb {
 
 namespace {
 
-constexpr int kLpThreads = 512;
-constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpMaxWarps = 16;
 constexpr int kLpValues = 16;           // logits of a thread in a block of them
 constexpr int kLpList = 2048;
 constexpr int kLpMaxCluster = 8;
@@ -52,6 +51,55 @@ __device__ __forceinline__ Key top_key(float v, uint32_t at)
     return ((Key)((u >> 31) ? ~u : u | 0x80000000u) << 32) | (0xffffffffu - at);
 }
 __device__ __forceinline__ uint32_t key_place(Key k) { return 0xffffffffu - (uint32_t)k; }
+__device__ __forceinline__ float key_value(Key k)
+{
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u);
+}
+
+// e^x for x <= 0 (and NaN): the hardware's 2^y with results below 2^-126 as 0.
+__device__ __forceinline__ float exp_of(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504f));
+    return r;
+}
+
+// Two fp32 numbers in one instruction of the multiply-add pipe.
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair pair_of(float a, float b)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void split(const Pair& p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair add2(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(const Pair& a, const Pair& b, const Pair& c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float ex2_of(float y)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+    return r;
+}
 
 struct LpSums {
     float m, s, d;
@@ -62,7 +110,7 @@ __device__ __forceinline__ LpSums join(const LpSums& a, const LpSums& b)
 {
     LpSums r;
     r.m = fmaxf(a.m, b.m);
-    const float da = a.m - r.m, db = b.m - r.m, fa = __expf(da), fb = __expf(db);
+    const float da = a.m - r.m, db = b.m - r.m, fa = exp_of(da), fb = exp_of(db);
     r.s = a.s * fa + b.s * fb;
     r.d = (fa == 0.0f ? 0.0f : fa * fmaf(da, a.s, a.d)) + (fb == 0.0f ? 0.0f : fb * fmaf(db, b.s, b.d));
     if (!(a.s == a.s) || !(b.s == b.s)) r.s = r.d = __int_as_float(0x7fffffff);
@@ -98,8 +146,8 @@ __device__ __forceinline__ Key merge32(Key best, Key more, int lane)
 }
 
 struct LpShared {
-    LpSums sums[kLpWarps];
-    Key lanes[kLpWarps][32];
+    LpSums sums[kLpMaxWarps];
+    Key lanes[kLpMaxWarps][32];
     Key best[32];                       // the best keys so far, descending
     Key bound;                          // no alternative is below it
     int count, overflow;
@@ -156,9 +204,10 @@ struct RowParts {
     }
 };
 
-template <int TYPE>
-__global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
+template <int TYPE, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const LpArgs a)
 {
+    constexpr int kLpThreads = WARPS * 32, kLpWarps = WARPS;
     using T = Elem<TYPE>;
     constexpr int V = 16 / sizeof(T), U = kLpValues / V;   // values of a vector, vectors of a thread in a block of logits
     extern __shared__ __align__(16) unsigned char lp_smem[];
@@ -177,18 +226,26 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
             if (threadIdx.x == 0) { sh.bound = 0ull; sh.count = 0; sh.overflow = 0; }
             __syncthreads();
         }
-        LpSums t = {lowest, 0.0f, 0.0f};
-        auto add = [&](float v) {
-            const float d = v - t.m, p = __expf(d);
-            t.s += p;
-            t.d = fmaf(p, fmaxf(d, -200.0f), t.d);      // p is 0 there
+        // two halves of the thread's sums, added up at the end
+        float m = lowest;
+        Pair s2 = pair_of(0.0f, 0.0f), d2 = s2;
+        const Pair log2e = pair_of(1.44269504f, 1.44269504f);
+        auto add = [&](float x0, float x1, const Pair& minus_m) {
+            const Pair d = add2(pair_of(x0, x1), minus_m);
+            float y0, y1, e0, e1;
+            split(mul2(d, log2e), y0, y1);
+            split(d, e0, e1);
+            const Pair p = pair_of(ex2_of(y0), ex2_of(y1));
+            s2 = add2(s2, p);
+            d2 = fma2(p, pair_of(fmaxf(e0, -200.0f), fmaxf(e1, -200.0f)), d2);   // p is 0 there
         };
-        auto raise = [&](float m) {
-            if (m > t.m) {
-                const float d = t.m - m, f = __expf(d);
-                t.d = f == 0.0f ? 0.0f : f * fmaf(d, t.s, t.d);
-                t.s *= f;
-                t.m = m;
+        auto raise = [&](float to) {
+            if (to > m) {
+                const float d = m - to, f = exp_of(d);
+                const Pair f2 = pair_of(f, f);
+                d2 = f == 0.0f ? pair_of(0.0f, 0.0f) : mul2(f2, fma2(pair_of(d, d), s2, d2));
+                s2 = f == 0.0f ? pair_of(0.0f, 0.0f) : mul2(f2, s2);
+                m = to;
             }
         };
         Key bound = 0ull;
@@ -203,13 +260,21 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
         };
         const int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
         bool first = true;
-        for (int64_t v0 = rank * step; v0 < rp.vecs || first; v0 += a.split * step) {
-            uint4 raw[U];
+        uint4 next[U];
+        auto load = [&](int64_t v0) {
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 const int64_t i = v0 + u * kLpThreads + threadIdx.x;
-                if (i < rp.vecs) raw[u] = __ldg(reinterpret_cast<const uint4*>(xv) + i);
+                next[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (i < rp.vecs) next[u] = __ldg(reinterpret_cast<const uint4*>(xv) + i);
             }
+        };
+        load(rank * step);
+        for (int64_t v0 = rank * step; v0 < rp.vecs || first; v0 += a.split * step) {
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) raw[u] = next[u];
+            load(v0 + a.split * step);
             // a few values before and after the vectors: the first block of
             // the row has them, one a thread
             float edge = ninf;
@@ -240,11 +305,12 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
                 for (int j = 0; j < V; j++) big = fmaxf(big, v[u][j]);
             }
             raise(big);
-            if (edge != ninf) add(edge);
+            const Pair minus_m = pair_of(-m, -m);
+            if (edge != ninf) add(edge, ninf, minus_m);
 #pragma unroll
             for (int u = 0; u < U; u++)
 #pragma unroll
-                for (int j = 0; j < V; j++) add(v[u][j]);
+                for (int j = 0; j < V; j += 2) add(v[u][j], v[u][j + 1], minus_m);
             if (a.top) {
                 auto at_of = [&](int u, int j) { return (uint32_t)(rp.head + (v0 + u * kLpThreads + threadIdx.x) * V + j); };
                 if (bound == 0ull) {                    // the same for every thread
@@ -269,14 +335,15 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
                     __syncthreads();
                     bound = sh.bound;
                 }
-                if (edge != ninf) offer(edge, edge_at);
+                if (edge > ninf) offer(edge, edge_at);
                 // most threads have nothing at or above the bound
-                if (top_key(big, 0u) >= bound) {
+                const float least = bound ? key_value(bound) : lowest;
+                if (big >= least) {
 #pragma unroll
                     for (int u = 0; u < U; u++)
 #pragma unroll
                         for (int j = 0; j < V; j++)
-                            if (v[u][j] != ninf) offer(v[u][j], at_of(u, j));
+                            if (v[u][j] >= least) offer(v[u][j], at_of(u, j));
                 }
                 if (__syncthreads_or(full)) {
                     if (warp == 0) cut_list(sh, a.top, lane);
@@ -288,6 +355,10 @@ __global__ void __launch_bounds__(kLpThreads, 2) logprobs_kernel(const LpArgs a)
             first = false;
         }
         // the block's sums
+        float sa, sb, da, db;
+        split(s2, sa, sb);
+        split(d2, da, db);
+        LpSums t = {m, sa + sb, da + db};
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             const LpSums b = {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.d, o)};
@@ -406,7 +477,7 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(const LpGradArgs a)
         if (lse != lse) g = lse;
         auto grad = [&](float v) {
             const float lp = fmaxf(v - lse, -200.0f);   // p is 0 there
-            return -__expf(lp) * fmaf(gh, lp, g);
+            return -exp_of(lp) * fmaf(gh, lp, g);
         };
         RowParts<T> rp(x, a.cols);
         if (((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15u) != 0) {
@@ -472,14 +543,18 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     // Rows that do not fill the SMs are split over clusters of 2, 4 or 8
     // blocks, as long as each has a block of logits.
     const int64_t sms = device_sm_count();
-    while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * kLpThreads * kLpValues) a.split *= 2;
-    const int64_t cap = 4 * sms / a.split;
+    // A short row takes 4 warps, a longer one 16.
+    const bool few = cols <= 4 * 32 * kLpValues * 2;
+    const int threads = few ? 128 : 512;
+    while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * threads * kLpValues) a.split *= 2;
+    const int64_t cap = 2 * (2048 / threads) * sms / a.split;
     const unsigned blocks = (unsigned)((rows < cap ? rows : cap) * a.split);
     using Kernel = void (*)(const LpArgs);
-    static const Kernel kernels[3] = {logprobs_kernel<ESB_F32>, logprobs_kernel<ESB_F16>, logprobs_kernel<ESB_BF16>};
+    static const Kernel kernels[2][3] = {{logprobs_kernel<ESB_F32, 16>, logprobs_kernel<ESB_F16, 16>, logprobs_kernel<ESB_BF16, 16>},
+                                         {logprobs_kernel<ESB_F32, 4>, logprobs_kernel<ESB_F16, 4>, logprobs_kernel<ESB_BF16, 4>}};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(kLpThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = sizeof(LpShared);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -491,7 +566,7 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernels[type], a);
+    return cudaLaunchKernelEx(&cfg, kernels[few][type], a);
 }
 
 cudaError_t launch_logprobs_grad(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids,
