@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
         };
         const int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
         bool first = true;
+        int blocks = 0;
         uint4 next[U];
         auto load = [&](int64_t v0) {
 #pragma unroll
@@ -345,7 +346,9 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
                         for (int j = 0; j < V; j++)
                             if (v[u][j] >= least) offer(v[u][j], at_of(u, j));
                 }
-                if (__syncthreads_or(full)) {
+                // every fourth block of logits (the list holds far more than four
+                // usually add): is the list half full?
+                if ((++blocks & 3) == 0 && __syncthreads_or(full)) {
                     if (warp == 0) cut_list(sh, a.top, lane);
                     __syncthreads();
                     bound = sh.bound;
@@ -543,14 +546,17 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     // Rows that do not fill the SMs are split over clusters of 2, 4 or 8
     // blocks, as long as each has a block of logits.
     const int64_t sms = device_sm_count();
-    // A short row takes 4 warps, a longer one 16.
-    const bool few = cols <= 4 * 32 * kLpValues * 2;
-    const int threads = few ? 128 : 512;
+    // Warps of a row: 4 for a short one; 16 where there are few rows (256 x
+    // 65537 fp32, 5 alternatives: 24 us, 31 with 8), 8 where many rows' barriers
+    // and joins should overlap (4096 x 49999 bf16: 99 us, 122 with 16).
+    const int size = cols <= 4 * 32 * kLpValues * 2 ? 2 : (rows >= 4 * sms ? 1 : 0);
+    const int threads = 512 >> size;
     while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * threads * kLpValues) a.split *= 2;
     const int64_t cap = 2 * (2048 / threads) * sms / a.split;
     const unsigned blocks = (unsigned)((rows < cap ? rows : cap) * a.split);
     using Kernel = void (*)(const LpArgs);
-    static const Kernel kernels[2][3] = {{logprobs_kernel<ESB_F32, 16>, logprobs_kernel<ESB_F16, 16>, logprobs_kernel<ESB_BF16, 16>},
+    static const Kernel kernels[3][3] = {{logprobs_kernel<ESB_F32, 16>, logprobs_kernel<ESB_F16, 16>, logprobs_kernel<ESB_BF16, 16>},
+                                         {logprobs_kernel<ESB_F32, 8>, logprobs_kernel<ESB_F16, 8>, logprobs_kernel<ESB_BF16, 8>},
                                          {logprobs_kernel<ESB_F32, 4>, logprobs_kernel<ESB_F16, 4>, logprobs_kernel<ESB_BF16, 4>}};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(blocks);
@@ -566,7 +572,7 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernels[few][type], a);
+    return cudaLaunchKernelEx(&cfg, kernels[size][type], a);
 }
 
 cudaError_t launch_logprobs_grad(const void* x, int type, int64_t rows, int64_t cols, int64_t ldx, const int64_t* ids,

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
 // bf16 with residual, codes and their values: 15 bytes for every 2 of x read),
 // latency-bound where there are few.
 template <int TYPE, int TPR, int NV>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rmsnorm_rows_kernel(const NormArgs a)
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(const NormArgs a)
 {
     using T = Elem<TYPE>;
     constexpr int THREADS = TPR < 128 ? 128 : TPR, PER = THREADS / TPR, NW = TPR / 32;
@@ -162,28 +162,34 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rmsnorm_rows_kernel(con
     griddep_wait();
     const int t = threadIdx.x % TPR, lanes = (int)a.group / 8;
     int flip = 0;
+    Raw8<T> rx[NV], rr[NV];                             // the next row, on its way
+    auto load = [&](int64_t row) {
+        const T* x = static_cast<const T*>(a.n.x) + row * a.n.ldx;
+        const T* r = static_cast<const T*>(a.n.residual) + row * a.n.ldr;
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            const int64_t e = (int64_t)(v * TPR + t) * 8, n = row < a.rows ? a.cols - e : 0;
+            rx[v].load(x + e, n, a.xvec);
+            if (a.n.residual) rr[v].load(r + e, n, a.rvec);
+        }
+    };
+    load((int64_t)blockIdx.x * PER + threadIdx.x / TPR);
     // a block's rows go on together, so that every thread meets every barrier
     for (int64_t row0 = (int64_t)blockIdx.x * PER; row0 < a.rows; row0 += (int64_t)gridDim.x * PER, flip ^= 1) {
         const int64_t row = row0 + threadIdx.x / TPR;
         const bool on = PER == 1 || row < a.rows;
-        const T* x = static_cast<const T*>(a.n.x) + row * a.n.ldx;
-        const T* r = a.n.residual ? static_cast<const T*>(a.n.residual) + row * a.n.ldr : nullptr;
         float z[NV][8];
 #pragma unroll
         for (int v = 0; v < NV; v++) {
-            const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
-            load8_to(x + e, n, a.xvec, z[v]);
-        }
-        if (r) {
-#pragma unroll
-            for (int v = 0; v < NV; v++) {
-                const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
+            rx[v].values(z[v]);
+            if (a.n.residual) {
                 float u[8];
-                load8_to(r + e, n, a.rvec, u);
+                rr[v].values(u);
 #pragma unroll
                 for (int i = 0; i < 8; i++) z[v][i] = __fadd_rn(z[v][i], u[i]);
             }
         }
+        load(row + (int64_t)gridDim.x * PER);
         float ss = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; v++)
@@ -329,7 +335,7 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_kernel(const NormGrad
 // it works on this one.  8192 x 4096 bf16: 268 MB of reads and writes (the
 // three kernels above read the gradient and h twice).
 template <int TYPE, int GTYPE, int TPR, int NV>
-__global__ void __launch_bounds__(TPR) rmsnorm_grad_rows_kernel(const NormGradArgs a)
+__global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGradArgs a)
 {
     using T = Elem<TYPE>;
     using G = Elem<GTYPE>;
@@ -345,23 +351,32 @@ __global__ void __launch_bounds__(TPR) rmsnorm_grad_rows_kernel(const NormGradAr
         for (int i = 0; i < 8; i++) { w[v][i] = 1.0f; dw[v][i] = 0.0f; }
         if (NV == 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], a.cols - e[v], a.wvec, w[v]);
     }
-    float n[NV][8], d[NV][8], rstd = 0.0f;
+    float rstd = 0.0f;
+    Raw8<T> rh[NV], rt[NV];                             // the next row, on its way
+    Raw8<G> rg[NV];
     auto load = [&](int64_t row) {
         const bool on = row < a.rows;
         if (on) rstd = a.n.rstd[row];
 #pragma unroll
         for (int v = 0; v < NV; v++) {
             const int64_t left = on ? a.cols - e[v] : 0;
-            load8_to(static_cast<const T*>(a.n.h) + row * a.n.ldh + e[v], left, a.hvec, n[v]);
-            load8_to(static_cast<const G*>(a.n.dy) + row * a.n.ldg + e[v], left, a.gvec, d[v]);
+            rh[v].load(static_cast<const T*>(a.n.h) + row * a.n.ldh + e[v], left, a.hvec);
+            rg[v].load(static_cast<const G*>(a.n.dy) + row * a.n.ldg + e[v], left, a.gvec);
+            if (NV == 1 && a.n.dh) rt[v].load(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[v], left, a.dhvec);
         }
     };
+    load(blockIdx.x);
     int flip = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, flip ^= 1) {
-        load(row);
         const float rs = rstd;
-        float t[8];
-        if (NV == 1 && a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[0], a.cols - e[0], a.dhvec, t);
+        float n[NV][8], d[NV][8], t[8];
+#pragma unroll
+        for (int v = 0; v < NV; v++) {
+            rh[v].values(n[v]);
+            rg[v].values(d[v]);
+        }
+        if (NV == 1 && a.n.dh) rt[0].values(t);
+        load(row + gridDim.x);
         float s = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; v++) {
