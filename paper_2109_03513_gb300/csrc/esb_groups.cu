@@ -34,7 +34,7 @@ __device__ __forceinline__ void project8(const GroupArgs& a, int64_t row, int64_
 {
     uint32_t w[B / 4];
     float q[8];
-    const int64_t n = a.cols - vec * 8;
+    const int n = left_of(a.cols, vec * 8);
     quantise8<B>(v, s, a.f, w, q);
     if (n < 8) zero_past<B>(w, n, a.f);
     uint32_t* p = a.codes + row * a.ldc + vec * (B / 4);
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
         if (a.rule == ESB_SCALE_ABSMAX) {
             uint32_t mx = 0u;
             for (int64_t e = e0 + lane * 8; e < e1; e += 256) {
-                load8_to(x + e, e1 - e, a.xvec, v);
+                load8_to(x + e, left_of(e1, e), a.xvec, v);
 #pragma unroll
                 for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(v[i], a.f.is_signed));
             }
@@ -81,14 +81,14 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
             float mean = 0.0f;
             if (a.f.is_signed) {
                 for (int64_t e = e0 + lane * 8; e < e1; e += 256) {
-                    load8_to(x + e, e1 - e, a.xvec, v);
+                    load8_to(x + e, left_of(e1, e), a.xvec, v);
 #pragma unroll
                     for (int i = 0; i < 8; i++) s1 += v[i];
                 }
                 mean = warp_sum(s1) / n;
             }
             for (int64_t e = e0 + lane * 8; e < e1; e += 256) {
-                load8_to(x + e, e1 - e, a.xvec, v);
+                load8_to(x + e, left_of(e1, e), a.xvec, v);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     const float d = e + i < e1 ? v[i] - mean : 0.0f;
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
         // the last group's warp also writes the words past the columns
         const int64_t end = gi == a.ngroups - 1 ? a.ldc * (32 / B) : e0 + a.group;
         for (int64_t e = e0 + lane * 8; e < end; e += 256) {
-            load8_to(x + e, e1 - e, a.xvec, v);
+            load8_to(x + e, left_of(e1, e), a.xvec, v);
             project8<B>(a, row, e / 8, v, s);
         }
     }
@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(con
         for (int u = 0; u < kChunks; u++) {
             in_row[u] = row;
             in_chunk[u] = chunk;
-            const int64_t e = (int64_t)chunk * 16, n = row < rows ? a.cols - e : 0;
+            const int64_t e = (int64_t)chunk * 16;
+            const int n = row < rows ? left_of(a.cols, e) : 0;
             const T* x = static_cast<const T*>(a.x) + row * a.ldx + e;
             raw[u][0].load(x, n, a.xvec);
             raw[u][1].load(x + 8, n - 8, a.xvec);
@@ -196,12 +197,13 @@ __global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(con
             const int64_t gi = in_chunk[u] / LANES;
             if (part == 0 && gi < a.ngroups) a.scales[in_row[u] * a.lds + gi] = alpha;
             const GroupScale s = make_scale(alpha, a.f);
+            const int left = left_of(a.cols, e);
             uint32_t w[2][B / 4];
             float r[2][8];
 #pragma unroll
             for (int h = 0; h < 2; h++) {
                 quantise8<B>(v[h], s, a.f, w[h], r[h]);
-                const int64_t n = a.cols - e - 8 * h;
+                const int n = left - 8 * h;
                 if (n < 8) zero_past<B>(w[h], n, a.f);
             }
             constexpr int WORDS = B / 2;                // of 16 codes
@@ -217,7 +219,7 @@ __global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(con
             if (!a.xq) continue;
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const int64_t n = a.cols - e - 8 * h;
+                const int n = left - 8 * h;
                 if (n <= 0) break;
                 element_values(v[h], s, a.f, r[h]);
                 store8_any(a.xq, a.xq_type, in_row[u] * a.ldq + e + 8 * h, n, a.qvec, r[h]);

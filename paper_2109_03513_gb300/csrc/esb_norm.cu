@@ -51,7 +51,7 @@ __device__ __forceinline__ void put_codes8(const NormArgs& a, int64_t row, int64
 {
     uint32_t w[2];
     float q[8];
-    const int64_t n = a.cols - e;
+    const int n = left_of(a.cols, e);
     quantise8<8>(y, s, a.f, w, q);
     if (n < 8) zero_past<8>(w, n, a.f);
     uint32_t* p = a.n.codes + row * a.n.ldc + e / 4;
@@ -82,10 +82,10 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
         const T* x = static_cast<const T*>(a.n.x) + row * a.n.ldx;
         const T* r = a.n.residual ? static_cast<const T*>(a.n.residual) + row * a.n.ldr : nullptr;
         auto sum8 = [&](int64_t e, float (&z)[8]) {
-            load8_to(x + e, a.cols - e, a.xvec, z);
+            load8_to(x + e, left_of(a.cols, e), a.xvec, z);
             if (r) {
                 float t[8];
-                load8_to(r + e, a.cols - e, a.rvec, t);
+                load8_to(r + e, left_of(a.cols, e), a.rvec, t);
 #pragma unroll
                 for (int i = 0; i < 8; i++) z[i] = __fadd_rn(z[i], t[i]);
             }
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
         if (a.n.rstd && threadIdx.x == 0) a.n.rstd[row] = rstd;
         auto norm8 = [&](int64_t e) {
             sum8(e, z);
-            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, a.cols - e, a.wvec, w);
+            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, left_of(a.cols, e), a.wvec, w);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 y[i] = __fmul_rn(z[i], rstd);
@@ -110,8 +110,8 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
             }
         };
         auto put8 = [&](int64_t e) {
-            if (a.n.h) store8_to(static_cast<T*>(a.n.h) + row * a.n.ldh + e, a.cols - e, a.hvec, z);
-            if (a.n.y) store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, a.cols - e, a.yvec, y);
+            if (a.n.h) store8_to(static_cast<T*>(a.n.h) + row * a.n.ldh + e, left_of(a.cols, e), a.hvec, z);
+            if (a.n.y) store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, left_of(a.cols, e), a.yvec, y);
         };
         if (!a.ngroups) {
             for (int64_t e = threadIdx.x * 8; e < a.cols; e += kNormThreads * 8) {
@@ -147,40 +147,63 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
 
 // ------------------------------------------------------- rows in registers
 
-// A row of up to TPR * NV * 8 values by TPR threads, held in registers from
-// its one read to its last write; the groups of codes are 4 to 32 lanes (32 to
-// 256 values), or the row.  HBM-bound where there are many rows (8192 x 4096
-// bf16 with residual, codes and their values: 15 bytes for every 2 of x read),
-// latency-bound where there are few.
-template <int TYPE, int TPR, int NV>
+// A row of up to 16 TPR values by TPR threads, 16 a thread, held in registers
+// from its one read to its last write; the next row is on its way meanwhile.
+// A group of codes is 2 to 16 lanes (32 to 256 values), or the row.  Many rows
+// are bound by instructions and HBM alike (8192 x 4096 bf16 with residual,
+// codes and values: 9 bytes for a value of x, 302 MB), few rows by latency.
+template <int TYPE, int TPR>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(const NormArgs a)
 {
     using T = Elem<TYPE>;
     constexpr int THREADS = TPR < 128 ? 128 : TPR, PER = THREADS / TPR, NW = TPR / 32;
+    constexpr bool AHEAD = TPR <= 512;                  // 1024 threads have 64 registers each: no next row, no weights
     __shared__ float shf[2][NW];
     __shared__ uint32_t shu[2][NW];
     griddep_wait();
-    const int t = threadIdx.x % TPR, lanes = (int)a.group / 8;
-    int flip = 0;
-    Raw8<T> rx[NV], rr[NV];                             // the next row, on its way
-    auto load = [&](int64_t row) {
-        const T* x = static_cast<const T*>(a.n.x) + row * a.n.ldx;
-        const T* r = static_cast<const T*>(a.n.residual) + row * a.n.ldr;
+    const int t = threadIdx.x % TPR, lanes = (int)a.group / 16, e = t * 16;
+    const int n = left_of(a.cols, e);
+    const float inv_cols = 1.0f / (float)a.cols;
+    int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * PER;
+    const T* px = static_cast<const T*>(a.n.x) + row * a.n.ldx + e;
+    const T* pr = static_cast<const T*>(a.n.residual) + row * a.n.ldr + e;
+    Raw8<T> rx[2], rr[2];
+    auto load = [&](bool on) {
+        const int k = on ? n : 0;
+        rx[0].load(px, k, a.xvec);
+        rx[1].load(px + 8, k - 8, a.xvec);
+        if (a.n.residual) {
+            rr[0].load(pr, k, a.rvec);
+            rr[1].load(pr + 8, k - 8, a.rvec);
+        }
+        px += step * a.n.ldx;
+        pr += step * a.n.ldr;
+    };
+    float w[2][8];
+    auto weights = [&]() {
 #pragma unroll
-        for (int v = 0; v < NV; v++) {
-            const int64_t e = (int64_t)(v * TPR + t) * 8, n = row < a.rows ? a.cols - e : 0;
-            rx[v].load(x + e, n, a.xvec);
-            if (a.n.residual) rr[v].load(r + e, n, a.rvec);
+        for (int v = 0; v < 2; v++) {
+            if (a.n.weight) {
+                load8_any(a.n.weight, a.n.w_type, e + 8 * v, n - 8 * v, a.wvec, w[v]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; i++) w[v][i] = 1.0f;
+            }
         }
     };
-    load((int64_t)blockIdx.x * PER + threadIdx.x / TPR);
+    if (AHEAD) {
+        load(row < a.rows);
+        weights();
+    }
+    int flip = 0;
     // a block's rows go on together, so that every thread meets every barrier
-    for (int64_t row0 = (int64_t)blockIdx.x * PER; row0 < a.rows; row0 += (int64_t)gridDim.x * PER, flip ^= 1) {
-        const int64_t row = row0 + threadIdx.x / TPR;
+    for (int64_t first = (int64_t)blockIdx.x * PER; first < a.rows; first += step, row += step, flip ^= 1) {
         const bool on = PER == 1 || row < a.rows;
-        float z[NV][8];
+        if (!AHEAD) load(on);
+        float z[2][8];
 #pragma unroll
-        for (int v = 0; v < NV; v++) {
+        for (int v = 0; v < 2; v++) {
             rx[v].values(z[v]);
             if (a.n.residual) {
                 float u[8];
@@ -189,13 +212,14 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(
                 for (int i = 0; i < 8; i++) z[v][i] = __fadd_rn(z[v][i], u[i]);
             }
         }
-        load(row + (int64_t)gridDim.x * PER);
-        float ss = 0.0f;
+        if (AHEAD) load(row + step < a.rows);
+        float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-        for (int v = 0; v < NV; v++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) ss = fmaf(z[v][i], z[v][i], ss);
-        ss = warp_sum(ss);
+        for (int i = 0; i < 8; i++) {
+            s0 = fmaf(z[0][i], z[0][i], s0);
+            s1 = fmaf(z[1][i], z[1][i], s1);
+        }
+        float ss = warp_sum(s0 + s1);
         if constexpr (NW > 1) {
             if ((threadIdx.x & 31) == 0) shf[flip][threadIdx.x >> 5] = ss;
             __syncthreads();
@@ -203,38 +227,33 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(
 #pragma unroll
             for (int i = 0; i < NW; i++) ss += shf[flip][i];
         }
-        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, (float)a.cols), a.n.eps)));
-        if (a.n.rstd && t == 0 && on) a.n.rstd[row] = rstd;
+        const float rstd = __frsqrt_rn(fmaf(ss, inv_cols, a.n.eps));
+        if (!on) continue;                              // only where a row is a warp: no barrier below
+        if (a.n.rstd && t == 0) a.n.rstd[row] = rstd;
+        if (a.n.h) {
+            T* h = static_cast<T*>(a.n.h) + row * a.n.ldh + e;
+            store8_to(h, n, a.hvec, z[0]);
+            store8_to(h + 8, n - 8, a.hvec, z[1]);
+        }
+        if (!AHEAD) weights();
+#pragma unroll
+        for (int v = 0; v < 2; v++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) z[v][i] = __fmul_rn(__fmul_rn(z[v][i], rstd), w[v][i]);
+        if (a.n.y) {
+            store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, n, a.yvec, z[0]);
+            store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e + 8, n - 8, a.yvec, z[1]);
+        }
+        if (!a.ngroups) continue;
+        // what lies past the row is 0 times rstd: 0, or NaN as the whole row
         uint32_t mx = 0u;
 #pragma unroll
-        for (int v = 0; v < NV; v++) {
-            const int64_t e = (int64_t)(v * TPR + t) * 8, n = on ? a.cols - e : 0;
-            if (a.n.h) store8_to(static_cast<T*>(a.n.h) + row * a.n.ldh + e, n, a.hvec, z[v]);
-            float w[8];
-            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, n, a.wvec, w);
+        for (int v = 0; v < 2; v++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                z[v][i] = __fmul_rn(z[v][i], rstd);
-                if (a.n.weight) z[v][i] = __fmul_rn(z[v][i], w[i]);
-            }
-            if (a.n.y) store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, n, a.yvec, z[v]);
-            if (a.ngroups == 1) {
-                // what lies past the row is 0 times rstd: NaN for a row that has none
-#pragma unroll
-                for (int i = 0; i < 8; i++) mx = max(mx, i < n ? magnitude_bits(z[v][i], a.f.is_signed) : 0u);
-            } else if (a.ngroups) {
-                uint32_t m = 0u;
-#pragma unroll
-                for (int i = 0; i < 8; i++) m = max(m, i < n ? magnitude_bits(z[v][i], a.f.is_signed) : 0u);
-                for (int o = lanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const float alpha = absmax_scale(m, a.f);
-                if (on && e < a.n.ldc * 4) {
-                    if (t % lanes == 0 && n > 0) a.n.scales[row * a.n.lds + e / a.group] = alpha;
-                    put_codes8(a, row, e, z[v], make_scale(alpha, a.f));
-                }
-            }
-        }
-        if (a.ngroups == 1) {
+            for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(z[v][i], a.f.is_signed));
+        if (a.ngroups > 1) {
+            for (int o = lanes / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        } else {
             mx = __reduce_max_sync(0xffffffffu, mx);
             if constexpr (NW > 1) {
                 if ((threadIdx.x & 31) == 0) shu[flip][threadIdx.x >> 5] = mx;
@@ -242,18 +261,40 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(
 #pragma unroll
                 for (int i = 0; i < NW; i++) mx = max(mx, shu[flip][i]);
             }
-            const float alpha = absmax_scale(mx, a.f);
-            if (t == 0 && on) a.n.scales[row * a.n.lds] = alpha;
+        }
+        const float alpha = absmax_scale(mx, a.f);
+        const int64_t left = a.n.ldc - (int64_t)t * 4;  // words of the row from this thread's first one on
+        if (left > 0) {
+            if (a.ngroups == 1) {
+                if (t == 0) a.n.scales[row * a.n.lds] = alpha;
+            } else if (t % lanes == 0 && n > 0) {
+                a.n.scales[row * a.n.lds + t / lanes] = alpha;
+            }
             const GroupScale s = make_scale(alpha, a.f);
+            uint32_t c[2][2];
+            float q[2][8];
 #pragma unroll
-            for (int v = 0; v < NV; v++) {
-                const int64_t e = (int64_t)(v * TPR + t) * 8;
-                if (on && e < a.n.ldc * 4) put_codes8(a, row, e, z[v], s);
+            for (int v = 0; v < 2; v++) {
+                quantise8<8>(z[v], s, a.f, c[v], q[v]);
+                if (n - 8 * v < 8) zero_past<8>(c[v], n - 8 * v, a.f);
+            }
+            uint32_t* p = a.n.codes + row * a.n.ldc + t * 4;
+            if (a.cvec && left >= 4) {
+                *reinterpret_cast<uint4*>(p) = make_uint4(c[0][0], c[0][1], c[1][0], c[1][1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (i < left) p[i] = c[i / 2][i % 2];
+            }
+            if (a.n.yq) {
+                element_values(z[0], s, a.f, q[0]);
+                element_values(z[1], s, a.f, q[1]);
+                store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q[0]);
+                store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e + 8, n - 8, a.qvec, q[1]);
             }
         }
         // words past those that the threads' values reach (a long row stride)
-        if (a.ngroups && on)
-            for (int64_t w = (int64_t)TPR * NV * 2 + t; w < a.n.ldc; w += TPR) a.n.codes[row * a.n.ldc + w] = a.f.zero_code * 0x01010101u;
+        for (int64_t i = (int64_t)TPR * 4 + t; i < a.n.ldc; i += TPR) a.n.codes[row * a.n.ldc + i] = a.f.zero_code * 0x01010101u;
     }
 }
 
@@ -281,9 +322,9 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dx_kernel(const NormGrad
         const float rstd = a.n.rstd[row];
         float n[8], d[8], t[8];
         auto both8 = [&](int64_t e) {
-            load8_to(h + e, a.cols - e, a.hvec, n);
-            load8_any(a.n.dy, a.n.g_type, row * a.n.ldg + e, a.cols - e, a.gvec, d);
-            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, a.cols - e, a.wvec, t);
+            load8_to(h + e, left_of(a.cols, e), a.hvec, n);
+            load8_any(a.n.dy, a.n.g_type, row * a.n.ldg + e, left_of(a.cols, e), a.gvec, d);
+            if (a.n.weight) load8_any(a.n.weight, a.n.w_type, e, left_of(a.cols, e), a.wvec, t);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 n[i] *= rstd;
@@ -299,13 +340,13 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dx_kernel(const NormGrad
         const float m = block_sum<NW>(s, shf) / (float)a.cols;
         for (int64_t e = threadIdx.x * 8; e < a.cols; e += kNormThreads * 8) {
             both8(e);
-            if (a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e, a.cols - e, a.dhvec, t);
+            if (a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e, left_of(a.cols, e), a.dhvec, t);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 d[i] = rstd * fmaf(-n[i], m, d[i]);
                 if (a.n.dh) d[i] += t[i];
             }
-            store8_to(static_cast<T*>(a.n.dx) + row * a.n.lddx + e, a.cols - e, a.dxvec, d);
+            store8_to(static_cast<T*>(a.n.dx) + row * a.n.lddx + e, left_of(a.cols, e), a.dxvec, d);
         }
     }
 }
@@ -322,12 +363,12 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_kernel(const NormGrad
     float s[8] = {}, n[8], d[8];
     for (int64_t row = blockIdx.y; row < a.rows; row += a.parts) {
         const float rstd = a.n.rstd[row];
-        load8_to(static_cast<const T*>(a.n.h) + row * a.n.ldh + e, a.cols - e, a.hvec, n);
-        load8_any(a.n.dy, a.n.g_type, row * a.n.ldg + e, a.cols - e, a.gvec, d);
+        load8_to(static_cast<const T*>(a.n.h) + row * a.n.ldh + e, left_of(a.cols, e), a.hvec, n);
+        load8_any(a.n.dy, a.n.g_type, row * a.n.ldg + e, left_of(a.cols, e), a.gvec, d);
 #pragma unroll
         for (int i = 0; i < 8; i++) s[i] = fmaf(d[i], n[i] * rstd, s[i]);
     }
-    store8_to(a.part + (int64_t)blockIdx.y * a.cols + e, a.cols - e, false, s);
+    store8_to(a.part + (int64_t)blockIdx.y * a.cols + e, left_of(a.cols, e), false, s);
 }
 
 // Both for rows in registers: a thread keeps its columns of every row of its
@@ -349,7 +390,7 @@ __global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGra
         e[v] = (int64_t)(v * TPR + threadIdx.x) * 8;
 #pragma unroll
         for (int i = 0; i < 8; i++) { w[v][i] = 1.0f; dw[v][i] = 0.0f; }
-        if (NV == 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], a.cols - e[v], a.wvec, w[v]);
+        if (NV == 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], left_of(a.cols, e[v]), a.wvec, w[v]);
     }
     float rstd = 0.0f;
     Raw8<T> rh[NV], rt[NV];                             // the next row, on its way
@@ -359,7 +400,7 @@ __global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGra
         if (on) rstd = a.n.rstd[row];
 #pragma unroll
         for (int v = 0; v < NV; v++) {
-            const int64_t left = on ? a.cols - e[v] : 0;
+            const int left = on ? left_of(a.cols, e[v]) : 0;
             rh[v].load(static_cast<const T*>(a.n.h) + row * a.n.ldh + e[v], left, a.hvec);
             rg[v].load(static_cast<const G*>(a.n.dy) + row * a.n.ldg + e[v], left, a.gvec);
             if (NV == 1 && a.n.dh) rt[v].load(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[v], left, a.dhvec);
@@ -381,7 +422,7 @@ __global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGra
 #pragma unroll
         for (int v = 0; v < NV; v++) {
             // of two vectors the weights (and dh below) are not kept: 64 registers a thread
-            if (NV > 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], a.cols - e[v], a.wvec, t);
+            if (NV > 1 && a.n.weight) load8_any(a.n.weight, a.n.w_type, e[v], left_of(a.cols, e[v]), a.wvec, t);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 n[v][i] *= rs;
@@ -400,18 +441,18 @@ __global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGra
         const float m = s / (float)a.cols;
 #pragma unroll
         for (int v = 0; v < NV; v++) {
-            if (NV > 1 && a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[v], a.cols - e[v], a.dhvec, t);
+            if (NV > 1 && a.n.dh) load8_to(static_cast<const T*>(a.n.dh) + row * a.n.lddh + e[v], left_of(a.cols, e[v]), a.dhvec, t);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 d[v][i] = rs * fmaf(-n[v][i], m, d[v][i]);
                 if (a.n.dh) d[v][i] += t[i];
             }
-            store8_to(static_cast<T*>(a.n.dx) + row * a.n.lddx + e[v], a.cols - e[v], a.dxvec, d[v]);
+            store8_to(static_cast<T*>(a.n.dx) + row * a.n.lddx + e[v], left_of(a.cols, e[v]), a.dxvec, d[v]);
         }
     }
     if (a.part) {
 #pragma unroll
-        for (int v = 0; v < NV; v++) store8_to(a.part + blockIdx.x * a.cols + e[v], a.cols - e[v], (a.cols & 3) == 0, dw[v]);
+        for (int v = 0; v < NV; v++) store8_to(a.part + blockIdx.x * a.cols + e[v], left_of(a.cols, e[v]), (a.cols & 3) == 0, dw[v]);
     }
 }
 
@@ -440,18 +481,13 @@ struct NormPlan {
     NormKernel kernel;
     int tpr;
 };
-// Threads for a row: few rows want all of an SM's loads at once, many rows few
-// barriers.
-template <int TYPE> NormPlan norm_plan(int64_t rows, int64_t cols, int64_t sms)
+template <int TYPE> NormPlan norm_plan(int64_t cols)
 {
-    if (cols <= 256) return {rmsnorm_rows_kernel<TYPE, 32, 1>, 32};
-    if (cols <= 512) return {rmsnorm_rows_kernel<TYPE, 32, 2>, 32};
-    if (cols <= 1024) return {rmsnorm_rows_kernel<TYPE, 128, 1>, 128};
-    if (cols <= 2048) return {rmsnorm_rows_kernel<TYPE, 256, 1>, 256};
-    if (cols <= 4096 && rows >= 4 * sms) return {rmsnorm_rows_kernel<TYPE, 256, 2>, 256};
-    if (cols <= 4096) return {rmsnorm_rows_kernel<TYPE, 512, 1>, 512};
-    if (cols <= 8192) return {rmsnorm_rows_kernel<TYPE, 512, 2>, 512};
-    if (cols <= 16384) return {rmsnorm_rows_kernel<TYPE, 1024, 2>, 1024};
+    if (cols <= 512) return {rmsnorm_rows_kernel<TYPE, 32>, 32};
+    if (cols <= 2048) return {rmsnorm_rows_kernel<TYPE, 128>, 128};
+    if (cols <= 4096) return {rmsnorm_rows_kernel<TYPE, 256>, 256};
+    if (cols <= 8192) return {rmsnorm_rows_kernel<TYPE, 512>, 512};
+    if (cols <= 16384) return {rmsnorm_rows_kernel<TYPE, 1024>, 1024};
     return {rmsnorm_kernel<TYPE>, 0};
 }
 
@@ -504,11 +540,11 @@ cudaError_t launch_rmsnorm(int64_t rows, int64_t cols, const esb_norm& n, cudaSt
     a.yvec = rows16(n.y, n.ldy, n.y_type);
     a.qvec = rows16(n.yq, n.ldq, n.y_type);
     a.wvec = rows16(n.weight, 0, n.w_type);
-    a.cvec = n.codes && (reinterpret_cast<uintptr_t>(n.codes) & 7u) == 0 && n.ldc % 2 == 0;
+    a.cvec = rows16(n.codes, n.ldc, ESB_F32);
     const int64_t sms = device_sm_count();
-    static NormPlan (*const plans[3])(int64_t, int64_t, int64_t) = {norm_plan<ESB_F32>, norm_plan<ESB_F16>, norm_plan<ESB_BF16>};
+    static NormPlan (*const plans[3])(int64_t) = {norm_plan<ESB_F32>, norm_plan<ESB_F16>, norm_plan<ESB_BF16>};
     static const NormKernel any[3] = {rmsnorm_kernel<ESB_F32>, rmsnorm_kernel<ESB_F16>, rmsnorm_kernel<ESB_BF16>};
-    NormPlan p = plans[n.x_type](rows, cols, sms);
+    const NormPlan p = plans[n.x_type](cols);
     const bool lanes = a.ngroups <= 1 || a.group == 32 || a.group == 64 || a.group == 128 || a.group == 256;
     if (!p.tpr || !lanes) {
         const int64_t cap = sms * 8;
@@ -516,7 +552,7 @@ cudaError_t launch_rmsnorm(int64_t rows, int64_t cols, const esb_norm& n, cudaSt
     }
     const int threads = p.tpr < 128 ? 128 : p.tpr;
     int64_t blocks = (rows + threads / p.tpr - 1) / (threads / p.tpr);
-    const int64_t cap = sms * (2048 / threads) * 2;
+    const int64_t cap = sms * (threads >= 1024 ? 1 : 768 / threads);   // about what the SMs hold: each block keeps its weights
     if (blocks > cap) blocks = cap;
     return launch_pdl(p.kernel, dim3((unsigned)blocks), dim3((unsigned)threads), 0, st, a);
 }

@@ -84,11 +84,18 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8])
     }
 }
 
+// What is left of `cols` values from place e on, as a count of a few of them.
+__device__ __forceinline__ int left_of(int64_t cols, int64_t e)
+{
+    const int64_t n = cols - e;
+    return n > 64 ? 64 : (n < 0 ? 0 : (int)n);
+}
+
 // The same for the first `n` of eight values (n may be <= 0), one by one
 // unless all eight are there and `vec` says that p is 16-byte aligned.
 // Values past n read as 0.
 template <class T>
-__device__ __forceinline__ void load8_to(const T* p, int64_t n, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8_to(const T* p, int n, bool vec, float (&v)[8])
 {
     if (vec && n >= 8) {
         load8<T>(p, v);
@@ -99,7 +106,7 @@ __device__ __forceinline__ void load8_to(const T* p, int64_t n, bool vec, float 
 }
 
 template <class T>
-__device__ __forceinline__ void store8_to(T* p, int64_t n, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8_to(T* p, int n, bool vec, const float (&v)[8])
 {
     if (vec && n >= 8) {
         store8<T>(p, v);
@@ -115,7 +122,7 @@ __device__ __forceinline__ void store8_to(T* p, int64_t n, bool vec, const float
 template <class T>
 struct Raw8 {
     uint32_t w[2 * sizeof(T)];
-    __device__ __forceinline__ void load(const T* p, int64_t n, bool vec)
+    __device__ __forceinline__ void load(const T* p, int n, bool vec)
     {
         if (vec && n >= 8) {
 #pragma unroll
@@ -145,13 +152,13 @@ struct Raw8 {
 };
 
 // Values of a type that the kernel learns at run time (uniform branches).
-__device__ __forceinline__ void load8_any(const void* p, int type, int64_t at, int64_t n, bool vec, float (&v)[8])
+__device__ __forceinline__ void load8_any(const void* p, int type, int64_t at, int n, bool vec, float (&v)[8])
 {
     if (type == ESB_F32) load8_to(static_cast<const float*>(p) + at, n, vec, v);
     else if (type == ESB_F16) load8_to(static_cast<const __half*>(p) + at, n, vec, v);
     else load8_to(static_cast<const __nv_bfloat16*>(p) + at, n, vec, v);
 }
-__device__ __forceinline__ void store8_any(void* p, int type, int64_t at, int64_t n, bool vec, const float (&v)[8])
+__device__ __forceinline__ void store8_any(void* p, int type, int64_t at, int n, bool vec, const float (&v)[8])
 {
     if (type == ESB_F32) store8_to(static_cast<float*>(p) + at, n, vec, v);
     else if (type == ESB_F16) store8_to(static_cast<__half*>(p) + at, n, vec, v);
@@ -362,15 +369,15 @@ __device__ __forceinline__ void element_values(const float (&x)[8], const GroupS
 // The words of eight codes of which only the first n are a row's: the rest
 // become the zero code.
 template <int B>
-__device__ __forceinline__ void zero_past(uint32_t (&w)[B / 4], int64_t n, const QuantFmt& f)
+__device__ __forceinline__ void zero_past(uint32_t (&w)[B / 4], int n, const QuantFmt& f)
 {
     constexpr int PER = 32 / B;
     constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
 #pragma unroll
     for (int i = 0; i < B / 4; i++) {
-        const int64_t k = n - i * PER;
+        const int k = n - i * PER;
         if (k >= PER) continue;
-        const uint32_t keep = k <= 0 ? 0u : (1u << (B * (int)k)) - 1u;
+        const uint32_t keep = k <= 0 ? 0u : (1u << (B * k)) - 1u;
         w[i] = (w[i] & keep) | ((f.zero_code * ONES) & ~keep);
     }
 }
