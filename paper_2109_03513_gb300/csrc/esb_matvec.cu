@@ -30,7 +30,7 @@
 #include <cuda_runtime.h>
 
 #include "esb_internal.h"
-#include "esb_rows.cuh"
+#include "esb_matvec.cuh"
 
 namespace esb {
 
@@ -39,33 +39,6 @@ namespace {
 constexpr int kRedLd = 20;          // floats between columns of a warp's 16 sums
 constexpr int kSteps = 4;           // steps of 128 codes of a row, 16 bytes a lane and row, that a warp has in flight
 constexpr int kSlice = 128 * kSteps;
-
-// fp16 high bytes of the elements by the code's low 3 bits; 2^16 and 2^4.
-struct MvTable {
-    uint32_t lo, hi, by16, by4;
-};
-
-struct MvArgs {
-    int64_t M, N, K;
-    const void* x;
-    int64_t ldx;
-    esb_coded xc;                   // for x_type ESB_CODES
-    esb_coded w;
-    int64_t xgroup, ngroups;
-    const float* bias;
-    void* y;
-    int64_t ldy;
-    MvTable tab;
-    int x_type, y_type, xvec;
-    uint32_t gmagic;                // 2^32 / (group / 32) rounded up, 0 for groups of 32
-    int mt, planes;                 // rows of x in a block, planes of each
-    int kc;                         // codes of a row in a block (a multiple of 512)
-    int zrow;                       // whether some lanes read zeros in place of x
-    int64_t wfull;                  // codes of a row that whole 16-byte words hold
-    int wk;                         // warps along a row (the others take other tiles)
-    int split;                      // blocks along a row (a cluster)
-    int hold;                       // tiles whose sums wait for one barrier
-};
 
 __device__ __forceinline__ uint4 ldg_stream(const uint32_t* p)
 {
@@ -98,31 +71,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
-// Eight codes as four fp16 pairs {0,2} {1,3} {4,6} {5,7}: the order in which
-// a word's sign bits lie at the top of alternate bytes.  The two shifts are
-// products with powers of two that the compiler does not know: the ALU pipe,
-// which the other eleven instructions take, bounds the kernel, and the
-// multiply-add pipe is free.
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
-{
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
-    return r;
-}
-__device__ __forceinline__ void decode8(uint32_t w, const MvTable& tb, uint32_t (&p)[4])
-{
-    const uint32_t sel = w & 0x77777777u;
-    const uint32_t m03 = prmt(tb.lo, tb.hi, sel), m47 = prmt(tb.lo, tb.hi, __umulhi(sel, tb.by16));
-    const uint32_t odd = prmt(m03, m47, 0x7531u) | (w & 0x80808080u);
-    const uint32_t even = prmt(m03, m47, 0x6420u) | ((w * tb.by4) & 0x80808080u);
-    p[0] = prmt(even, 0u, 0x1404u);
-    p[1] = prmt(odd, 0u, 0x1404u);
-    p[2] = prmt(even, 0u, 0x3424u);
-    p[3] = prmt(odd, 0u, 0x3424u);
-}
-
-__device__ __forceinline__ uint32_t half2_of(float a, float b) { return pack2<__half>(a, b); }
-
 // Shared memory: for every plane of every row kc halves -- 8 at a time in the
 // pair order above, the four lanes' eights of a word next to each other --
 // and 64 bytes of padding (lanes of neighbouring columns read other banks), a
@@ -145,113 +93,19 @@ __device__ __forceinline__ float ld_cluster(const float* p, int rank)
     return v;
 }
 
-// Eight values of x at block i of the 16 of a step: scaled, split into
-// planes, in pair order.  All 32 lanes take part.
-template <int NT, int R, int TYPE>
-__device__ __forceinline__ void put_x8(const MvArgs& a, float (&v)[8], int i, unsigned char* at, float* f)
-{
-    constexpr int LANES = 16 / R;                       // lanes that share a scale
-    float back = 1.0f;
-    if constexpr (TYPE != ESB_F16) {
-        uint32_t mx = 0u;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const uint32_t u = __float_as_uint(v[j]) & 0x7fffffffu;
-            mx = max(mx, u < 0x7f800000u ? u : 0u);
-        }
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const int e = max((int)(mx >> 23), 15);         // exponent field; 2^(14 - (e - 127)) <= 2^126
-        const float s = __uint_as_float((uint32_t)(268 - e) << 23);
-        back = __uint_as_float((uint32_t)(e - 14) << 23);
-#pragma unroll
-        for (int j = 0; j < 8; j++) v[j] *= s;
+// Where stage_x puts a plane's eights and a column's scales.
+template <int NT, int R>
+struct XsPlace {
+    unsigned char* xs;
+    float* fx;
+    int stride;
+    __device__ __forceinline__ uint4* values(int row, int b) const
+    {
+        const int i = b & 15;
+        return reinterpret_cast<uint4*>(xs + (size_t)row * stride + (size_t)(b >> 4) * 256 + ((i & 3) * 4 + (i >> 2)) * 16);
     }
-    if constexpr (TYPE == ESB_F32) {
-        float lo[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float hi = __half2float(__float2half_rn(v[j]));
-            lo[j] = fabsf(hi) < __int_as_float(0x7f800000) ? (v[j] - hi) * 2048.0f : 0.0f;
-            v[j] = hi;
-        }
-        *reinterpret_cast<uint4*>(at + xs_stride(a.kc)) = make_uint4(half2_of(lo[0], lo[2]), half2_of(lo[1], lo[3]),
-                                                                     half2_of(lo[4], lo[6]), half2_of(lo[5], lo[7]));
-        if (i % LANES == 0) f[R] = back * (1.0f / 2048.0f);
-    }
-    *reinterpret_cast<uint4*>(at) = make_uint4(half2_of(v[0], v[2]), half2_of(v[1], v[3]), half2_of(v[4], v[6]), half2_of(v[5], v[7]));
-    if (i % LANES == 0) *f = back;
-}
-
-// Rows m0 .. m0 + mt - 1 of x, codes k0 .. k0 + kc - 1, into shared memory: a
-// warp takes 256 values of a row at a time, several such parts in flight.
-template <int NT, int R, int WARPS, int TYPE>
-__device__ __forceinline__ void stage_x(const MvArgs& a, int64_t m0, int mt, int64_t k0, unsigned char* xs, float* fx, const uint16_t* xtab)
-{
-    constexpr int U = TYPE == ESB_F32 ? 4 : 8, WORDS = TYPE == ESB_F32 ? 8 : (TYPE == ESB_CODES ? 2 : 4);
-    const int stride = xs_stride(a.kc), parts = a.kc / 256, total = mt * parts;
-    const int lane = threadIdx.x & 31, i = lane & 15;
-    for (int q0 = threadIdx.x >> 5; q0 < total; q0 += U * WARPS) {
-        uint32_t raw[U][WORDS];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int q = q0 + u * WARPS;
-            if (q >= total) break;
-            const int m = q / parts;
-            const int64_t k = k0 + (q - m * parts) * 256 + lane * 8, n = a.K - k;
-            if constexpr (TYPE == ESB_CODES) {
-                const uint32_t* xw = a.xc.codes + (m0 + m) * a.xc.ld + k / 4;
-                raw[u][0] = n > 0 ? __ldg(xw) : 0u;
-                raw[u][1] = n > 4 ? __ldg(xw + 1) : 0u;
-            } else {
-                using T = Elem<TYPE>;
-                const T* p = static_cast<const T*>(a.x) + (m0 + m) * a.ldx + k;
-                if (a.xvec && n >= 8) {
-#pragma unroll
-                    for (int j = 0; j < WORDS; j += 4) {
-                        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + j / 4);
-                        raw[u][j] = v.x; raw[u][j + 1] = v.y; raw[u][j + 2] = v.z; raw[u][j + 3] = v.w;
-                    }
-                } else if constexpr (TYPE == ESB_F32) {
-#pragma unroll
-                    for (int j = 0; j < 8; j++) raw[u][j] = j < n ? __float_as_uint(p[j]) : 0u;
-                } else {
-                    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        raw[u][j] = (2 * j < n ? h[2 * j] : 0u) | ((2 * j + 1 < n ? (uint32_t)h[2 * j + 1] : 0u) << 16);
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int q = q0 + u * WARPS;
-            if (q >= total) break;
-            const int m = q / parts, b = (q - m * parts) * 32 + lane, step = b >> 4, r = i / (16 / R);
-            unsigned char* at = xs + (size_t)(m * a.planes) * stride + (size_t)(step * 128 + ((i & 3) * 4 + (i >> 2)) * 8) * 2;
-            float* f = fx + step * 8 * NT + m * a.planes * R + r;
-            if constexpr (TYPE == ESB_CODES) {
-                const int64_t k = k0 + (int64_t)b * 8, n = a.K - k;
-                uint32_t h[8];
-#pragma unroll
-                for (int j = 0; j < 8; j++) h[j] = j < n ? xtab[(raw[u][j >> 2] >> (8 * (j & 3))) & 255u] : 0u;
-                *reinterpret_cast<uint4*>(at) = make_uint4(h[0] | (h[2] << 16), h[1] | (h[3] << 16), h[4] | (h[6] << 16), h[5] | (h[7] << 16));
-                if (i % (16 / R) == 0)
-                    *f = n > 0 ? a.xc.scales[(m0 + m) * a.xc.lds + k / a.xgroup] * (a.xc.fmt.k == 2 ? 65536.0f : 1.0f) : 0.0f;
-            } else {
-                float v[8];
-                if constexpr (TYPE == ESB_F32) {
-#pragma unroll
-                    for (int j = 0; j < 8; j++) v[j] = __uint_as_float(raw[u][j]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; j++) unpack2<Elem<TYPE>>(raw[u][j], v[2 * j], v[2 * j + 1]);
-                }
-                put_x8<NT, R, TYPE>(a, v, i, at, f);
-            }
-        }
-    }
-}
+    __device__ __forceinline__ float* scale(int row, int step, int r) const { return fx + step * 8 * NT + row * R + r; }
+};
 
 template <int NT, int R, int WARPS, int BLOCKS>
 __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs a)
@@ -327,17 +181,10 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     if (a.zrow)
         for (int i = threadIdx.x * 16; i < a.kc * 2; i += THREADS * 16) *reinterpret_cast<uint4*>(zeros + i) = make_uint4(0u, 0u, 0u, 0u);
     if (a.x_type == ESB_CODES) {
-        // k = 2 reaches 1.75 * 2^30; its elements are scaled by 2^-16
-        for (int i = threadIdx.x; i < 256; i += THREADS) {
-            const __half h = __float2half_rn(code_value(i, 8, a.xc.fmt.k) * (a.xc.fmt.k == 2 ? 1.0f / 65536.0f : 1.0f));
-            xtab[i] = *reinterpret_cast<const uint16_t*>(&h);
-        }
+        for (int i = threadIdx.x; i < 256; i += THREADS) xtab[i] = x_code_half(i, a.xc.fmt.k);
         __syncthreads();
     }
-    if (a.x_type == ESB_BF16) stage_x<NT, R, WARPS, ESB_BF16>(a, m0, mt, k0, xs, fx, xtab);
-    else if (a.x_type == ESB_CODES) stage_x<NT, R, WARPS, ESB_CODES>(a, m0, mt, k0, xs, fx, xtab);
-    else if (a.x_type == ESB_F16) stage_x<NT, R, WARPS, ESB_F16>(a, m0, mt, k0, xs, fx, xtab);
-    else stage_x<NT, R, WARPS, ESB_F32>(a, m0, mt, k0, xs, fx, xtab);
+    stage_x<R>(a, m0, mt, k0, XsPlace<NT, R>{xs, fx, xs_stride(a.kc)}, xtab, WARPS, warp);
     __syncthreads();
 
     // where this lane reads x for column 8 i + g: its row's plane, or zeros
@@ -350,13 +197,7 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     }
     const uint32_t fp = smem_u32(fx) + t * 8;
 
-    auto put = [&](int n, int m, float v) {
-        if (a.bias) v += a.bias[n];
-        const int64_t at = (m0 + m) * a.ldy + n;
-        if (a.y_type == ESB_F32) static_cast<float*>(a.y)[at] = v;
-        else if (a.y_type == ESB_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(v);
-        else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-    };
+    auto put = [&](int n, int m, float v) { put_y(a, m0 + m, n, v); };
 
     int flip = 0, held = 0;                             // held: tiles whose sums wait in red's half
     for (int base = first; base < tiles; base += stride) {
@@ -530,6 +371,9 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
     a.planes = x_type == ESB_F32 ? 2 : 1;
     a.wfull = std::min<int64_t>(w.ld * 8, (int64_t)1 << 20);
 
+    cudaError_t e = cudaSuccess;
+    if (launch_matvec_tc(a, r, st, &e)) return e;
+
     // Rows a block takes at once: up to 32 columns' worth, fewer where x would
     // not fit; the row's codes over up to 8 blocks (a cluster) where that
     // makes x fit.
@@ -569,7 +413,6 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         if (!a.wk || cost < best) { best = cost; a.wk = wk; }
     }
     const int64_t want = (tiles + p.warps / a.wk - 1) / (p.warps / a.wk), cap = at_once;
-    cudaError_t e = cudaSuccess;
     if (smem > 47 * 1024) e = cudaFuncSetAttribute(p.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
     if (e != cudaSuccess) return e;
     for (int64_t p0 = 0; p0 < passes; p0 += 65535) {    // grid.z holds 65535 passes

@@ -223,6 +223,49 @@ def test_matvec_coded_rows(M, N, K, group, xgroup, xk):
     assert esb.esb_matvec_groups(xc, w).dtype == torch.bfloat16
 
 
+# enough matrix rows for every SM to get tiles of 128
+@pytest.mark.parametrize("M,N,K,group", [(1, 16384, 512, 128), (1, 15700, 1000, 64), (2, 20001, 64, 32), (5, 19457, 577, 96),
+                                         (8, 30000, 33, 0), (16, 15616, 4096, 128), (17, 16000, 2050, 256), (32, 40000, 300, 64),
+                                         (40, 15999, 1024, 32), (3, 60000, 130, 128), (24, 16000, 700, 128), (12, 20000, 513, 96),
+                                         (33, 15616, 4096, 128)])
+@pytest.mark.parametrize("x", [torch.float32, torch.float16, torch.bfloat16, "codes"])
+def test_matvec_many_columns(M, N, K, group, x):
+    w = make_w(N, K, group, (M + N) % 4)
+    rows = rand((M, K), 2)
+    if x == "codes":
+        rows = esb.esb_project_groups(rows, esb.Fmt(8, 6), 0)[0]
+        x64 = values64(rows)
+    else:
+        rows = rows.to(x)
+        x64 = rows.double()
+    bias = rand((N,), 3)
+    out = torch.full((M, N + 3), 5.0, dtype=torch.float32, device="cuda")
+    y = esb.esb_matvec_groups(rows, w, bias=bias, y=out[:, 1:N + 1])
+    w64 = values64(w)
+    want = x64 @ w64.t() + bias.double()
+    close(y, want, matvec_bound(x64, w64, K) + U * want.abs(), torch.float32)
+    assert (out[:, 0] == 5).all() and (out[:, N + 1:] == 5).all()
+    assert torch.equal(y, esb.esb_matvec_groups(rows, w, bias=bias, y_dtype=torch.float32))
+    assert esb.esb_get_status() == 0
+
+
+def test_matvec_many_columns_special_values_and_padding():
+    K, N = 333, 16001
+    x = rand((5, K), 9)
+    x[0, 3] = float("inf")
+    x[1, 200] = float("nan")
+    x[3] = 0
+    x[4, 100] = -float("inf")
+    w = esb.esb_project_groups(rand((N, K), 3).abs() + 0.5, esb.Fmt(4, 2), 64)[0]     # no zero weight
+    codes = torch.randint(-2 ** 31, 2 ** 31 - 1, (N, 48), dtype=torch.int32, device="cuda")
+    codes[:, :42] = w.codes[:, :42]
+    scales = torch.full((N, 9), float("nan"), device="cuda")
+    scales[:, :6] = w.scales
+    y = esb.esb_matvec_groups(x, esb.Coded(codes, scales[:, :6], w.fmt, K, 64))
+    assert (y[0] == float("inf")).all() and torch.isnan(y[1]).all() and (y[3] == 0).all() and (y[4] == -float("inf")).all()
+    close(y[2:3], x[2:3].double() @ values64(w).t(), matvec_bound(x[2:3].double(), values64(w), K), torch.float32)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_matvec_wide_range_rows(dtype):
     # values over the whole of the type's range, in blocks of their own size
