@@ -109,15 +109,16 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
 }
 
 // Groups of 32, 64, 128 or 256 values: 16 a lane, LANES lanes to a group, the
-// values in registers from the scale to the codes, kChunks times 16 of them in
-// flight.  Rows are padded to whole groups (`chunks` sixteens); a thread goes
-// on by dr rows and dc sixteens.  Instructions bound it (16384 x 4096 bf16 to
-// (4,2) with values, 302 MB of reads and writes): a value may cost 24 at the
-// copy rate, and the quotient, its rounding and sign, the element's value and
-// a sixteenth of the group's scale take about as many.
-constexpr int kChunks = 2;
+// values in registers from the scale to the codes.  Rows are padded to whole
+// groups (`chunks` sixteens); a thread goes on by dr rows and dc sixteens.
+// Instructions bound it: a value may cost 24 at the copy rate, and the
+// quotient, its rounding and sign, the element's value and a sixteenth of the
+// group's scale take about as many.  16384 x 4096 bf16 to (4,2) with values
+// (302 MB of reads and writes, 45 us at the copy rate): 72 us with 16 values a
+// thread and four blocks on an SM, 78 to 91 with 32 in flight.
+constexpr int kChunks = 1;
 template <int TYPE, int B, int LANES>
-__global__ void __launch_bounds__(kGroupThreads) project_small_groups_kernel(const GroupArgs a, int chunks, int dr, int dc)
+__global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(const GroupArgs a, int chunks, int dr, int dc)
 {
     using T = Elem<TYPE>;
     griddep_wait();
@@ -270,7 +271,7 @@ cudaError_t launch_project_groups(const void* x, int x_type, int64_t rows, int64
                                                        {small_kernel<ESB_F16, 4>, small_kernel<ESB_F16, 8>},
                                                        {small_kernel<ESB_BF16, 4>, small_kernel<ESB_BF16, 8>}};
         int64_t blocks = (rows * chunks + kGroupThreads - 1) / kGroupThreads;
-        const int64_t cap = sms * 8;
+        const int64_t cap = sms * 16;
         if (blocks > cap) blocks = cap;
         const int64_t threads = blocks * kGroupThreads;
         return launch_pdl(pick[x_type][f.b == 8](lanes), dim3((unsigned)blocks), dim3(kGroupThreads), 0, st, a, (int)chunks,

@@ -150,10 +150,12 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
 // A row of up to 16 TPR values by TPR threads, 16 a thread, held in registers
 // from its one read to its last write; the next row is on its way meanwhile.
 // A group of codes is 2 to 16 lanes (32 to 256 values), or the row.  Many rows
-// are bound by instructions and HBM alike (8192 x 4096 bf16 with residual,
-// codes and values: 9 bytes for a value of x, 302 MB), few rows by latency.
+// are bound by instructions and HBM alike: 8192 x 4096 bf16 with residual,
+// codes and values (9 bytes for a value of x, 302 MB, 45 us at the copy rate)
+// 73 us with two blocks of 256 on an SM, 81 with three.  Few rows are bound by
+// latency: one row of 4096 takes 3.5 us.
 template <int TYPE, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, 1) rmsnorm_rows_kernel(const NormArgs a)
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR < 256 ? 4 : 2)) rmsnorm_rows_kernel(const NormArgs a)
 {
     using T = Elem<TYPE>;
     constexpr int THREADS = TPR < 128 ? 128 : TPR, PER = THREADS / TPR, NW = TPR / 32;
@@ -373,10 +375,11 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_dw_kernel(const NormGrad
 
 // Both for rows in registers: a thread keeps its columns of every row of its
 // block, their weights and their part of dweight, and loads the next row while
-// it works on this one.  8192 x 4096 bf16: 268 MB of reads and writes (the
-// three kernels above read the gradient and h twice).
+// it works on this one.  8192 x 4096 bf16, 268 MB of reads and writes (the
+// kernels above read the gradient and h twice): forward and backward together
+// 100 us with two blocks of 512 on an SM, 117 with one; 79 at the copy rate.
 template <int TYPE, int GTYPE, int TPR, int NV>
-__global__ void __launch_bounds__(TPR, 1) rmsnorm_grad_rows_kernel(const NormGradArgs a)
+__global__ void __launch_bounds__(TPR, TPR >= 1024 ? 1 : (TPR < 128 ? 8 : (TYPE == ESB_F32 ? 512 : 1024) / TPR)) rmsnorm_grad_rows_kernel(const NormGradArgs a)
 {
     using T = Elem<TYPE>;
     using G = Elem<GTYPE>;
@@ -552,7 +555,7 @@ cudaError_t launch_rmsnorm(int64_t rows, int64_t cols, const esb_norm& n, cudaSt
     }
     const int threads = p.tpr < 128 ? 128 : p.tpr;
     int64_t blocks = (rows + threads / p.tpr - 1) / (threads / p.tpr);
-    const int64_t cap = sms * (threads >= 1024 ? 1 : 768 / threads);   // about what the SMs hold: each block keeps its weights
+    const int64_t cap = sms * (threads >= 1024 ? 1 : 512 / threads);   // what the SMs hold at once: each block keeps its weights
     if (blocks > cap) blocks = cap;
     return launch_pdl(p.kernel, dim3((unsigned)blocks), dim3((unsigned)threads), 0, st, a);
 }
