@@ -6,8 +6,9 @@
 // joined over the block, and over the blocks of a cluster where a few rows
 // would leave SMs idle.  With M, S and D those of the row,
 //   lse = M + log S,  entropy = log S - D / S.
-// HBM-bound: 2 or 4 bytes a logit; at the measured copy rate an SM gets about
-// 11 (bf16) issue slots a logit, and the pass takes about 9.
+// 2 or 4 bytes a logit from HBM; at the measured copy rate a bf16 logit has
+// about 11 issue slots.  Differences, products and sums go in pairs (two fp32
+// numbers an instruction), the largest of 16 logits in pairs of 16 bits.
 //
 // The alternatives come out of the same pass.  A key orders logits by value,
 // then by place.  After a row's first block of logits the best keys of the 32
@@ -204,6 +205,31 @@ struct RowParts {
     }
 };
 
+// Larger and smaller halves of two pairs of 16-bit numbers (the number of a
+// number and NaN).
+template <class T> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b);
+template <class T> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max2<__nv_bfloat16>(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <> __device__ __forceinline__ uint32_t min2<__nv_bfloat16>(uint32_t a, uint32_t b)
+{
+    const __nv_bfloat162 r = __hmin2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <> __device__ __forceinline__ uint32_t max2<__half>(uint32_t a, uint32_t b)
+{
+    const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_t b)
+{
+    const __half2 r = __hmin2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 template <int TYPE, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const LpArgs a)
 {
@@ -230,14 +256,18 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
         float m = lowest;
         Pair s2 = pair_of(0.0f, 0.0f), d2 = s2;
         const Pair log2e = pair_of(1.44269504f, 1.44269504f);
-        auto add = [&](float x0, float x1, const Pair& minus_m) {
-            const Pair d = add2(pair_of(x0, x1), minus_m);
-            float y0, y1, e0, e1;
+        auto add = [&](float x0, float x1, const Pair& minus_m, bool clamp) {
+            Pair d = add2(pair_of(x0, x1), minus_m);
+            float y0, y1;
             split(mul2(d, log2e), y0, y1);
-            split(d, e0, e1);
             const Pair p = pair_of(ex2_of(y0), ex2_of(y1));
             s2 = add2(s2, p);
-            d2 = fma2(p, pair_of(fmaxf(e0, -200.0f), fmaxf(e1, -200.0f)), d2);   // p is 0 there
+            if (clamp) {
+                // x - m = -inf as a number; p is 0 there
+                split(d, y0, y1);
+                d = pair_of(fmaxf(y0, -200.0f), fmaxf(y1, -200.0f));
+            }
+            d2 = fma2(p, d, d2);
         };
         auto raise = [&](float to) {
             if (to > m) {
@@ -258,16 +288,23 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
             else sh.overflow = 1;
             full |= i >= kLpList / 2;
         };
-        const int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
+        constexpr int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
         bool first = true;
         int blocks = 0;
         uint4 next[U];
         auto load = [&](int64_t v0) {
+            const uint4* from = reinterpret_cast<const uint4*>(xv) + v0 + threadIdx.x;
+            if (v0 + step <= rp.vecs) {
 #pragma unroll
-            for (int u = 0; u < U; u++) {
-                const int64_t i = v0 + u * kLpThreads + threadIdx.x;
-                next[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (i < rp.vecs) next[u] = __ldg(reinterpret_cast<const uint4*>(xv) + i);
+                for (int u = 0; u < U; u++) next[u] = __ldg(from + u * kLpThreads);
+            } else {
+                // -inf past the row
+                constexpr uint32_t F = TYPE == ESB_F32 ? 0xff800000u : (TYPE == ESB_F16 ? 0xfc00fc00u : 0xff80ff80u);
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    next[u] = make_uint4(F, F, F, F);
+                    if (v0 + u * kLpThreads + threadIdx.x < rp.vecs) next[u] = __ldg(from + u * kLpThreads);
+                }
             }
         };
         load(rank * step);
@@ -286,9 +323,9 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
             }
             float v[U][V];
             float big = fmaxf(lowest, edge);                // the thread's largest
+            bool masked = true;                             // whether one may be -inf
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const int64_t i = v0 + u * kLpThreads + threadIdx.x;
                 if constexpr (V == 8) {
                     unpack2<T>(raw[u].x, v[u][0], v[u][1]);
                     unpack2<T>(raw[u].y, v[u][2], v[u][3]);
@@ -298,20 +335,44 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
                     v[u][0] = __uint_as_float(raw[u].x); v[u][1] = __uint_as_float(raw[u].y);
                     v[u][2] = __uint_as_float(raw[u].z); v[u][3] = __uint_as_float(raw[u].w);
                 }
-                if (i >= rp.vecs) {
+            }
+            if constexpr (V == 8) {
+                // in pairs of 16 bits: the largest, and whether any is -inf
+                uint32_t hi = raw[0].x, lo = raw[0].x;
 #pragma unroll
-                    for (int j = 0; j < V; j++) v[u][j] = ninf;
+                for (int u = 0; u < U; u++) {
+                    const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+#pragma unroll
+                    for (int j = u ? 0 : 1; j < 4; j++) {
+                        hi = max2<T>(hi, w[j]);
+                        lo = min2<T>(lo, w[j]);
+                    }
                 }
+                float a0, a1;
+                unpack2<T>(hi, a0, a1);
+                big = fmaxf(big, fmaxf(a0, a1));
+                unpack2<T>(lo, a0, a1);
+                masked = fminf(a0, a1) == ninf;
+            } else {
 #pragma unroll
-                for (int j = 0; j < V; j++) big = fmaxf(big, v[u][j]);
+                for (int u = 0; u < U; u++)
+#pragma unroll
+                    for (int j = 0; j < V; j++) big = fmaxf(big, v[u][j]);
             }
             raise(big);
             const Pair minus_m = pair_of(-m, -m);
-            if (edge != ninf) add(edge, ninf, minus_m);
+            if (edge != ninf) add(edge, ninf, minus_m, true);
+            if (V == 8 && !masked) {
 #pragma unroll
-            for (int u = 0; u < U; u++)
+                for (int u = 0; u < U; u++)
 #pragma unroll
-                for (int j = 0; j < V; j += 2) add(v[u][j], v[u][j + 1], minus_m);
+                    for (int j = 0; j < V; j += 2) add(v[u][j], v[u][j + 1], minus_m, false);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; u++)
+#pragma unroll
+                    for (int j = 0; j < V; j += 2) add(v[u][j], v[u][j + 1], minus_m, true);
+            }
             if (a.top) {
                 auto at_of = [&](int u, int j) { return (uint32_t)(rp.head + (v0 + u * kLpThreads + threadIdx.x) * V + j); };
                 if (bound == 0ull) {                    // the same for every thread
