@@ -29,7 +29,7 @@ namespace esb {
 namespace {
 
 constexpr int kLpMaxWarps = 16;
-constexpr int kLpValues = 16;           // logits of a thread in a block of them
+constexpr int kLpValues = 16;           // logits of a thread in a block of them; half a warp takes them one each
 constexpr int kLpList = 2048;
 constexpr int kLpMaxCluster = 8;
 
@@ -231,7 +231,7 @@ template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_
 }
 
 template <int TYPE, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const LpArgs a)
+__global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 : 32 / WARPS) logprobs_kernel(const LpArgs a)
 {
     constexpr int kLpThreads = WARPS * 32, kLpWarps = WARPS;
     using T = Elem<TYPE>;
@@ -374,18 +374,18 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
                     for (int j = 0; j < V; j += 2) add(v[u][j], v[u][j + 1], minus_m, true);
             }
             if (a.top) {
-                auto at_of = [&](int u, int j) { return (uint32_t)(rp.head + (v0 + u * kLpThreads + threadIdx.x) * V + j); };
+                // of value n of the thread t
+                auto place = [&](int t, int n) { return (uint32_t)(rp.head + (v0 + n / V * kLpThreads + t) * V + n % V); };
                 if (bound == 0ull) {                    // the same for every thread
                     // the best key of every lane over the warps
                     Key k = top_key(edge, edge_at);
+                    int n = -1;                         // the thread's largest is met first at its lowest place
 #pragma unroll
-                    for (int u = 0; u < U; u++)
-#pragma unroll
-                        for (int j = 0; j < V; j++)
-                            if (v[u][j] == big) {       // the block's largest is met first at its lowest place
-                                const Key c = top_key(v[u][j], at_of(u, j));
-                                k = c > k ? c : k;
-                            }
+                    for (int i = kLpValues - 1; i >= 0; i--) n = v[i / V][i % V] == big ? i : n;
+                    if (n >= 0) {
+                        const Key c = top_key(big, place(threadIdx.x, n));
+                        k = c > k ? c : k;
+                    }
                     sh.lanes[warp][lane] = k;
                     __syncthreads();
                     if (warp == 0) {
@@ -398,14 +398,22 @@ __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) logprobs_kernel(const 
                     bound = sh.bound;
                 }
                 if (edge > ninf) offer(edge, edge_at);
-                // most threads have nothing at or above the bound
+                // Most threads have nothing at or above the bound.  The warp
+                // takes those that do two at a time, 16 lanes for the values
+                // of each, read again: few instructions, and in one place.
                 const float least = bound ? key_value(bound) : lowest;
-                if (big >= least) {
-#pragma unroll
-                    for (int u = 0; u < U; u++)
-#pragma unroll
-                        for (int j = 0; j < V; j++)
-                            if (v[u][j] >= least) offer(v[u][j], at_of(u, j));
+                for (unsigned hits = __ballot_sync(0xffffffffu, big >= least); hits; hits &= hits - 1) {
+                    const unsigned more = hits & (hits - 1);
+                    const unsigned mine = lane < kLpValues ? hits : more;
+                    if (mine) {
+                        const int t = warp * 32 + __ffs(mine) - 1, n = lane % kLpValues;
+                        if (v0 + n / V * kLpThreads + t < rp.vecs) {
+                            const uint32_t at = place(t, n);
+                            const float w = to_f32(x[at]);
+                            if (w >= least) offer(w, at);
+                        }
+                    }
+                    if (more) hits = more;
                 }
                 // every fourth block of logits (the list holds far more than four
                 // usually add): is the list half full?
