@@ -14,10 +14,9 @@
 // then by place.  After a row's first block of logits the best keys of the 32
 // lanes, each over all warps, are 32 logits of the row, so the top-th best of
 // them is a bound that no alternative lies below; from then on a thread puts
-// logits at or above the bound into a list, which one warp sorts and cuts to
-// the best 32 when it fills up, raising the bound.  A block of logits that
-// would overflow the list (rows that ascend) takes the row again, once for
-// each alternative.
+// logits at or above the bound into a list, which is sorted and cut to the best
+// 32 now and then, raising the bound.  Where it overflows all the same (rows
+// that ascend), the row is taken again in steps that it holds.
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -31,6 +30,7 @@ namespace {
 constexpr int kLpMaxWarps = 16;
 constexpr int kLpValues = 16;           // logits of a thread in a block of them; half a warp takes them one each
 constexpr int kLpList = 2048;
+constexpr int kLpFull = 128;            // keys in the list that are worth a cut
 constexpr int kLpMaxCluster = 8;
 
 using Key = unsigned long long;
@@ -147,7 +147,7 @@ __device__ __forceinline__ Key merge32(Key best, Key more, int lane)
 }
 
 struct LpShared {
-    LpSums sums[kLpMaxWarps];
+    LpSums sums[kLpMaxWarps], total;
     Key lanes[kLpMaxWarps][32];
     Key best[32];                       // the best keys so far, descending
     Key bound;                          // no alternative is below it
@@ -157,18 +157,29 @@ struct LpShared {
     Key list[kLpList];
 };
 
-// Warp 0: the list's keys into the best 32; the bound is the top-th of them.
-__device__ __forceinline__ void cut_list(LpShared& sh, int top, int lane)
+// The list's keys into the best 32, by the whole block (the list is complete,
+// and a barrier follows): every warp sorts its part, warp 0 takes them
+// together.  The bound is the top-th of them.
+template <int WARPS>
+__device__ __forceinline__ void cut_list(LpShared& sh, int top, int warp, int lane)
 {
     const int n = min(sh.count, kLpList);
-    Key best = sh.best[lane];
-    for (int i = 0; i < n; i += 32) best = merge32(best, sort32(i + lane < n ? sh.list[i + lane] : 0ull, lane), lane);
-    sh.best[lane] = best;
-    const Key b = ((Key)__shfl_sync(0xffffffffu, (uint32_t)(best >> 32), top - 1) << 32) | __shfl_sync(0xffffffffu, (uint32_t)best, top - 1);
-    __syncwarp();
-    if (lane == 0) {
-        if (b > sh.bound) sh.bound = b;
-        sh.count = 0;
+    Key mine = 0ull;
+    for (int i = warp * 32; i < n; i += WARPS * 32) {
+        const Key k = sort32(i + lane < n ? sh.list[i + lane] : 0ull, lane);
+        mine = i < WARPS * 32 ? k : merge32(mine, k, lane);
+    }
+    if (warp * 32 < n) sh.lanes[warp][lane] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        Key best = sh.best[lane];
+        for (int w = 0; w < WARPS && w * 32 < n; w++) best = merge32(best, sh.lanes[w][lane], lane);
+        sh.best[lane] = best;
+        const Key b = ((Key)__shfl_sync(0xffffffffu, (uint32_t)(best >> 32), top - 1) << 32) | __shfl_sync(0xffffffffu, (uint32_t)best, top - 1);
+        if (lane == 0) {
+            if (b > sh.bound) sh.bound = b;
+            sh.count = 0;
+        }
     }
 }
 
@@ -279,14 +290,14 @@ __global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 
             }
         };
         Key bound = 0ull;
-        bool full = false;              // this thread has met a list that is half full
+        bool full = false;              // this thread has met a list that is worth a cut
         auto offer = [&](float v, uint32_t at) {
             const Key k = top_key(v, at);
             if (k < bound || !k) return;
             const int i = atomicAdd(&sh.count, 1);
             if (i < kLpList) sh.list[i] = k;
             else sh.overflow = 1;
-            full |= i >= kLpList / 2;
+            full |= i >= kLpFull;
         };
         constexpr int64_t step = (int64_t)kLpThreads * U;   // vectors of a block of logits
         bool first = true;
@@ -415,10 +426,11 @@ __global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 
                     }
                     if (more) hits = more;
                 }
-                // every fourth block of logits (the list holds far more than four
-                // usually add): is the list half full?
-                if ((++blocks & 3) == 0 && __syncthreads_or(full)) {
-                    if (warp == 0) cut_list(sh, a.top, lane);
+                // Every fourth block of logits, and for many alternatives the
+                // first, whose bound is far below them: a cut?  The list holds
+                // more than four blocks usually add.
+                if (((++blocks & 3) == 0 || (blocks == 1 && a.top > 12)) && __syncthreads_or(full)) {
+                    cut_list<WARPS>(sh, a.top, warp, lane);
                     __syncthreads();
                     bound = sh.bound;
                     full = false;
@@ -438,7 +450,7 @@ __global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 
         }
         if (lane == 0) sh.sums[warp] = t;
         __syncthreads();
-        if (warp == 0) {
+        if (warp == (a.top ? kLpWarps - 1 : 0)) {       // while warp 0 sorts
             if (lane < kLpWarps) t = sh.sums[lane];
             else t = {lowest, 0.0f, 0.0f};
 #pragma unroll
@@ -446,35 +458,34 @@ __global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 
                 const LpSums b = {__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.s, o), __shfl_xor_sync(0xffffffffu, t.d, o)};
                 t = join(t, b);
             }
-            if (a.top) cut_list(sh, a.top, lane);
+            if (lane == 0) sh.total = t;
         }
-        if (a.top && sh.overflow) {
-            // uniform after the barrier above; rare: this block's part of the
-            // row again, for each alternative the best key below the last one
-            Key last = ~0ull;
-            for (int j = 0; j < a.top; j++) {
-                Key k = 0ull;
-                for (int64_t e = threadIdx.x; e < a.cols; e += kLpThreads) {
-                    const bool in = e < rp.head || e >= rp.tail_at ? rank == 0 : ((e - rp.head) / V / step) % a.split == rank;
-                    const Key c = in ? top_key(to_f32(x[e]), (uint32_t)e) : 0ull;
-                    if (c < last && c > k) k = c;
-                }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    const Key b = shfl_key(k, o);
-                    k = b > k ? b : k;
-                }
+        if (a.top) {
+            if (sh.overflow) {
+                // uniform after the barrier above; rare: this block's part of
+                // the row again, a value a thread between barriers
+                if (threadIdx.x < 32) sh.best[threadIdx.x] = 0ull;
+                if (threadIdx.x == 0) sh.count = 0;
+                bound = sh.bound;
+                full = false;
                 __syncthreads();
-                if (lane == 0) sh.lanes[0][warp] = k;
-                __syncthreads();
-                k = sh.lanes[0][0];
-#pragma unroll
-                for (int w = 1; w < kLpWarps; w++) k = sh.lanes[0][w] > k ? sh.lanes[0][w] : k;
-                last = k;
-                if (threadIdx.x == 0) sh.best[j] = k;
+                for (int64_t e0 = 0; e0 < a.cols; e0 += kLpThreads) {
+                    const int64_t e = e0 + threadIdx.x;
+                    if (e < a.cols) {
+                        const uint32_t block = (uint32_t)((uint64_t)(e - rp.head) / (uint64_t)(V * step));
+                        const bool in = e < rp.head || e >= rp.tail_at ? rank == 0 : (int)(block % (uint32_t)a.split) == rank;
+                        if (in) offer(to_f32(x[e]), (uint32_t)e);
+                    }
+                    if (__syncthreads_or(full)) {
+                        cut_list<WARPS>(sh, a.top, warp, lane);
+                        __syncthreads();
+                        bound = sh.bound;
+                        full = false;
+                    }
+                }
             }
-            if (threadIdx.x >= a.top && threadIdx.x < 32) sh.best[threadIdx.x] = 0ull;
-            __syncthreads();
+            cut_list<WARPS>(sh, a.top, warp, lane);
+            t = sh.total;
         }
         // the cluster's sums and keys, in block 0
         Key best = 0ull;

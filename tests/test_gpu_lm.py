@@ -572,6 +572,18 @@ def test_logprobs_ties_and_few_values(dtype, cols):
     close(out.entropy, ent, LSE_ERR * (2 + ent.abs()) * 2, torch.float32)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 150001), (2, 60000), (700, 20000)])
+@pytest.mark.parametrize("top", [1, 13, 32])
+def test_logprobs_alternatives_of_ascending_rows(rows, cols, top):
+    # every logit is an alternative when it is met: more candidates than a list of them holds
+    x = (torch.arange(cols, device="cuda") * 2.0 ** -16).repeat(rows, 1)
+    x[:, cols // 3: cols // 3 + 50] = float("nan") if rows == 2 else -float("inf")
+    x[rows // 2, 5] = 7.0
+    out = esb.esb_logprobs(x, None, top=top)
+    v = torch.where(torch.isnan(x), torch.full_like(x, -float("inf")), x)
+    assert torch.equal(out.top_ids, torch.sort(v, dim=1, descending=True, stable=True).indices[:, :top])
+
+
 @pytest.mark.parametrize("cols", [3, 700, 70000])
 def test_logprobs_empty_and_special_rows(cols):
     x = rand((6, cols), 1)
