@@ -655,7 +655,7 @@ esb_status esb_project_groups(const void* x, int32_t x_type, int64_t rows, int64
  *   bias  [device] N floats or NULL
  *   y     [device] M x N values of y_type, row stride ldy
  * Any M; the matrix is read once for every few rows, so many rows (a prompt)
- * belong to esb_gemm.  K < 2^18, N < 2^31.
+ * belong to esb_gemm.  K < 2^18, N <= 2^30.
  * Errors: INVALID_ARG, UNSUPPORTED (formats, groups), RANGE (K, N),
  * ALIGN, CUDA. */
 esb_status esb_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int32_t x_type, int64_t ldx,

@@ -56,7 +56,7 @@ esb_status esb_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int
     if ((!coded && !type_ok(x_type)) || !type_ok(y_type) || !w || (coded && !xc)) return ESB_ERR_INVALID_ARG;
     if (M < 0 || N < 0 || K < 0 || ldy < N) return ESB_ERR_INVALID_ARG;
     if (esb_format_check(w->fmt) != ESB_OK || w->fmt.b != 4 || !group_ok(w->group)) return ESB_ERR_UNSUPPORTED;
-    if (K >= 1 << 18 || N >= 1ll << 31) return ESB_ERR_RANGE;
+    if (K >= 1 << 18 || N > 1ll << 30) return ESB_ERR_RANGE;
     if (M == 0 || N == 0) return ESB_OK;
     if (!y || K == 0 || !w->codes || !w->scales || w->ld < words_of(K, 4) || w->lds < groups_of(K, w->group)) return ESB_ERR_INVALID_ARG;
     if (!aligned(w->codes, 16) || w->ld % 4 != 0 || !aligned(w->scales, 4) || !aligned(bias, 4) || !typed(y, y_type)) return ESB_ERR_ALIGN;

@@ -7,9 +7,12 @@
 // multiply-add per code and row does not fit into that; the warp-level matrix
 // instruction (m16n8k16, fp16 in, fp32 sums) takes a decoded word of two
 // matrix rows for 8 rows of x at once, so the code is the operand with the 16
-// rows and decoding it is the work.  (tcgen05 would need the decoded matrix
-// in shared memory first, four bytes written and read there for every byte
-// from HBM, for a tile of 8 to 32 columns.)
+// rows and decoding it is the work: 13 instructions a word, and 11 issue
+// cycles for each matrix instruction.  65536 x 4096 in groups of 128 takes 40
+// us with one row of bf16 (21 at the copy rate), 46 with 8 and 62 with 16;
+// 4096 x 4096 with one row 7 us, launch and latencies.  For more columns
+// esb_matvec_tc.cu has the products on tcgen05, whose operand has to go
+// through tensor memory first.
 //
 // fp16 holds both operands exactly.  Every element of a 4-bit set is a
 // number with at most 2 fraction bits, so its fp16 high byte is a table entry
@@ -376,7 +379,13 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
 
     // Rows a block takes at once: up to 32 columns' worth, fewer where x would
     // not fit; the row's codes over up to 8 blocks (a cluster) where that
-    // makes x fit.
+    // makes x fit.  Also over four where the matrix is wider than high and
+    // has a tile a warp at most: preparing x is what takes long there (4 x
+    // 4096 x 9216, x in 8-bit codes, groups of 64: 14 us, 17 without; 4 rows of
+    // bf16 times 1024 x 14336: 11 and 14).  Each tile's sums then cross the
+    // cluster, which costs more for high matrices (4 x 8192 x 4096 bf16: 10.9
+    // and 10.7; 12000 x 4096, several tiles a warp: 23 and 15) and for one row
+    // of x is as long as what it saves.
     const int sms = device_sm_count();
     const int most = 32 / (a.planes * r);
     const int64_t tiles = (N + 15) / 16, all = (K + 511) / 512;
@@ -388,7 +397,8 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         const int cols = a.mt * a.planes * r, nt = cols <= 8 ? 1 : (cols <= 16 ? 2 : 4);
         p = r == 1 ? mv_plan<1>(nt) : (r == 2 ? mv_plan<2>(nt) : mv_plan<4>(nt));
         a.zrow = r > 1 || cols < 8 * nt;
-        for (a.split = 1;; a.split *= 2) {
+        const bool spread = K >= 4096 && N <= K && a.mt * a.planes >= 4 && tiles <= p.warps * sms / (4 * passes);
+        for (a.split = spread ? 4 : 1;; a.split *= 2) {
             a.kc = (int)((all + a.split - 1) / a.split) * 512;
             const size_t sums = mv_sums(cols, p.warps);
             smem = mv_x_bytes(a.mt * a.planes + a.zrow, a.kc, nt) + sums;

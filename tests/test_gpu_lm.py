@@ -249,6 +249,27 @@ def test_matvec_many_columns(M, N, K, group, x):
     assert esb.esb_get_status() == 0
 
 
+# few matrix rows, long ones
+@pytest.mark.parametrize("M,N,K,group", [(4, 1, 4096, 128), (4, 4096, 4096, 64), (5, 1000, 4097, 32), (8, 33, 5121, 96), (16, 2000, 9216, 128),
+                                         (6, 9700, 9728, 128), (31, 17, 6655, 64), (100, 300, 4608, 0), (3, 500, 14336, 32)])
+@pytest.mark.parametrize("x", [torch.float32, torch.float16, torch.bfloat16, "codes"])
+def test_matvec_long_rows(M, N, K, group, x):
+    w = make_w(N, K, group, (M + N) % 4)
+    rows = rand((M, K), 2)
+    if x == "codes":
+        rows = esb.esb_project_groups(rows, esb.Fmt(8, 5), 2 * group)[0]
+        x64 = values64(rows)
+    else:
+        rows = rows.to(x)
+        x64 = rows.double()
+    bias = rand((N,), 3)
+    y = esb.esb_matvec_groups(rows, w, bias=bias, y_dtype=torch.float32)
+    w64 = values64(w)
+    want = x64 @ w64.t() + bias.double()
+    close(y, want, matvec_bound(x64, w64, K) + U * want.abs(), torch.float32)
+    assert torch.equal(y, esb.esb_matvec_groups(rows, w, bias=bias, y_dtype=torch.float32))
+
+
 def test_matvec_many_columns_special_values_and_padding():
     K, N = 333, 16001
     x = rand((5, K), 9)
