@@ -878,17 +878,17 @@ def esb_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, top: 
     if not 0 <= top <= ESB_MAX_TOP:
         raise ValueError(f"top must be 0..{ESB_MAX_TOP}")
     dev = logits.device
-    st = torch.empty((3, rows), dtype=torch.float32, device=dev)     # one allocation for the rows' numbers
-    p = st.data_ptr()
-    tl = ti = None
+    lp = None if ip is None else torch.empty(rows, dtype=torch.float32, device=dev)
+    ent = torch.empty(rows, dtype=torch.float32, device=dev)
+    lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    tl = ti = tlp = tip = None
     if top:
         tl = torch.empty((rows, top), dtype=torch.float32, device=dev)
         ti = torch.empty((rows, top), dtype=torch.int64, device=dev)
-    _check(lib().esb_logprobs(logits.data_ptr(), ty, rows, cols, ldx, ip, top, p if ip else None, p + 4 * rows,
-                              p + 8 * rows, tl.data_ptr() if top else None, ti.data_ptr() if top else None,
-                              _stream(stream)), "esb_logprobs")
-    logp, ent, lse = st.unbind(0)
-    return LogProbs(logp if ip else None, ent, lse, tl, ti)
+        tlp, tip = tl.data_ptr(), ti.data_ptr()
+    _check(lib().esb_logprobs(logits.data_ptr(), ty, rows, cols, ldx, ip, top, None if lp is None else lp.data_ptr(),
+                              ent.data_ptr(), lse.data_ptr(), tlp, tip, _stream(stream)), "esb_logprobs")
+    return LogProbs(lp, ent, lse, tl, ti)
 
 
 def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse: torch.Tensor,
