@@ -9,6 +9,9 @@
 // 2 or 4 bytes a logit from HBM; at the measured copy rate a bf16 logit has
 // about 11 issue slots.  Differences, products and sums go in pairs (two fp32
 // numbers an instruction), the largest of 16 logits in pairs of 16 bits.
+// 4096 x 49999 bf16: 92 us without alternatives (60 at the copy rate), bound by
+// instructions; 159 with 8 and 238 with 32 of them, which add barriers and
+// sorts.  A row of 131072 with 8: 8.5 us, all latency.
 //
 // The alternatives come out of the same pass.  A key orders logits by value,
 // then by place.  After a row's first block of logits the best keys of the 32
@@ -241,6 +244,9 @@ template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
+// Registers: 64 a thread; for fp32 in blocks of 8 warps more, with three of them
+// on an SM (2048 x 65536: 89 us, 99 with four blocks, whose loads run less far
+// ahead; 16 warps are slower that way, 28 us for 256 x 65537 and not 24).
 template <int TYPE, int WARPS>
 __global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 : 32 / WARPS) logprobs_kernel(const LpArgs a)
 {
@@ -628,7 +634,8 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     const int64_t sms = device_sm_count();
     // Warps of a row: 4 for a short one; 16 where there are few rows (256 x
     // 65537 fp32, 5 alternatives: 24 us, 31 with 8), 8 where many rows' barriers
-    // and joins should overlap (4096 x 49999 bf16: 99 us, 122 with 16).
+    // and joins should overlap (4096 x 49999 bf16: 99 us, 122 with 16; with 8
+    // alternatives 163, 185 with 4).
     const int size = cols <= 4 * 32 * kLpValues * 2 ? 2 : (rows >= 4 * sms ? 1 : 0);
     const int threads = 512 >> size;
     while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * threads * kLpValues) a.split *= 2;
