@@ -35,7 +35,7 @@ __device__ __forceinline__ void project8(const GroupArgs& a, int64_t row, int64_
     uint32_t w[B / 4];
     float q[8];
     const int n = left_of(a.cols, vec * 8);
-    quantise8<B>(v, s, a.f, w, q);
+    quantise8<B, true>(v, s, a.f, w, q);
     if (n < 8) zero_past<B>(w, n, a.f);
     uint32_t* p = a.codes + row * a.ldc + vec * (B / 4);
     if (B == 8 && a.cvec && vec * 2 + 1 < a.ldc) {
@@ -111,12 +111,13 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
 // Groups of 32, 64, 128 or 256 values: 16 a lane, LANES lanes to a group, the
 // values in registers from the scale to the codes.  Rows are padded to whole
 // groups (`chunks` sixteens); a thread goes on by dr rows and dc sixteens.
-// Instructions bound it: a value may cost 24 at the copy rate, and the
-// quotient, its rounding and sign, the element's value and a sixteenth of the
-// group's scale take about as many.  16384 x 4096 bf16 to (4,2) with values
-// (302 MB of reads and writes, 45 us at the copy rate): 72 us with 16 values a
-// thread and four blocks on an SM, 78 to 91 with 32 in flight.
-constexpr int kChunks = 1;
+// Instructions and HBM bound it alike: a value may cost 24 at the copy rate, and
+// the quotient, its rounding and sign, the element's value and a sixteenth of
+// the group's scale take about as many.  16384 x 4096 bf16 to (4,2) with values
+// (304 MB of reads and writes, 45 us at the copy rate): 62 us with the next
+// sixteen loaded ahead, one eight after the other from there to its stores, and
+// four blocks on an SM; 73 without the load ahead, 66 with three blocks and 73
+// with five, whose registers spill; 72 with blocks of a single sixteen a thread.
 template <int TYPE, int B, int LANES>
 __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(const GroupArgs a, int chunks, int dr, int dc)
 {
@@ -131,100 +132,98 @@ __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(
         for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     };
+    Raw8<T> next[2];
+    auto load = [&]() {
+        const int64_t e = (int64_t)chunk * 16;
+        const int n = row < rows ? left_of(a.cols, e) : 0;
+        const T* x = static_cast<const T*>(a.x) + row * a.ldx + e;
+        next[0].load(x, n, a.xvec);
+        next[1].load(x + 8, n - 8, a.xvec);
+    };
+    load();
     while (__any_sync(0xffffffffu, row < rows)) {
-        Raw8<T> raw[kChunks][2];
-        int in_row[kChunks], in_chunk[kChunks];
-#pragma unroll
-        for (int u = 0; u < kChunks; u++) {
-            in_row[u] = row;
-            in_chunk[u] = chunk;
-            const int64_t e = (int64_t)chunk * 16;
-            const int n = row < rows ? left_of(a.cols, e) : 0;
-            const T* x = static_cast<const T*>(a.x) + row * a.ldx + e;
-            raw[u][0].load(x, n, a.xvec);
-            raw[u][1].load(x + 8, n - 8, a.xvec);
-            row += dr;
-            chunk += dc;
-            if (chunk >= chunks) { chunk -= chunks; row++; }
-        }
-#pragma unroll
-        for (int u = 0; u < kChunks; u++) {
-            const int64_t e = (int64_t)in_chunk[u] * 16;
-            float v[2][8];
-            raw[u][0].values(v[0]);
-            raw[u][1].values(v[1]);
-            float alpha;
-            if (a.rule == ESB_SCALE_ABSMAX) {
-                uint32_t mx = 0u;
-                if (TYPE != ESB_F32 && a.f.is_signed) {
-                    // magnitudes in pairs of 16 bits, which order as the numbers do
-#pragma unroll
-                    for (int h = 0; h < 2; h++)
-#pragma unroll
-                        for (int i = 0; i < 4; i++) mx = __vmaxu2(mx, raw[u][h].w[i] & 0x7fff7fffu);
-                    mx = max(mx & 0xffffu, mx >> 16);
-                    const uint16_t m16 = (uint16_t)mx;
-                    mx = __float_as_uint(to_f32(*reinterpret_cast<const T*>(&m16)));
-                } else {
-#pragma unroll
-                    for (int h = 0; h < 2; h++)
-#pragma unroll
-                        for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(v[h][i], a.f.is_signed));
-                }
-#pragma unroll
-                for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                alpha = absmax_scale(mx, a.f);
-            } else {
-                const int64_t left = a.cols - (e - part * 16);
-                const float n = (float)(left < 16 * LANES ? left : 16 * LANES);
-                float mean = 0.0f, s2 = 0.0f;
-                if (a.f.is_signed) {
-#pragma unroll
-                    for (int h = 0; h < 2; h++)
-#pragma unroll
-                        for (int i = 0; i < 8; i++) mean += v[h][i];
-                    mean = total(mean) / n;
-                }
+        const Raw8<T> raw[2] = {next[0], next[1]};
+        const int in_row = row, in_chunk = chunk;
+        row += dr;
+        chunk += dc;
+        if (chunk >= chunks) { chunk -= chunks; row++; }
+        load();
+        const int64_t e = (int64_t)in_chunk * 16;
+        float v[8];
+        float alpha;
+        if (a.rule == ESB_SCALE_ABSMAX) {
+            uint32_t mx = 0u;
+            if (TYPE != ESB_F32 && a.f.is_signed) {
+                // magnitudes in pairs of 16 bits, which order as the numbers do
 #pragma unroll
                 for (int h = 0; h < 2; h++)
 #pragma unroll
-                    for (int i = 0; i < 8; i++) {
-                        const float d = e + 8 * h + i < a.cols ? v[h][i] - mean : 0.0f;
-                        s2 = fmaf(d, d, s2);
-                    }
-                alpha = __fmul_rn(a.astar, __fadd_rn(__fsqrt_rn(total(s2) / n), 1e-7f));
-            }
-            if (in_row[u] >= rows) continue;
-            const int64_t gi = in_chunk[u] / LANES;
-            if (part == 0 && gi < a.ngroups) a.scales[in_row[u] * a.lds + gi] = alpha;
-            const GroupScale s = make_scale(alpha, a.f);
-            const int left = left_of(a.cols, e);
-            uint32_t w[2][B / 4];
-            float r[2][8];
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                quantise8<B>(v[h], s, a.f, w[h], r[h]);
-                const int n = left - 8 * h;
-                if (n < 8) zero_past<B>(w[h], n, a.f);
-            }
-            constexpr int WORDS = B / 2;                // of 16 codes
-            uint32_t* p = a.codes + in_row[u] * a.ldc + (int64_t)in_chunk[u] * WORDS;
-            if (a.cvec && (int64_t)(in_chunk[u] + 1) * WORDS <= a.ldc) {
-                if constexpr (B == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0][0], w[1][0]);
-                else *reinterpret_cast<uint4*>(p) = make_uint4(w[0][0], w[0][B / 4 - 1], w[1][0], w[1][B / 4 - 1]);
+                    for (int i = 0; i < 4; i++) mx = __vmaxu2(mx, raw[h].w[i] & 0x7fff7fffu);
+                mx = max(mx & 0xffffu, mx >> 16);
+                const uint16_t m16 = (uint16_t)mx;
+                mx = __float_as_uint(to_f32(*reinterpret_cast<const T*>(&m16)));
             } else {
 #pragma unroll
-                for (int i = 0; i < WORDS; i++)
-                    if ((int64_t)in_chunk[u] * WORDS + i < a.ldc) p[i] = w[i / (B / 4)][i % (B / 4)];
+                for (int h = 0; h < 2; h++) {
+                    raw[h].values(v);
+                    mx = max(mx, largest_of8(v, a.f.is_signed));
+                }
             }
-            if (!a.xq) continue;
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            alpha = absmax_scale(mx, a.f);
+        } else {
+            const int64_t left = a.cols - (e - part * 16);
+            const float n = (float)(left < 16 * LANES ? left : 16 * LANES);
+            float mean = 0.0f, s2 = 0.0f;
+            if (a.f.is_signed) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    raw[h].values(v);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) mean += v[i];
+                }
+                mean = total(mean) / n;
+            }
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const int n = left - 8 * h;
-                if (n <= 0) break;
-                element_values(v[h], s, a.f, r[h]);
-                store8_any(a.xq, a.xq_type, in_row[u] * a.ldq + e + 8 * h, n, a.qvec, r[h]);
+                raw[h].values(v);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float d = e + 8 * h + i < a.cols ? v[i] - mean : 0.0f;
+                    s2 = fmaf(d, d, s2);
+                }
             }
+            alpha = __fmul_rn(a.astar, __fadd_rn(__fsqrt_rn(total(s2) / n), 1e-7f));
+        }
+        if (in_row >= rows) continue;
+        const int64_t gi = in_chunk / LANES;
+        if (part == 0 && gi < a.ngroups) a.scales[in_row * a.lds + gi] = alpha;
+        const GroupScale s = make_scale(alpha, a.f);
+        const int left = left_of(a.cols, e);
+        uint32_t w[2][B / 4];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            float r[8];
+            const int n = left - 8 * h;
+            raw[h].values(v);
+            if (a.rule == ESB_SCALE_ABSMAX) quantise8<B, false>(v, s, a.f, w[h], r);
+            else quantise8<B, true>(v, s, a.f, w[h], r);
+            if (n < 8) zero_past<B>(w[h], n, a.f);
+            if (a.xq && n > 0) {
+                element_values(v, s, a.f, r);
+                store8_any(a.xq, a.xq_type, in_row * a.ldq + e + 8 * h, n, a.qvec, r);
+            }
+        }
+        constexpr int WORDS = B / 2;                    // of 16 codes
+        uint32_t* p = a.codes + in_row * a.ldc + (int64_t)in_chunk * WORDS;
+        if (a.cvec && (int64_t)(in_chunk + 1) * WORDS <= a.ldc) {
+            if constexpr (B == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0][0], w[1][0]);
+            else *reinterpret_cast<uint4*>(p) = make_uint4(w[0][0], w[0][B / 4 - 1], w[1][0], w[1][B / 4 - 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; i++)
+                if ((int64_t)in_chunk * WORDS + i < a.ldc) p[i] = w[i / (B / 4)][i % (B / 4)];
         }
     }
 }

@@ -69,35 +69,6 @@ __device__ __forceinline__ float exp_of(float x)
     return r;
 }
 
-// Two fp32 numbers in one instruction of the multiply-add pipe.
-struct Pair {
-    unsigned long long v;
-};
-__device__ __forceinline__ Pair pair_of(float a, float b)
-{
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
-    return p;
-}
-__device__ __forceinline__ void split(const Pair& p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
-__device__ __forceinline__ Pair add2(const Pair& a, const Pair& b)
-{
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair mul2(const Pair& a, const Pair& b)
-{
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair fma2(const Pair& a, const Pair& b, const Pair& c)
-{
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
 __device__ __forceinline__ float ex2_of(float y)
 {
     float r;

@@ -52,7 +52,7 @@ __device__ __forceinline__ void put_codes8(const NormArgs& a, int64_t row, int64
     uint32_t w[2];
     float q[8];
     const int n = left_of(a.cols, e);
-    quantise8<8>(y, s, a.f, w, q);
+    quantise8<8, false>(y, s, a.f, w, q);
     if (n < 8) zero_past<8>(w, n, a.f);
     uint32_t* p = a.n.codes + row * a.n.ldc + e / 4;
     if (a.cvec && e / 4 + 1 < a.n.ldc) {
@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
 // A group of codes is 2 to 16 lanes (32 to 256 values), or the row.  Many rows
 // are bound by instructions and HBM alike: 8192 x 4096 bf16 with residual,
 // codes and values (9 bytes for a value of x, 302 MB, 45 us at the copy rate)
-// 73 us with two blocks of 256 on an SM, 81 with three.  Few rows are bound by
-// latency: one row of 4096 takes 3.5 us.
+// 62 us with two blocks of 256 on an SM, 67 with three.  Few rows are bound by
+// latency: one row of 4096 takes 3.3 us.
 template <int TYPE, int TPR>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR < 256 ? 4 : 2)) rmsnorm_rows_kernel(const NormArgs a)
 {
@@ -211,16 +211,20 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
                 float u[8];
                 rr[v].values(u);
 #pragma unroll
-                for (int i = 0; i < 8; i++) z[v][i] = __fadd_rn(z[v][i], u[i]);
+                for (int i = 0; i < 8; i += 2) split(add2(pair_of(z[v][i], z[v][i + 1]), pair_of(u[i], u[i + 1])), z[v][i], z[v][i + 1]);
             }
         }
         if (AHEAD) load(row + step < a.rows);
-        float s0 = 0.0f, s1 = 0.0f;
+        Pair sq = pair_of(0.0f, 0.0f);
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            s0 = fmaf(z[0][i], z[0][i], s0);
-            s1 = fmaf(z[1][i], z[1][i], s1);
-        }
+        for (int v = 0; v < 2; v++)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const Pair p = pair_of(z[v][i], z[v][i + 1]);
+                sq = fma2(p, p, sq);
+            }
+        float s0, s1;
+        split(sq, s0, s1);
         float ss = warp_sum(s0 + s1);
         if constexpr (NW > 1) {
             if ((threadIdx.x & 31) == 0) shf[flip][threadIdx.x >> 5] = ss;
@@ -241,7 +245,8 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
 #pragma unroll
         for (int v = 0; v < 2; v++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) z[v][i] = __fmul_rn(__fmul_rn(z[v][i], rstd), w[v][i]);
+            for (int i = 0; i < 8; i += 2)
+                split(mul2(mul2(pair_of(z[v][i], z[v][i + 1]), pair_of(rstd, rstd)), pair_of(w[v][i], w[v][i + 1])), z[v][i], z[v][i + 1]);
         if (a.n.y) {
             store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e, n, a.yvec, z[0]);
             store8_any(a.n.y, a.n.y_type, row * a.n.ldy + e + 8, n - 8, a.yvec, z[1]);
@@ -250,9 +255,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
         // what lies past the row is 0 times rstd: 0, or NaN as the whole row
         uint32_t mx = 0u;
 #pragma unroll
-        for (int v = 0; v < 2; v++)
-#pragma unroll
-            for (int i = 0; i < 8; i++) mx = max(mx, magnitude_bits(z[v][i], a.f.is_signed));
+        for (int v = 0; v < 2; v++) mx = max(mx, largest_of8(z[v], a.f.is_signed));
         if (a.ngroups > 1) {
             for (int o = lanes / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         } else {
@@ -274,11 +277,15 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
             }
             const GroupScale s = make_scale(alpha, a.f);
             uint32_t c[2][2];
-            float q[2][8];
 #pragma unroll
             for (int v = 0; v < 2; v++) {
-                quantise8<8>(z[v], s, a.f, c[v], q[v]);
+                float q[8];
+                quantise8<8, false>(z[v], s, a.f, c[v], q);
                 if (n - 8 * v < 8) zero_past<8>(c[v], n - 8 * v, a.f);
+                if (a.n.yq) {
+                    element_values(z[v], s, a.f, q);
+                    store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e + 8 * v, n - 8 * v, a.qvec, q);
+                }
             }
             uint32_t* p = a.n.codes + row * a.n.ldc + t * 4;
             if (a.cvec && left >= 4) {
@@ -287,12 +294,6 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
 #pragma unroll
                 for (int i = 0; i < 4; i++)
                     if (i < left) p[i] = c[i / 2][i % 2];
-            }
-            if (a.n.yq) {
-                element_values(z[0], s, a.f, q[0]);
-                element_values(z[1], s, a.f, q[1]);
-                store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e, n, a.qvec, q[0]);
-                store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e + 8, n - 8, a.qvec, q[1]);
             }
         }
         // words past those that the threads' values reach (a long row stride)

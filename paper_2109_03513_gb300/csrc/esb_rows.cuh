@@ -172,6 +172,42 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// Two fp32 numbers in one instruction of the multiply-add pipe.
+struct Pair {
+    unsigned long long v;
+};
+__device__ __forceinline__ Pair pair_of(float a, float b)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void split(const Pair& p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v)); }
+__device__ __forceinline__ Pair add2(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(const Pair& a, const Pair& b, const Pair& c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Pair add2_rz(const Pair& a, const Pair& b)
+{
+    Pair r;
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+
 // ------------------------------------------------ projection, own scales
 
 // Projection constants of a format with b = 4 or 8.
@@ -216,7 +252,7 @@ __device__ __forceinline__ GroupScale make_scale(float alpha, const QuantFmt& f)
 }
 
 // The scale of a group with this largest magnitude: it over C, rounded to
-// nearest (in the middle of fp32's range as fast_quotient below).
+// nearest (in the middle of fp32's range as fast_quotients below).
 __device__ __forceinline__ float absmax_scale(uint32_t mx, const QuantFmt& f)
 {
     const float a = __uint_as_float(mx);
@@ -226,17 +262,17 @@ __device__ __forceinline__ float absmax_scale(uint32_t mx, const QuantFmt& f)
     return __fmaf_rn(__fmaf_rn(-q, f.C, a), f.rC, q);
 }
 
-// 2^k |x| / alpha, rounded to nearest as IEEE division of |x| by alpha (the
-// power of two is exact).  Many values share alpha, so the correctly rounded
-// reciprocal y of the step is found once; q = a y is then within two units of
-// the quotient, one step with the exact remainder makes it faithful, and by
-// Markstein's theorem (Computation of elementary functions on the IBM RISC
-// System/6000 processor, 1990) a second one rounds it correctly.
-__device__ __forceinline__ float fast_quotient(float a, const GroupScale& s)
+// 2^k |x| / alpha for two values, rounded to nearest as IEEE division of |x|
+// by alpha (the power of two is exact).  Many values share alpha, so the
+// correctly rounded reciprocal y of the step is found once; q = a y is then
+// within two units of the quotient, one step with the exact remainder makes it
+// faithful, and by Markstein's theorem (Computation of elementary functions on
+// the IBM RISC System/6000 processor, 1990) a second one rounds it correctly.
+__device__ __forceinline__ Pair fast_quotients(const Pair& a, const Pair& rcp, const Pair& minus_step)
 {
-    float q = __fmul_rn(a, s.rcp);
-    q = __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
-    return __fmaf_rn(__fmaf_rn(-q, s.step, a), s.rcp, q);
+    Pair q = mul2(a, rcp);
+    q = fma2(fma2(q, minus_step, a), rcp, q);
+    return fma2(fma2(q, minus_step, a), rcp, q);
 }
 
 // t = 2^k |x| / alpha on the set: r receives the element (times 2^k), the
@@ -288,24 +324,39 @@ static __device__ __noinline__ uint2 place_any(float x, float alpha, const Quant
 // one add and a mask; zero keeps sign 0.  r receives the elements' magnitudes
 // times 2^k (element_values turns them into numbers).  In a group with a
 // finite scale no value is NaN.
-template <int B, bool LINEAR>
+// CLAMP: quotients may be past the largest element.  (Under a group's own
+// absmax scale they pass it by a unit in the last place at most, which the
+// rounding to the set takes back.)
+template <int B, bool LINEAR, bool CLAMP>
 __device__ __forceinline__ void places8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
 {
     constexpr int PER = 32 / B;
     constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
+    const Pair rcp = pair_of(s.rcp, s.rcp), minus_step = pair_of(-s.step, -s.step);
+    const Pair half = pair_of(0.5f, 0.5f), whole = pair_of(8388608.0f, 8388608.0f), minus_whole = pair_of(-8388608.0f, -8388608.0f);
 #pragma unroll
     for (int i = 0; i < B / 4; i++) w[i] = LINEAR ? 0u - 0x4B000000u * ONES : 0u;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const float t = fminf(fast_quotient(fabsf(x[i]), s), f.Ck);
+    for (int i = 0; i < 8; i += 2) {
+        Pair t = fast_quotients(pair_of(fabsf(x[i]), fabsf(x[i + 1])), rcp, minus_step);
+        float t0, t1;
+        if constexpr (CLAMP || !LINEAR) split(t, t0, t1);
+        if constexpr (CLAMP) {
+            t0 = fminf(t0, f.Ck);
+            t1 = fminf(t1, f.Ck);
+            t = pair_of(t0, t1);
+        }
         if constexpr (LINEAR) {
             // the place is the low bits of the sum; what lies above them is
             // taken off the word at once
-            const float big = __fadd_rz(__fadd_rz(t, 0.5f), 8388608.0f);
-            r[i] = big - 8388608.0f;
-            w[i / PER] += __float_as_uint(big) * (1u << (B * (i % PER)));
+            const Pair big = add2_rz(add2_rz(t, half), whole);
+            split(big, t0, t1);
+            w[i / PER] += __float_as_uint(t0) * (1u << (B * (i % PER)));
+            w[i / PER] += __float_as_uint(t1) * (1u << (B * (i % PER + 1)));
+            split(add2(big, minus_whole), r[i], r[i + 1]);
         } else {
-            w[i / PER] += round_away(t, false, f.k, f.pk, r[i]) << (B * (i % PER));
+            w[i / PER] += round_away(t0, false, f.k, f.pk, r[i]) << (B * (i % PER));
+            w[i / PER] += round_away(t1, false, f.k, f.pk, r[i + 1]) << (B * (i % PER + 1));
         }
     }
 }
@@ -326,15 +377,15 @@ __device__ __forceinline__ void signs8(const float (&x)[8], uint32_t (&S)[B / 4]
         S[0] = tops(1, 3, 5, 7) | (tops(0, 2, 4, 6) >> 4);
     }
 }
-template <int B>
+template <int B, bool CLAMP>
 __device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
 {
     constexpr int PER = 32 / B;
     constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
     constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
     if (s.fast && f.plain) {
-        if (f.linear) places8<B, true>(x, s, f, w, r);
-        else places8<B, false>(x, s, f, w, r);
+        if (f.linear) places8<B, true, CLAMP>(x, s, f, w, r);
+        else places8<B, false, CLAMP>(x, s, f, w, r);
     } else {
 #pragma unroll
         for (int i = 0; i < B / 4; i++) w[i] = 0u;
@@ -363,7 +414,11 @@ __device__ __forceinline__ void element_values(const float (&x)[8], const GroupS
         for (int i = 0; i < 8; i++) r[i] *= f.ipk;
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++) r[i] = __uint_as_float(__float_as_uint(__fmul_rn(by, r[i])) ^ (__float_as_uint(x[i]) & 0x80000000u));
+    for (int i = 0; i < 8; i += 2) {
+        split(mul2(pair_of(by, by), pair_of(r[i], r[i + 1])), r[i], r[i + 1]);
+        r[i] = __uint_as_float(__float_as_uint(r[i]) ^ (__float_as_uint(x[i]) & 0x80000000u));
+        r[i + 1] = __uint_as_float(__float_as_uint(r[i + 1]) ^ (__float_as_uint(x[i + 1]) & 0x80000000u));
+    }
 }
 
 // The words of eight codes of which only the first n are a row's: the rest
@@ -389,6 +444,32 @@ __device__ __forceinline__ uint32_t magnitude_bits(float x, int is_signed)
 {
     const uint32_t u = __float_as_uint(x), a = u & 0x7fffffffu;
     return (is_signed || a > 0x7f800000u || !(u >> 31)) ? a : 0u;
+}
+// The largest magnitude_bits of eight values, up to NaN's bits: the maximum
+// of three numbers is one instruction, and NaN where one of them is.
+__device__ __forceinline__ float max_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_nan_abs(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t largest_of8(const float (&v)[8], int is_signed)
+{
+    float m = 0.0f;
+    if (is_signed) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) m = max_nan_abs(m, v[i], v[i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) m = max_nan(m, v[i], v[i + 1]);
+    }
+    return __float_as_uint(m) & 0x7fffffffu;
 }
 
 }  // namespace esb
