@@ -9,7 +9,7 @@
 // 2 or 4 bytes a logit from HBM; at the measured copy rate a bf16 logit has
 // about 11 issue slots.  Differences, products and sums go in pairs (two fp32
 // numbers an instruction), the largest of 16 logits in pairs of 16 bits.
-// 4096 x 49999 bf16: 92 us without alternatives (60 at the copy rate), bound by
+// 4096 x 49999 bf16: 87 us without alternatives (60 at the copy rate), bound by
 // instructions; 159 with 8 and 238 with 32 of them, which add barriers and
 // sorts.  A row of 131072 with 8: 8.5 us, all latency.
 //
@@ -215,11 +215,11 @@ template <> __device__ __forceinline__ uint32_t min2<__half>(uint32_t a, uint32_
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// Registers: 64 a thread; for fp32 in blocks of 8 warps more, with three of them
-// on an SM (2048 x 65536: 89 us, 99 with four blocks, whose loads run less far
-// ahead; 16 warps are slower that way, 28 us for 256 x 65537 and not 24).
+// Registers: 64 a thread; for fp32 and up to 8 warps a block more, with 24 warps
+// on an SM (2048 x 65536: 89 us, 99 with 32, whose loads run less far ahead;
+// blocks of 16 are slower that way, 28 us for 256 x 65537 and not 24).
 template <int TYPE, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, TYPE == ESB_F32 && WARPS == 8 ? 3 : 32 / WARPS) logprobs_kernel(const LpArgs a)
+__global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 24 : 32) / WARPS) logprobs_kernel(const LpArgs a)
 {
     constexpr int kLpThreads = WARPS * 32, kLpWarps = WARPS;
     using T = Elem<TYPE>;
@@ -603,11 +603,13 @@ cudaError_t launch_logprobs(const void* x, int type, int64_t rows, int64_t cols,
     // Rows that do not fill the SMs are split over clusters of 2, 4 or 8
     // blocks, as long as each has a block of logits.
     const int64_t sms = device_sm_count();
-    // Warps of a row: 4 for a short one; 16 where there are few rows (256 x
-    // 65537 fp32, 5 alternatives: 24 us, 31 with 8), 8 where many rows' barriers
-    // and joins should overlap (4096 x 49999 bf16: 99 us, 122 with 16; with 8
-    // alternatives 163, 185 with 4).
-    const int size = cols <= 4 * 32 * kLpValues * 2 ? 2 : (rows >= 4 * sms ? 1 : 0);
+    // Warps of a row: 16 where there are few rows (256 x 65537 fp32, 5
+    // alternatives: 24 us, 31 with 8); where many rows' barriers and joins
+    // overlap, 8 with alternatives, whose list is a block's (4096 x 49999 bf16, 8
+    // of them: 163 us, 185 with 4), and 4 without (87 us, 92 with 8, 122 with 16)
+    // or for short rows.
+    const bool small = cols <= 4 * 32 * kLpValues * 2, many = rows >= 4 * sms;
+    const int size = small || (many && !top) ? 2 : (many ? 1 : 0);
     const int threads = 512 >> size;
     while (a.split < kLpMaxCluster && rows * a.split * 2 <= 2 * sms && cols > (int64_t)a.split * threads * kLpValues) a.split *= 2;
     const int64_t cap = 2 * (2048 / threads) * sms / a.split;
