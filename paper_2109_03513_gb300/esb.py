@@ -717,14 +717,15 @@ def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ES
     ty, ldx = _rows(x, "x")
     rows, cols = x.shape
     codes, ldc, scales, lds = _coded_out(x, rows, cols, f, group, codes, scales)
-    if xq is None and want_xq:
-        xq = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
     qp, qt, ldq = None, 0, 0
     if xq is not None:
         qt, ldq = _rows(xq, "xq")
         qp = xq.data_ptr()
         if xq.shape != x.shape:
             raise ValueError("xq must have the shape of x")
+    elif want_xq:
+        xq = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        qp, qt, ldq = xq.data_ptr(), ty, cols
     _check(lib().esb_project_groups(x.data_ptr(), ty, rows, cols, ldx, f.c(), rounding, rule, group, codes.data_ptr(),
                                     ldc, scales.data_ptr(), lds, qp, qt, ldq, _stream(stream)), "esb_project_groups")
     return Coded(codes, scales, f, cols, group), xq
@@ -748,10 +749,15 @@ def esb_matvec_groups(x, w: Coded, bias: Optional[torch.Tensor] = None, y: Optio
     if xk != k:
         raise ValueError("x and w must have the same number of columns")
     if y is None:
-        y = torch.empty((m, n), dtype=y_dtype or (torch.bfloat16 if coded else x.dtype), device=w.codes.device)
-    yt, ldy = _rows(y, "y")
-    if y.shape != (m, n):
-        raise ValueError("y must be (rows of x, rows of w)")
+        dtype = y_dtype or (torch.bfloat16 if coded else x.dtype)
+        yt, ldy = _TYPES.get(dtype), n
+        if yt is None:
+            raise ValueError("y must be float32, float16 or bfloat16")
+        y = torch.empty((m, n), dtype=dtype, device=w.codes.device)
+    else:
+        yt, ldy = _rows(y, "y")
+        if y.shape != (m, n):
+            raise ValueError("y must be (rows of x, rows of w)")
     _check(lib().esb_matvec_groups(m, n, k, xp, xt, ldx, xcp, ctypes.byref(wc),
                                    None if bias is None else _vector(bias, "bias", n, torch.float32), y.data_ptr(), yt,
                                    ldy, _stream(stream)), "esb_matvec_groups")
@@ -786,20 +792,25 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
     if residual is not None:
         a.ldr = _rows_like(residual, "residual", shape, dtype)
         a.residual = residual.data_ptr()
-        if h is None:
-            h = torch.empty(shape, dtype=dtype, device=x.device)
     if weight is not None:
         a.weight, a.w_type = _weight(weight, cols)
     if h is not None:
         a.ldh = _rows_like(h, "h", shape, dtype)
         a.h = h.data_ptr()
-    if y is None and (fmt is None if want_y is None else want_y):
-        y = torch.empty(shape, dtype=y_dtype or dtype, device=x.device)
+    elif residual is not None:
+        h = torch.empty(shape, dtype=dtype, device=x.device)
+        a.h, a.ldh = h.data_ptr(), cols
     if y is not None:
         a.y_type, a.ldy = _rows(y, "y")
         a.y = y.data_ptr()
         if y.shape != shape:
             raise ValueError("y must have the shape of x")
+    elif fmt is None if want_y is None else want_y:
+        yt = a.x_type if y_dtype is None else _TYPES.get(y_dtype)
+        if yt is None:
+            raise ValueError("y must be float32, float16 or bfloat16")
+        y = torch.empty(shape, dtype=y_dtype or dtype, device=x.device)
+        a.y, a.y_type, a.ldy = y.data_ptr(), yt, cols
     if yq is not None:
         if y is not None and y.dtype != yq.dtype:
             raise ValueError("y and yq must have one type")
@@ -807,10 +818,11 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
         a.yq = yq.data_ptr()
         if yq.shape != shape:
             raise ValueError("yq must have the shape of x")
-    if rstd is None and want_rstd:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     if rstd is not None:
         a.rstd = _vector(rstd, "rstd", rows, torch.float32)
+    elif want_rstd:
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        a.rstd = rstd.data_ptr()
     coded = None
     if fmt is not None:
         codes, a.ldc, scales, a.lds = _coded_out(x, rows, cols, fmt, group, codes, scales)
@@ -842,7 +854,9 @@ def esb_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[tor
         a.weight, a.w_type = _weight(weight, cols)
     if dx is None:
         dx = torch.empty(shape, dtype=dtype, device=h.device)
-    a.lddx = _rows_like(dx, "dx", shape, dtype)
+        a.lddx = cols
+    else:
+        a.lddx = _rows_like(dx, "dx", shape, dtype)
     a.dx = dx.data_ptr()
     wp, nb = None, 0
     if dweight is None and (weight is not None if want_dweight is None else want_dweight):
