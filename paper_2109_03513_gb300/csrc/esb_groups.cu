@@ -2,6 +2,7 @@
 // values of a row: alpha = max|x| / C, or the DDA scale of the group
 // (Sec. III-D with the group as the tensor), then Eq. cheap_projection.
 #include <cstdint>
+#include <type_traits>
 #include <cuda_runtime.h>
 
 #include "esb_internal.h"
@@ -114,10 +115,12 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
 // Instructions and HBM bound it alike: a value may cost 24 at the copy rate, and
 // the quotient, its rounding and sign, the element's value and a sixteenth of
 // the group's scale take about as many.  16384 x 4096 bf16 to (4,2) with values
-// (304 MB of reads and writes, 45 us at the copy rate): 62 us with the next
-// sixteen loaded ahead, one eight after the other from there to its stores, and
-// four blocks on an SM; 73 without the load ahead, 66 with three blocks and 73
-// with five, whose registers spill; 72 with blocks of a single sixteen a thread.
+// (304 MB of reads and writes, 45 us at the copy rate): 56 us with the next
+// sixteen loaded ahead, one eight after the other from there to its stores, few
+// branches for whole sixteens, and four blocks on an SM.  62 with a branch at
+// every eight's kind and stores; with those, 73 without the load ahead, 66 with
+// three blocks and 73 with five, whose registers spill, 72 with blocks of a
+// single sixteen a thread.
 template <int TYPE, int B, int LANES>
 __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(const GroupArgs a, int chunks, int dr, int dc)
 {
@@ -132,6 +135,9 @@ __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(
         for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         return v;
     };
+    // whole sixteens of a signed set under absmax scales, written by vectors and
+    // with values of x's type, take few branches
+    const bool straight = a.f.plain && a.rule == ESB_SCALE_ABSMAX && a.cvec && (!a.xq || (a.xq_type == TYPE && a.qvec));
     Raw8<T> next[2];
     auto load = [&]() {
         const int64_t e = (int64_t)chunk * 16;
@@ -202,6 +208,32 @@ __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(
         const GroupScale s = make_scale(alpha, a.f);
         const int left = left_of(a.cols, e);
         uint32_t w[2][B / 4];
+        constexpr int WORDS = B / 2;                    // of 16 codes
+        uint32_t* p = a.codes + in_row * a.ldc + (int64_t)in_chunk * WORDS;
+        auto put_words = [&]() {
+            if constexpr (B == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0][0], w[1][0]);
+            else *reinterpret_cast<uint4*>(p) = make_uint4(w[0][0], w[0][B / 4 - 1], w[1][0], w[1][B / 4 - 1]);
+        };
+        if (straight && left >= 16 && s.fast) {
+            T* q = static_cast<T*>(a.xq) + in_row * a.ldq + e;
+            auto sixteen = [&](auto linear) {
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    float r[8];
+                    raw[h].values(v);
+                    places8<B, decltype(linear)::value, false>(v, s, a.f, w[h], r);
+                    codes8<B>(v, a.f, w[h]);
+                    if (a.xq) {
+                        element_values(v, s, a.f, r);
+                        store8<T>(q + 8 * h, r);
+                    }
+                }
+            };
+            if (a.f.linear) sixteen(std::true_type());
+            else sixteen(std::false_type());
+            put_words();
+            continue;
+        }
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             float r[8];
@@ -215,11 +247,8 @@ __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(
                 store8_any(a.xq, a.xq_type, in_row * a.ldq + e + 8 * h, n, a.qvec, r);
             }
         }
-        constexpr int WORDS = B / 2;                    // of 16 codes
-        uint32_t* p = a.codes + in_row * a.ldc + (int64_t)in_chunk * WORDS;
         if (a.cvec && (int64_t)(in_chunk + 1) * WORDS <= a.ldc) {
-            if constexpr (B == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0][0], w[1][0]);
-            else *reinterpret_cast<uint4*>(p) = make_uint4(w[0][0], w[0][B / 4 - 1], w[1][0], w[1][B / 4 - 1]);
+            put_words();
         } else {
 #pragma unroll
             for (int i = 0; i < WORDS; i++)

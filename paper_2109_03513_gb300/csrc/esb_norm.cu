@@ -1,6 +1,7 @@
 // esb_norm.cu -- root-mean-square norm with the residual's addition, its
 // output plain or in ESB codes with scales, and its gradient.
 #include <cstdint>
+#include <type_traits>
 #include <cuda_runtime.h>
 
 #include "esb_internal.h"
@@ -152,8 +153,9 @@ __global__ void __launch_bounds__(kNormThreads) rmsnorm_kernel(const NormArgs a)
 // A group of codes is 2 to 16 lanes (32 to 256 values), or the row.  Many rows
 // are bound by instructions and HBM alike: 8192 x 4096 bf16 with residual,
 // codes and values (9 bytes for a value of x, 302 MB, 45 us at the copy rate)
-// 62 us with two blocks of 256 on an SM, 67 with three.  Few rows are bound by
-// latency: one row of 4096 takes 3.3 us.
+// 58 us with two blocks of 256 on an SM, 66 with three; 62 with a branch at every
+// eight's kind and stores.  Few rows are bound by latency: one row of 4096
+// takes 3.2 us.
 template <int TYPE, int TPR>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR < 256 ? 4 : 2)) rmsnorm_rows_kernel(const NormArgs a)
 {
@@ -198,6 +200,9 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
         load(row < a.rows);
         weights();
     }
+    // whole sixteens of a signed set, written by vectors and with values of x's
+    // type, take few branches
+    const bool straight = n >= 16 && a.f.plain && a.cvec && (!a.n.yq || (a.n.y_type == TYPE && a.qvec));
     int flip = 0;
     // a block's rows go on together, so that every thread meets every barrier
     for (int64_t first = (int64_t)blockIdx.x * PER; first < a.rows; first += step, row += step, flip ^= 1) {
@@ -277,23 +282,42 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR, TPR >= 512 ? 1 : (TPR <
             }
             const GroupScale s = make_scale(alpha, a.f);
             uint32_t c[2][2];
-#pragma unroll
-            for (int v = 0; v < 2; v++) {
-                float q[8];
-                quantise8<8, false>(z[v], s, a.f, c[v], q);
-                if (n - 8 * v < 8) zero_past<8>(c[v], n - 8 * v, a.f);
-                if (a.n.yq) {
-                    element_values(z[v], s, a.f, q);
-                    store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e + 8 * v, n - 8 * v, a.qvec, q);
-                }
-            }
             uint32_t* p = a.n.codes + row * a.n.ldc + t * 4;
-            if (a.cvec && left >= 4) {
+            if (straight && s.fast) {
+                T* yq = static_cast<T*>(a.n.yq) + row * a.n.ldq + e;
+                auto sixteen = [&](auto linear) {
+#pragma unroll
+                    for (int v = 0; v < 2; v++) {
+                        float q[8];
+                        places8<8, decltype(linear)::value, false>(z[v], s, a.f, c[v], q);
+                        codes8<8>(z[v], a.f, c[v]);
+                        if (a.n.yq) {
+                            element_values(z[v], s, a.f, q);
+                            store8<T>(yq + 8 * v, q);
+                        }
+                    }
+                };
+                if (a.f.linear) sixteen(std::true_type());
+                else sixteen(std::false_type());
                 *reinterpret_cast<uint4*>(p) = make_uint4(c[0][0], c[0][1], c[1][0], c[1][1]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    if (i < left) p[i] = c[i / 2][i % 2];
+                for (int v = 0; v < 2; v++) {
+                    float q[8];
+                    quantise8<8, false>(z[v], s, a.f, c[v], q);
+                    if (n - 8 * v < 8) zero_past<8>(c[v], n - 8 * v, a.f);
+                    if (a.n.yq) {
+                        element_values(z[v], s, a.f, q);
+                        store8_any(a.n.yq, a.n.y_type, row * a.n.ldq + e + 8 * v, n - 8 * v, a.qvec, q);
+                    }
+                }
+                if (a.cvec && left >= 4) {
+                    *reinterpret_cast<uint4*>(p) = make_uint4(c[0][0], c[0][1], c[1][0], c[1][1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; i++)
+                        if (i < left) p[i] = c[i / 2][i % 2];
+                }
             }
         }
         // words past those that the threads' values reach (a long row stride)

@@ -377,12 +377,24 @@ __device__ __forceinline__ void signs8(const float (&x)[8], uint32_t (&S)[B / 4]
         S[0] = tops(1, 3, 5, 7) | (tops(0, 2, 4, 6) >> 4);
     }
 }
+// Places to codes, with the signs of x.
+template <int B>
+__device__ __forceinline__ void codes8(const float (&x)[8], const QuantFmt& f, uint32_t (&w)[B / 4])
+{
+    constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
+    constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
+    uint32_t S[B / 4];
+    signs8<B>(x, S);
+#pragma unroll
+    for (int i = 0; i < B / 4; i++) {
+        const uint32_t nz = (w[i] + (TOP - ONES)) & TOP;
+        w[i] = ((w[i] + f.rotate) & ~TOP) | (S[i] & nz);
+    }
+}
 template <int B, bool CLAMP>
 __device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
 {
     constexpr int PER = 32 / B;
-    constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
-    constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
     if (s.fast && f.plain) {
         if (f.linear) places8<B, true, CLAMP>(x, s, f, w, r);
         else places8<B, false, CLAMP>(x, s, f, w, r);
@@ -396,13 +408,7 @@ __device__ __forceinline__ void quantise8(const float (&x)[8], const GroupScale&
             r[i] = __uint_as_float(p.y);
         }
     }
-    uint32_t S[B / 4];
-    signs8<B>(x, S);
-#pragma unroll
-    for (int i = 0; i < B / 4; i++) {
-        const uint32_t nz = (w[i] + (TOP - ONES)) & TOP;
-        w[i] = ((w[i] + f.rotate) & ~TOP) | (S[i] & nz);
-    }
+    codes8<B>(x, f, w);
 }
 
 // The numbers that the codes of x stand for, alpha q, from r.
