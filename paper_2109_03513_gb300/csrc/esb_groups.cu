@@ -220,12 +220,29 @@ __global__ void __launch_bounds__(kGroupThreads, 4) project_small_groups_kernel(
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     float r[8];
-                    raw[h].values(v);
-                    places8<B, decltype(linear)::value, false>(v, s, a.f, w[h], r);
-                    codes8<B>(v, a.f, w[h]);
-                    if (a.xq) {
-                        element_values(v, s, a.f, r);
-                        store8<T>(q + 8 * h, r);
+                    if constexpr (TYPE == ESB_F32) {
+                        raw[h].values(v);
+                        places8<B, decltype(linear)::value, false>(v, s, a.f, w[h], r);
+                        codes8<B>(v, a.f, w[h]);
+                        if (a.xq) {
+                            element_values(v, s, a.f, r);
+                            store8<T>(q + 8 * h, r);
+                        }
+                    } else {
+                        // signs in pairs of 16 bits, off and on again
+#pragma unroll
+                        for (int i = 0; i < 4; i++) unpack2<T>(raw[h].w[i] & 0x7fff7fffu, v[2 * i], v[2 * i + 1]);
+                        places8<B, decltype(linear)::value, false, true>(v, s, a.f, w[h], r);
+                        codes8<B>(raw[h].w, a.f, w[h]);
+                        if (a.xq) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                split(mul2(pair_of(s.step, s.step), pair_of(r[2 * i], r[2 * i + 1])), r[2 * i], r[2 * i + 1]);
+                                y[i] = pack2<T>(r[2 * i], r[2 * i + 1]) | (raw[h].w[i] & 0x80008000u);
+                            }
+                            *reinterpret_cast<uint4*>(q + 8 * h) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
                     }
                 }
             };

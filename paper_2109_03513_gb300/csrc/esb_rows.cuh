@@ -326,8 +326,8 @@ static __device__ __noinline__ uint2 place_any(float x, float alpha, const Quant
 // finite scale no value is NaN.
 // CLAMP: quotients may be past the largest element.  (Under a group's own
 // absmax scale they pass it by a unit in the last place at most, which the
-// rounding to the set takes back.)
-template <int B, bool LINEAR, bool CLAMP>
+// rounding to the set takes back.)  MAG: x are magnitudes.
+template <int B, bool LINEAR, bool CLAMP, bool MAG = false>
 __device__ __forceinline__ void places8(const float (&x)[8], const GroupScale& s, const QuantFmt& f, uint32_t (&w)[B / 4], float (&r)[8])
 {
     constexpr int PER = 32 / B;
@@ -338,7 +338,7 @@ __device__ __forceinline__ void places8(const float (&x)[8], const GroupScale& s
     for (int i = 0; i < B / 4; i++) w[i] = LINEAR ? 0u - 0x4B000000u * ONES : 0u;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-        Pair t = fast_quotients(pair_of(fabsf(x[i]), fabsf(x[i + 1])), rcp, minus_step);
+        Pair t = fast_quotients(MAG ? pair_of(x[i], x[i + 1]) : pair_of(fabsf(x[i]), fabsf(x[i + 1])), rcp, minus_step);
         float t0, t1;
         if constexpr (CLAMP || !LINEAR) split(t, t0, t1);
         if constexpr (CLAMP) {
@@ -377,9 +377,21 @@ __device__ __forceinline__ void signs8(const float (&x)[8], uint32_t (&S)[B / 4]
         S[0] = tops(1, 3, 5, 7) | (tops(0, 2, 4, 6) >> 4);
     }
 }
-// Places to codes, with the signs of x.
+// The same from four pairs of 16-bit numbers.
 template <int B>
-__device__ __forceinline__ void codes8(const float (&x)[8], const QuantFmt& f, uint32_t (&w)[B / 4])
+__device__ __forceinline__ void signs8(const uint32_t (&x)[4], uint32_t (&S)[B / 4])
+{
+    if constexpr (B == 8) {
+        S[0] = __byte_perm(x[0], x[1], 0x7531) & 0x80808080u;
+        S[1] = __byte_perm(x[2], x[3], 0x7531) & 0x80808080u;
+    } else {
+        const uint32_t a = __byte_perm(x[0], x[1], 0x7351), b = __byte_perm(x[2], x[3], 0x7351);
+        S[0] = (__byte_perm(a, b, 0x7632) & 0x80808080u) | ((__byte_perm(a, b, 0x5410) & 0x80808080u) >> 4);
+    }
+}
+// Places to codes, with the signs of x (eight numbers, or four pairs of 16 bits).
+template <int B, class X>
+__device__ __forceinline__ void codes8(const X& x, const QuantFmt& f, uint32_t (&w)[B / 4])
 {
     constexpr uint32_t TOP = B == 4 ? 0x88888888u : 0x80808080u;   // the codes' sign bits
     constexpr uint32_t ONES = B == 4 ? 0x11111111u : 0x01010101u;
