@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kGroupThreads) project_groups_kernel(const Gro
 // Instructions and HBM bound it alike: a value may cost 24 at the copy rate, and
 // the quotient, its rounding and sign, the element's value and a sixteenth of
 // the group's scale take about as many.  16384 x 4096 bf16 to (4,2) with values
-// (304 MB of reads and writes, 45 us at the copy rate): 56 us with the next
+// (304 MB of reads and writes, 45 us at the copy rate): 55 us with the next
 // sixteen loaded ahead, one eight after the other from there to its stores, few
 // branches for whole sixteens, and four blocks on an SM.  62 with a branch at
 // every eight's kind and stores; with those, 73 without the load ahead, 66 with
