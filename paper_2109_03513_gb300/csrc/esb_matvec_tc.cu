@@ -28,6 +28,7 @@
 
 #include "esb_internal.h"
 #include "esb_matvec.cuh"
+#include "esb_matvec_plan.h"
 #include "esb_tc.cuh"
 
 namespace esb {
@@ -36,11 +37,6 @@ namespace {
 
 constexpr int kTcDecode = 16, kTcScale = 8, kTcCopy = kTcDecode + kTcScale, kTcIssue = kTcCopy + 1, kTcWarps = kTcIssue + 1;
 constexpr int kTcThreads = kTcWarps * 32;
-constexpr int kTcStage = 256;                   // codes of a row in a stage: one TMA tile of 128 rows of 128 bytes, swizzled
-constexpr int kTcStageBytes = 128 * kTcStage / 2;
-constexpr int kTcStepsOfStage = kTcStage / 128;
-constexpr int kTcMaxStages = 8, kTcMaxA = 5, kTcMaxD = 12;
-constexpr size_t kTcSmem = 225 * 1024;
 
 // Where stage_x puts x: K-major rows of 128 bytes (64 values) in 8-row atoms
 // with the 128-byte swizzle, and the columns' scales of every step and group.
@@ -60,6 +56,7 @@ struct TcArgs {
     MvArgs a;
     int r;                                      // groups of a step: 1, 2 or 4
     int stages, na, nd;                         // slots of the three rings
+    int slot_first;                             // the decoding warps' order of waits
     int* status;
 };
 
@@ -217,7 +214,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) matvec_tc_kernel(const __grid_c
             const uint32_t half = (uint32_t)(first % kTcStepsOfStage) * 4u, turn = (uint32_t)lane & 7u;
             bool ok = true;
             for (int q = 0; q < my_tiles * steps_of_tile / 4 && ok; q++) {
-                ok = warp_wait(&full[st.at], st.parity, err);
+                ok = (!ta.slot_first || warp_wait(&afree[sl.at], sl.parity ^ 1u, err)) && warp_wait(&full[st.at], st.parity, err);
                 if (!ok) break;
                 const uint32_t at = my_row + st.at * kTcStageBytes;
                 uint32_t w[16];
@@ -391,50 +388,22 @@ EncodeTiled encode_tiled()
     return fn;
 }
 
-size_t tc_smem(int nc, int kc, int r, int stages)
-{
-    return 1024 + (size_t)(kc / 64) * nc * 128 + (size_t)stages * kTcStageBytes + (size_t)(kc / 128) * r * nc * 4 + 2 * nc * 128 * 4;
-}
-
 }  // namespace
 
 bool launch_matvec_tc(const MvArgs& args, int r, cudaStream_t st, cudaError_t* err)
 {
-    // Where the other kernel would take more than one pass of 32 columns, or
-    // nearly fills one with rows alone (times above).
-    const int64_t columns = args.M * args.planes * r;
-    if (columns <= 32 && !(r == 1 && columns > 20)) return false;
+    const int64_t sms = device_sm_count(), tiles = (args.N + 127) / 128;
+    MvTcPlan p;
+    if (!plan_matvec_tc(args.M, args.N, args.K, args.planes, r, (int)sms, p)) return false;
     TcArgs t;
     t.a = args;
     t.r = r;
-    const int64_t sms = device_sm_count(), tiles = (args.N + 127) / 128;
-    const int64_t kc = (args.K + 511) / 512 * 512;      // steps in fours
-    if (kc > 16384) return false;
-    t.a.kc = (int)kc;
-    // 32 columns where the rows need them and x then fits, else 16.  At least
-    // four slots of A: the decoding warps of step c know from their last step,
-    // c - 4, that what lay in its slot before is done, so all steps to c - 4 - na
-    // are, and the use before the last of c's own slot, c - 2 na, must be among
-    // them for a barrier's parity to tell its uses apart.
-    // (groups of 32 have sums for two steps only with 32 columns: 16 then)
-    int nc = args.M * args.planes <= 16 || r == 4 ? 16 : 32;
-    size_t smem = 0;
-    for (;; nc = 16) {
-        for (t.stages = kTcMaxStages; t.stages >= 2; t.stages--) {
-            smem = tc_smem(nc, t.a.kc, r, t.stages);
-            if (smem <= kTcSmem) break;
-        }
-        if (t.stages >= 2 || nc == 16) break;
-    }
-    if (t.stages < 2) return false;
-    t.a.mt = (int)std::min<int64_t>(args.M, nc / args.planes);
-    const int64_t passes = (args.M + t.a.mt - 1) / t.a.mt;
-    if (passes > 65535) return false;
-    t.a.mt = (int)((args.M + passes - 1) / passes);
-    t.na = nc == 16 ? 5 : 4;
-    t.nd = std::min(kTcMaxD, (512 - t.na * 64) / (r * nc));
-    // Too few tiles for the SMs: the other kernel splits rows among warps.
-    if (tiles * passes * 5 < sms * 4) return false;
+    t.a.kc = p.kc;
+    t.a.mt = p.mt;
+    t.stages = p.stages;
+    t.na = p.na;
+    t.nd = p.nd;
+    t.slot_first = p.slot_first;
     t.status = device_status_ptr();
     CUtensorMap map;
     const EncodeTiled encode = encode_tiled();
@@ -448,11 +417,11 @@ bool launch_matvec_tc(const MvArgs& args, int r, cudaStream_t st, cudaError_t* e
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
         return false;
     using Kernel = void (*)(const CUtensorMap, const TcArgs);
-    const Kernel kernel = nc == 16 ? matvec_tc_kernel<16> : matvec_tc_kernel<32>;
+    const Kernel kernel = p.nc == 16 ? matvec_tc_kernel<16> : matvec_tc_kernel<32>;
     *err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kTcSmem);
     if (*err != cudaSuccess) return true;
-    const unsigned gx = (unsigned)std::min<int64_t>(tiles, std::max<int64_t>(1, sms / passes));
-    *err = launch_pdl(kernel, dim3(gx, (unsigned)passes), dim3(kTcThreads), smem, st, map, t);
+    const unsigned gx = (unsigned)std::min<int64_t>(tiles, std::max<int64_t>(1, sms / p.passes));
+    *err = launch_pdl(kernel, dim3(gx, (unsigned)p.passes), dim3(kTcThreads), p.smem, st, map, t);
     return true;
 }
 
