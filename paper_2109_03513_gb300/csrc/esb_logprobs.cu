@@ -261,8 +261,9 @@ __global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 2
             if (to > m) {
                 const float d = m - to, f = exp_of(d);
                 const Pair f2 = pair_of(f, f);
+                // d may be -inf where f is 0; s2 never is, and keeps NaN
                 d2 = f == 0.0f ? pair_of(0.0f, 0.0f) : mul2(f2, fma2(pair_of(d, d), s2, d2));
-                s2 = f == 0.0f ? pair_of(0.0f, 0.0f) : mul2(f2, s2);
+                s2 = mul2(f2, s2);
                 m = to;
             }
         };

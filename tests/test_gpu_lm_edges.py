@@ -29,3 +29,42 @@ def test_matvec_many_columns_short_rings(M, N, K, group, x):
     for _ in range(20):
         assert torch.equal(y, esb.esb_matvec_groups(rows, w, y_dtype=torch.float32))
     assert esb.esb_get_status() == 0
+
+
+# ------------------------------------------------------------- log probabilities
+
+@pytest.mark.parametrize("rows,cols", [(1, 30000), (2, 200001), (700, 40000), (5, 3000)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("top", [0, 3])
+def test_logprobs_nan_stays_whatever_follows(rows, cols, dtype, top):
+    # what a thread has met is rescaled by a factor of 0 when a much larger logit follows: a NaN is not lost by it
+    part = cols // 2
+    good = rand((1, cols), 1, dtype, 3.0).expand(rows, cols)
+    ids = torch.full((rows,), cols - 1, dtype=torch.int64, device="cuda")
+    want = esb.esb_logprobs(good.contiguous(), ids, top=top)
+    assert torch.isfinite(want.lse).all()
+    for case in ("block", "one of the masked", "one of the far below", "infinity"):
+        x = good.contiguous().clone()
+        r = rows // 2
+        if case == "block":
+            x[r, :part] = float("nan")
+        elif case == "one of the masked":
+            x[r, :part] = -float("inf")
+            x[r, part // 3] = float("nan")
+        elif case == "one of the far below":
+            x[r, :part] = 0.0
+            x[r, part // 3] = float("nan")
+            x[r, part:] = 120.0
+        else:
+            x[r, :part] = -float("inf")
+            x[r, part // 3] = float("inf")
+        out = esb.esb_logprobs(x, ids, top=top)
+        assert torch.isnan(out.lse[r]) and torch.isnan(out.logp[r]) and torch.isnan(out.entropy[r]), case
+        others = torch.arange(rows, device="cuda") != r
+        assert torch.equal(out.lse[others], want.lse[others]) and torch.equal(out.entropy[others], want.entropy[others])
+        if top:
+            v = torch.where(torch.isnan(x[r]), torch.full_like(x[r], -float("inf")), x[r]).float()
+            assert torch.equal(out.top_ids[r], torch.sort(v, descending=True, stable=True).indices[:top])
+        g = torch.ones(rows, device="cuda")
+        dx = esb.esb_logprobs_backward(x, ids, out.lse, out.entropy, g, g)
+        assert torch.isnan(dx[r]).all() and torch.isfinite(dx[others]).all(), case
