@@ -651,7 +651,8 @@ esb_status esb_project_groups(const void* x, int32_t x_type, int64_t rows, int64
  *   xc    [host] the coded rows, b = 8 and 2 <= k <= 7, their group 0 or a
  *         multiple of w's group
  *   w     [host] the matrix: N rows of K codes, b = 4, rows 16-byte aligned
- *         (ld a multiple of 4)
+ *         (ld a multiple of 4); a row is read in whole 16 bytes, up to the
+ *         one with its last code, whatever ld is
  *   bias  [device] N floats or NULL
  *   y     [device] M x N values of y_type, row stride ldy
  * Any M; the matrix is read once for every few rows, so many rows (a prompt)

@@ -34,14 +34,15 @@
 
 #include "esb_internal.h"
 #include "esb_matvec.cuh"
+#include "esb_matvec_plan.h"
 
 namespace esb {
 
 namespace {
 
 constexpr int kRedLd = 20;          // floats between columns of a warp's 16 sums
-constexpr int kSteps = 4;           // steps of 128 codes of a row, 16 bytes a lane and row, that a warp has in flight
-constexpr int kSlice = 128 * kSteps;
+// (kSteps: steps of 128 codes of a row, 16 bytes a lane and row, that a warp has
+// in flight; kSlice: their codes)
 
 __device__ __forceinline__ uint4 ldg_stream(const uint32_t* p)
 {
@@ -152,12 +153,11 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
         }
     };
     auto load_step = [&](int c) {
-        if (p_k + kSlice <= (int)a.wfull) {
+        if (p_k + kSlice <= a.row_codes) {
             buf[c][0] = ldg_stream(pw[0] + c * 16);
             buf[c][1] = ldg_stream(pw[1] + c * 16);
         } else {
-            // past the row's end its last words will do: x is 0 there
-            const int o = min(c * 16, (int)a.wfull / 8 - 4 - (p_k / 8 + t * 4));
+            const int o = mv_end_words(p_k, t, c, a.row_codes);
             buf[c][0] = ldg_stream(pw[0] + o);
             buf[c][1] = ldg_stream(pw[1] + o);
         }
@@ -372,7 +372,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
     a.tab.by4 = 1u << 4;
     const int r = a.w.group % 128 == 0 ? 1 : (a.w.group % 64 == 0 ? 2 : 4);
     a.planes = x_type == ESB_F32 ? 2 : 1;
-    a.wfull = std::min<int64_t>(w.ld * 8, (int64_t)1 << 20);
+    a.row_codes = (int)mv_row_codes(K);
 
     cudaError_t e = cudaSuccess;
     if (launch_matvec_tc(a, r, st, &e)) return e;

@@ -1,12 +1,37 @@
-// esb_matvec_plan.h -- host arithmetic of esb_matvec_groups that needs no
-// CUDA: which calls the tcgen05 kernel takes and the sizes of its rings.
+// esb_matvec_plan.h -- arithmetic of esb_matvec_groups that needs no CUDA:
+// where a row of the matrix ends, which calls the tcgen05 kernel takes and the
+// sizes of its rings.
 #pragma once
 
 #include <algorithm>
 #include <cstddef>
 #include <cstdint>
 
+#ifdef __CUDACC__
+#define ESB_HOST_DEVICE __host__ __device__ __forceinline__
+#else
+#define ESB_HOST_DEVICE inline
+#endif
+
 namespace esb {
+
+// Codes of a row of K that the kernels read: whole 16 bytes, which a row of ld
+// words (a multiple of four) has.  Never by ld: a row may be the last of a
+// matrix cut out of a wider one.
+inline int64_t mv_row_codes(int64_t K) { return (K + 31) / 32 * 32; }
+
+// The warp-level kernel's slice: four steps of 128 codes, 16 bytes of each for
+// each of four lanes.
+constexpr int kSteps = 4;
+constexpr int kSlice = 128 * kSteps;
+// Words from lane t's place in the slice that starts at code k to those of its
+// step c that it reads, where the row of `codes` (mv_row_codes) ends within the
+// slice: past the end its last words will do, x is 0 there.
+ESB_HOST_DEVICE int mv_end_words(int k, int t, int c, int codes)
+{
+    const int last = codes / 8 - 4 - (k / 8 + t * 4);
+    return c * 16 < last ? c * 16 : last;
+}
 
 constexpr int kTcStage = 256;                   // codes of a row in a stage: one TMA tile of 128 rows of 128 bytes, swizzled
 constexpr int kTcStageBytes = 128 * kTcStage / 2;

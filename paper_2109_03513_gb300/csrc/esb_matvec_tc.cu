@@ -408,8 +408,8 @@ bool launch_matvec_tc(const MvArgs& args, int r, cudaStream_t st, cudaError_t* e
     CUtensorMap map;
     const EncodeTiled encode = encode_tiled();
     if (!encode) return false;
-    // the row's whole words of 16 bytes, rows ld words apart
-    const cuuint64_t dims[2] = {(cuuint64_t)std::min<int64_t>(args.w.ld, (int64_t)1 << 30), (cuuint64_t)args.N}, strides[1] = {(cuuint64_t)args.w.ld * 4};
+    // rows ld words apart, of the words that are read
+    const cuuint64_t dims[2] = {(cuuint64_t)args.row_codes / 8, (cuuint64_t)args.N}, strides[1] = {(cuuint64_t)args.w.ld * 4};
     const cuuint32_t box[2] = {kTcStage / 8, 128}, steps[2] = {1, 1};
     if (strides[0] >= (cuuint64_t)1 << 40 ||
         encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint32_t*>(args.w.codes), dims, strides, box, steps,

@@ -31,6 +31,21 @@ def test_matvec_many_columns_short_rings(M, N, K, group, x):
     assert esb.esb_get_status() == 0
 
 
+# (small, wide; by both kernels) the last row ends its storage, so nothing behind it may be read
+@pytest.mark.parametrize("M,N,K,group", [(1, 40, 64, 32), (3, 33, 333, 64), (2, 50, 1000, 0), (4, 200, 4100, 128), (5, 19457, 577, 96),
+                                         (40, 16000, 1030, 128)])
+def test_matvec_matrix_cut_out_of_a_wider_one(M, N, K, group):
+    w = make_w(N, K, group, 2)
+    words = -(-K // 32) * 4
+    ld = words + 124
+    store = torch.randint(-2 ** 31, 2 ** 31 - 1, ((N - 1) * ld + words,), dtype=torch.int32, device="cuda")
+    codes = torch.as_strided(store, (N, words), (ld, 1))
+    codes.copy_(w.codes[:, :words])
+    x = rand((M, K), 3, torch.bfloat16)
+    assert torch.equal(esb.esb_matvec_groups(x, esb.Coded(codes, w.scales, w.fmt, K, group)), esb.esb_matvec_groups(x, w))
+    assert esb.esb_get_status() == 0
+
+
 # ------------------------------------------------------------- log probabilities
 
 @pytest.mark.parametrize("rows,cols", [(1, 30000), (2, 200001), (700, 40000), (5, 3000)])

@@ -1,5 +1,6 @@
 """The host arithmetic of esb_matvec_groups (csrc/esb_matvec_plan.h), compiled
-by itself: the rings of the tcgen05 kernel tell their uses apart."""
+by itself: a row of the matrix is not read past its end, and the rings of the
+tcgen05 kernel tell their uses apart."""
 import ctypes
 import os
 import shutil
@@ -18,6 +19,9 @@ extern "C" int plan_tc(int64_t M, int64_t N, int64_t K, int planes, int r, int s
     for (int i = 0; i < 9; i++) out[i] = v[i];
     return 1;
 }
+extern "C" int64_t row_codes(int64_t K) { return esb::mv_row_codes(K); }
+extern "C" int slice() { return esb::kSlice; }
+extern "C" int end_words(int k, int t, int c, int codes) { return esb::mv_end_words(k, t, c, codes); }
 """
 
 
@@ -33,6 +37,7 @@ def shim(tmp_path_factory):
                     "-o", str(so)], check=True)
     lib = ctypes.CDLL(str(so))
     lib.plan_tc.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int] * 3 + [ctypes.c_void_p]
+    lib.row_codes.argtypes, lib.row_codes.restype = [ctypes.c_int64], ctypes.c_int64
     return lib
 
 
@@ -77,3 +82,20 @@ def test_rings_of_stages_tell_their_uses_apart(shim):
         for c in range(64):
             assert decoder_is_behind(stages, na, slot_first, c), (stages, na, slot_first, c)
             assert c - 2 * na <= c - 4 - na      # the slot of A's own uses, by the products before step c - 4's
+
+
+def test_rows_are_not_read_past_their_end(shim):
+    size = shim.slice()
+    for K in [*range(1, 1100), 4095, 4096, 4097, (1 << 18) - 1]:
+        words = -(-K // 8)
+        codes = shim.row_codes(K)
+        # whole 16 bytes, no more than the smallest stride of such rows; the tcgen05 kernel's copies end there
+        assert codes % 32 == 0 and codes // 8 == -(-words // 4) * 4
+        # the warp-level kernel: every slice of a row but the last lies within it, and in the last one every lane's words
+        k = (K - 1) // size * size
+        for t in range(4):
+            for c in range(4):
+                at = k // 8 + 4 * t + (16 * c if k + size <= codes else shim.end_words(k, t, c, codes))
+                assert 0 <= at and at + 4 <= codes // 8, (K, t, c)
+                if 128 * c + 32 * t + k < K:             # codes of the row: in their place
+                    assert at == k // 8 + 16 * c + 4 * t
