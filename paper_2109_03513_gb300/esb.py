@@ -634,6 +634,18 @@ class Coded(NamedTuple):
                          self.group, self.fmt.c())
 
 
+def _empty_on(stream):
+    """torch.empty for what a call on `stream` makes.  Memory belongs to the stream that is current when it is
+    allocated: from another stream's it could still be in use, and a workspace would be given on when the call returns."""
+    if stream is None:
+        return torch.empty
+
+    def empty(*size, **kw):
+        with torch.cuda.stream(stream):
+            return torch.empty(*size, **kw)
+    return empty
+
+
 # The checks below are short on purpose: at a decoding step's sizes they cost
 # more than the kernels.
 
@@ -693,16 +705,16 @@ def _groups(cols: int, group: int) -> int:
     return -(-cols // group) if 0 < group < cols else 1
 
 
-def _coded_out(x: torch.Tensor, rows: int, cols: int, f: Fmt, group: int, codes, scales):
+def _coded_out(x: torch.Tensor, rows: int, cols: int, f: Fmt, group: int, codes, scales, empty):
     """Code words and scales of a (rows, cols) result, made where not given -> (codes, ldc, scales, lds)."""
     if codes is None:
         ldc = (-(-cols // (32 // f.b)) + 3) & -4 if 2 <= f.b <= 8 else 4
-        codes = torch.empty((rows, ldc), dtype=torch.int32, device=x.device)
+        codes = empty((rows, ldc), dtype=torch.int32, device=x.device)
     else:
         ldc = _words(codes, "codes", rows)
     if scales is None:
         lds = _groups(cols, group)
-        scales = torch.empty((rows, lds), dtype=torch.float32, device=x.device)
+        scales = empty((rows, lds), dtype=torch.float32, device=x.device)
     else:
         lds = _rows_like(scales, "scales", (rows, _groups(cols, group)), torch.float32)
     return codes, ldc, scales, lds
@@ -716,7 +728,8 @@ def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ES
     row -> (Coded, the numbers the codes stand for (rows, cols) | None)."""
     ty, ldx = _rows(x, "x")
     rows, cols = x.shape
-    codes, ldc, scales, lds = _coded_out(x, rows, cols, f, group, codes, scales)
+    empty = _empty_on(stream)
+    codes, ldc, scales, lds = _coded_out(x, rows, cols, f, group, codes, scales, empty)
     qp, qt, ldq = None, 0, 0
     if xq is not None:
         qt, ldq = _rows(xq, "xq")
@@ -724,7 +737,7 @@ def esb_project_groups(x: torch.Tensor, f: Fmt, group: int = 128, rule: int = ES
         if xq.shape != x.shape:
             raise ValueError("xq must have the shape of x")
     elif want_xq:
-        xq = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        xq = empty((rows, cols), dtype=x.dtype, device=x.device)
         qp, qt, ldq = xq.data_ptr(), ty, cols
     _check(lib().esb_project_groups(x.data_ptr(), ty, rows, cols, ldx, f.c(), rounding, rule, group, codes.data_ptr(),
                                     ldc, scales.data_ptr(), lds, qp, qt, ldq, _stream(stream)), "esb_project_groups")
@@ -753,7 +766,7 @@ def esb_matvec_groups(x, w: Coded, bias: Optional[torch.Tensor] = None, y: Optio
         yt, ldy = _TYPES.get(dtype), n
         if yt is None:
             raise ValueError("y must be float32, float16 or bfloat16")
-        y = torch.empty((m, n), dtype=dtype, device=w.codes.device)
+        y = _empty_on(stream)((m, n), dtype=dtype, device=w.codes.device)
     else:
         yt, ldy = _rows(y, "y")
         if y.shape != (m, n):
@@ -784,6 +797,7 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
     """RMS norm of x + residual -> NormOut.  h is written when there is a
     residual or a tensor for it; y unless `fmt` asks for codes (or want_y says);
     yq when there is a tensor for it."""
+    empty = _empty_on(stream)
     a = esb_norm()
     a.x_type, a.ldx = _rows(x, "x")
     a.x, a.eps = x.data_ptr(), eps
@@ -798,7 +812,7 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
         a.ldh = _rows_like(h, "h", shape, dtype)
         a.h = h.data_ptr()
     elif residual is not None:
-        h = torch.empty(shape, dtype=dtype, device=x.device)
+        h = empty(shape, dtype=dtype, device=x.device)
         a.h, a.ldh = h.data_ptr(), cols
     if y is not None:
         a.y_type, a.ldy = _rows(y, "y")
@@ -809,7 +823,7 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
         yt = a.x_type if y_dtype is None else _TYPES.get(y_dtype)
         if yt is None:
             raise ValueError("y must be float32, float16 or bfloat16")
-        y = torch.empty(shape, dtype=y_dtype or dtype, device=x.device)
+        y = empty(shape, dtype=y_dtype or dtype, device=x.device)
         a.y, a.y_type, a.ldy = y.data_ptr(), yt, cols
     if yq is not None:
         if y is not None and y.dtype != yq.dtype:
@@ -821,11 +835,11 @@ def esb_rmsnorm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e
     if rstd is not None:
         a.rstd = _vector(rstd, "rstd", rows, torch.float32)
     elif want_rstd:
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        rstd = empty(rows, dtype=torch.float32, device=x.device)
         a.rstd = rstd.data_ptr()
     coded = None
     if fmt is not None:
-        codes, a.ldc, scales, a.lds = _coded_out(x, rows, cols, fmt, group, codes, scales)
+        codes, a.ldc, scales, a.lds = _coded_out(x, rows, cols, fmt, group, codes, scales, empty)
         a.codes, a.scales, a.group, a.fmt, a.rounding = codes.data_ptr(), scales.data_ptr(), group, fmt.c(), rounding
         coded = Coded(codes, scales, fmt, cols, group)
     _check(lib().esb_rmsnorm(rows, cols, ctypes.byref(a), _stream(stream)), "esb_rmsnorm")
@@ -839,6 +853,7 @@ def esb_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[tor
                          stream=None) -> tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Gradient of esb_rmsnorm -> (dx, of x and of the residual alike; dweight
     fp32 | None).  dweight is computed when there is a weight, unless want_dweight says."""
+    empty = _empty_on(stream)
     a = esb_norm_grad()
     a.x_type, a.ldh = _rows(h, "h")
     a.g_type, a.ldg = _rows(dy, "dy")
@@ -853,19 +868,19 @@ def esb_rmsnorm_backward(dy: torch.Tensor, h: torch.Tensor, weight: Optional[tor
     if weight is not None:
         a.weight, a.w_type = _weight(weight, cols)
     if dx is None:
-        dx = torch.empty(shape, dtype=dtype, device=h.device)
+        dx = empty(shape, dtype=dtype, device=h.device)
         a.lddx = cols
     else:
         a.lddx = _rows_like(dx, "dx", shape, dtype)
     a.dx = dx.data_ptr()
     wp, nb = None, 0
     if dweight is None and (weight is not None if want_dweight is None else want_dweight):
-        dweight = torch.empty(cols, dtype=torch.float32, device=h.device)
+        dweight = empty(cols, dtype=torch.float32, device=h.device)
     if dweight is not None:
         a.dweight = _vector(dweight, "dweight", cols, torch.float32)
         if workspace is None:
             nb = int(lib().esb_rmsnorm_backward_workspace_bytes(rows, cols))
-            workspace = torch.empty(nb, dtype=torch.uint8, device=h.device)
+            workspace = empty(nb, dtype=torch.uint8, device=h.device)
         else:
             _dev(workspace, "workspace")
             nb = workspace.numel() * workspace.element_size()
@@ -891,14 +906,14 @@ def esb_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, top: 
     ip = None if ids is None else _vector(ids, "ids", rows, torch.int64)
     if not 0 <= top <= ESB_MAX_TOP:
         raise ValueError(f"top must be 0..{ESB_MAX_TOP}")
-    dev = logits.device
-    lp = None if ip is None else torch.empty(rows, dtype=torch.float32, device=dev)
-    ent = torch.empty(rows, dtype=torch.float32, device=dev)
-    lse = torch.empty(rows, dtype=torch.float32, device=dev)
+    dev, empty = logits.device, _empty_on(stream)
+    lp = None if ip is None else empty(rows, dtype=torch.float32, device=dev)
+    ent = empty(rows, dtype=torch.float32, device=dev)
+    lse = empty(rows, dtype=torch.float32, device=dev)
     tl = ti = tlp = tip = None
     if top:
-        tl = torch.empty((rows, top), dtype=torch.float32, device=dev)
-        ti = torch.empty((rows, top), dtype=torch.int64, device=dev)
+        tl = empty((rows, top), dtype=torch.float32, device=dev)
+        ti = empty((rows, top), dtype=torch.int64, device=dev)
         tlp, tip = tl.data_ptr(), ti.data_ptr()
     _check(lib().esb_logprobs(logits.data_ptr(), ty, rows, cols, ldx, ip, top, None if lp is None else lp.data_ptr(),
                               ent.data_ptr(), lse.data_ptr(), tlp, tip, _stream(stream)), "esb_logprobs")
@@ -919,7 +934,7 @@ def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse
     hp = None if dentropy is None else _vector(dentropy, "dentropy", rows, f32)
     ip = None if ids is None else _vector(ids, "ids", rows, torch.int64)
     if dlogits is None:
-        dlogits = torch.empty(shape, dtype=logits.dtype, device=logits.device)
+        dlogits = _empty_on(stream)(shape, dtype=logits.dtype, device=logits.device)
     ldd = _rows_like(dlogits, "dlogits", shape, logits.dtype)
     _check(lib().esb_logprobs_backward(logits.data_ptr(), ty, rows, cols, ldx, ip, lp, ep, gp, hp, dlogits.data_ptr(),
                                        ldd, _stream(stream)), "esb_logprobs_backward")

@@ -83,3 +83,63 @@ def test_logprobs_nan_stays_whatever_follows(rows, cols, dtype, top):
         g = torch.ones(rows, device="cuda")
         dx = esb.esb_logprobs_backward(x, ids, out.lse, out.entropy, g, g)
         assert torch.isnan(dx[r]).all() and torch.isfinite(dx[others]).all(), case
+
+
+# ------------------------------------------------------------- other streams
+
+DELAY = 100_000_000                     # clocks that a stream is kept busy, some 50 ms: longer than the host takes for a few calls
+
+
+def test_backward_workspace_belongs_to_the_call_s_stream():
+    # what the current stream allocates after the call is not the workspace that the call's stream has yet to write
+    rows, cols = 4096, 1024
+    h, dy, w = rand((rows, cols), 1), rand((rows, cols), 2), rand((cols,), 3)
+    rstd = esb.esb_rmsnorm(h, None, want_rstd=True).rstd
+    dx, dw = torch.empty_like(h), torch.empty(cols, device="cuda")
+    want, want_w = esb.esb_rmsnorm_backward(dy, h, w, rstd)
+    nb = esb.lib().esb_rmsnorm_backward_workspace_bytes(rows, cols)
+    torch.full((1,), 7, dtype=torch.uint8, device="cuda")      # loads what fills below: a load may wait for the device
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(DELAY)
+    esb.esb_rmsnorm_backward(dy, h, w, rstd, dx=dx, dweight=dw, stream=st)
+    others = [torch.full((nb,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    assert torch.equal(dx, want) and torch.equal(dw, want_w)
+    assert all((t == 7).all() for t in others)
+
+
+def lm_calls():
+    """Each call with the outputs that it makes itself, as a function of the stream."""
+    x, r, w, dy = rand((64, 512), 1), rand((64, 512), 2), rand((512,), 3), rand((64, 512), 4)
+    m = make_w(128, 512, 64, 2)
+    rstd = esb.esb_rmsnorm(x, None, want_rstd=True).rstd
+    ids = torch.arange(64, device="cuda")
+    lp = esb.esb_logprobs(x, ids)
+    return {
+        "project": lambda st: [*esb.esb_project_groups(x, esb.Fmt(4, 2), 64, want_xq=True, stream=st)[0][:2],
+                               esb.esb_project_groups(x, esb.Fmt(4, 2), 64, want_xq=True, stream=st)[1]],
+        "matvec": lambda st: [esb.esb_matvec_groups(x, m, stream=st)],
+        "norm": lambda st: (lambda o: [o.h, o.y, o.rstd, *o.coded[:2]])(esb.esb_rmsnorm(x, w, residual=r, want_y=True, want_rstd=True,
+                                                                                       fmt=esb.Fmt(8, 6), stream=st)),
+        "norm backward": lambda st: list(esb.esb_rmsnorm_backward(dy, x, w, rstd, stream=st)),
+        "logprobs": lambda st: list(esb.esb_logprobs(x, ids, top=4, stream=st)),
+        "logprobs backward": lambda st: [esb.esb_logprobs_backward(x, ids, lp.lse, None, lp.logp, stream=st)],
+    }
+
+
+@pytest.mark.parametrize("name", ["project", "matvec", "norm", "norm backward", "logprobs", "logprobs backward"])
+def test_outputs_belong_to_the_call_s_stream(name):
+    # memory that the current stream has yet to write, freed on the host, is not where another stream's outputs go
+    call = lm_calls()[name]
+    want = [t.clone() for t in call(None)]
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(DELAY)
+    for t in want:                      # blocks of each output's size, with work waiting on them
+        for _ in range(4):
+            torch.empty_like(t).fill_(3)
+    got = call(st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
