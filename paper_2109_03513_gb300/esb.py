@@ -630,6 +630,8 @@ class Coded(NamedTuple):
     def c(self, name: str) -> esb_coded:
         n = self.codes.shape[0]
         lds = _rows_like(self.scales, name + ".scales", (n, _groups(self.cols, self.group)), torch.float32)
+        if self.codes.dim() == 2 and self.codes.shape[1] * 32 < self.cols * self.fmt.b:
+            raise ValueError(f"{name}.codes must hold {self.cols} codes a row")
         return esb_coded(self.codes.data_ptr(), _words(self.codes, name + ".codes", n), self.scales.data_ptr(), lds,
                          self.group, self.fmt.c())
 
@@ -712,6 +714,8 @@ def _coded_out(x: torch.Tensor, rows: int, cols: int, f: Fmt, group: int, codes,
         codes = empty((rows, ldc), dtype=torch.int32, device=x.device)
     else:
         ldc = _words(codes, "codes", rows)
+        if not codes.is_contiguous():   # every word of the stride is written
+            raise ValueError("codes must be contiguous")
     if scales is None:
         lds = _groups(cols, group)
         scales = empty((rows, lds), dtype=torch.float32, device=x.device)
