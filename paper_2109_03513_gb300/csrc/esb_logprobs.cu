@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 2
             }
             float v[U][V];
             float big = fmaxf(lowest, edge);                // the thread's largest
-            bool masked = true;                             // whether one may be -inf
+            float least_of = ninf;                          // its smallest (fp32: not looked for)
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 if constexpr (V == 8) {
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 2
                 }
             }
             if constexpr (V == 8) {
-                // in pairs of 16 bits: the largest, and whether any is -inf
+                // in pairs of 16 bits: the largest and the smallest
                 uint32_t hi = raw[0].x, lo = raw[0].x;
 #pragma unroll
                 for (int u = 0; u < U; u++) {
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 2
                 unpack2<T>(hi, a0, a1);
                 big = fmaxf(big, fmaxf(a0, a1));
                 unpack2<T>(lo, a0, a1);
-                masked = fminf(a0, a1) == ninf;
+                least_of = fminf(a0, a1);
             } else {
 #pragma unroll
                 for (int u = 0; u < U; u++)
@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(WARPS * 32, (TYPE == ESB_F32 && WARPS < 16 ? 2
             raise(big);
             const Pair minus_m = pair_of(-m, -m);
             if (edge != ninf) add(edge, ninf, minus_m, true);
-            if (V == 8 && !masked) {
+            // a difference of -inf: a masked logit, or bf16's lowest from its largest
+            if (V == 8 && least_of - m > ninf) {
 #pragma unroll
                 for (int u = 0; u < U; u++)
 #pragma unroll

@@ -85,6 +85,30 @@ def test_logprobs_nan_stays_whatever_follows(rows, cols, dtype, top):
         assert torch.isnan(dx[r]).all() and torch.isfinite(dx[others]).all(), case
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [40, 5000, 40000])
+def test_logprobs_from_the_type_s_lowest_to_its_largest(dtype, cols):
+    # a difference of two finite logits may be past fp32's range: its probability is 0 and it adds nothing to the entropy
+    big = torch.finfo(dtype).max
+    x = rand((4, cols), 1, dtype)
+    x[0, ::3], x[0, 7] = -big, big
+    x[1] = -big
+    x[1, cols - 1] = big
+    x[2, :] = big
+    x[2, 1::2] = -big
+    x[3, 5] = big
+    ids = torch.tensor([7, cols - 1, 0, 5], device="cuda")
+    out = esb.esb_logprobs(x, ids, top=2)
+    n = (cols + 1) // 2
+    want = torch.tensor([0.0, 0.0, n, 0.0], dtype=torch.float64, device="cuda").clamp_min(1).log()
+    # a logarithm and a sum of ones: a few units
+    assert ((out.entropy.double() - want).abs() <= 8 * U * (1 + want)).all()
+    assert ((out.logp.double() + want).abs() <= 8 * U * (1 + want)).all()
+    assert torch.equal(out.top_ids[[0, 1, 3], 0], ids[[0, 1, 3]]) and (out.lse.double() - big).abs().max() <= 2 * U * big + 16
+    dx = esb.esb_logprobs_backward(x, ids, out.lse, out.entropy, torch.ones(4, device="cuda"), torch.ones(4, device="cuda"))
+    assert torch.isfinite(dx).all()
+
+
 # ------------------------------------------------------------- other streams
 
 DELAY = 100_000_000                     # clocks that a stream is kept busy, some 50 ms: longer than the host takes for a few calls
