@@ -40,6 +40,7 @@ namespace esb {
 
 namespace {
 
+constexpr int kMvWarps = 16, kMvThreads = kMvWarps * 32;   // of a block, one on an SM
 constexpr int kRedLd = 20;          // floats between columns of a warp's 16 sums
 // (kSteps: steps of 128 codes of a row, 16 bytes a lane and row, that a warp has
 // in flight; kSlice: their codes)
@@ -82,7 +83,7 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 // and the warps' sums, twice.
 __host__ __device__ inline int xs_stride(int kc) { return kc * 2 + 64; }
 __host__ inline size_t mv_x_bytes(int rows, int kc, int nt) { return (size_t)rows * xs_stride(kc) + (size_t)(kc / 128) * 8 * nt * 4; }
-__host__ inline size_t mv_sums(int cols, int warps) { return (size_t)2 * warps * cols * kRedLd * 4; }
+__host__ inline size_t mv_sums(int cols) { return (size_t)2 * kMvWarps * cols * kRedLd * 4; }
 
 __device__ __forceinline__ void cluster_barrier()
 {
@@ -111,12 +112,11 @@ struct XsPlace {
     __device__ __forceinline__ float* scale(int row, int step, int r) const { return fx + step * 8 * NT + row * R + r; }
 };
 
-template <int NT, int R, int WARPS, int BLOCKS>
-__global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs a)
+template <int NT, int R>
+__global__ void __launch_bounds__(kMvThreads, 1) matvec_kernel(const MvArgs a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ uint16_t xtab[256];
-    constexpr int THREADS = WARPS * 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int64_t m0 = (int64_t)blockIdx.z * a.mt;
     const int mt = (int)min((int64_t)a.mt, a.M - m0);
@@ -128,9 +128,9 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
     float* fx = reinterpret_cast<float*>(zeros + (a.zrow ? xs_stride(a.kc) : 0));
     float* red = fx + (a.kc / 128) * 8 * NT;
     const int part = a.mt * a.planes * R * kRedLd;      // floats of a warp's sums of a tile
-    const int batch = WARPS * part;
+    const int batch = kMvWarps * part;
 
-    const int wn = WARPS / a.wk;                        // tiles of 16 rows in work at once
+    const int wn = kMvWarps / a.wk;                     // tiles of 16 rows in work at once
     const int wi = warp / a.wk, wj = warp % a.wk;       // this warp's tile of them, and its place along the row
     const int N = (int)a.N, tiles = (N + 15) / 16, stride = (int)gridDim.x * wn;
     const int first = (int)blockIdx.x * wn;
@@ -179,15 +179,15 @@ __global__ void __launch_bounds__(WARPS * 32, BLOCKS) matvec_kernel(const MvArgs
         load_scales();
     }
 
-    for (int i = threadIdx.x; i < (a.kc / 128) * 8 * NT; i += THREADS)
+    for (int i = threadIdx.x; i < (a.kc / 128) * 8 * NT; i += kMvThreads)
         if (i % (8 * NT) >= cols) fx[i] = 0.0f;
     if (a.zrow)
-        for (int i = threadIdx.x * 16; i < a.kc * 2; i += THREADS * 16) *reinterpret_cast<uint4*>(zeros + i) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = threadIdx.x * 16; i < a.kc * 2; i += kMvThreads * 16) *reinterpret_cast<uint4*>(zeros + i) = make_uint4(0u, 0u, 0u, 0u);
     if (a.x_type == ESB_CODES) {
-        for (int i = threadIdx.x; i < 256; i += THREADS) xtab[i] = x_code_half(i, a.xc.fmt.k);
+        for (int i = threadIdx.x; i < 256; i += kMvThreads) xtab[i] = x_code_half(i, a.xc.fmt.k);
         __syncthreads();
     }
-    stage_x<R>(a, m0, mt, k0, XsPlace<NT, R>{xs, fx, xs_stride(a.kc)}, xtab, WARPS, warp);
+    stage_x<R>(a, m0, mt, k0, XsPlace<NT, R>{xs, fx, xs_stride(a.kc)}, xtab, kMvWarps, warp);
     __syncthreads();
 
     // where this lane reads x for column 8 i + g: its row's plane, or zeros
@@ -337,15 +337,9 @@ void element_bytes(int k, uint32_t& lo, uint32_t& hi)
 
 using MvKernel = void (*)(const MvArgs);
 constexpr size_t kMvSmem = 225 * 1024;
-struct MvPlan {
-    MvKernel kernel;
-    int warps, blocks;
-};
-template <int R> MvPlan mv_plan(int nt)
+template <int R> MvKernel mv_kernel(int nt)
 {
-    if (nt == 1) return {matvec_kernel<1, R, 16, 1>, 16, 1};
-    if (nt == 2) return {matvec_kernel<2, R, 16, 1>, 16, 1};
-    return {matvec_kernel<4, R, 16, 1>, 16, 1};
+    return nt == 1 ? matvec_kernel<1, R> : (nt == 2 ? matvec_kernel<2, R> : matvec_kernel<4, R>);
 }
 
 }  // namespace
@@ -390,40 +384,39 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
     const int most = 32 / (a.planes * r);
     const int64_t tiles = (N + 15) / 16, all = (K + 511) / 512;
     int64_t passes = (M + most - 1) / most;
-    MvPlan p;
+    MvKernel kernel;
     size_t smem;
     for (;; passes *= 2) {
         a.mt = (int)((M + passes - 1) / passes);
         const int cols = a.mt * a.planes * r, nt = cols <= 8 ? 1 : (cols <= 16 ? 2 : 4);
-        p = r == 1 ? mv_plan<1>(nt) : (r == 2 ? mv_plan<2>(nt) : mv_plan<4>(nt));
+        kernel = r == 1 ? mv_kernel<1>(nt) : (r == 2 ? mv_kernel<2>(nt) : mv_kernel<4>(nt));
         a.zrow = r > 1 || cols < 8 * nt;
-        const bool spread = K >= 4096 && N <= K && a.mt * a.planes >= 4 && tiles <= p.warps * sms / (4 * passes);
+        const bool spread = K >= 4096 && N <= K && a.mt * a.planes >= 4 && tiles <= kMvWarps * sms / (4 * passes);
         for (a.split = spread ? 4 : 1;; a.split *= 2) {
             a.kc = (int)((all + a.split - 1) / a.split) * 512;
-            const size_t sums = mv_sums(cols, p.warps);
+            const size_t sums = mv_sums(cols);
             smem = mv_x_bytes(a.mt * a.planes + a.zrow, a.kc, nt) + sums;
             a.hold = 1;
             while (a.hold < 4 && (a.hold + 1) * sums <= 16 * 1024) a.hold++;
             smem += (a.hold - 1) * sums;
-            if (a.split == 8 || smem <= kMvSmem / p.blocks) break;
+            if (a.split == 8 || smem <= kMvSmem) break;
         }
         if (smem <= kMvSmem || a.mt == 1) break;
     }
     passes = (M + a.mt - 1) / a.mt;
-    const int64_t at_once = std::max<int64_t>(1, p.blocks * sms / (a.split * std::min<int64_t>(passes, sms)));   // blocks of a pass on the SMs
+    const int64_t at_once = std::max<int64_t>(1, sms / (a.split * std::min<int64_t>(passes, sms)));   // blocks of a pass on the SMs
     // Warps along a row: as few rounds as possible of tiles of so many slices,
     // each with a quarter slice's worth of work besides.
     const int64_t slices = a.kc / kSlice;
     double best = 0.0;
     a.wk = 0;
-    for (int wk = 1; wk <= p.warps; wk *= 2) {
-        if (wk > slices || p.warps % wk || p.warps / wk > 16) continue;
-        const int64_t wn = p.warps / wk, rounds = (tiles + wn * at_once - 1) / (wn * at_once);
+    for (int wk = 1; wk <= kMvWarps && wk <= slices; wk *= 2) {
+        const int64_t wn = kMvWarps / wk, rounds = (tiles + wn * at_once - 1) / (wn * at_once);
         const double cost = (double)rounds * ((double)((slices + wk - 1) / wk) + 0.25);
         if (!a.wk || cost < best) { best = cost; a.wk = wk; }
     }
-    const int64_t want = (tiles + p.warps / a.wk - 1) / (p.warps / a.wk), cap = at_once;
-    if (smem > 47 * 1024) e = cudaFuncSetAttribute(p.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
+    const int64_t want = (tiles + kMvWarps / a.wk - 1) / (kMvWarps / a.wk), cap = at_once;
+    if (smem > 47 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMvSmem);
     if (e != cudaSuccess) return e;
     for (int64_t p0 = 0; p0 < passes; p0 += 65535) {    // grid.z holds 65535 passes
         const int64_t np = passes - p0 < 65535 ? passes - p0 : 65535;
@@ -438,7 +431,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(want < cap ? want : cap), (unsigned)a.split, (unsigned)np);
-        cfg.blockDim = dim3((unsigned)p.warps * 32);
+        cfg.blockDim = dim3(kMvThreads);
         cfg.dynamicSmemBytes = smem;
         cfg.stream = st;
         cudaLaunchAttribute attr[2];
@@ -450,7 +443,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
         attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr;
         cfg.numAttrs = a.split > 1 ? 2 : 1;
-        e = cudaLaunchKernelEx(&cfg, p.kernel, b);
+        e = cudaLaunchKernelEx(&cfg, kernel, b);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

@@ -62,7 +62,6 @@ inline bool plan_matvec_tc(int64_t M, int64_t N, int64_t K, int planes, int r, i
     if (columns <= 32 && !(r == 1 && columns > 20)) return false;
     const int64_t tiles = (N + 127) / 128;
     const int64_t kc = (K + 511) / 512 * 512;   // steps in fours
-    if (kc > 16384) return false;
     p.kc = (int)kc;
     // 32 columns where the rows need them and x then fits, else 16.  At least
     // four slots of A: the decoding warps of step c know from their last step,
@@ -79,7 +78,7 @@ inline bool plan_matvec_tc(int64_t M, int64_t N, int64_t K, int planes, int r, i
         }
         if (p.stages >= 2 || p.nc == 16) break;
     }
-    if (p.stages < 2) return false;
+    if (p.stages < 2) return false;             // K above 5120: x leaves no room for two stages
     p.mt = (int)std::min<int64_t>(M, p.nc / planes);
     p.passes = (M + p.mt - 1) / p.mt;
     if (p.passes > 65535) return false;

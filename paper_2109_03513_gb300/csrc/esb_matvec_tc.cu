@@ -12,7 +12,10 @@
 // into fp32 registers.  Instructions bound it, about 29 a word of which 13
 // decode: 65536 x 4096 with 32 rows of bf16 takes 103 us in groups of 128
 // (133 by the other kernel) and 216 in groups of 32 (302), with 16 rows 65
-// and 132 (63 and 159), with 4 rows 55 and 108 (45 and 61).
+// and 132 (63 and 159), with 4 rows 55 and 108 (45 and 61).  It takes calls of
+// more columns than the other kernel's one pass (esb_matvec_plan.h), where x
+// leaves shared memory for two code stages (K to 5120) and the matrix has tiles
+// for four SMs of five.
 //
 // Roles of a block (one on an SM, tiles of 128 matrix rows in turn): warps
 // 0..15 decode, steps of 128 codes c to the four warps c % 4; 16..23 scale,

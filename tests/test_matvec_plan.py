@@ -73,6 +73,7 @@ def test_rings_of_stages_tell_their_uses_apart(shim):
                     p = plan(shim, M, 65536, K, planes, r)
                     if p is None:
                         continue
+                    assert K <= 5120
                     seen.add((p["stages"], p["na"], bool(p["slot_first"])))
                     assert p["kc"] >= K and p["kc"] % 512 == 0 and p["mt"] * planes <= p["nc"] and p["mt"] * p["passes"] >= M
                     assert p["smem"] <= 225 * 1024 and p["na"] * 64 + p["nd"] * r * p["nc"] <= 512
