@@ -601,7 +601,9 @@ esb_status esb_avgpool_nhwc(const uint32_t* X, int64_t ldx, esb_format f,
  * Rows are row-major with a stride in elements (last dimension contiguous,
  * any alignment; rows that start on 16-byte boundaries are read and written
  * by wide accesses).  `*_type` names an element type; sums, statistics and
- * norms are held in fp32, and a result is rounded once, to its output type. */
+ * norms are held in fp32, and a result is rounded once, to its output type.
+ * Where rows or cols is 0 a call that is not refused writes nothing (but
+ * esb_rmsnorm_backward a dweight of zeros). */
 enum { ESB_F32 = 0, ESB_F16 = 1, ESB_BF16 = 2, ESB_CODES = 3 };
 
 /* A matrix of packed codes with a scale for each `group` consecutive values
@@ -655,8 +657,12 @@ esb_status esb_project_groups(const void* x, int32_t x_type, int64_t rows, int64
  *         one with its last code, whatever ld is
  *   bias  [device] N floats or NULL
  *   y     [device] M x N values of y_type, row stride ldy
- * Any M; the matrix is read once for every few rows, so many rows (a prompt)
- * belong to esb_gemm.  K < 2^18, N <= 2^30.
+ * Products are of fp16 numbers, sums fp32: codes, fp16 and bf16 rows take
+ * part as they are (bf16: but for bits below 2^-39 of the largest of the up to
+ * 128 values around), fp32 rows with 22 significant bits.
+ * Any M, but made for few: the matrix is decoded again for every 8 to 32
+ * rows, so a prompt's many rows take that many times as long.  (esb_gemm does
+ * not take group scales.)  K < 2^18, N <= 2^30.
  * Errors: INVALID_ARG, UNSUPPORTED (formats, groups), RANGE (K, N),
  * ALIGN, CUDA. */
 esb_status esb_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x, int32_t x_type, int64_t ldx,
@@ -731,7 +737,8 @@ esb_status esb_rmsnorm_backward(int64_t rows, int64_t cols, const esb_norm_grad*
  * A logit of -inf is a masked token (p = 0).  A row with no other logit has
  * lse = logp = -inf and entropy 0; NaN or +inf in a row makes its numbers NaN.
  * An id outside 0 .. cols - 1 (a negative label of a position without one)
- * has logp 0.
+ * has logp 0.  Exponentials are the hardware's: e^-d of a difference d to the
+ * row's largest logit is off by some 2 + 1.2 d units in the last place.
  *   ids       [device] rows int64, or NULL with logp NULL
  *   logp, entropy, lse [device] rows floats, each may be NULL
  *   top_logp, top_ids  [device] rows x top; where a row has fewer logits

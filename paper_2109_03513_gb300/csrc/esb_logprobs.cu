@@ -62,6 +62,10 @@ __device__ __forceinline__ float key_value(Key k)
 }
 
 // e^x for x <= 0 (and NaN): the hardware's 2^y with results below 2^-126 as 0.
+// y is rounded, so the result is off by some 2 + 1.2 |x| units in the last
+// place: far terms, whose share of a sum is e^x, have the large errors.  A
+// more exact e^x would take several more of the instructions that bound the
+// pass.
 __device__ __forceinline__ float exp_of(float x)
 {
     float r;

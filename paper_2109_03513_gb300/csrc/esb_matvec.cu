@@ -1,25 +1,27 @@
 // esb_matvec.cu -- few rows times a matrix of 4-bit ESB codes with group
 // scales: y[m][n] = bias[n] + sum_g s[n][g] sum_{k in g} q(W[n][k]) x[m][k].
 //
-// The matrix is read once for every 8 to 32 rows, so HBM bounds the call: at
+// The matrix is read once for every 8 to 32 rows, so HBM sets the floor: at
 // the measured copy rate an SM receives about 43 codes a clock, which leaves
 // some 20 instruction slots of its lanes for a word of 8 codes.  A
 // multiply-add per code and row does not fit into that; the warp-level matrix
 // instruction (m16n8k16, fp16 in, fp32 sums) takes a decoded word of two
 // matrix rows for 8 rows of x at once, so the code is the operand with the 16
 // rows and decoding it is the work: 13 instructions a word, and 11 issue
-// cycles for each matrix instruction.  65536 x 4096 in groups of 128 takes 40
-// us with one row of bf16 (21 at the copy rate), 46 with 8 and 62 with 16;
-// 4096 x 4096 with one row 7 us, launch and latencies.  For more columns
+// cycles for each matrix instruction.  No pipe is full (1 x 65536 x 4096: issue
+// 48%, ALU 55%, tensor 18%): a warp decodes and multiplies in turn, and 16 warps
+// on an SM do not hide the one behind the other.  65536 x 4096 in groups of 128
+// takes 40 us with one row of bf16 (21 at the copy rate), 46 with 8 and 62 with
+// 16; 4096 x 4096 with one row 7 us, launch and latencies.  For more columns
 // esb_matvec_tc.cu has the products on tcgen05, whose operand has to go
 // through tensor memory first.
 //
 // fp16 holds both operands exactly.  Every element of a 4-bit set is a
 // number with at most 2 fraction bits, so its fp16 high byte is a table entry
 // (8 bytes in two registers: one byte permutation looks four codes up) and
-// its low byte is 0.  Rows of x are scaled by a power of two for every 128
-// values (64, 32 where groups are that short), so that the largest lies in
-// [2^14, 2^15): bf16's 8 bits fit, and a value loses bits only below 2^-39 of
+// its low byte is 0.  fp16 rows of x are taken as they are; bf16 and fp32 rows
+// are scaled by a power of two for every 128 values (64, 32 where groups are
+// that short), so that the largest lies in [2^14, 2^15): bf16's 8 bits fit, and a value loses bits only below 2^-39 of
 // the largest.  fp32 rows become two such planes (11 bits each, 2^-22 of the
 // value remains); 8-bit codes are exact and bring their own scales.
 //
