@@ -155,11 +155,11 @@ __global__ void __launch_bounds__(kMvThreads, 1) matvec_kernel(const MvArgs a)
         }
     };
     auto load_step = [&](int c) {
-        if (p_k + kSlice <= a.row_codes) {
+        if (p_k + kSlice <= (int)a.row_codes) {
             buf[c][0] = ldg_stream(pw[0] + c * 16);
             buf[c][1] = ldg_stream(pw[1] + c * 16);
         } else {
-            const int o = mv_end_words(p_k, t, c, a.row_codes);
+            const int o = mv_end_words(p_k, t, c, (int)a.row_codes);
             buf[c][0] = ldg_stream(pw[0] + o);
             buf[c][1] = ldg_stream(pw[1] + o);
         }
@@ -368,7 +368,7 @@ cudaError_t launch_matvec_groups(int64_t M, int64_t N, int64_t K, const void* x,
     a.tab.by4 = 1u << 4;
     const int r = a.w.group % 128 == 0 ? 1 : (a.w.group % 64 == 0 ? 2 : 4);
     a.planes = x_type == ESB_F32 ? 2 : 1;
-    a.row_codes = (int)mv_row_codes(K);
+    a.row_codes = mv_row_codes(K);
 
     cudaError_t e = cudaSuccess;
     if (launch_matvec_tc(a, r, st, &e)) return e;

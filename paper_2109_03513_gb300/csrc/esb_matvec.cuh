@@ -32,7 +32,7 @@ struct MvArgs {
     int mt, planes;                 // rows of x in a block, planes of each
     int kc;                         // codes of a row in a block (a multiple of 512)
     int zrow;                       // whether some lanes read zeros in place of x
-    int row_codes;                  // codes of a row of the matrix that are read (mv_row_codes)
+    int64_t row_codes;              // codes of a row of the matrix that are read (mv_row_codes)
     int wk;                         // warps along a row (the others take other tiles)
     int split;                      // blocks along a row (a cluster)
     int hold;                       // tiles whose sums wait for one barrier
