@@ -760,6 +760,162 @@ esb_status esb_logprobs_backward(const void* x, int32_t x_type, int64_t rows, in
                                  const int64_t* ids, const float* lse, const float* entropy, const float* dlogp,
                                  const float* dentropy, void* dx, int64_t lddx, void* stream);
 
+/* ------------------------------------------- a decoder's attention
+ *
+ * What stands between the products of a decoder's layer: norms of the heads
+ * of queries and keys with the position rotation, a paged cache of keys and
+ * values in 4-bit ESB codes, and attention over it.  No paper counterpart but
+ * the projection (Sec. III-C) of cached rows and its scales (absmax, or
+ * Sec. III-D with a head's values as the tensor).
+ *
+ * Queries, keys and values are rows of one token each, a head's values
+ * consecutive, heads one after the other; rows have a stride in elements (so
+ * they may be parts of one projection's rows). */
+
+/* Rotation of the first `dim` values of a head in pairs (i, i + dim/2), or
+ * (2 i, 2 i + 1) if interleaved: (a, b) -> (a c - b s, b c + a s). */
+typedef struct esb_rotation {
+    const float* table;        /* [device] positions rows of dim floats, stride ld: cos of the dim/2 angles, then their sines */
+    int64_t positions, ld;
+    int32_t dim;               /* even, at most the head's values; 0: no rotation */
+    int32_t interleaved;
+} esb_rotation;
+/* A position outside 0 .. positions - 1 gives NaN. */
+
+/* Root-mean-square norm of every head of queries and keys, then the rotation:
+ *   rstd = 1 / sqrt(mean(x^2) + eps) over a head,  y = R(position) (x rstd weight)
+ * in fp32, rounded once.  y may lie on x with the same stride. */
+typedef struct esb_heads {
+    const void* x;             /* [device] tokens x (heads * head_dim) of x_type */
+    int64_t ldx;
+    void* y;                   /* [device] the same of x_type */
+    int64_t ldy;
+    const void* weight;        /* [device] head_dim values of w_type, or NULL: ones */
+    float* rstd;               /* [device] tokens x heads, or NULL */
+    int32_t heads;             /* 0: there is no such tensor */
+} esb_heads;
+typedef struct esb_head_norm {
+    esb_heads part[2];         /* queries and keys, each with a weight of its own */
+    const int64_t* positions;  /* [device] tokens (with rotation) */
+    esb_rotation rotation;
+    int32_t head_dim;          /* a multiple of 8, 8 .. 256 */
+    int32_t x_type, w_type;
+    float eps;                 /* >= 0, finite */
+} esb_head_norm;
+/* Errors: INVALID_ARG, UNSUPPORTED (head_dim, rotation's dim), RANGE (tokens or
+ * heads of 2^31 and more), ALIGN, CUDA. */
+esb_status esb_headnorm(int64_t tokens, const esb_head_norm* a, void* stream);
+
+/* Its gradient, from x and rstd of the forward pass: with g the rotation of dy
+ * back, e = g weight and n = x rstd of a head,
+ *   dx = rstd (e - n mean(e n)),  dweight = sum over tokens and heads of g n
+ * Every sum has a fixed order.  dx may lie on dy or x with the same stride. */
+typedef struct esb_heads_grad {
+    const void* dy;            /* [device] tokens x (heads * head_dim) of x_type */
+    int64_t ldg;
+    const void* x;             /* [device] the same */
+    int64_t ldx;
+    const float* rstd;         /* [device] tokens x heads */
+    const void* weight;        /* [device] head_dim of w_type, or NULL: ones */
+    void* dx;                  /* [device] the same */
+    int64_t lddx;
+    float* dweight;            /* [device] head_dim floats, or NULL */
+    int32_t heads;
+} esb_heads_grad;
+typedef struct esb_head_norm_grad {
+    esb_heads_grad part[2];
+    const int64_t* positions;
+    esb_rotation rotation;
+    int32_t head_dim, x_type, w_type;
+} esb_head_norm_grad;
+/*   workspace  [device] >= esb_headnorm_backward_workspace_bytes(tokens,
+ *              heads of both, head_dim) bytes, 16-byte aligned (with a
+ *              dweight; else it may be NULL)
+ * Errors: as esb_headnorm. */
+size_t esb_headnorm_backward_workspace_bytes(int64_t tokens, int64_t heads, int32_t head_dim);
+esb_status esb_headnorm_backward(int64_t tokens, const esb_head_norm_grad* a, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A cache of keys and values in pages of page_size places: codes of a place
+ * and head are esb_row_words(head_dim, 4) words (a head's values in order, 8 a
+ * word, the rest the zero code), with one scale:
+ *   value = scale q(code),  b = 4, signed, 0 <= k <= 3
+ * A page is `heads` times page_size rows of words, then the next head; pages
+ * are page_ld words (a multiple of 4) and page_lds scales apart. */
+typedef struct esb_kv_cache {
+    uint32_t *k_codes, *v_codes;   /* [device] 16-byte aligned */
+    float *k_scales, *v_scales;    /* [device] pages of heads x page_size floats */
+    int64_t pages, page_ld, page_lds;
+    int32_t heads, page_size, head_dim;   /* page_size a multiple of 16, head_dim a multiple of 8, 8 .. 256 */
+    esb_format k_fmt, v_fmt;
+} esb_kv_cache;
+
+/* Keys (rotated by their positions) and values of new tokens into the cache.
+ * A rotated key is rounded once to fp32; then scale and codes are those of
+ * esb_project_groups with the head's values as the group (zeros, NaN and
+ * infinities as there; a NaN or infinity among rotated values makes the scale
+ * not finite).
+ *   slots      [device] tokens: page * page_size + place; a token whose slot is
+ *              negative or past the cache is left out.  Slots of the other tokens
+ *              are different: where two are the same, the row is either token's, or
+ *              parts of both.
+ *   positions  [device] tokens (with rotation)
+ *   rotation   [host] or NULL
+ *   kq, vq     [device] the numbers the codes stand for, tokens x (heads *
+ *              head_dim) of q_type, or NULL; rows of tokens left out are not written
+ * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes), RANGE, ALIGN, CUDA. */
+typedef struct esb_append {
+    const void *k, *v;         /* [device] tokens x (heads * head_dim) of x_type */
+    int64_t ldk, ldv;
+    const int64_t *slots, *positions;
+    const esb_rotation* rotation;
+    void *kq, *vq;
+    int64_t ldkq, ldvq;
+    int32_t x_type, q_type, rule, rounding;
+} esb_append;
+esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb_append* a, void* stream);
+
+/* Attention of queries over the cache of their sequences:
+ *   out = sum_p v_p exp(scale q.k_p) / sum_p exp(scale q.k_p)
+ * over the places p <= t, and p > t - window where window > 0, with t the
+ * query's place: the last of a sequence's queries has place lens - 1, the one
+ * before it lens - 2 and so on.  Queries are rotated by their places first.
+ * Query head h reads the cache's head h / (q_heads / heads).
+ *   starts   [device] seqs + 1: the queries of sequence i are rows starts[i]
+ *            .. starts[i + 1] - 1; or NULL: one each.  Rows of no sequence are
+ *            not written.
+ *   lens     [device] seqs: places in use, the queries' own among them (they
+ *            are appended before)
+ *   pages    [device] seqs rows of max_pages page numbers, stride ld_pages; places
+ *            past them, and on pages outside 0 .. pages - 1, are not seen
+ *   lse      [device] tokens x q_heads: log sum exp(scale q.k), or NULL
+ * A query that sees no place has out 0 and lse -inf.  A NaN among what a query
+ * sees makes its numbers NaN; what it does not see has no effect, whatever it is.
+ * Products are of fp16 numbers, sums fp32: codes take part as they are; queries
+ * and weights (probabilities times a value's scale) with 11 significant bits
+ * where queries are bf16, else with 22.  v's scales are exact between 2^-100 and
+ * 2^100.
+ *   workspace  [device] >= esb_cache_attention_workspace_bytes bytes, 16-byte
+ *              aligned; nothing is kept in it between calls
+ * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes, q_heads not a multiple of
+ * heads), RANGE, ALIGN, CUDA. */
+typedef struct esb_attention {
+    const void* q;             /* [device] tokens x (q_heads * head_dim) of q_type */
+    int64_t ldq;
+    void* out;                 /* [device] the same of out_type */
+    int64_t ldo;
+    float* lse;
+    const int32_t *starts, *lens, *pages;
+    int64_t ld_pages;
+    const esb_rotation* rotation;   /* [host] or NULL */
+    int32_t seqs, max_pages, q_heads, window;
+    int32_t q_type, out_type;
+    float scale;
+} esb_attention;
+size_t esb_cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t q_heads, int32_t heads, int32_t head_dim,
+                                           int32_t q_type);
+esb_status esb_cache_attention(int64_t tokens, const esb_kv_cache* cache, const esb_attention* a, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* ----------------------------------------------------- peak measurement */
 
 /* Microbenchmarks of the tensor-pipe rates the contraction's roofline is

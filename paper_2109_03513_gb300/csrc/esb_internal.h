@@ -121,6 +121,17 @@ cudaError_t launch_logprobs_grad(const void* x, int type, int64_t rows, int64_t 
                                  const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dx,
                                  int64_t lddx, cudaStream_t st);
 
+// A decoder's attention: norms of heads with rotation (esb_headnorm.cu),
+// appending to a 4-bit cache (esb_cache.cu), attention over it
+// (esb_attention.cu).
+cudaError_t launch_headnorm(int64_t tokens, const esb_head_norm& a, cudaStream_t st);
+size_t headnorm_grad_workspace_bytes(int64_t tokens, int64_t heads, int head_dim);
+cudaError_t launch_headnorm_grad(int64_t tokens, const esb_head_norm_grad& a, void* workspace, cudaStream_t st);
+cudaError_t launch_cache_append(int64_t tokens, const esb_kv_cache& c, const esb_append& a, double alpha_star_k, double alpha_star_v,
+                                cudaStream_t st);
+size_t attention_workspace_bytes(int64_t tokens, int64_t seqs, int q_heads, int heads, int head_dim, int q_type);
+cudaError_t launch_attention(int64_t tokens, const esb_kv_cache& c, const esb_attention& a, void* workspace, cudaStream_t st);
+
 // Tensor-pipe peak microbenchmarks (esb_peak.cu): kind 0 tcgen05 f8f6f4,
 // kind 1 mma.sync s8; *flops receives the operations of the launch.
 cudaError_t launch_peak(int kind, int64_t iters, int64_t* flops, cudaStream_t st);

@@ -3,6 +3,7 @@
 // contracts are in include/esb.h.
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include <cuda_runtime.h>
 
@@ -22,6 +23,29 @@ int64_t words_of(int64_t cols, int b) { return (cols + 32 / b - 1) / (32 / b); }
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 // Rows of a type start on that type's boundary.
 bool typed(const void* p, int32_t t) { return aligned(p, t == ESB_F32 ? 4 : 2); }
+bool head_ok(int32_t d) { return d >= 8 && d <= 256 && d % 8 == 0; }
+// A rotation that there may be (`used`: for tokens with these positions).
+esb_status rotation_ok(const esb_rotation* r, int32_t head_dim, bool used, const int64_t* positions)
+{
+    if (!r || r->dim == 0) return ESB_OK;
+    if (r->dim < 0 || r->dim % 2 != 0 || r->dim > head_dim) return ESB_ERR_UNSUPPORTED;
+    if (!r->table || r->positions < 0 || r->ld < r->dim || (used && !positions)) return ESB_ERR_INVALID_ARG;
+    return aligned(r->table, 4) && aligned(positions, 8) ? ESB_OK : ESB_ERR_ALIGN;
+}
+esb_status cache_ok(const esb_kv_cache* c)
+{
+    if (!c) return ESB_ERR_INVALID_ARG;
+    for (const esb_format& f : {c->k_fmt, c->v_fmt})
+        if (esb_format_check(f) != ESB_OK || f.b != 4 || !f.is_signed) return ESB_ERR_UNSUPPORTED;
+    if (!head_ok(c->head_dim) || c->page_size <= 0 || c->page_size % 16 != 0) return ESB_ERR_UNSUPPORTED;
+    if (c->pages < 0 || c->heads <= 0) return ESB_ERR_INVALID_ARG;
+    if (c->heads >= 1 << 23 || c->page_size > 1 << 30 || c->pages > 1ll << 31) return ESB_ERR_RANGE;
+    const int64_t rows = (int64_t)c->heads * c->page_size;
+    if (c->pages > 0 && (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales)) return ESB_ERR_INVALID_ARG;
+    if (c->pages > 1 && (c->page_ld < rows * esb_row_words(c->head_dim, 4) || c->page_lds < rows)) return ESB_ERR_INVALID_ARG;
+    return aligned(c->k_codes, 16) && aligned(c->v_codes, 16) && (c->pages <= 1 || c->page_ld % 4 == 0) && aligned(c->k_scales, 4) &&
+                   aligned(c->v_scales, 4) ? ESB_OK : ESB_ERR_ALIGN;
+}
 esb_status done(cudaError_t e) { return e == cudaSuccess ? ESB_OK : ESB_ERR_CUDA; }
 
 }  // namespace
@@ -148,6 +172,131 @@ esb_status esb_logprobs_backward(const void* x, int32_t x_type, int64_t rows, in
         return ESB_ERR_ALIGN;
     return done(launch_logprobs_grad(x, x_type, rows, cols, ldx, ids, lse, entropy, dlogp, dentropy, dx, lddx,
                                      static_cast<cudaStream_t>(stream)));
+}
+
+esb_status esb_headnorm(int64_t tokens, const esb_head_norm* a, void* stream)
+{
+    if (!a || tokens < 0 || !(std::isfinite(a->eps) && a->eps >= 0.0f) || !type_ok(a->x_type)) return ESB_ERR_INVALID_ARG;
+    if (!head_ok(a->head_dim)) return ESB_ERR_UNSUPPORTED;
+    if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
+    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens > 0, a->positions);
+    if (r != ESB_OK) return r;
+    int64_t heads = 0;
+    for (const esb_heads& h : a->part) {
+        if (h.heads < 0) return ESB_ERR_INVALID_ARG;
+        if (h.heads >= 1 << 23) return ESB_ERR_RANGE;
+        heads += h.heads;
+        if (h.heads == 0 || tokens == 0) continue;
+        const int64_t cols = (int64_t)h.heads * a->head_dim;
+        if (!h.x || !h.y || h.ldx < cols || h.ldy < cols || (h.weight && !type_ok(a->w_type))) return ESB_ERR_INVALID_ARG;
+        if (!typed(h.x, a->x_type) || !typed(h.y, a->x_type) || !aligned(h.rstd, 4) || (h.weight && !typed(h.weight, a->w_type)))
+            return ESB_ERR_ALIGN;
+    }
+    if (tokens == 0 || heads == 0) return ESB_OK;
+    return done(launch_headnorm(tokens, *a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t esb_headnorm_backward_workspace_bytes(int64_t tokens, int64_t heads, int32_t head_dim)
+{
+    return tokens > 0 && tokens < 1ll << 31 && heads > 0 && heads < 1 << 24 && head_ok(head_dim)
+               ? headnorm_grad_workspace_bytes(tokens, heads, head_dim) : 0;
+}
+
+esb_status esb_headnorm_backward(int64_t tokens, const esb_head_norm_grad* a, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!a || tokens < 0 || !type_ok(a->x_type)) return ESB_ERR_INVALID_ARG;
+    if (!head_ok(a->head_dim)) return ESB_ERR_UNSUPPORTED;
+    if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
+    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens > 0, a->positions);
+    if (r != ESB_OK) return r;
+    int64_t heads = 0;
+    bool sums = false;
+    for (const esb_heads_grad& h : a->part) {
+        if (h.heads < 0) return ESB_ERR_INVALID_ARG;
+        if (h.heads >= 1 << 23) return ESB_ERR_RANGE;
+        heads += h.heads;
+        if (!aligned(h.dweight, 4)) return ESB_ERR_ALIGN;
+        sums = sums || h.dweight;
+        if (h.heads == 0 || tokens == 0) continue;
+        const int64_t cols = (int64_t)h.heads * a->head_dim;
+        if (!h.x || !h.dy || !h.dx || !h.rstd || h.ldx < cols || h.ldg < cols || h.lddx < cols || (h.weight && !type_ok(a->w_type)))
+            return ESB_ERR_INVALID_ARG;
+        if (!typed(h.x, a->x_type) || !typed(h.dy, a->x_type) || !typed(h.dx, a->x_type) || !aligned(h.rstd, 4) ||
+            (h.weight && !typed(h.weight, a->w_type)))
+            return ESB_ERR_ALIGN;
+    }
+    if (tokens == 0 || heads == 0) {    // nothing adds to the weights' gradients
+        for (const esb_heads_grad& h : a->part)
+            if (h.dweight) {
+                const cudaError_t e = cudaMemsetAsync(h.dweight, 0, sizeof(float) * (size_t)a->head_dim, static_cast<cudaStream_t>(stream));
+                if (e != cudaSuccess) return ESB_ERR_CUDA;
+            }
+        return ESB_OK;
+    }
+    if (sums) {
+        if (!workspace || workspace_bytes < headnorm_grad_workspace_bytes(tokens, heads, a->head_dim)) return ESB_ERR_INVALID_ARG;
+        if (!aligned(workspace, 16)) return ESB_ERR_ALIGN;
+    }
+    return done(launch_headnorm_grad(tokens, *a, workspace, static_cast<cudaStream_t>(stream)));
+}
+
+esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* c, const esb_append* a, void* stream)
+{
+    if (!a || tokens < 0 || !type_ok(a->x_type) || ((a->kq || a->vq) && !type_ok(a->q_type)) || !rounding_ok(a->rounding) ||
+        (a->rule != ESB_SCALE_ABSMAX && a->rule != ESB_SCALE_DDA))
+        return ESB_ERR_INVALID_ARG;
+    esb_status r = cache_ok(c);
+    if (r != ESB_OK) return r;
+    if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
+    r = rotation_ok(a->rotation, c->head_dim, tokens > 0, a->positions);
+    if (r != ESB_OK) return r;
+    if (tokens == 0) return ESB_OK;
+    const int64_t cols = (int64_t)c->heads * c->head_dim;
+    if (!a->k || !a->v || !a->slots || a->ldk < cols || a->ldv < cols || (a->kq && a->ldkq < cols) || (a->vq && a->ldvq < cols))
+        return ESB_ERR_INVALID_ARG;
+    if (!typed(a->k, a->x_type) || !typed(a->v, a->x_type) || !aligned(a->slots, 8) || (a->kq && !typed(a->kq, a->q_type)) ||
+        (a->vq && !typed(a->vq, a->q_type)))
+        return ESB_ERR_ALIGN;
+    double sk = 0.0, sv = 0.0;
+    if (a->rule == ESB_SCALE_DDA) {
+        r = esb_alpha_star(4, c->k_fmt.k, &sk, nullptr);
+        if (r == ESB_OK) r = esb_alpha_star(4, c->v_fmt.k, &sv, nullptr);
+        if (r != ESB_OK) return r;
+    }
+    return done(launch_cache_append(tokens, *c, *a, sk, sv, static_cast<cudaStream_t>(stream)));
+}
+
+size_t esb_cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t q_type)
+{
+    if (tokens <= 0 || tokens >= 1ll << 31 || seqs <= 0 || heads <= 0 || q_heads <= 0 || q_heads % heads != 0 || !head_ok(head_dim) || !type_ok(q_type))
+        return 0;
+    return attention_workspace_bytes(tokens, seqs, q_heads, heads, head_dim, q_type);
+}
+
+esb_status esb_cache_attention(int64_t tokens, const esb_kv_cache* c, const esb_attention* a, void* workspace, size_t workspace_bytes,
+                               void* stream)
+{
+    if (!a || tokens < 0 || a->seqs < 0 || a->max_pages < 0 || a->window < 0 || !std::isfinite(a->scale) || !type_ok(a->q_type) ||
+        !type_ok(a->out_type))
+        return ESB_ERR_INVALID_ARG;
+    esb_status r = cache_ok(c);
+    if (r != ESB_OK) return r;
+    if (a->q_heads <= 0 || a->q_heads % c->heads != 0) return ESB_ERR_UNSUPPORTED;
+    if (tokens >= 1ll << 31 || a->q_heads >= 1 << 23 || (int64_t)a->max_pages * c->page_size > 1 << 30) return ESB_ERR_RANGE;
+    r = rotation_ok(a->rotation, c->head_dim, false, nullptr);
+    if (r != ESB_OK) return r;
+    if (tokens == 0 || a->seqs == 0) return ESB_OK;
+    const int64_t cols = (int64_t)a->q_heads * c->head_dim;
+    if (!a->q || !a->out || !a->lens || (!a->pages && a->max_pages > 0) || a->ldq < cols || a->ldo < cols || a->ld_pages < a->max_pages ||
+        (!a->starts && tokens != a->seqs))
+        return ESB_ERR_INVALID_ARG;
+    if (!typed(a->q, a->q_type) || !typed(a->out, a->out_type) || !aligned(a->lse, 4) || !aligned(a->starts, 4) || !aligned(a->lens, 4) ||
+        !aligned(a->pages, 4))
+        return ESB_ERR_ALIGN;
+    if (!workspace || workspace_bytes < attention_workspace_bytes(tokens, a->seqs, a->q_heads, c->heads, c->head_dim, a->q_type))
+        return ESB_ERR_INVALID_ARG;
+    if (!aligned(workspace, 16)) return ESB_ERR_ALIGN;
+    return done(launch_attention(tokens, *c, *a, workspace, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

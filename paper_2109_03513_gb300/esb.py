@@ -86,6 +86,54 @@ class esb_norm_grad(ctypes.Structure):
     ]
 
 
+class esb_rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int64), ("ld", ctypes.c_int64), ("dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class esb_heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("rstd", ctypes.c_void_p), ("heads", ctypes.c_int32)]
+
+
+class esb_head_norm(ctypes.Structure):
+    _fields_ = [("part", esb_heads * 2), ("positions", ctypes.c_void_p), ("rotation", esb_rotation), ("head_dim", ctypes.c_int32),
+                ("x_type", ctypes.c_int32), ("w_type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class esb_heads_grad(ctypes.Structure):
+    _fields_ = [("dy", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("rstd", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("lddx", ctypes.c_int64),
+                ("dweight", ctypes.c_void_p), ("heads", ctypes.c_int32)]
+
+
+class esb_head_norm_grad(ctypes.Structure):
+    _fields_ = [("part", esb_heads_grad * 2), ("positions", ctypes.c_void_p), ("rotation", esb_rotation),
+                ("head_dim", ctypes.c_int32), ("x_type", ctypes.c_int32), ("w_type", ctypes.c_int32)]
+
+
+class esb_kv_cache(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_ld", ctypes.c_int64),
+                ("page_lds", ctypes.c_int64), ("heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("k_fmt", esb_format), ("v_fmt", esb_format)]
+
+
+class esb_append(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("rotation", ctypes.c_void_p),
+                ("kq", ctypes.c_void_p), ("vq", ctypes.c_void_p), ("ldkq", ctypes.c_int64), ("ldvq", ctypes.c_int64),
+                ("x_type", ctypes.c_int32), ("q_type", ctypes.c_int32), ("rule", ctypes.c_int32), ("rounding", ctypes.c_int32)]
+
+
+class esb_attention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+                ("ld_pages", ctypes.c_int64), ("rotation", ctypes.c_void_p), ("seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("q_type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 @dataclass(frozen=True)
 class Fmt:
     """ESB format: b total bits, k fraction bits (k+1 significant bits)."""
@@ -149,6 +197,12 @@ SIGNATURES = {
     "esb_logprobs": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _I32, _P, _P, _P, _P, _P, _P]),
     "esb_logprobs_backward": (_I32, [_P, _I32, _I64, _I64, _I64, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "esb_get_status": (_I32, [_P, _P]),
+    "esb_headnorm": (_I32, [_I64, _P, _P]),
+    "esb_headnorm_backward_workspace_bytes": (_SZ, [_I64, _I64, _I32]),
+    "esb_headnorm_backward": (_I32, [_I64, _P, _P, _SZ, _P]),
+    "esb_cache_append": (_I32, [_I64, _P, _P, _P]),
+    "esb_cache_attention_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32, _I32, _I32]),
+    "esb_cache_attention": (_I32, [_I64, _P, _P, _P, _SZ, _P]),
     "esb_peak_launch": (_I32, [_I32, _I64, _P, _P]),
 }
 
@@ -943,6 +997,304 @@ def esb_logprobs_backward(logits: torch.Tensor, ids: Optional[torch.Tensor], lse
     _check(lib().esb_logprobs_backward(logits.data_ptr(), ty, rows, cols, ldx, ip, lp, ep, gp, hp, dlogits.data_ptr(),
                                        ldd, _stream(stream)), "esb_logprobs_backward")
     return dlogits
+
+
+class Rotation(NamedTuple):
+    """The rotation of heads by their positions: table (positions, dim) float32, the cosines of a position's dim / 2
+    angles, then their sines; pairs (i, i + dim / 2), or (2 i, 2 i + 1) if interleaved."""
+    table: torch.Tensor
+    interleaved: bool = False
+
+    def c(self) -> esb_rotation:
+        t = self.table
+        if t.dim() != 2 or t.dtype != torch.float32 or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
+            raise ValueError("rotation.table must be a 2-D CUDA float32 tensor with contiguous rows")
+        return esb_rotation(t.data_ptr(), t.shape[0], t.stride(0) if t.shape[0] > 1 else t.shape[1], t.shape[1], 1 if self.interleaved else 0)
+
+
+def rotation(dim: int, positions: int, base: float = 10000.0, frequencies=None, interleaved: bool = False,
+             device="cuda") -> Rotation:
+    """A Rotation for positions 0 .. positions - 1 with the angles position * base^(-2 i / dim), or position *
+    frequencies[i] (dim / 2 numbers), computed in 64 bits."""
+    if dim <= 0 or dim % 2 or positions <= 0:
+        raise ValueError("dim must be even and positive, positions positive")
+    if frequencies is None:
+        f = base ** (-torch.arange(0, dim, 2, dtype=torch.float64, device=device) / dim)
+    else:
+        f = torch.as_tensor(frequencies, dtype=torch.float64, device=device)
+        if f.shape != (dim // 2,):
+            raise ValueError("frequencies must have dim / 2 numbers")
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * f
+    return Rotation(torch.cat([a.cos(), a.sin()], 1).float(), interleaved)
+
+
+def _turn(rot: Optional[Rotation], positions, tokens: int) -> tuple[esb_rotation, Optional[int]]:
+    """(rotation, address of the tokens' positions)."""
+    if rot is None:
+        return esb_rotation(), None
+    if positions is None:
+        raise ValueError("a rotation needs positions")
+    return rot.c(), _vector(positions, "positions", tokens, torch.int64)
+
+
+def _head_count(t: torch.Tensor, name: str, head_dim: int) -> int:
+    if head_dim <= 0 or t.shape[1] % head_dim:
+        raise ValueError(f"{name} must have whole heads of head_dim values a row")
+    return t.shape[1] // head_dim
+
+
+class HeadNorm(NamedTuple):
+    """What esb_headnorm wrote: queries, keys, and 1 / rms of each token's heads (tokens, heads) (None where not wanted)."""
+    q: Optional[torch.Tensor]
+    k: Optional[torch.Tensor]
+    q_rstd: Optional[torch.Tensor]
+    k_rstd: Optional[torch.Tensor]
+
+
+def esb_headnorm(q: Optional[torch.Tensor], k: Optional[torch.Tensor], head_dim: int,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 rotation: Optional[Rotation] = None, positions: Optional[torch.Tensor] = None,
+                 qy: Optional[torch.Tensor] = None, ky: Optional[torch.Tensor] = None, want_rstd: bool = False,
+                 stream=None) -> HeadNorm:
+    """RMS norm of every head of queries and keys (tokens, heads * head_dim) and the rotation by the tokens' positions
+    (tokens,) int64 -> HeadNorm.  One of q and k may be None; qy, ky may be q, k."""
+    x0 = q if q is not None else k
+    if x0 is None:
+        raise ValueError("q or k must be given")
+    empty = _empty_on(stream)
+    a = esb_head_norm()
+    a.head_dim, a.eps = head_dim, eps
+    tokens, dtype = x0.shape[0], x0.dtype
+    outs, stats = [], []
+    wt = None
+    for part, name, x, w, y in ((a.part[0], "q", q, q_weight, qy), (a.part[1], "k", k, k_weight, ky)):
+        if x is None:
+            outs.append(None)
+            stats.append(None)
+            continue
+        a.x_type, part.ldx = _rows(x, name)
+        if x.shape[0] != tokens or x.dtype != dtype:
+            raise ValueError("q and k must have the same tokens and type")
+        part.x, part.heads = x.data_ptr(), _head_count(x, name, head_dim)
+        if w is not None:
+            part.weight, a.w_type = _weight(w, head_dim)
+            if wt is not None and wt != w.dtype:
+                raise ValueError("q_weight and k_weight must have one type")
+            wt = w.dtype
+        if y is None:
+            y = empty(x.shape, dtype=dtype, device=x.device)
+        part.ldy = _rows_like(y, name + "y", x.shape, dtype)
+        part.y = y.data_ptr()
+        outs.append(y)
+        r = None
+        if want_rstd:
+            r = empty((tokens, part.heads), dtype=torch.float32, device=x.device)
+            part.rstd = r.data_ptr()
+        stats.append(r)
+    a.rotation, a.positions = _turn(rotation, positions, tokens)
+    _check(lib().esb_headnorm(tokens, ctypes.byref(a), _stream(stream)), "esb_headnorm")
+    return HeadNorm(*outs, *stats)
+
+
+class HeadNormGrad(NamedTuple):
+    """Gradients of esb_headnorm: of queries and keys, and fp32 ones of their weights (None where not wanted)."""
+    dq: Optional[torch.Tensor]
+    dk: Optional[torch.Tensor]
+    dq_weight: Optional[torch.Tensor]
+    dk_weight: Optional[torch.Tensor]
+
+
+def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor], q: Optional[torch.Tensor],
+                          k: Optional[torch.Tensor], head_dim: int, q_weight: Optional[torch.Tensor],
+                          k_weight: Optional[torch.Tensor], q_rstd: Optional[torch.Tensor], k_rstd: Optional[torch.Tensor],
+                          rotation: Optional[Rotation] = None, positions: Optional[torch.Tensor] = None,
+                          dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> HeadNormGrad:
+    """Gradient of esb_headnorm from gq, gk (of its queries and keys), its inputs and its rstd -> HeadNormGrad.  A
+    weight's gradient is computed where there is the weight."""
+    x0 = q if q is not None else k
+    if x0 is None:
+        raise ValueError("q or k must be given")
+    empty = _empty_on(stream)
+    a = esb_head_norm_grad()
+    a.head_dim = head_dim
+    tokens, dtype = x0.shape[0], x0.dtype
+    outs, sums = [], []
+    heads, wt = 0, None
+    for part, name, x, g, w, r, d in ((a.part[0], "q", q, gq, q_weight, q_rstd, dq), (a.part[1], "k", k, gk, k_weight, k_rstd, dk)):
+        if x is None:
+            outs.append(None)
+            sums.append(None)
+            continue
+        a.x_type, part.ldx = _rows(x, name)
+        if x.shape[0] != tokens or x.dtype != dtype:
+            raise ValueError("q and k must have the same tokens and type")
+        if g is None or r is None:
+            raise ValueError(f"g{name} and {name}_rstd must be given")
+        part.x, part.heads = x.data_ptr(), _head_count(x, name, head_dim)
+        heads += part.heads
+        part.ldg = _rows_like(g, "g" + name, x.shape, dtype)
+        part.dy = g.data_ptr()
+        if r.shape != (tokens, part.heads) or not r.is_contiguous():
+            raise ValueError(f"{name}_rstd must be contiguous {(tokens, part.heads)} float32")
+        part.rstd = _vector(r.view(-1), name + "_rstd", tokens * part.heads, torch.float32)
+        dw = None
+        if w is not None:
+            part.weight, a.w_type = _weight(w, head_dim)
+            if wt is not None and wt != w.dtype:
+                raise ValueError("q_weight and k_weight must have one type")
+            wt = w.dtype
+            dw = empty(head_dim, dtype=torch.float32, device=x.device)
+            part.dweight = dw.data_ptr()
+        sums.append(dw)
+        if d is None:
+            d = empty(x.shape, dtype=dtype, device=x.device)
+        part.lddx = _rows_like(d, "d" + name, x.shape, dtype)
+        part.dx = d.data_ptr()
+        outs.append(d)
+    a.rotation, a.positions = _turn(rotation, positions, tokens)
+    wp, nb = None, 0
+    if any(s is not None for s in sums):
+        if workspace is None:
+            nb = int(lib().esb_headnorm_backward_workspace_bytes(tokens, heads, head_dim))
+            workspace = empty(nb, dtype=torch.uint8, device=x0.device)
+        else:
+            _dev(workspace, "workspace")
+            nb = workspace.numel() * workspace.element_size()
+        wp = workspace.data_ptr()
+    _check(lib().esb_headnorm_backward(tokens, ctypes.byref(a), wp, nb, _stream(stream)), "esb_headnorm_backward")
+    return HeadNormGrad(*outs, *sums)
+
+
+class KvCache(NamedTuple):
+    """A paged cache of keys and values in 4-bit ESB codes: codes (pages, heads, page_size, words) int32 with
+    words = esb_row_words(head_dim, 4), scales (pages, heads, page_size) float32.  Pages may lie apart."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    head_dim: int
+    k_fmt: Fmt
+    v_fmt: Fmt
+
+    def c(self) -> esb_kv_cache:
+        shape = self.k_codes.shape
+        if len(shape) != 4 or shape[3] != (self.head_dim + 31) // 32 * 4:
+            raise ValueError("codes must be (pages, heads, page_size, esb_row_words(head_dim, 4))")
+        pages, heads, size, words = shape
+        ld = lds = 0
+        for codes, scales in ((self.k_codes, self.k_scales), (self.v_codes, self.v_scales)):
+            if codes.dtype != torch.int32 or scales.dtype != torch.float32 or not codes.is_cuda or not scales.is_cuda:
+                raise ValueError("codes must be CUDA int32, scales CUDA float32")
+            if codes.shape != shape or scales.shape != shape[:3]:
+                raise ValueError("keys and values must have one shape, scales (pages, heads, page_size)")
+            if pages and not (codes[0].is_contiguous() and scales[0].is_contiguous()):
+                raise ValueError("a page's codes and scales must be contiguous")
+            at = (codes.stride(0), scales.stride(0)) if pages > 1 else (heads * size * words, heads * size)
+            if ld and at != (ld, lds):
+                raise ValueError("keys and values must have pages equally far apart")
+            ld, lds = at
+        return esb_kv_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
+                            pages, ld, lds, heads, size, self.head_dim, self.k_fmt.c(), self.v_fmt.c())
+
+
+def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, k_fmt: Fmt = Fmt(4, 2), v_fmt: Fmt = Fmt(4, 2),
+             device="cuda") -> KvCache:
+    """An empty KvCache (every value 0)."""
+    words = esb_row_words(head_dim, 4)
+    made = [t for _ in range(2) for t in (torch.zeros((pages, heads, page_size, words), dtype=torch.int32, device=device),
+                                          torch.zeros((pages, heads, page_size), dtype=torch.float32, device=device))]
+    return KvCache(*made, head_dim, k_fmt, v_fmt)
+
+
+def esb_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+                     rotation: Optional[Rotation] = None, positions: Optional[torch.Tensor] = None,
+                     rule: int = ESB_SCALE_ABSMAX, rounding: int = ESB_ROUND_HALF_AWAY, kq: Optional[torch.Tensor] = None,
+                     vq: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keys (rotated by their positions) and values (tokens, heads * head_dim) into the cache at slots (tokens,) int64:
+    page * page_size + place, negative ones left out.  Where two slots are equal the row is not defined.  kq, vq: the
+    numbers the codes stand for."""
+    c = cache.c()
+    a = esb_append()
+    tokens = k.shape[0]
+    a.x_type, a.ldk = _rows(k, "k")
+    if k.shape[1] != c.heads * c.head_dim:
+        raise ValueError("k must have the cache's heads")
+    a.ldv = _rows_like(v, "v", k.shape, k.dtype)
+    a.k, a.v, a.slots = k.data_ptr(), v.data_ptr(), _vector(slots, "slots", tokens, torch.int64)
+    a.rule, a.rounding = rule, rounding
+    if kq is not None:
+        a.q_type, a.ldkq = _rows(kq, "kq")
+        a.kq = kq.data_ptr()
+        if kq.shape != k.shape:
+            raise ValueError("kq must have the shape of k")
+    if vq is not None:
+        t, a.ldvq = _rows(vq, "vq")
+        if vq.shape != k.shape or (kq is not None and t != a.q_type):
+            raise ValueError("vq must have the shape of v and the type of kq")
+        a.q_type, a.vq = t, vq.data_ptr()
+    r = None
+    if rotation is not None:
+        r, a.positions = _turn(rotation, positions, tokens)
+        a.rotation = ctypes.addressof(r)
+    _check(lib().esb_cache_append(tokens, ctypes.byref(c), ctypes.byref(a), _stream(stream)), "esb_cache_append")
+
+
+def esb_cache_attention(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, pages: torch.Tensor,
+                        starts: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                        rotation: Optional[Rotation] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+                        want_lse: bool = False, workspace: Optional[torch.Tensor] = None,
+                        stream=None) -> tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Attention of queries (tokens, q_heads * head_dim), rotated by their places, over the cache -> (out, log sum exp
+    (tokens, q_heads) | None).  lens (sequences,) int32: places in use, the queries' own at their end; pages
+    (sequences, most pages) int32; starts (sequences + 1,) int32: each sequence's queries are rows starts[i] .. starts[i
+    + 1] - 1 (None: one each; rows of no sequence are not written).  scale: 1 / sqrt(head_dim) unless given; window: places
+    seen, the query's own among them (0: all)."""
+    c = cache.c()
+    a = esb_attention()
+    empty = _empty_on(stream)
+    a.q_type, a.ldq = _rows(q, "q")
+    tokens, cols = q.shape
+    a.q_heads = _head_count(q, "q", c.head_dim)
+    seqs = lens.shape[0] if lens.dim() == 1 else -1
+    a.q, a.lens, a.seqs = q.data_ptr(), _vector(lens, "lens", seqs, torch.int32), seqs
+    if pages.dtype != torch.int32 or not pages.is_cuda or pages.dim() != 2 or pages.shape[0] != seqs or \
+            (pages.shape[1] > 1 and pages.stride(1) != 1):
+        raise ValueError("pages must be a 2-D CUDA int32 tensor with a contiguous row for each sequence")
+    a.max_pages, a.ld_pages = pages.shape[1], pages.stride(0) if seqs > 1 else pages.shape[1]
+    a.pages = pages.data_ptr()
+    if starts is not None:
+        a.starts = _vector(starts, "starts", seqs + 1, torch.int32)
+    elif tokens != seqs:
+        raise ValueError("q must have a row for each sequence, or starts")
+    a.scale = c.head_dim ** -0.5 if scale is None else scale
+    a.window = window
+    r = None
+    if rotation is not None:
+        r = rotation.c()
+        a.rotation = ctypes.addressof(r)
+    if out is None:
+        # rows of no sequence are not written
+        out = empty((tokens, cols), dtype=q.dtype, device=q.device)
+        a.out_type, a.ldo = a.q_type, cols
+    else:
+        a.out_type, a.ldo = _rows(out, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    a.out = out.data_ptr()
+    lse = None
+    if want_lse:
+        lse = empty((tokens, a.q_heads), dtype=torch.float32, device=q.device)
+        a.lse = lse.data_ptr()
+    if workspace is None:
+        nb = int(lib().esb_cache_attention_workspace_bytes(tokens, seqs, a.q_heads, c.heads, c.head_dim, a.q_type))
+        workspace = empty(nb, dtype=torch.uint8, device=q.device)
+    else:
+        _dev(workspace, "workspace")
+        nb = workspace.numel() * workspace.element_size()
+    _check(lib().esb_cache_attention(tokens, ctypes.byref(c), ctypes.byref(a), workspace.data_ptr(), nb, _stream(stream)),
+           "esb_cache_attention")
+    return out, lse
 
 
 ESB_PEAK_TCGEN05_F8F6F4 = 0
