@@ -840,7 +840,8 @@ esb_status esb_headnorm_backward(int64_t tokens, const esb_head_norm_grad* a, vo
  * word, the rest the zero code), with one scale:
  *   value = scale q(code),  b = 4, signed, 0 <= k <= 3
  * A page is `heads` times page_size rows of words, then the next head; pages
- * are page_ld words (a multiple of 4) and page_lds scales apart. */
+ * are page_ld words (a multiple of 4, below 2^34) and page_lds scales (below
+ * 2^32) apart. */
 typedef struct esb_kv_cache {
     uint32_t *k_codes, *v_codes;   /* [device] 16-byte aligned */
     float *k_scales, *v_scales;    /* [device] pages of heads x page_size floats */

@@ -1,0 +1,889 @@
+// esb_attention.cuh -- attention of queries over a paged cache of keys and
+// values in 4-bit ESB codes.
+//
+// One pass over the cache with the running maximum and sum of the softmax.  A
+// tile is the queries of a sequence that share a head of the cache, up to R =
+// 8 NT rows (row = query * group + head in the group).  Places go in stages of
+// 16: a warp copies a stage's codes and scales to shared memory some stages
+// ahead, decodes them to fp16 (exact: at most 3 significant bits) straight into
+// operands of the matrix instruction,
+//   S' (16 places x 8 rows)  = K Q'        over the head's values,
+//   O' (values x 8 rows)    += V' P'       over the 16 places,
+// so that a place's scale is a factor of a row of S' and of a row of P', and
+// the rows of a tile are columns everywhere: 8 rows fill an instruction, which
+// a single query's group of heads often just does.
+//
+// Weights carry v's scale: with u = score + log2(v's scale) and M the largest u
+// so far (up to 2^8; it is raised when a u passes that), the weight 2^(score -
+// M) v_scale is of order 1 whatever the scales are, and is rounded to fp16.
+//
+// The work, blocks of 64 places of all tiles in a row, is cut into equal parts,
+// one for each thread block, wherever that cuts a tile; parts of tiles go to
+// the workspace, and a second kernel joins them in their order.
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "esb_internal.h"
+#include "esb_rotate.cuh"
+#include "esb_rows.cuh"
+
+namespace esb {
+
+struct AttnArgs {
+    const void* q;
+    int64_t ldq;
+    void* out;
+    int64_t ldo;
+    float* lse;
+    const int32_t *starts, *lens, *pages;
+    int64_t ld_pages, tokens;
+    const uint32_t *kc, *vc;
+    const float *ks, *vs;
+    int64_t npages;
+    uint32_t page16, page_lds;                          // a page in 16 bytes of codes, and in scales
+    uint2 klut, vlut;                                   // high bytes of the fp16 numbers of codes 0..7; LIN: x = what turns a code into its place
+    int seqs, max_pages, heads, group, D, chunks, page_size, page_shift, window;
+    int q_type, out_type, qvec, ovec;
+    float scale2, vunit;                                // scale log2(e) and K's unit; V's unit
+    RotArgs rot;
+    float* partial;                                     // slots of R x (DP + 2) floats
+    int4* head;                                         // slots
+};
+
+namespace {
+
+constexpr int kAtWarps = 4, kAtThreads = 32 * kAtWarps;
+constexpr int kAtPlaces = 16;                           // of a stage
+constexpr int kAtBlock = kAtPlaces * kAtWarps;          // places of a block of work
+constexpr int kAtMinBlocks = 2;                         // of a thread block, while there is enough work
+
+// ------------------------------------------------------------ instructions
+
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t s)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(s));
+    return r;
+}
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t a)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(a));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float r;
+    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end_stage() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Eight codes to four pairs of fp16 numbers, codes i and i + 4 in pair i.
+// LIN, sets of one spacing (k = 2, 3): a number is its place among 0..7 with a
+// sign, and a place in bits 8..10 of an fp16 number is that many 2^-16 (below
+// 2^11 of its last places fp16 is fixed point), so no table is needed.  Other
+// sets: a number is its high byte, found by a permute with its code.  Signs and
+// places are put in order for four codes at once, then spread; a shift to the
+// left is a multiplication, on the pipe that has nothing to do.
+// Ten instructions a word (thirteen with the table), nine and twelve of them on
+// the pipe that bounds the kernel.
+template <bool LIN>
+__device__ __forceinline__ void decode8(uint32_t w, const uint2& lut, uint32_t (&r)[4])
+{
+    uint32_t a, b;                                      // codes 0, 2, 4, 6 and 1, 3, 5, 7 as bytes
+    if constexpr (LIN) {
+        a = (w & 0x07070707u) ^ (((w * 16u) & 0x80808080u) | lut.x);
+        b = ((w >> 4) & 0x07070707u) ^ ((w & 0x80808080u) | lut.x);
+    } else {
+        const uint32_t m = w & 0x77777777u;
+        const uint32_t x = prmt(lut.x, lut.y, m), y = prmt(lut.x, lut.y, m >> 16);
+        a = prmt(x, y, 0x6420u) | ((w * 16u) & 0x80808080u);
+        b = prmt(x, y, 0x7531u) | (w & 0x80808080u);
+    }
+    r[0] = prmt(a, 0u, 0x2404u);
+    r[1] = prmt(b, 0u, 0x2404u);
+    r[2] = a & 0xFF00FF00u;
+    r[3] = b & 0xFF00FF00u;
+}
+
+// ----------------------------------------------------------- shared memory
+
+// A stage: 16 rows of K's codes, 16 of V's, their scales.  Rows are spread so
+// that neither the reads of K (a row a quad, all its words) nor those of V (every
+// second row, two of a row's words a lane) meet a bank twice.
+template <int DP> struct Stage {
+    static constexpr int kRow = DP / 2;                 // bytes of a row of codes
+    static constexpr int kBytes = 2 * kAtPlaces * kRow + 2 * kAtPlaces * 4;
+    static constexpr int kV = kAtPlaces * kRow, kKs = 2 * kV;
+    __device__ __forceinline__ static uint32_t at(int row, int chunk)
+    {
+        if constexpr (DP == 64) return (row >> 2) * 128 + (((row & 3) ^ ((row >> 2) & 1)) * 32) + chunk * 16;
+        else if constexpr (DP == 128)
+            return (row >> 1) * 128 + ((row ^ (row >> 1)) & 1) * 64 + ((chunk ^ (((row >> 2) & 1) << 1)) * 16);
+        else return row * 128 + ((chunk ^ ((row & 1) << 2) ^ (((row >> 1) & 3) << 1)) * 16);
+    }
+};
+
+template <int DP, int NT, int NP> struct Shape {
+    static constexpr int R = 8 * NT, kSteps = DP / 16;
+    static constexpr int kStages = DP == 256 ? 4 : 6;
+    static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
+    static constexpr int kSm = NT == 1 ? (DP == 256 ? 3 : 4) : (NT == 2 && DP <= 128 && NP == 1 ? 3 : 2);
+    static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
+    static constexpr int kRing = kAtWarps * kStages * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;
+    static constexpr int kSums = kAtWarps * R * 8;      // maxima and sums of the warps
+    static constexpr int kBytes = (kRing > kMerge ? kRing : kMerge) + kQueryBytes + kSums + 4 * R;
+    static constexpr int kSlot = R * (DP + 2);          // floats of a part of a tile
+};
+
+// -------------------------------------------------------------------- work
+
+struct Seq {
+    int64_t row0;                       // of q
+    int nq, len, seen;                  // queries, places in use, places that the page table holds
+};
+__device__ __forceinline__ Seq sequence(const AttnArgs& a, int b)
+{
+    Seq s;
+    int64_t r0 = b, r1 = b + 1;
+    if (a.starts) { r0 = a.starts[b]; r1 = a.starts[b + 1]; }
+    r0 = r0 < 0 ? 0 : (r0 > a.tokens ? a.tokens : r0);
+    r1 = r1 < r0 ? r0 : (r1 > a.tokens ? a.tokens : r1);
+    s.row0 = r0;
+    s.nq = (int)(r1 - r0);
+    s.len = max(a.lens[b], 0);
+    const int64_t held = (int64_t)a.max_pages * a.page_size;
+    s.seen = s.len < held ? s.len : (int)held;
+    return s;
+}
+template <int R> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (int)(((int64_t)s.nq * a.group + R - 1) / R); }
+
+struct Tile {
+    int lo, hi, blocks;                 // places lo .. hi - 1, lo a multiple of 16; blocks of work (one where there are none)
+};
+template <int R> __device__ __forceinline__ Tile tile_of(const AttnArgs& a, const Seq& s, int i)
+{
+    Tile t;
+    const int64_t rows = (int64_t)s.nq * a.group, first = (int64_t)i * R, last = min(first + R, rows) - 1;
+    const int64_t p0 = (int64_t)s.len - s.nq + first / a.group, p1 = (int64_t)s.len - s.nq + last / a.group;
+    t.hi = (int)max((int64_t)0, min(p1 + 1, (int64_t)s.seen));
+    t.lo = a.window > 0 ? (int)max((int64_t)0, p0 - a.window + 1) & ~(kAtPlaces - 1) : 0;
+    t.blocks = t.hi > t.lo ? (t.hi - t.lo + kAtBlock - 1) / kAtBlock : 1;
+    return t;
+}
+
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kAtWarps; w++) v += sh[w];
+    return v;
+}
+
+// Work of sequences b0 + thread (0 past the end), long ones by the whole block.
+template <int R>
+__device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* sh)
+{
+    const int b = b0 + threadIdx.x;
+    int64_t w = 0;
+    bool many = false;
+    if (b < a.seqs) {
+        const Seq s = sequence(a, b);
+        const int n = tiles_of<R>(a, s);
+        many = n > 8;
+        if (!many)
+            for (int i = 0; i < n; i++) w += tile_of<R>(a, s, i).blocks;
+    }
+    if (a.starts && __syncthreads_or(many)) {
+        __shared__ unsigned list[kAtWarps];
+        const unsigned m = __ballot_sync(0xffffffffu, many);
+        if ((threadIdx.x & 31) == 0) list[threadIdx.x >> 5] = m;
+        __syncthreads();
+        for (int k = 0; k < kAtThreads; k++) {
+            if (!(list[k >> 5] >> (k & 31) & 1u)) continue;
+            const Seq s = sequence(a, b0 + k);
+            const int n = tiles_of<R>(a, s);
+            int64_t part = 0;
+            for (int i = threadIdx.x; i < n; i += kAtThreads) part += tile_of<R>(a, s, i).blocks;
+            part = block_sum(part, sh);
+            if (threadIdx.x == k) w = part;
+        }
+        __syncthreads();
+    }
+    return w * a.heads;
+}
+
+// Which of the block's threads holds place `at` of their works in a row, and
+// what of `at` is left there.
+struct Found {
+    int who;
+    int64_t rest;
+};
+__device__ __forceinline__ Found find(int64_t w, int64_t at, int64_t* sh, int64_t& total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int64_t p = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, p, o);
+        if (lane >= o) p += t;
+    }
+    __syncthreads();
+    if (lane == 31) sh[warp] = p;
+    if (threadIdx.x == 0) sh[kAtWarps] = -1;
+    __syncthreads();
+    total = 0;
+    int64_t before = 0;
+#pragma unroll
+    for (int k = 0; k < kAtWarps; k++) {
+        if (k < warp) before += sh[k];
+        total += sh[k];
+    }
+    p += before;                                        // works up to this thread's end
+    if (at < p && at >= p - w) {
+        sh[kAtWarps] = threadIdx.x;
+        sh[kAtWarps + 1] = at - (p - w);
+    }
+    __syncthreads();
+    Found f;
+    f.who = (int)sh[kAtWarps];
+    f.rest = sh[kAtWarps + 1];
+    return f;
+}
+
+// ------------------------------------------------------------------ kernel
+
+template <int DP, int NT, int NP, bool LIN>
+__global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_kernel(const AttnArgs a)
+{
+    using Sh = Shape<DP, NT, NP>;
+    using St = Stage<DP>;
+    constexpr int R = Sh::R, STEPS = Sh::kSteps, W = DP / 8, WK = W / 4, WV = W / 8, ST = Sh::kStages;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int64_t sh[kAtWarps + 2];
+    unsigned char* ring = smem;
+    float* merge = reinterpret_cast<float*>(smem);
+    uint2* qf = reinterpret_cast<uint2*>(smem + (Sh::kRing > Sh::kMerge ? Sh::kRing : Sh::kMerge));
+    float2* sums = reinterpret_cast<float2*>(reinterpret_cast<unsigned char*>(qf) + Sh::kQueryBytes);
+    float* qscale = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(sums) + Sh::kSums);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const float ninf = __int_as_float(0xff800000);
+    griddep_wait();
+
+    // this block's part of the work: sequence, head, tile and block of places
+    const int me = blockIdx.x;
+    int4 slot_head[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+    int64_t left = 0, rest = 0;
+    int b = 0, head = 0, tile = 0;
+    {
+        int64_t w = work_of<R>(a, 0, sh), total = 0;
+        if (a.seqs <= kAtThreads) total = block_sum(w, sh);
+        else
+            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) total += block_sum(b0 ? work_of<R>(a, b0, sh) : w, sh);
+        const int64_t least = total / kAtMinBlocks, n = least < 1 ? 1 : (least < gridDim.x ? least : gridDim.x);
+        if (me < n && total > 0) {
+            int64_t at = total * me / n;
+            left = total * (me + 1) / n - at;
+            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) {
+                if (b0) w = work_of<R>(a, b0, sh);
+                int64_t sum;
+                const Found f = find(w, at, sh, sum);
+                if (f.who >= 0) { b = b0 + f.who; rest = f.rest; break; }
+                at -= sum;
+            }
+            const Seq s = sequence(a, b);
+            const int n_tiles = tiles_of<R>(a, s);
+            if (n_tiles == 1) {
+                const int per = tile_of<R>(a, s, 0).blocks;
+                head = (int)(rest / per);
+                rest -= (int64_t)head * per;
+            } else {
+                int64_t per = 0;
+                for (int i = threadIdx.x; i < n_tiles; i += kAtThreads) per += tile_of<R>(a, s, i).blocks;
+                per = block_sum(per, sh);
+                head = (int)(rest / per);
+                rest -= (int64_t)head * per;
+                for (int i0 = 0; i0 < n_tiles; i0 += kAtThreads) {
+                    const int i = i0 + threadIdx.x;
+                    int64_t sum;
+                    const Found f = find(i < n_tiles ? tile_of<R>(a, s, i).blocks : 0, rest, sh, sum);
+                    if (f.who >= 0) { tile = i0 + f.who; rest = f.rest; break; }
+                    rest -= sum;
+                }
+            }
+        }
+    }
+
+    // where this lane's copies of a stage go
+    const int copies = kAtPlaces * a.chunks;
+    uint32_t to[W / 8];
+#pragma unroll
+    for (int i = 0; i < W / 8; i++) {
+        const int c = lane + 32 * i;
+        to[i] = c < copies ? St::at(c / a.chunks, c % a.chunks) : 0xffffffffu;
+    }
+    const uint32_t my_ring = smem_u32(ring) + warp * ST * St::kBytes;
+
+    while (left > 0) {
+        const Seq s = sequence(a, b);
+        const Tile tl = tile_of<R>(a, s, tile);
+        const int blocks = (int)min((int64_t)tl.blocks - rest, left), first_block = (int)rest;
+        const int64_t rows = (int64_t)s.nq * a.group, row0 = (int64_t)tile * R;
+        const int n_rows = (int)min((int64_t)R, rows - row0);
+
+        __syncthreads();                                // the last tile's shared memory has been read
+        const int32_t* table = a.pages + (int64_t)b * a.ld_pages;
+        const int place0 = tl.lo + (first_block * kAtWarps + warp) * kAtPlaces;
+        const int end = min(tl.hi, tl.lo + (first_block + blocks) * kAtBlock);
+        const int stages = end > place0 ? (end - place0 + kAtBlock - 1) / kAtBlock : 0;
+        const int64_t head_row = (int64_t)head * a.page_size;
+        const char* kg = reinterpret_cast<const char*>(a.kc) + (head_row * a.chunks + lane) * 16;
+        const char* vg = reinterpret_cast<const char*>(a.vc) + (head_row * a.chunks + lane) * 16;
+        const float* sg = (lane < 16 ? a.ks : a.vs) + head_row + (lane & 15);
+        auto page_at = [&](int i, int p) {
+            return i < stages ? __ldg(table + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size)) : -1;
+        };
+        int next_page = page_at(0, place0), issued = 0, issue_place = place0;
+        uint32_t issue_to = 0u, there = 0u;             // the ring's next stage; which of its stages hold a page that is there
+        auto issue = [&]() {
+            const int page = next_page, p = issue_place;
+            issue_place += kAtBlock;
+            next_page = page_at(++issued, issue_place);
+            const uint32_t bit = 1u << issue_to;
+            there &= ~bit;
+            if (page >= 0 && page < a.npages) {
+                there |= bit;
+                const int in = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
+                const uint64_t at = (uint64_t)(uint32_t)page * a.page16 + (uint32_t)(in * a.chunks);
+                const uint32_t base = my_ring + issue_to * St::kBytes;
+                const char *k = kg + at * 16, *v = vg + at * 16;
+#pragma unroll
+                for (int c = 0; c < W / 8; c++)
+                    if (to[c] != 0xffffffffu) {
+                        copy16(base + to[c], k + 512 * c);
+                        copy16(base + St::kV + to[c], v + 512 * c);
+                    }
+                copy4(base + St::kKs + 4 * lane, sg + (uint64_t)(uint32_t)page * a.page_lds + in);
+            }
+            copies_end_stage();
+            issue_to = issue_to == ST - 1 ? 0u : issue_to + 1u;
+        };
+#pragma unroll
+        for (int i = 0; i < ST - 1; i++) issue();
+
+        // queries: rotated, scaled, each row by a power of two that puts its
+        // largest below 2^15, as operands of the matrix instruction
+        for (int nt = warp; nt < NT; nt += kAtWarps) {
+            const int r = nt * 8 + g;
+            const bool on = r < n_rows;
+            const int64_t row = row0 + (on ? r : 0), token = row / a.group;
+            const int64_t at = (s.row0 + token) * a.ldq + ((int64_t)head * a.group + (row - token * a.group)) * a.D;
+            const int64_t pos = (int64_t)s.len - s.nq + token;
+            float v[WK][8];
+            float big = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WK; k++) {
+                const int word = DP == 256 ? (k < 4 ? 4 * t + k : 16 + 4 * t + k - 4) : WK * t + k, d = 8 * word;
+                if (on && d < a.D) {
+                    if (a.rot.dim) {
+                        if (a.q_type == ESB_F32) rotated8(static_cast<const float*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
+                        else if (a.q_type == ESB_F16) rotated8(static_cast<const __half*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
+                        else rotated8(static_cast<const __nv_bfloat16*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
+                    } else {
+                        load8_any(a.q, a.q_type, at + d, a.D - d, a.qvec, v[k]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; i++) v[k][i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(v[k][i]));
+            }
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            // 2^e takes the largest to 2^14 .. 2^15; the ends of fp32 stay in range
+            const int e = big > 0.0f && big < __int_as_float(0x7f800000) ? 14 - max(-112, min(126, ((int)(__float_as_uint(big) >> 23) - 127))) : 0;
+            const float up = __uint_as_float((uint32_t)(e / 2 + 127) << 23), up2 = __uint_as_float((uint32_t)(e - e / 2 + 127) << 23);
+            if (t == 0) qscale[r] = a.scale2 * __uint_as_float((uint32_t)(127 - e / 2) << 23) * __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+#pragma unroll
+            for (int k = 0; k < WK; k++) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[k][i] = v[k][i] * up * up2;
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    uint2 hi, lo;
+                    hi.x = pack2<__half>(v[k][2 * h], v[k][2 * h + 4]);
+                    hi.y = pack2<__half>(v[k][2 * h + 1], v[k][2 * h + 5]);
+                    qf[((nt * NP) * STEPS + 2 * k + h) * 32 + lane] = hi;
+                    if constexpr (NP == 2) {
+                        float x[4];
+                        unpack2<__half>(hi.x, x[0], x[1]);
+                        unpack2<__half>(hi.y, x[2], x[3]);
+                        lo.x = pack2<__half>(v[k][2 * h] - x[0], v[k][2 * h + 4] - x[1]);
+                        lo.y = pack2<__half>(v[k][2 * h + 1] - x[2], v[k][2 * h + 5] - x[3]);
+                        qf[((nt * NP + 1) * STEPS + 2 * k + h) * 32 + lane] = lo;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        uint2 qr[Sh::kQueryRegs ? NT * NP * STEPS : 1];
+        if constexpr (Sh::kQueryRegs) {
+#pragma unroll
+            for (int i = 0; i < NT * NP * STEPS; i++) qr[i] = qf[i * 32 + lane];
+        }
+        // this lane's columns: rows 2 t and 2 t + 1 of every eight
+        float fq[NT][2], M[NT][2], L[NT][2];
+        int qhi[NT][2], qlo[NT][2];                     // places that they see
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                const int r = nt * 8 + 2 * t + c;
+                const int64_t pos = (int64_t)s.len - s.nq + (row0 + r) / a.group;
+                fq[nt][c] = qscale[r];
+                M[nt][c] = ninf;
+                L[nt][c] = 0.0f;
+                qhi[nt][c] = r < n_rows ? (int)max((int64_t)0, min(pos + 1, (int64_t)s.seen)) : 0;
+                qlo[nt][c] = a.window > 0 ? (int)max((int64_t)0, pos - a.window + 1) : 0;
+            }
+        // stages between these are seen by every row
+        const int64_t p0 = (int64_t)s.len - s.nq + row0 / a.group, p1 = (int64_t)s.len - s.nq + (row0 + n_rows - 1) / a.group;
+        const int all_hi = (int)max((int64_t)0, min(p0 + 1, (int64_t)s.seen)), all_lo = a.window > 0 ? (int)max((int64_t)0, p1 - a.window + 1) : 0;
+
+        float o[DP / 16][NT][4];
+#pragma unroll
+        for (int i = 0; i < DP / 16; i++)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int c = 0; c < 4; c++) o[i][nt][c] = 0.0f;
+
+        uint32_t use = 0u;
+        for (int i = 0, place = place0; i < stages; i++, place += kAtBlock) {
+            copies_wait<ST - 2>();
+            __syncwarp();                               // every lane's copies of this stage; all have read the one before
+            const bool here = there >> use & 1u;
+            const unsigned char* sm = ring + (warp * ST + use) * St::kBytes;
+            use = use == ST - 1 ? 0u : use + 1u;
+            issue();
+            if (!here) continue;
+
+            // scores: rows g and g + 8 of the stage
+            // (two chains of products where a warp has few columns)
+            constexpr int CH = NT == 1 ? 2 : 1;
+            float sc[NT][4], part[CH][NT][4];
+#pragma unroll
+            for (int h = 0; h < CH; h++)
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int c = 0; c < 4; c++) part[h][nt][c] = 0.0f;
+            {
+                uint32_t k0[WK], k1[WK];
+                auto words = [&](int row, uint32_t (&w)[WK]) {
+                    if constexpr (DP == 64) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(sm + St::at(row, t >> 1) + (t & 1) * 8);
+                        w[0] = v.x; w[1] = v.y;
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < WK / 4; h++) {
+                            const uint4 v = *reinterpret_cast<const uint4*>(sm + St::at(row, t + 4 * h));
+                            w[4 * h] = v.x; w[4 * h + 1] = v.y; w[4 * h + 2] = v.z; w[4 * h + 3] = v.w;
+                        }
+                    }
+                };
+                words(g, k0);
+                words(g + 8, k1);
+#pragma unroll
+                for (int k = 0; k < WK; k++) {
+                    uint32_t x[4], y[4];
+                    decode8<LIN>(k0[k], a.klut, x);
+                    decode8<LIN>(k1[k], a.klut, y);
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                            for (int p = 0; p < NP; p++) {
+                                const int at = (nt * NP + p) * STEPS + 2 * k + h;
+                                uint2 q;
+                                if constexpr (Sh::kQueryRegs) q = qr[at];
+                                else q = qf[at * 32 + lane];
+                                mma16(part[h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
+                            }
+                }
+            }
+            const float* scales = reinterpret_cast<const float*>(sm + St::kKs);
+            const float ks0 = scales[g], ks1 = scales[g + 8], vs0 = scales[16 + g], vs1 = scales[24 + g];
+            // log2 of v's scales, where they have one
+            const float lv0 = fmaxf(fminf(lg2(fabsf(vs0)), 100.0f), -100.0f), lv1 = fmaxf(fminf(lg2(fabsf(vs1)), 100.0f), -100.0f);
+            const bool whole = place + kAtPlaces <= all_hi && place >= all_lo;
+            bool raise = false;
+            // scores less the maximum (what is not seen: -inf, whatever the maximum is)
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                for (int c = 0; c < 2; c++) {
+                    float x = part[0][nt][c], y = part[0][nt][2 + c];
+                    if constexpr (CH == 2) {
+                        x += part[CH - 1][nt][c];
+                        y += part[CH - 1][nt][2 + c];
+                    }
+                    part[0][nt][c] = x * ks0;
+                    part[0][nt][2 + c] = y * ks1;
+                    x = fmaf(part[0][nt][c], fq[nt][c], -M[nt][c]);
+                    y = fmaf(part[0][nt][2 + c], fq[nt][c], -M[nt][c]);
+                    if (!whole) {
+                        if (place + g >= qhi[nt][c] || place + g < qlo[nt][c]) x = ninf;
+                        if (place + g + 8 >= qhi[nt][c] || place + g + 8 < qlo[nt][c]) y = ninf;
+                    }
+                    raise |= fmaxf(x + lv0, y + lv1) > 8.0f;
+                    sc[nt][c] = x;
+                    sc[nt][2 + c] = y;
+                }
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int c = 0; c < 2; c++) {
+                        const float x = sc[nt][c] == ninf ? ninf : part[0][nt][c] * fq[nt][c];
+                        const float y = sc[nt][2 + c] == ninf ? ninf : part[0][nt][2 + c] * fq[nt][c];
+                        float m = fmaxf(x + lv0, y + lv1);
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                        m = fmaxf(m, M[nt][c]);
+                        const float f = m > M[nt][c] ? ex2(M[nt][c] - m) : 1.0f;
+                        M[nt][c] = m;
+                        L[nt][c] *= f;
+                        sc[nt][c] = x == ninf ? ninf : x - m;
+                        sc[nt][2 + c] = y == ninf ? ninf : y - m;
+#pragma unroll
+                        for (int k = 0; k < DP / 16; k++) {
+                            o[k][nt][c] *= f;
+                            o[k][nt][2 + c] *= f;
+                        }
+                    }
+            }
+            // weights, turned into the second product's operand
+            uint32_t p0[NT][NP], p1[NT][NP];
+#pragma unroll
+            for (int nt = 0; nt < NT; nt++) {
+                float w[4];
+#pragma unroll
+                for (int c = 0; c < 4; c++) {
+                    const float e = ex2(sc[nt][c]);
+                    L[nt][c & 1] += e;
+                    w[c] = e * (c < 2 ? vs0 : vs1);
+                    if (!whole && sc[nt][c] == ninf) w[c] = 0.0f;  // a scale that is not seen may be NaN
+                }
+                const uint32_t h0 = pack2<__half>(w[0], w[1]), h1 = pack2<__half>(w[2], w[3]);
+                p0[nt][0] = transposed(h0);
+                p1[nt][0] = transposed(h1);
+                if constexpr (NP == 2) {
+                    float x[4];
+                    unpack2<__half>(h0, x[0], x[1]);
+                    unpack2<__half>(h1, x[2], x[3]);
+                    p0[nt][NP - 1] = transposed(pack2<__half>(w[0] - x[0], w[1] - x[1]));
+                    p1[nt][NP - 1] = transposed(pack2<__half>(w[2] - x[2], w[3] - x[3]));
+                }
+            }
+            // values: this lane's words of places 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+            uint32_t v[4][WV];
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int row = 2 * t + (k & 1) + 8 * (k >> 1);
+                const unsigned char* vm = sm + St::kV;
+                if constexpr (DP == 64) v[k][0] = *reinterpret_cast<const uint32_t*>(vm + St::at(row, g >> 2) + (g & 3) * 4);
+                else if constexpr (DP == 128) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(vm + St::at(row, g >> 1) + (g & 1) * 8);
+                    v[k][0] = x.x; v[k][1] = x.y;
+                } else {
+                    const uint4 x = *reinterpret_cast<const uint4*>(vm + St::at(row, g));
+                    v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
+                }
+            }
+            // a pair of places' codes of the same four values, the second place's above
+            auto pair_codes = [](uint32_t x, uint32_t y, int upper) { return prmt(x, y, upper ? 0x7632u : 0x5410u); };
+            if constexpr (WV == 1) {
+                // rows g: values 0..3 of the word, rows g + 8: values 4..7
+                uint32_t x0[4], x1[4], y0[4], y1[4];
+                decode8<LIN>(pair_codes(v[0][0], v[1][0], 0), a.vlut, x0);
+                decode8<LIN>(pair_codes(v[2][0], v[3][0], 0), a.vlut, x1);
+                decode8<LIN>(pair_codes(v[0][0], v[1][0], 1), a.vlut, y0);
+                decode8<LIN>(pair_codes(v[2][0], v[3][0], 1), a.vlut, y1);
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int p = 0; p < NP; p++) mma16(o[k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+            } else {
+                // rows g: the first word's values, rows g + 8: the second's
+#pragma unroll
+                for (int wp = 0; wp < WV / 2; wp++)
+#pragma unroll
+                    for (int up = 0; up < 2; up++) {
+                        uint32_t x0[4], x1[4], y0[4], y1[4];
+                        constexpr int LAST = WV - 1;
+                        const int second = 2 * wp + 1 < LAST ? 2 * wp + 1 : LAST;
+                        decode8<LIN>(pair_codes(v[0][2 * wp], v[1][2 * wp], up), a.vlut, x0);
+                        decode8<LIN>(pair_codes(v[2][2 * wp], v[3][2 * wp], up), a.vlut, x1);
+                        decode8<LIN>(pair_codes(v[0][second], v[1][second], up), a.vlut, y0);
+                        decode8<LIN>(pair_codes(v[2][second], v[3][second], up), a.vlut, y1);
+#pragma unroll
+                        for (int k = 0; k < 4; k++)
+#pragma unroll
+                            for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                for (int p = 0; p < NP; p++)
+                                    mma16(o[8 * wp + 4 * up + k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                    }
+            }
+        }
+        copies_wait<0>();
+
+        // the warps' sums together: each against the largest maximum
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                float l = L[nt][c];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                if (g == 0) sums[warp * R + nt * 8 + 2 * t + c] = make_float2(M[nt][c], l);
+            }
+        __syncthreads();                                // the warps are done with their rings
+        // value e of a lane's column: the lane's 16 (8, 32) values in a row
+        constexpr int PER = DP / 8;
+#pragma unroll
+        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                float* to_row = merge + (warp * R + nt * 8 + 2 * t + c) * DP + g * PER;
+#pragma unroll
+                for (int e = 0; e < PER; e += 4) {
+                    float x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const int d = e + k;
+                        // words of a lane in pairs: rows g of the first word's tiles, rows g + 8 of the second's
+                        const int i = DP == 64 ? d & 3 : (d >> 4) * 8 + (d & 7), up = DP == 64 ? d >> 2 : (d >> 3) & 1;
+                        x[k] = o[i][nt][2 * up + c];
+                    }
+                    *reinterpret_cast<float4*>(to_row + e) = make_float4(x[0], x[1], x[2], x[3]);
+                }
+            }
+        __syncthreads();
+        const bool begins = first_block == 0, ends = first_block + blocks == tl.blocks;
+        const int which = begins ? 1 : 0;
+        float* slot = a.partial + (int64_t)(2 * me + which) * Sh::kSlot;
+        for (int i = threadIdx.x; i < n_rows * (DP / 8); i += kAtThreads) {
+            const int r = i / (DP / 8), d = (i - r * (DP / 8)) * 8;
+            if (d >= a.D) continue;
+            float m = ninf, l = 0.0f, f[kAtWarps], y[8];
+#pragma unroll
+            for (int w = 0; w < kAtWarps; w++) m = fmaxf(m, sums[w * R + r].x);
+#pragma unroll
+            for (int k = 0; k < 8; k++) y[k] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kAtWarps; w++) {
+                const float2 x = sums[w * R + r];
+                f[w] = x.x == ninf ? 0.0f : ex2(x.x - m);
+                // a sum that is NaN without a maximum stays NaN
+                l += x.x == ninf ? (x.y == x.y ? 0.0f : x.y) : f[w] * x.y;
+                const float* from = merge + (w * R + r) * DP + d;
+#pragma unroll
+                for (int k = 0; k < 8; k++) y[k] = x.x == ninf ? y[k] : fmaf(f[w], from[k], y[k]);
+            }
+            if (begins && ends) {
+                const int64_t row = row0 + r, token = row / a.group;
+                const int64_t qh = (int64_t)head * a.group + (row - token * a.group);
+                const float inv = l == 0.0f ? 0.0f : __fdiv_rn(a.vunit, l);
+#pragma unroll
+                for (int k = 0; k < 8; k++) y[k] = l == 0.0f ? 0.0f : (l == l ? y[k] * inv : l);
+                store8_any(a.out, a.out_type, (s.row0 + token) * a.ldo + qh * a.D + d, a.D - d, a.ovec, y);
+                if (a.lse && d == 0)
+                    a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : (m == ninf ? l : m * 0.69314718f + logf(l));
+            } else {
+                store8<float>(slot + (int64_t)r * DP + d, y);
+                if (d == 0) {
+                    slot[R * DP + r] = m;
+                    slot[R * DP + R + r] = l;
+                }
+            }
+        }
+        if (!(begins && ends)) {
+            const int4 h = make_int4(ends ? 3 : 1, b, head, tile);
+            if (begins) slot_head[1] = h;
+            else slot_head[0] = h;
+        }
+        left -= blocks;
+        rest = 0;
+        if (ends) {
+            if (++tile >= tiles_of<R>(a, s)) {
+                tile = 0;
+                if (++head >= a.heads) {
+                    head = 0;
+                    // the next sequence with queries
+                    while (left > 0 && ++b < a.seqs)
+                        if (sequence(a, b).nq > 0) break;
+                    if (b >= a.seqs) break;
+                }
+            }
+        }
+    }
+    if (threadIdx.x < 2) a.head[2 * me + threadIdx.x] = slot_head[threadIdx.x];
+}
+
+// Joins the parts of a tile that begins in part `x` of the work and goes on in
+// the following ones.
+template <int DP, int R>
+__global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a, int parts)
+{
+    constexpr int SLOT = R * (DP + 2);
+    griddep_wait();
+    const int p0 = blockIdx.x;
+    const int4 h = a.head[2 * p0 + 1];
+    if (!(h.x & 1)) return;
+    const Seq s = sequence(a, h.y);
+    const int64_t row = (int64_t)h.w * R + blockIdx.y, rows = (int64_t)s.nq * a.group;
+    if (row >= rows) return;
+    const int r = blockIdx.y;
+    // the part that ends the tile
+    __shared__ int last;
+    if (threadIdx.x == 0) last = parts - 1;
+    __syncthreads();
+    for (int base = p0 + 1; base < parts; base += 128) {
+        const int p = base + threadIdx.x;
+        if (p < parts && (a.head[2 * p].x & 3) == 3) atomicMin(&last, p);
+        __syncthreads();
+        const bool found = last < base + 128;
+        __syncthreads();
+        if (found) break;
+    }
+    const int n = last - p0 + 1;
+    auto slot = [&](int i) { return a.partial + (int64_t)(i == 0 ? 2 * p0 + 1 : 2 * (p0 + i)) * SLOT; };
+    __shared__ float wm[4];
+    const float ninf = __int_as_float(0xff800000);
+    float m = ninf;
+    for (int i = threadIdx.x; i < n; i += 128) m = fmaxf(m, slot(i)[R * DP + r]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) wm[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    // four values a thread and, where a row has fewer than 128 threads' worth, every few parts
+    constexpr int T = DP / 4, WAYS = 128 / T > 0 ? 128 / T : 1;
+    const int d = threadIdx.x % T * 4, way = threadIdx.x / T;
+    float y[4] = {0.0f, 0.0f, 0.0f, 0.0f}, l = 0.0f;
+#pragma unroll 4
+    for (int i = way; i < n; i += WAYS) {
+        const float* p = slot(i);
+        const float pm = p[R * DP + r], pl = p[R * DP + R + r];
+        const float4 v = *reinterpret_cast<const float4*>(p + r * DP + d);
+        if (pm == ninf) {
+            l += pl == pl ? 0.0f : pl;
+            continue;
+        }
+        const float f = ex2(pm - m);
+        l = fmaf(f, pl, l);
+        y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
+    }
+    __shared__ float parts_of[WAYS][T][5];
+    float* mine = parts_of[way][threadIdx.x % T];
+    mine[0] = y[0]; mine[1] = y[1]; mine[2] = y[2]; mine[3] = y[3]; mine[4] = l;
+    __syncthreads();
+    if (way != 0 || d >= a.D) return;
+#pragma unroll
+    for (int k = 1; k < WAYS; k++) {
+        const float* p = parts_of[k][threadIdx.x % T];
+        y[0] += p[0]; y[1] += p[1]; y[2] += p[2]; y[3] += p[3]; l += p[4];
+    }
+    const int64_t token = row / a.group, qh = (int64_t)h.z * a.group + (row - token * a.group);
+    const float inv = l == 0.0f ? 0.0f : __fdiv_rn(a.vunit, l);
+    const int64_t at = (s.row0 + token) * a.ldo + qh * a.D + d;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        const float v = l == 0.0f ? 0.0f : (l == l ? y[k] * inv : l);
+        if (a.out_type == ESB_F32) static_cast<float*>(a.out)[at + k] = v;
+        else if (a.out_type == ESB_F16) static_cast<__half*>(a.out)[at + k] = from_f32<__half>(v);
+        else static_cast<__nv_bfloat16*>(a.out)[at + k] = from_f32<__nv_bfloat16>(v);
+    }
+    if (a.lse && d == 0)
+        a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : (m == ninf ? l : m * 0.69314718f + logf(l));
+}
+
+template <int DP, int NT, int NP, bool LIN>
+cudaError_t run_attention(const AttnArgs& in, void* workspace, cudaStream_t st)
+{
+    using Sh = Shape<DP, NT, NP>;
+    AttnArgs a = in;
+    const int parts = device_sm_count() * Sh::kSm;
+    a.head = static_cast<int4*>(workspace);
+    a.partial = reinterpret_cast<float*>(a.head + 2 * parts);
+    cudaError_t e = cudaFuncSetAttribute(attention_kernel<DP, NT, NP, LIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(attention_kernel<DP, NT, NP, LIN>, dim3((unsigned)parts), dim3(kAtThreads), Sh::kBytes, st, a);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attention_join_kernel<DP, Sh::R>, dim3((unsigned)parts, Sh::R), dim3(128), 0, st, a, parts);
+}
+template <int DP, int NT, int NP> size_t workspace_of()
+{
+    using Sh = Shape<DP, NT, NP>;
+    return (size_t)(device_sm_count() * Sh::kSm) * 2 * (sizeof(int4) + sizeof(float) * Sh::kSlot);
+}
+
+// One of a head size's shapes: NT eights of rows, NP planes of queries and weights.
+template <int DP, int NT, int NP> struct Variant {
+    static cudaError_t run(const AttnArgs& a, bool lin, void* workspace, cudaStream_t st)
+    {
+        return lin ? run_attention<DP, NT, NP, true>(a, workspace, st) : run_attention<DP, NT, NP, false>(a, workspace, st);
+    }
+    static size_t bytes() { return workspace_of<DP, NT, NP>(); }
+};
+
+}  // namespace
+
+// What each head size's translation unit has: the most eights of rows for a
+// number of planes, a launch, and the bytes of its workspace.
+#define ESB_ATTENTION_SHAPES(X) X(64) X(128) X(256)
+#define ESB_DECLARE(DP)                                                                                              \
+    int attention_most_##DP(int planes);                                                                             \
+    cudaError_t attention_run_##DP(const AttnArgs& a, int nt, int planes, bool lin, void* workspace, cudaStream_t st); \
+    size_t attention_bytes_##DP(int nt, int planes);
+ESB_ATTENTION_SHAPES(ESB_DECLARE)
+#undef ESB_DECLARE
+
+}  // namespace esb
