@@ -10,8 +10,7 @@
 #include <cuda_runtime.h>
 
 #include "esb_internal.h"
-#include "esb_rotate.cuh"
-#include "esb_rows.cuh"
+#include "esb_heads.cuh"
 
 namespace esb {
 
@@ -31,12 +30,10 @@ struct HeadPart {
 
 struct HeadArgs {
     HeadPart part[2];
+    HeadWork work;
     const int64_t* positions;
     RotArgs rot;
-    int64_t tokens;
-    int D, heads;                       // heads of both parts
-    int iter, chunks;                   // heads of a lane's group in one item; items of a token
-    int w_type, tvec;
+    int D, w_type, tvec;
     float eps, inv_d;
     float* partial;                     // gradient: blocks x 2 x D
 };
@@ -48,117 +45,6 @@ __device__ __forceinline__ float value_at(const void* p, int type, int i)
     return to_f32(static_cast<const __nv_bfloat16*>(p)[i]);
 }
 
-// The pairs that a lane holds: (first, first + i) of `count`.
-struct PairPlace {
-    int j0, count;
-    bool rows;                          // neighbours in memory: 16 values in a row
-    int half;
-    __device__ __forceinline__ PairPlace(int j, int pairs, const RotArgs& r)
-    {
-        j0 = j;
-        count = min(8, max(0, pairs - j));
-        half = r.dim >> 1;
-        rows = r.inter || j0 >= half;
-    }
-    __device__ __forceinline__ int first(int i, const RotArgs& r) const { return r.inter || j0 + i >= half ? 2 * (j0 + i) : j0 + i; }
-    __device__ __forceinline__ int second(int i, const RotArgs& r) const { return r.inter || j0 + i >= half ? 2 * (j0 + i) + 1 : j0 + i + half; }
-};
-
-// A lane's 16 values as they lie in memory.
-template <class T, bool VEC>
-struct RawPairs {
-    Raw8<T> u, w;
-    __device__ __forceinline__ void load(const T* x, const PairPlace& p, const RotArgs& r, bool on)
-    {
-        if constexpr (VEC) {
-            const bool in = on && p.count > 0;
-            const int at = p.rows ? 2 * p.j0 : p.j0;
-            u.load(x + at, in ? 8 : 0, true);
-            w.load(x + (p.rows ? at + 8 : at + p.half), in ? 8 : 0, true);
-        } else {
-            uint32_t a[8], b[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const bool in = on && i < p.count;
-                if constexpr (sizeof(T) == 4) {
-                    a[i] = in ? __float_as_uint(x[p.first(i, r)]) : 0u;
-                    b[i] = in ? __float_as_uint(x[p.second(i, r)]) : 0u;
-                } else {
-                    const uint16_t* h = reinterpret_cast<const uint16_t*>(x);
-                    a[i] = in ? h[p.first(i, r)] : 0u;
-                    b[i] = in ? h[p.second(i, r)] : 0u;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < (int)(2 * sizeof(T)); i++) {
-                u.w[i] = sizeof(T) == 4 ? a[i] : a[(2 * i) & 7] | (a[(2 * i + 1) & 7] << 16);
-                w.w[i] = sizeof(T) == 4 ? b[i] : b[(2 * i) & 7] | (b[(2 * i + 1) & 7] << 16);
-            }
-        }
-    }
-    __device__ __forceinline__ void values(const PairPlace& p, float (&a)[8], float (&b)[8]) const
-    {
-        float x[8], y[8];
-        u.values(x);
-        w.values(y);
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const bool rows = VEC && p.rows;
-            a[i] = rows ? (i < 4 ? x[(2 * i) & 7] : y[(2 * i) & 7]) : x[i];
-            b[i] = rows ? (i < 4 ? x[(2 * i + 1) & 7] : y[(2 * i + 1) & 7]) : y[i];
-        }
-    }
-};
-
-template <class T, bool VEC>
-__device__ __forceinline__ void store_pairs(T* y, const PairPlace& p, const RotArgs& r, const float (&a)[8], const float (&b)[8])
-{
-    if constexpr (VEC) {
-        if (p.count <= 0) return;
-        float u[8], w[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            u[i] = p.rows ? ((i & 1) ? b[i / 2] : a[i / 2]) : a[i];
-            w[i] = p.rows ? ((i & 1) ? b[4 + i / 2] : a[4 + i / 2]) : b[i];
-        }
-        const int at = p.rows ? 2 * p.j0 : p.j0;
-        store8<T>(y + at, u);
-        store8<T>(y + (p.rows ? at + 8 : at + p.half), w);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (i < p.count) {
-                y[p.first(i, r)] = from_f32<T>(a[i]);
-                y[p.second(i, r)] = from_f32<T>(b[i]);
-            }
-    }
-}
-
-// cos and sin of a lane's pairs; pairs past the rotated ones are left as they are.
-__device__ __forceinline__ void load_turn(const HeadArgs& a, const PairPlace& p, int64_t pos, float (&c)[8], float (&s)[8])
-{
-    const RotArgs& r = a.rot;
-    if (a.tvec && p.j0 + 8 <= p.half) {
-        const bool in = pos >= 0 && pos < r.positions;
-        const float* t = r.table + (in ? pos : 0) * r.ld + p.j0;
-        const float4 c0 = __ldg(reinterpret_cast<const float4*>(t)), c1 = __ldg(reinterpret_cast<const float4*>(t + 4));
-        const float4 s0 = __ldg(reinterpret_cast<const float4*>(t + p.half)), s1 = __ldg(reinterpret_cast<const float4*>(t + p.half + 4));
-        c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
-        s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
-        if (!in) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) c[i] = s[i] = __int_as_float(0x7fffffff);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        c[i] = 1.0f;
-        s[i] = 0.0f;
-        if (i < p.count && p.j0 + i < p.half) rot_at(r, pos, p.j0 + i, c[i], s[i]);
-    }
-}
-
 template <int L>
 __device__ __forceinline__ float group_sum(float v)
 {
@@ -167,66 +53,59 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
-// Which heads a lane's group takes of an item, and of which part.
-struct HeadPlace {
-    int head, part;
-    bool on;
-    __device__ __forceinline__ HeadPlace(const HeadArgs& a, int h)
-    {
-        on = h < a.heads;
-        part = h >= a.part[0].heads;
-        head = part ? h - a.part[0].heads : h;
+__device__ __forceinline__ void load_weights(const HeadArgs& a, int part, const PairPlace& p, float (&wa)[8], float (&wb)[8])
+{
+    const void* w = a.part[part].weight;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        wa[i] = w && i < p.count ? value_at(w, a.w_type, p.first(i, a.rot)) : 1.0f;
+        wb[i] = w && i < p.count ? value_at(w, a.w_type, p.second(i, a.rot)) : 1.0f;
     }
-};
+}
 
+// Bound by HBM and by the latency of few values in flight: 24 warps on an SM
+// with one head of a lane's group ahead.
 template <int TYPE, int L, bool VEC>
-__global__ void __launch_bounds__(kHnThreads) headnorm_kernel(const HeadArgs a)
+__global__ void __launch_bounds__(kHnThreads, TYPE == ESB_F32 ? 2 : 3) headnorm_kernel(const HeadArgs a)
 {
     using T = Elem<TYPE>;
-    constexpr int G = 32 / L;           // heads of a warp at a time
     griddep_wait();
-    const int lane = threadIdx.x & 31, group = lane / L;
-    const PairPlace p((lane % L) * 8, a.D / 2, a.rot);
-    float wa[2][8], wb[2][8];
-#pragma unroll
-    for (int k = 0; k < 2; k++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const bool in = a.part[k].weight && i < p.count;
-            wa[k][i] = in ? value_at(a.part[k].weight, a.w_type, p.first(i, a.rot)) : 1.0f;
-            wb[k][i] = in ? value_at(a.part[k].weight, a.w_type, p.second(i, a.rot)) : 1.0f;
+    const PairPlace p((threadIdx.x % L) * 8, a.D / 2, a.rot);
+    float wa[8], wb[8], c[8], s[8];
+    int weights = -1;
+    HeadWalk<L, kHnWarps> at = {}, to = {};   // where the work is, where the loads are
+    RawPairs<T, VEC> next;
+    int64_t next_pos = 0, at_pos;
+    auto load = [&]() {
+        const HeadPart& part = a.part[to.part];
+        if (to.it == 0) next_pos = a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
+        next.load(static_cast<const T*>(part.x) + (to.on ? to.token * part.ldx + (int64_t)to.head * a.D : 0), p, a.rot, to.on);
+    };
+    to.start(a.work);
+    load();
+    at = to;
+    while (at.more(a.work)) {
+        const RawPairs<T, VEC> raw = next;
+        at_pos = next_pos;
+        to.next(a.work);
+        load();
+        if (at.it == 0) {
+            if (a.rot.dim && at.token < a.work.tokens) load_turn(a.rot, a.tvec, p, at_pos, c, s);
+            if (at.part != weights) load_weights(a, weights = at.part, p, wa, wb);
         }
-    const int64_t items = a.tokens * a.chunks, step = (int64_t)gridDim.x * kHnWarps;
-    for (int64_t item = (int64_t)blockIdx.x * kHnWarps + (threadIdx.x >> 5); item < items; item += step) {
-        const int64_t token = item / a.chunks;
-        const int h0 = (int)(item - token * a.chunks) * a.iter * G + group;
-        float c[8], s[8];
-        if (a.rot.dim) load_turn(a, p, __ldg(a.positions + token), c, s);
-        RawPairs<T, VEC> next;
-        auto load = [&](int it) {
-            const HeadPlace hp(a, h0 + it * G);
-            const bool on = hp.on && it < a.iter;
-            const HeadPart& part = a.part[hp.part];
-            next.load(static_cast<const T*>(part.x) + (on ? token * part.ldx + (int64_t)hp.head * a.D : 0), p, a.rot, on);
-        };
-        load(0);
-        for (int it = 0; it < a.iter; it++) {
-            const RawPairs<T, VEC> raw = next;
-            const HeadPlace hp(a, h0 + it * G);
-            load(it + 1);
-            float u[8], v[8];
-            raw.values(p, u, v);
-            float ss = 0.0f;
+        float u[8], v[8];
+        raw.values(p, u, v);
+        float ss = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; i++) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
-            const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(fmaf(group_sum<L>(ss), a.inv_d, a.eps)));
-            if (!hp.on) continue;
-            const HeadPart& part = a.part[hp.part];
-            if (part.rstd_out && p.j0 == 0) part.rstd_out[token * part.heads + hp.head] = rstd;
+        for (int i = 0; i < 8; i++) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
+        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(fmaf(group_sum<L>(ss), a.inv_d, a.eps)));
+        if (at.on) {
+            const HeadPart& part = a.part[at.part];
+            if (part.rstd_out && p.j0 == 0) part.rstd_out[at.token * part.heads + at.head] = rstd;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                u[i] *= rstd * (hp.part ? wa[1][i] : wa[0][i]);
-                v[i] *= rstd * (hp.part ? wb[1][i] : wb[0][i]);
+                u[i] *= rstd * wa[i];
+                v[i] *= rstd * wb[i];
             }
             if (a.rot.dim && p.j0 < p.half) {
 #pragma unroll
@@ -236,8 +115,9 @@ __global__ void __launch_bounds__(kHnThreads) headnorm_kernel(const HeadArgs a)
                     v[i] = fmaf(v[i], c[i], x * s[i]);
                 }
             }
-            store_pairs<T, VEC>(static_cast<T*>(part.y) + token * part.ldy + (int64_t)hp.head * a.D, p, a.rot, u, v);
+            store_pairs<T, VEC>(static_cast<T*>(part.y) + at.token * part.ldy + (int64_t)at.head * a.D, p, a.rot, u, v);
         }
+        at = to;
     }
 }
 
@@ -245,93 +125,98 @@ template <int TYPE, int L, bool VEC>
 __global__ void __launch_bounds__(kHnThreads, kHnGradBlocks) headnorm_grad_kernel(const HeadArgs a)
 {
     using T = Elem<TYPE>;
-    constexpr int G = 32 / L;
     __shared__ float sums[kHnWarps][2][256];
     griddep_wait();
-    const int lane = threadIdx.x & 31, group = lane / L, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const PairPlace p((lane % L) * 8, a.D / 2, a.rot);
-    float da[2][8] = {}, db[2][8] = {};
-    const int64_t items = a.tokens * a.chunks, step = (int64_t)gridDim.x * kHnWarps;
-    for (int64_t item = (int64_t)blockIdx.x * kHnWarps + warp; item < items; item += step) {
-        const int64_t token = item / a.chunks;
-        const int h0 = (int)(item - token * a.chunks) * a.iter * G + group;
-        float c[8], s[8];
-        if (a.rot.dim) load_turn(a, p, __ldg(a.positions + token), c, s);
-        RawPairs<T, VEC> next_x;
-        RawPairs<T, VEC> next_g;
-        float next_r = 0.0f;
-        auto load = [&](int it) {
-            const HeadPlace hp(a, h0 + it * G);
-            const bool on = hp.on && it < a.iter;
-            const HeadPart& part = a.part[hp.part];
-            const int64_t at = on ? (int64_t)hp.head * a.D : 0, t = on ? token : 0;
-            next_x.load(static_cast<const T*>(part.x) + t * part.ldx + at, p, a.rot, on);
-            next_g.load(static_cast<const T*>(part.dy) + t * part.ldg + at, p, a.rot, on);
-            next_r = on ? part.rstd_in[token * part.heads + hp.head] : 0.0f;
-        };
-        load(0);
-        for (int it = 0; it < a.iter; it++) {
-            const RawPairs<T, VEC> rx = next_x;
-            const RawPairs<T, VEC> rg = next_g;
-            const float rstd = next_r;
-            const HeadPlace hp(a, h0 + it * G);
-            load(it + 1);
-            float u[8], v[8], g[8], h[8];
-            rx.values(p, u, v);
-            rg.values(p, g, h);
-            if (a.rot.dim && p.j0 < p.half) {
+    for (int i = threadIdx.x; i < kHnWarps * 2 * 256; i += kHnThreads) (&sums[0][0][0])[i] = 0.0f;
+    __syncthreads();
+    float wa[8], wb[8], c[8], s[8], da[8], db[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float x = g[i];
-                    g[i] = fmaf(x, c[i], h[i] * s[i]);
-                    h[i] = fmaf(h[i], c[i], -(x * s[i]));
-                }
-            }
-            const HeadPart& part = a.part[hp.part];
-            float dot = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u[i] *= rstd;           // n
-                v[i] *= rstd;
-                if (hp.on) {
-                    const float x = g[i] * u[i], y = h[i] * v[i];
-                    da[0][i] += hp.part ? 0.0f : x;
-                    db[0][i] += hp.part ? 0.0f : y;
-                    da[1][i] += hp.part ? x : 0.0f;
-                    db[1][i] += hp.part ? y : 0.0f;
-                }
-                if (part.weight && i < p.count) {   // read again from the first-level cache: the sums have the registers
-                    g[i] *= value_at(part.weight, a.w_type, p.first(i, a.rot));
-                    h[i] *= value_at(part.weight, a.w_type, p.second(i, a.rot));
-                }
-                dot = fmaf(g[i], u[i], fmaf(h[i], v[i], dot));
-            }
-            dot = group_sum<L>(dot) * a.inv_d;
-            if (!hp.on) continue;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u[i] = rstd * fmaf(-u[i], dot, g[i]);
-                v[i] = rstd * fmaf(-v[i], dot, h[i]);
-            }
-            store_pairs<T, VEC>(static_cast<T*>(part.y) + token * part.ldy + (int64_t)hp.head * a.D, p, a.rot, u, v);
-        }
-    }
-    if (!a.partial) return;
-#pragma unroll
-    for (int k = 0; k < 2; k++)
+    for (int i = 0; i < 8; i++) da[i] = db[i] = 0.0f;
+    int weights = -1;
+    auto flush = [&]() {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            float x = da[k][i], y = db[k][i];
+            float x = da[i], y = db[i];
 #pragma unroll
             for (int o = L; o < 32; o <<= 1) {
                 x += __shfl_xor_sync(0xffffffffu, x, o);
                 y += __shfl_xor_sync(0xffffffffu, y, o);
             }
-            if (group == 0 && i < p.count) {
-                sums[warp][k][p.first(i, a.rot)] = x;
-                sums[warp][k][p.second(i, a.rot)] = y;
+            if (lane < L && i < p.count) {
+                sums[warp][weights][p.first(i, a.rot)] = x;
+                sums[warp][weights][p.second(i, a.rot)] = y;
+            }
+            da[i] = db[i] = 0.0f;
+        }
+    };
+    HeadWalk<L, kHnWarps> at = {}, to = {};
+    RawPairs<T, VEC> next_x, next_g;
+    float next_r;
+    int64_t next_pos = 0, at_pos;
+    auto load = [&]() {
+        const HeadPart& part = a.part[to.part];
+        if (to.it == 0) next_pos = a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
+        const int64_t h = to.on ? (int64_t)to.head * a.D : 0, t = to.on ? to.token : 0;
+        next_x.load(static_cast<const T*>(part.x) + t * part.ldx + h, p, a.rot, to.on);
+        next_g.load(static_cast<const T*>(part.dy) + t * part.ldg + h, p, a.rot, to.on);
+        next_r = to.on ? part.rstd_in[to.token * part.heads + to.head] : 0.0f;
+    };
+    to.start(a.work);
+    load();
+    at = to;
+    while (at.more(a.work)) {
+        const RawPairs<T, VEC> rx = next_x, rg = next_g;
+        const float rstd = next_r;
+        at_pos = next_pos;
+        to.next(a.work);
+        load();
+        if (at.it == 0) {
+            if (a.rot.dim && at.token < a.work.tokens) load_turn(a.rot, a.tvec, p, at_pos, c, s);
+            if (at.part != weights) {
+                if (weights >= 0) flush();
+                load_weights(a, weights = at.part, p, wa, wb);
             }
         }
+        float u[8], v[8], g[8], h[8];
+        rx.values(p, u, v);
+        rg.values(p, g, h);
+        if (a.rot.dim && p.j0 < p.half) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float x = g[i];
+                g[i] = fmaf(x, c[i], h[i] * s[i]);
+                h[i] = fmaf(h[i], c[i], -(x * s[i]));
+            }
+        }
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            u[i] *= rstd;               // n
+            v[i] *= rstd;
+            if (at.on) {
+                da[i] = fmaf(g[i], u[i], da[i]);
+                db[i] = fmaf(h[i], v[i], db[i]);
+            }
+            g[i] *= wa[i];
+            h[i] *= wb[i];
+            dot = fmaf(g[i], u[i], fmaf(h[i], v[i], dot));
+        }
+        dot = group_sum<L>(dot) * a.inv_d;
+        if (at.on) {
+            const HeadPart& part = a.part[at.part];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                u[i] = rstd * fmaf(-u[i], dot, g[i]);
+                v[i] = rstd * fmaf(-v[i], dot, h[i]);
+            }
+            store_pairs<T, VEC>(static_cast<T*>(part.y) + at.token * part.ldy + (int64_t)at.head * a.D, p, a.rot, u, v);
+        }
+        at = to;
+    }
+    if (!a.partial) return;
+    if (weights >= 0) flush();
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.D; i += kHnThreads) {
         const int k = i >= a.D, e = i - k * a.D;
@@ -360,26 +245,9 @@ __global__ void __launch_bounds__(1024) headnorm_dweight_kernel(const float* par
     }
 }
 
-int lanes_of(int D) { return D <= 64 ? 4 : D <= 128 ? 8 : 16; }
-
-// Heads of a lane's group in an item: a token's, while that leaves 16 warps for every SM.
-void split_heads(HeadArgs& a, int L)
+int64_t blocks_of(const HeadArgs& a, int64_t most)
 {
-    const int per = 32 / L, full = (a.heads + per - 1) / per;
-    const int64_t items = 16ll * device_sm_count();
-    const int64_t iter = a.tokens >= items ? full : full * a.tokens / items;
-    a.iter = (int)std::clamp<int64_t>(iter, 1, full);
-    a.chunks = (full + a.iter - 1) / a.iter;
-}
-
-int64_t blocks_of(const HeadArgs& a, int per_sm)
-{
-    return std::min<int64_t>((a.tokens * a.chunks + kHnWarps - 1) / kHnWarps, (int64_t)per_sm * device_sm_count());
-}
-
-bool rows16(const void* p, int64_t ld, int type)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * type_bytes(type) % 16 == 0;
+    return std::min((a.work.part[0].items + a.work.part[1].items + kHnWarps - 1) / kHnWarps, most);
 }
 
 using HnKernel = void (*)(const HeadArgs);
@@ -400,15 +268,12 @@ template <int TYPE, bool VEC> HnKernel grad_kernel(int L)
     }
 }
 
-// A lane's values are two vectors: whole eights of pairs on both sides of the rotation's end.
-bool pairs_of_vectors(int D, const esb_rotation& r) { return D % 16 == 0 && (r.interleaved || r.dim % 16 == 0); }
-
 }  // namespace
 
 cudaError_t launch_headnorm(int64_t tokens, const esb_head_norm& n, cudaStream_t st)
 {
     HeadArgs a = {};
-    bool vec = pairs_of_vectors(n.head_dim, n.rotation);
+    bool vec = pairs_of_vectors(n.head_dim, n.rotation.dim, n.rotation.interleaved);
     for (int k = 0; k < 2; k++) {
         const esb_heads& h = n.part[k];
         HeadPart& p = a.part[k];
@@ -418,28 +283,28 @@ cudaError_t launch_headnorm(int64_t tokens, const esb_head_norm& n, cudaStream_t
         vec = vec && rows16(h.x, h.ldx, n.x_type) && rows16(h.y, h.ldy, n.x_type);
     }
     a.positions = n.positions; a.rot = make_rot(&n.rotation, n.head_dim);
-    a.tokens = tokens; a.D = n.head_dim; a.heads = n.part[0].heads + n.part[1].heads;
+    a.D = n.head_dim;
     a.w_type = n.w_type; a.tvec = a.rot.vec; a.eps = n.eps; a.inv_d = 1.0f / (float)n.head_dim;
     const int L = lanes_of(a.D);
-    split_heads(a, L);
+    const int64_t most = (int64_t)device_sm_count() * (n.x_type == ESB_F32 ? 2 : 3);
+    a.work = split_heads(tokens, a.part[0].heads, a.part[1].heads, L, most * kHnWarps);
     static HnKernel (*const pick[3][2])(int) = {{norm_kernel<ESB_F32, false>, norm_kernel<ESB_F32, true>},
                                                 {norm_kernel<ESB_F16, false>, norm_kernel<ESB_F16, true>},
                                                 {norm_kernel<ESB_BF16, false>, norm_kernel<ESB_BF16, true>}};
-    return launch_pdl(pick[n.x_type][vec](L), dim3((unsigned)blocks_of(a, 8)), dim3(kHnThreads), 0, st, a);
+    return launch_pdl(pick[n.x_type][vec](L), dim3((unsigned)blocks_of(a, most)), dim3(kHnThreads), 0, st, a);
 }
 
+// A part of the sums for every block that there may be.
 size_t headnorm_grad_workspace_bytes(int64_t tokens, int64_t heads, int head_dim)
 {
-    HeadArgs a = {};
-    a.tokens = tokens; a.heads = (int)heads; a.D = head_dim;
-    split_heads(a, lanes_of(head_dim));
-    return sizeof(float) * 2 * (size_t)head_dim * (size_t)blocks_of(a, kHnGradBlocks);
+    const int64_t rows = (tokens * heads + kHnWarps - 1) / kHnWarps + 1;
+    return sizeof(float) * 2 * (size_t)head_dim * (size_t)std::min<int64_t>(rows, (int64_t)kHnGradBlocks * device_sm_count());
 }
 
 cudaError_t launch_headnorm_grad(int64_t tokens, const esb_head_norm_grad& n, void* workspace, cudaStream_t st)
 {
     HeadArgs a = {};
-    bool vec = pairs_of_vectors(n.head_dim, n.rotation), sums = false;
+    bool vec = pairs_of_vectors(n.head_dim, n.rotation.dim, n.rotation.interleaved), sums = false;
     for (int k = 0; k < 2; k++) {
         const esb_heads_grad& h = n.part[k];
         HeadPart& p = a.part[k];
@@ -451,12 +316,13 @@ cudaError_t launch_headnorm_grad(int64_t tokens, const esb_head_norm_grad& n, vo
         vec = vec && rows16(h.x, h.ldx, n.x_type) && rows16(h.dy, h.ldg, n.x_type) && rows16(h.dx, h.lddx, n.x_type);
     }
     a.positions = n.positions; a.rot = make_rot(&n.rotation, n.head_dim);
-    a.tokens = tokens; a.D = n.head_dim; a.heads = n.part[0].heads + n.part[1].heads;
+    a.D = n.head_dim;
     a.w_type = n.w_type; a.tvec = a.rot.vec; a.inv_d = 1.0f / (float)n.head_dim;
     a.partial = sums ? static_cast<float*>(workspace) : nullptr;
     const int L = lanes_of(a.D);
-    split_heads(a, L);
-    const int blocks = (int)blocks_of(a, kHnGradBlocks);
+    const int64_t most = (int64_t)kHnGradBlocks * device_sm_count();
+    a.work = split_heads(tokens, a.part[0].heads, a.part[1].heads, L, most * kHnWarps);
+    const int blocks = (int)blocks_of(a, most);
     static HnKernel (*const pick[3][2])(int) = {{grad_kernel<ESB_F32, false>, grad_kernel<ESB_F32, true>},
                                                 {grad_kernel<ESB_F16, false>, grad_kernel<ESB_F16, true>},
                                                 {grad_kernel<ESB_BF16, false>, grad_kernel<ESB_BF16, true>}};

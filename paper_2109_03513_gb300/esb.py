@@ -1178,24 +1178,27 @@ class KvCache(NamedTuple):
     v_fmt: Fmt
 
     def c(self) -> esb_kv_cache:
-        shape = self.k_codes.shape
-        if len(shape) != 4 or shape[3] != (self.head_dim + 31) // 32 * 4:
+        kc, ks, vc, vs, d, kf, vf = self
+        shape = kc.shape
+        if len(shape) != 4 or shape[3] != (d + 31) // 32 * 4:
             raise ValueError("codes must be (pages, heads, page_size, esb_row_words(head_dim, 4))")
         pages, heads, size, words = shape
-        ld = lds = 0
-        for codes, scales in ((self.k_codes, self.k_scales), (self.v_codes, self.v_scales)):
-            if codes.dtype != torch.int32 or scales.dtype != torch.float32 or not codes.is_cuda or not scales.is_cuda:
-                raise ValueError("codes must be CUDA int32, scales CUDA float32")
-            if codes.shape != shape or scales.shape != shape[:3]:
-                raise ValueError("keys and values must have one shape, scales (pages, heads, page_size)")
-            if pages and not (codes[0].is_contiguous() and scales[0].is_contiguous()):
-                raise ValueError("a page's codes and scales must be contiguous")
-            at = (codes.stride(0), scales.stride(0)) if pages > 1 else (heads * size * words, heads * size)
-            if ld and at != (ld, lds):
-                raise ValueError("keys and values must have pages equally far apart")
-            ld, lds = at
-        return esb_kv_cache(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr(),
-                            pages, ld, lds, heads, size, self.head_dim, self.k_fmt.c(), self.v_fmt.c())
+        if kc.dtype != torch.int32 or vc.dtype != torch.int32 or ks.dtype != torch.float32 or vs.dtype != torch.float32 or \
+                not (kc.is_cuda and vc.is_cuda and ks.is_cuda and vs.is_cuda):
+            raise ValueError("codes must be CUDA int32, scales CUDA float32")
+        row = shape[:3]
+        if vc.shape != shape or ks.shape != row or vs.shape != row:
+            raise ValueError("keys and values must have one shape, scales (pages, heads, page_size)")
+        ld, lds = heads * size * words, heads * size
+        cst, sst = kc.stride(), ks.stride()
+        if pages > 1 and heads and size:
+            ld, lds = cst[0], sst[0]
+        if vc.stride() != cst or vs.stride() != sst:
+            raise ValueError("keys and values must have the same strides")
+        if pages and (cst[3] != 1 or (cst[2] != words and size > 1) or (cst[1] != size * words and heads > 1) or
+                      (sst[2] != 1 and size > 1) or (sst[1] != size and heads > 1)):
+            raise ValueError("a page's codes and scales must be contiguous")
+        return esb_kv_cache(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, ld, lds, heads, size, d, kf.c(), vf.c())
 
 
 def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, k_fmt: Fmt = Fmt(4, 2), v_fmt: Fmt = Fmt(4, 2),
