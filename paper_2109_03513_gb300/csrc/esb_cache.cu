@@ -9,6 +9,7 @@
 // 15 values a last place is a step of the set now and then.
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 #include <cuda_runtime.h>
 
 #include "esb_internal.h"
@@ -18,7 +19,8 @@ namespace esb {
 
 namespace {
 
-constexpr int kApThreads = 256;
+constexpr int kApThreads = 256, kApBlocks = 2;     // on an SM
+constexpr int kApAhead = 1;             // heads of a group that are loaded before they are needed
 
 struct AppendSide {
     const void* x;
@@ -36,7 +38,7 @@ struct AppendArgs {
     AppendSide side[2];                 // keys, values
     const int64_t *slots, *positions;
     int64_t tokens, places, page_ld, page_lds;
-    int heads, page_size, D, words, q_type, rule, tvec;
+    int heads, page_size, page_shift, D, words, q_type, rule, tvec;
     RotArgs rot;
     HeadWork work;
 };
@@ -68,102 +70,134 @@ __device__ __forceinline__ float scale_of(const AppendArgs& a, const AppendSide&
     return __fmul_rn(s.astar, __fadd_rn(__fsqrt_rn(total(s2) / (float)a.D), 1e-7f));
 }
 
-// Heads of whole vectors: a lane holds 8 pairs of a key as the rotation pairs
-// them, or 16 of a value's numbers, the next head's ahead; a warp keeps a
-// token's cos and sin for several heads.
-template <int TYPE, int L>
-__global__ void __launch_bounds__(kApThreads, TYPE == ESB_F32 ? 2 : 3) append_pairs_kernel(const AppendArgs a)
+// One token's head: its scale, then codes and values of the lane's two vectors
+// of 8 from d0 and d1 on (there: the lane has them).
+template <int L>
+__device__ __forceinline__ void append_head(const AppendArgs& a, const AppendSide& s, bool on, int64_t slot, int64_t token, int head, int j0,
+                                            bool there, int d0, int d1, const float (&u)[8], const float (&v)[8])
 {
-    using T = Elem<TYPE>;
-    griddep_wait();
-    RotArgs none = {};
-    const int j0 = (threadIdx.x % L) * 8;
-    const PairPlace pk(j0, a.D / 2, a.rot), pv(j0, a.D / 2, none);
-    float c[8], sn[8];
-    HeadWalk<L, kApThreads / 32> at = {}, to = {};
-    RawPairs<T, true> next;
-    int64_t next_slot = -1, next_pos = 0, slot, pos;
-    auto load = [&]() {
-        const AppendSide& s = a.side[to.part];
-        if (to.it == 0) {
-            next_slot = to.token < a.work.tokens && to.on ? __ldg(a.slots + to.token) : -1;
-            next_pos = a.rot.dim && to.part == 0 && to.on ? __ldg(a.positions + to.token) : 0;
+    const float alpha = scale_of<L>(a, s, u, v, there ? 8 : 0, there ? 8 : 0);
+    if (!on) return;
+    const int64_t page = a.page_shift >= 0 ? slot >> a.page_shift : slot / a.page_size;
+    const int place = (int)(slot - page * a.page_size);
+    const int row = head * a.page_size + place;
+    if (j0 == 0) s.scales[page * a.page_lds + row] = alpha;
+    uint32_t* codes = s.codes + page * a.page_ld + (int64_t)row * a.words;
+    if (!there) {
+        if (2 * j0 < a.words * 8) {                     // the words behind the values
+            const uint32_t z = s.f.zero_code * 0x11111111u;
+            *reinterpret_cast<uint2*>(codes + j0 / 4) = make_uint2(z, z);
         }
-        const T* x = static_cast<const T*>(s.x) + (to.on ? to.token * s.ldx + (int64_t)to.head * a.D : 0);
-        if (to.part) next.load(x, pv, none, to.on);
-        else next.load(x, pk, a.rot, to.on);
-    };
-    to.start(a.work);
-    load();
-    at = to;
-    while (at.more(a.work)) {
-        const RawPairs<T, true> raw = next;
-        slot = next_slot;
-        pos = next_pos;
-        to.next(a.work);
-        load();
-        const bool key = at.part == 0;
-        if (at.it == 0 && key && a.rot.dim) load_turn(a.rot, a.tvec, pk, pos, c, sn);
-        const bool on = at.on && slot >= 0 && slot < a.places;
-        const bool rows = key ? pk.rows : true;
-        float u[8], v[8];
-        if (key) {
-            raw.values(pk, u, v);
-            if (a.rot.dim && pk.j0 < pk.half) {
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float x = u[i];
-                    u[i] = dot2_rn(x, c[i], v[i], -sn[i]);
-                    v[i] = dot2_rn(v[i], c[i], x, sn[i]);
-                }
-            }
-            if (pk.rows) {
-                float x[8], y[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) { x[i] = u[i]; y[i] = v[i]; }
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    u[i] = (i & 1) ? y[i / 2] : x[i / 2];
-                    v[i] = (i & 1) ? y[4 + i / 2] : x[4 + i / 2];
-                }
-            }
-        } else {
-            raw.u.values(u);
-            raw.w.values(v);
-        }
-        const AppendSide& s = a.side[at.part];
-        const int there = pv.count > 0 ? 8 : 0;
-        const float alpha = scale_of<L>(a, s, u, v, there, there);
-        if (on) {
-            const int64_t page = slot / a.page_size;
-            const int place = (int)(slot - page * a.page_size);
-            if (j0 == 0) s.scales[page * a.page_lds + (int64_t)at.head * a.page_size + place] = alpha;
-            const GroupScale g = make_scale(alpha, s.f);
-            uint32_t w0[1], w1[1];
-            float q0[8], q1[8];
-            quantise8<4, true>(u, g, s.f, w0, q0);
-            quantise8<4, true>(v, g, s.f, w1, q1);
-            uint32_t* codes = s.codes + page * a.page_ld + ((int64_t)at.head * a.page_size + place) * a.words;
-            const int d0 = rows ? 2 * j0 : j0, d1 = rows ? d0 + 8 : j0 + pk.half;
-            if (pv.count > 0) {
-                if (rows) *reinterpret_cast<uint2*>(codes + d0 / 8) = make_uint2(w0[0], w1[0]);
-                else { codes[d0 / 8] = w0[0]; codes[d1 / 8] = w1[0]; }
-                if (s.q) {
-                    element_values(u, g, s.f, q0);
-                    element_values(v, g, s.f, q1);
-                    const int64_t row = at.token * s.ldq + (int64_t)at.head * a.D;
-                    store8_any(s.q, a.q_type, row + d0, 8, s.qvec, q0);
-                    store8_any(s.q, a.q_type, row + d1, 8, s.qvec, q1);
-                }
-            } else if (2 * j0 < a.words * 8) {              // the words behind the values
-                const uint32_t z = s.f.zero_code * 0x11111111u;
-                *reinterpret_cast<uint2*>(codes + j0 / 4) = make_uint2(z, z);
-            }
-        }
-        at = to;
+        return;
+    }
+    const GroupScale g = make_scale(alpha, s.f);
+    uint32_t w0[1], w1[1];
+    float q0[8], q1[8];
+    if (a.rule == ESB_SCALE_ABSMAX) {                   // no quotient is past the largest element
+        quantise8<4, false>(u, g, s.f, w0, q0);
+        quantise8<4, false>(v, g, s.f, w1, q1);
+    } else {
+        quantise8<4, true>(u, g, s.f, w0, q0);
+        quantise8<4, true>(v, g, s.f, w1, q1);
+    }
+    if (d1 == d0 + 8) {
+        *reinterpret_cast<uint2*>(codes + d0 / 8) = make_uint2(w0[0], w1[0]);
+    } else {
+        codes[d0 / 8] = w0[0];
+        codes[d1 / 8] = w1[0];
+    }
+    if (s.q) {
+        element_values(u, g, s.f, q0);
+        element_values(v, g, s.f, q1);
+        const int64_t at = token * s.ldq + head * a.D;
+        store8_any(s.q, a.q_type, at + d0, 8, s.qvec, q0);
+        store8_any(s.q, a.q_type, at + d1, 8, s.qvec, q1);
     }
 }
 
+// Heads of whole vectors: a lane holds 8 pairs of a key as the rotation pairs
+// them, or 16 of a value's numbers, the next head's ahead; a warp keeps a
+// token's cos and sin for several heads.
+template <int TYPE, int L, int MODE>
+__global__ void __launch_bounds__(kApThreads, kApBlocks) append_pairs_kernel(const AppendArgs a)
+{
+    using T = Elem<TYPE>;
+    griddep_wait();
+    const int j0 = (threadIdx.x % L) * 8;
+#pragma unroll 1
+    for (int k = 0; k < 2; k++) {
+        HeadWalk<L, kApThreads / 32> to(a.work, k);
+        if (!to.more()) continue;
+        const AppendSide& s = a.side[k];
+        const T* x = static_cast<const T*>(s.x);
+        const int64_t ldx = s.ldx;
+        // keys and values go the same way but for the rotation
+        auto walk = [&](auto mode, const RotArgs& rot) {
+            constexpr int M = decltype(mode)::value;
+            const PairPlace p(j0, a.D / 2, rot);
+            const bool turns = M == kPairHalves || (rot.dim && p.j0 < p.half);
+            const int d0 = p.vec0<M>(), d1 = p.vec1<M>();
+            float c[8], sn[8];
+            RawPairs<T, M> next[kApAhead];
+            HeadAt there[kApAhead];
+            auto load = [&](int i) {
+                there[i] = HeadAt(to);
+                if (there[i].first && to.on) {
+                    there[i].slot = __ldg(a.slots + to.token);
+                    if (turns) there[i].pos = __ldg(a.positions + to.token);
+                }
+                next[i].load(x + (to.on ? to.token * ldx + to.head * a.D : 0), p, rot, to.on);
+                to.next();
+            };
+#pragma unroll
+            for (int i = 0; i < kApAhead; i++) load(i);
+            int64_t slot = -1;
+            while (there[0].more) {
+                const RawPairs<T, M> raw = next[0];
+                const HeadAt at = there[0];
+#pragma unroll
+                for (int i = 0; i + 1 < kApAhead; i++) {
+                    next[i] = next[i + 1];
+                    there[i] = there[i + 1];
+                }
+                load(kApAhead - 1);
+                if (at.first) {
+                    slot = at.slot;
+                    if (turns) load_turn(rot, a.tvec, p, at.pos, c, sn);
+                }
+                float u[8], v[8];
+                raw.u.values(u);
+                raw.w.values(v);
+                if (turns) {
+                    float f[8], g[8];
+                    if (p.in_rows<M>()) {
+                        rows_to_pairs(u, v, f, g);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) { f[i] = u[i]; g[i] = v[i]; }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) {
+                        const Pair x0 = pair_of(f[i], f[i + 1]), x1 = pair_of(g[i], g[i + 1]), cc = pair_of(c[i], c[i + 1]);
+                        const Pair sp = pair_of(sn[i], sn[i + 1]), sm = pair_of(-sn[i], -sn[i + 1]);
+                        split(dot2_rn(x0, cc, x1, sm), f[i], f[i + 1]);
+                        split(dot2_rn(x1, cc, x0, sp), g[i], g[i + 1]);
+                    }
+                    if (p.in_rows<M>()) {
+                        pairs_to_rows(f, g, u, v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; i++) { u[i] = f[i]; v[i] = g[i]; }
+                    }
+                }
+                append_head<L>(a, s, at.on && slot >= 0 && slot < a.places, slot, at.token, at.head, j0, p.count > 0, d0, d1, u, v);
+            }
+        };
+        RotArgs none = {};
+        if (k == 0) walk(std::integral_constant<int, MODE>(), a.rot);
+        else walk(std::integral_constant<int, kPairRows>(), none);
+    }
+}
 // Any heads: a lane holds 16 consecutive values, and reads a pair's other half again.
 template <int TYPE, int L>
 __global__ void __launch_bounds__(kApThreads) append_kernel(const AppendArgs a)
@@ -216,13 +250,18 @@ __global__ void __launch_bounds__(kApThreads) append_kernel(const AppendArgs a)
 }
 
 using ApKernel = void (*)(const AppendArgs);
-template <int TYPE> ApKernel append_of(int L, bool pairs)
+template <int TYPE, int L> ApKernel append_of(int mode)
 {
-    switch (L) {
-    case 4: return pairs ? append_pairs_kernel<TYPE, 4> : append_kernel<TYPE, 4>;
-    case 8: return pairs ? append_pairs_kernel<TYPE, 8> : append_kernel<TYPE, 8>;
-    default: return pairs ? append_pairs_kernel<TYPE, 16> : append_kernel<TYPE, 16>;
+    switch (mode) {
+    case kPairHalves: return append_pairs_kernel<TYPE, L, kPairHalves>;
+    case kPairRows: return append_pairs_kernel<TYPE, L, kPairRows>;
+    case kPairMixed: return append_pairs_kernel<TYPE, L, kPairMixed>;
+    default: return append_kernel<TYPE, L>;
     }
+}
+template <int TYPE> ApKernel append_of(int L, int mode)
+{
+    return L == 4 ? append_of<TYPE, 4>(mode) : L == 8 ? append_of<TYPE, 8>(mode) : append_of<TYPE, 16>(mode);
 }
 
 }  // namespace
@@ -244,21 +283,24 @@ cudaError_t launch_cache_append(int64_t tokens, const esb_kv_cache& c, const esb
     a.slots = n.slots; a.positions = n.positions; a.tokens = tokens; a.places = c.pages * c.page_size;
     a.page_ld = c.page_ld; a.page_lds = c.page_lds;
     a.heads = c.heads; a.page_size = c.page_size; a.D = c.head_dim; a.words = (c.head_dim + 31) / 32 * 4;
+    a.page_shift = -1;
+    for (int i = 4; i < 31; i++)
+        if (c.page_size == 1 << i) a.page_shift = i;
     a.q_type = n.q_type; a.rule = n.rule; a.rot = make_rot(n.rotation, c.head_dim);
     a.tvec = a.rot.vec;
     const int L = lanes_of(a.D);
-    static ApKernel (*const pick[3])(int, bool) = {append_of<ESB_F32>, append_of<ESB_F16>, append_of<ESB_BF16>};
-    const bool pairs = pairs_of_vectors(a.D, a.rot.dim, a.rot.inter) && a.side[0].xvec && a.side[1].xvec;
+    static ApKernel (*const pick[3])(int, int) = {append_of<ESB_F32>, append_of<ESB_F16>, append_of<ESB_BF16>};
+    const int mode = pair_mode(a.D, a.rot.dim, a.rot.inter, a.side[0].xvec && a.side[1].xvec);
     int64_t blocks;
-    if (pairs) {
-        const int64_t most = (int64_t)device_sm_count() * (n.x_type == ESB_F32 ? 2 : 3), warps = kApThreads / 32;
+    if (mode != kPairAny) {
+        const int64_t most = (int64_t)device_sm_count() * (kApBlocks), warps = kApThreads / 32;
         a.work = split_heads(tokens, c.heads, c.heads, L, most * warps);
         blocks = std::min((a.work.part[0].items + a.work.part[1].items + warps - 1) / warps, most);
     } else {
         const int64_t per = kApThreads / L;
         blocks = std::min<int64_t>((tokens * 2 * c.heads + per - 1) / per, 8ll * device_sm_count());
     }
-    return launch_pdl(pick[n.x_type](L, pairs), dim3((unsigned)blocks), dim3(kApThreads), 0, st, a);
+    return launch_pdl(pick[n.x_type](L, mode), dim3((unsigned)blocks), dim3(kApThreads), 0, st, a);
 }
 
 }  // namespace esb

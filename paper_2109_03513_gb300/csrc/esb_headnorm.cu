@@ -17,7 +17,8 @@ namespace esb {
 namespace {
 
 constexpr int kHnThreads = 256, kHnWarps = kHnThreads / 32;
-constexpr int kHnGradBlocks = 2;        // blocks on an SM of the gradient
+constexpr int kHnBlocks = 2;            // on an SM
+constexpr int kHnAhead = 2;             // heads of a group that are loaded before they are needed (the gradient: one, with two values each)
 
 struct HeadPart {
     const void *x, *dy, *weight;
@@ -63,160 +64,165 @@ __device__ __forceinline__ void load_weights(const HeadArgs& a, int part, const 
     }
 }
 
-// Bound by HBM and by the latency of few values in flight: 24 warps on an SM
-// with one head of a lane's group ahead.
-template <int TYPE, int L, bool VEC>
-__global__ void __launch_bounds__(kHnThreads, TYPE == ESB_F32 ? 2 : 3) headnorm_kernel(const HeadArgs a)
+// Bound by HBM and by the latency of few values in flight: 16 warps on an SM
+// with kHnAhead heads of a lane's group ahead.
+template <int TYPE, int L, int MODE>
+__global__ void __launch_bounds__(kHnThreads, kHnBlocks) headnorm_kernel(const HeadArgs a)
 {
     using T = Elem<TYPE>;
     griddep_wait();
     const PairPlace p((threadIdx.x % L) * 8, a.D / 2, a.rot);
-    float wa[8], wb[8], c[8], s[8];
-    int weights = -1;
-    HeadWalk<L, kHnWarps> at = {}, to = {};   // where the work is, where the loads are
-    RawPairs<T, VEC> next;
-    int64_t next_pos = 0, at_pos;
-    auto load = [&]() {
-        const HeadPart& part = a.part[to.part];
-        if (to.it == 0) next_pos = a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
-        next.load(static_cast<const T*>(part.x) + (to.on ? to.token * part.ldx + (int64_t)to.head * a.D : 0), p, a.rot, to.on);
-    };
-    to.start(a.work);
-    load();
-    at = to;
-    while (at.more(a.work)) {
-        const RawPairs<T, VEC> raw = next;
-        at_pos = next_pos;
-        to.next(a.work);
-        load();
-        if (at.it == 0) {
-            if (a.rot.dim && at.token < a.work.tokens) load_turn(a.rot, a.tvec, p, at_pos, c, s);
-            if (at.part != weights) load_weights(a, weights = at.part, p, wa, wb);
-        }
-        float u[8], v[8];
-        raw.values(p, u, v);
-        float ss = 0.0f;
+    const bool turns = MODE == kPairHalves || (a.rot.dim && p.j0 < p.half);
+#pragma unroll 1
+    for (int k = 0; k < 2; k++) {
+        HeadWalk<L, kHnWarps> to(a.work, k);
+        if (!to.more()) continue;
+        const T* x = static_cast<const T*>(a.part[k].x);
+        T* y = static_cast<T*>(a.part[k].y);
+        float* rstds = a.part[k].rstd_out;
+        const int64_t ldx = a.part[k].ldx, ldy = a.part[k].ldy;
+        float wa[8], wb[8], c[8], s[8];
+        load_weights(a, k, p, wa, wb);
+        RawPairs<T, MODE> next[kHnAhead];
+        HeadAt there[kHnAhead];
+        auto load = [&](int i) {
+            there[i] = HeadAt(to);
+            there[i].pos = there[i].first && a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
+            next[i].load(x + (to.on ? to.token * ldx + to.head * a.D : 0), p, a.rot, to.on);
+            to.next();
+        };
 #pragma unroll
-        for (int i = 0; i < 8; i++) ss = fmaf(u[i], u[i], fmaf(v[i], v[i], ss));
-        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(fmaf(group_sum<L>(ss), a.inv_d, a.eps)));
-        if (at.on) {
-            const HeadPart& part = a.part[at.part];
-            if (part.rstd_out && p.j0 == 0) part.rstd_out[at.token * part.heads + at.head] = rstd;
+        for (int i = 0; i < kHnAhead; i++) load(i);
+        while (there[0].more) {
+            const RawPairs<T, MODE> raw = next[0];
+            const HeadAt at = there[0];
+            const int64_t pos = at.pos;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u[i] *= rstd * wa[i];
-                v[i] *= rstd * wb[i];
+            for (int i = 0; i + 1 < kHnAhead; i++) {
+                next[i] = next[i + 1];
+                there[i] = there[i + 1];
             }
-            if (a.rot.dim && p.j0 < p.half) {
+            load(kHnAhead - 1);
+            if (at.first && turns) load_turn(a.rot, a.tvec, p, pos, c, s);
+            float u[8], v[8];
+            raw.values(p, u, v);
+            Pair ss = pair_of(0.0f, 0.0f);
 #pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const float x = u[i];
-                    u[i] = fmaf(x, c[i], -(v[i] * s[i]));
-                    v[i] = fmaf(v[i], c[i], x * s[i]);
+            for (int i = 0; i < 8; i += 2) {
+                const Pair q = pair_of(u[i], u[i + 1]), r = pair_of(v[i], v[i + 1]);
+                ss = fma2(q, q, fma2(r, r, ss));
+            }
+            float s0, s1;
+            split(ss, s0, s1);
+            const float rstd = rsqrt_of(fmaf(group_sum<L>(s0 + s1), a.inv_d, a.eps));
+            if (at.on) {
+                if (rstds && p.j0 == 0) rstds[(int64_t)at.token * to.heads + at.head] = rstd;
+                const Pair rr = pair_of(rstd, rstd);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    split(mul2(mul2(rr, pair_of(wa[i], wa[i + 1])), pair_of(u[i], u[i + 1])), u[i], u[i + 1]);
+                    split(mul2(mul2(rr, pair_of(wb[i], wb[i + 1])), pair_of(v[i], v[i + 1])), v[i], v[i + 1]);
                 }
+                if (turns) turn_pairs<false>(u, v, c, s);
+                store_pairs<T, MODE>(y + at.token * ldy + at.head * a.D, p, a.rot, u, v);
             }
-            store_pairs<T, VEC>(static_cast<T*>(part.y) + at.token * part.ldy + (int64_t)at.head * a.D, p, a.rot, u, v);
         }
-        at = to;
     }
 }
 
-template <int TYPE, int L, bool VEC>
-__global__ void __launch_bounds__(kHnThreads, kHnGradBlocks) headnorm_grad_kernel(const HeadArgs a)
+template <int TYPE, int L, int MODE>
+__global__ void __launch_bounds__(kHnThreads, kHnBlocks) headnorm_grad_kernel(const HeadArgs a)
 {
     using T = Elem<TYPE>;
     __shared__ float sums[kHnWarps][2][256];
     griddep_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const PairPlace p((lane % L) * 8, a.D / 2, a.rot);
-    for (int i = threadIdx.x; i < kHnWarps * 2 * 256; i += kHnThreads) (&sums[0][0][0])[i] = 0.0f;
-    __syncthreads();
-    float wa[8], wb[8], c[8], s[8], da[8], db[8];
+    const bool turns = MODE == kPairHalves || (a.rot.dim && p.j0 < p.half);
+#pragma unroll 1
+    for (int k = 0; k < 2; k++) {
+        HeadWalk<L, kHnWarps> to(a.work, k);
+        const T *x = static_cast<const T*>(a.part[k].x), *dy = static_cast<const T*>(a.part[k].dy);
+        T* dx = static_cast<T*>(a.part[k].y);
+        const float* rstds = a.part[k].rstd_in;
+        const int64_t ldx = a.part[k].ldx, ldg = a.part[k].ldg, lddx = a.part[k].ldy;
+        float wa[8], wb[8], c[8], s[8];
+        Pair da[4], db[4];
+        load_weights(a, k, p, wa, wb);
 #pragma unroll
-    for (int i = 0; i < 8; i++) da[i] = db[i] = 0.0f;
-    int weights = -1;
-    auto flush = [&]() {
+        for (int i = 0; i < 4; i++) da[i] = db[i] = pair_of(0.0f, 0.0f);
+        RawPairs<T, MODE> next_x, next_g;
+        float next_r = 0.0f;
+        HeadAt there;
+        auto load = [&]() {
+            there = HeadAt(to);
+            there.pos = there.first && a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
+            const int h = to.head * a.D;
+            next_x.load(x + (to.on ? to.token * ldx + h : 0), p, a.rot, to.on);
+            next_g.load(dy + (to.on ? to.token * ldg + h : 0), p, a.rot, to.on);
+            next_r = to.on ? rstds[(int64_t)to.token * to.heads + to.head] : 0.0f;   // a head that is not there adds nothing
+            to.next();
+        };
+        there = HeadAt(to);
+        if (there.more) load();
+        while (there.more) {
+            const RawPairs<T, MODE> rx = next_x, rg = next_g;
+            const float rstd = next_r;
+            const HeadAt at = there;
+            load();
+            if (at.first && turns) load_turn(a.rot, a.tvec, p, at.pos, c, s);
+            float u[8], v[8], g[8], h[8];
+            rx.values(p, u, v);
+            rg.values(p, g, h);
+            if (turns && at.on) turn_pairs<true>(g, h, c, s);
+            const Pair rr = pair_of(rstd, rstd);
+            Pair dots = pair_of(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                // n, the weights' sums, g weight
+                const Pair n0 = mul2(pair_of(u[i], u[i + 1]), rr), n1 = mul2(pair_of(v[i], v[i + 1]), rr);
+                const Pair g0 = pair_of(g[i], g[i + 1]), g1 = pair_of(h[i], h[i + 1]);
+                da[i / 2] = fma2(g0, n0, da[i / 2]);
+                db[i / 2] = fma2(g1, n1, db[i / 2]);
+                const Pair e0 = mul2(g0, pair_of(wa[i], wa[i + 1])), e1 = mul2(g1, pair_of(wb[i], wb[i + 1]));
+                dots = fma2(e0, n0, fma2(e1, n1, dots));
+                split(n0, u[i], u[i + 1]);
+                split(n1, v[i], v[i + 1]);
+                split(e0, g[i], g[i + 1]);
+                split(e1, h[i], h[i + 1]);
+            }
+            float d0, d1;
+            split(dots, d0, d1);
+            const float dot = group_sum<L>(d0 + d1) * a.inv_d;
+            if (at.on) {
+                const Pair minus = pair_of(-dot, -dot);
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    split(mul2(rr, fma2(pair_of(u[i], u[i + 1]), minus, pair_of(g[i], g[i + 1]))), u[i], u[i + 1]);
+                    split(mul2(rr, fma2(pair_of(v[i], v[i + 1]), minus, pair_of(h[i], h[i + 1]))), v[i], v[i + 1]);
+                }
+                store_pairs<T, MODE>(dx + at.token * lddx + at.head * a.D, p, a.rot, u, v);
+            }
+        }
+        // this warp's sums: its lanes' groups joined
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            float x = da[i], y = db[i];
+            float x0, x1, y0, y1;
+            split(da[i / 2], x0, x1);
+            split(db[i / 2], y0, y1);
+            float xs = i & 1 ? x1 : x0, ys = i & 1 ? y1 : y0;
 #pragma unroll
             for (int o = L; o < 32; o <<= 1) {
-                x += __shfl_xor_sync(0xffffffffu, x, o);
-                y += __shfl_xor_sync(0xffffffffu, y, o);
+                xs += __shfl_xor_sync(0xffffffffu, xs, o);
+                ys += __shfl_xor_sync(0xffffffffu, ys, o);
             }
             if (lane < L && i < p.count) {
-                sums[warp][weights][p.first(i, a.rot)] = x;
-                sums[warp][weights][p.second(i, a.rot)] = y;
-            }
-            da[i] = db[i] = 0.0f;
-        }
-    };
-    HeadWalk<L, kHnWarps> at = {}, to = {};
-    RawPairs<T, VEC> next_x, next_g;
-    float next_r;
-    int64_t next_pos = 0, at_pos;
-    auto load = [&]() {
-        const HeadPart& part = a.part[to.part];
-        if (to.it == 0) next_pos = a.rot.dim && to.on ? __ldg(a.positions + to.token) : 0;
-        const int64_t h = to.on ? (int64_t)to.head * a.D : 0, t = to.on ? to.token : 0;
-        next_x.load(static_cast<const T*>(part.x) + t * part.ldx + h, p, a.rot, to.on);
-        next_g.load(static_cast<const T*>(part.dy) + t * part.ldg + h, p, a.rot, to.on);
-        next_r = to.on ? part.rstd_in[to.token * part.heads + to.head] : 0.0f;
-    };
-    to.start(a.work);
-    load();
-    at = to;
-    while (at.more(a.work)) {
-        const RawPairs<T, VEC> rx = next_x, rg = next_g;
-        const float rstd = next_r;
-        at_pos = next_pos;
-        to.next(a.work);
-        load();
-        if (at.it == 0) {
-            if (a.rot.dim && at.token < a.work.tokens) load_turn(a.rot, a.tvec, p, at_pos, c, s);
-            if (at.part != weights) {
-                if (weights >= 0) flush();
-                load_weights(a, weights = at.part, p, wa, wb);
+                sums[warp][k][p.first(i, a.rot)] = xs;
+                sums[warp][k][p.second(i, a.rot)] = ys;
             }
         }
-        float u[8], v[8], g[8], h[8];
-        rx.values(p, u, v);
-        rg.values(p, g, h);
-        if (a.rot.dim && p.j0 < p.half) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float x = g[i];
-                g[i] = fmaf(x, c[i], h[i] * s[i]);
-                h[i] = fmaf(h[i], c[i], -(x * s[i]));
-            }
-        }
-        float dot = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            u[i] *= rstd;               // n
-            v[i] *= rstd;
-            if (at.on) {
-                da[i] = fmaf(g[i], u[i], da[i]);
-                db[i] = fmaf(h[i], v[i], db[i]);
-            }
-            g[i] *= wa[i];
-            h[i] *= wb[i];
-            dot = fmaf(g[i], u[i], fmaf(h[i], v[i], dot));
-        }
-        dot = group_sum<L>(dot) * a.inv_d;
-        if (at.on) {
-            const HeadPart& part = a.part[at.part];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                u[i] = rstd * fmaf(-u[i], dot, g[i]);
-                v[i] = rstd * fmaf(-v[i], dot, h[i]);
-            }
-            store_pairs<T, VEC>(static_cast<T*>(part.y) + at.token * part.ldy + (int64_t)at.head * a.D, p, a.rot, u, v);
-        }
-        at = to;
     }
     if (!a.partial) return;
-    if (weights >= 0) flush();
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.D; i += kHnThreads) {
         const int k = i >= a.D, e = i - k * a.D;
@@ -251,21 +257,22 @@ int64_t blocks_of(const HeadArgs& a, int64_t most)
 }
 
 using HnKernel = void (*)(const HeadArgs);
-template <int TYPE, bool VEC> HnKernel norm_kernel(int L)
+template <int TYPE, int L> HnKernel kernel_of(int mode, bool grad)
 {
-    switch (L) {
-    case 4: return headnorm_kernel<TYPE, 4, VEC>;
-    case 8: return headnorm_kernel<TYPE, 8, VEC>;
-    default: return headnorm_kernel<TYPE, 16, VEC>;
+    switch (mode) {
+    case kPairHalves: return grad ? headnorm_grad_kernel<TYPE, L, kPairHalves> : headnorm_kernel<TYPE, L, kPairHalves>;
+    case kPairRows: return grad ? headnorm_grad_kernel<TYPE, L, kPairRows> : headnorm_kernel<TYPE, L, kPairRows>;
+    case kPairMixed: return grad ? headnorm_grad_kernel<TYPE, L, kPairMixed> : headnorm_kernel<TYPE, L, kPairMixed>;
+    default: return grad ? headnorm_grad_kernel<TYPE, L, kPairAny> : headnorm_kernel<TYPE, L, kPairAny>;
     }
 }
-template <int TYPE, bool VEC> HnKernel grad_kernel(int L)
+template <int TYPE> HnKernel kernel_of(int L, int mode, bool grad)
 {
-    switch (L) {
-    case 4: return headnorm_grad_kernel<TYPE, 4, VEC>;
-    case 8: return headnorm_grad_kernel<TYPE, 8, VEC>;
-    default: return headnorm_grad_kernel<TYPE, 16, VEC>;
-    }
+    return L == 4 ? kernel_of<TYPE, 4>(mode, grad) : L == 8 ? kernel_of<TYPE, 8>(mode, grad) : kernel_of<TYPE, 16>(mode, grad);
+}
+HnKernel kernel_of(int type, int L, int mode, bool grad)
+{
+    return type == ESB_F32 ? kernel_of<ESB_F32>(L, mode, grad) : type == ESB_F16 ? kernel_of<ESB_F16>(L, mode, grad) : kernel_of<ESB_BF16>(L, mode, grad);
 }
 
 }  // namespace
@@ -273,7 +280,7 @@ template <int TYPE, bool VEC> HnKernel grad_kernel(int L)
 cudaError_t launch_headnorm(int64_t tokens, const esb_head_norm& n, cudaStream_t st)
 {
     HeadArgs a = {};
-    bool vec = pairs_of_vectors(n.head_dim, n.rotation.dim, n.rotation.interleaved);
+    bool vec = true;
     for (int k = 0; k < 2; k++) {
         const esb_heads& h = n.part[k];
         HeadPart& p = a.part[k];
@@ -286,25 +293,23 @@ cudaError_t launch_headnorm(int64_t tokens, const esb_head_norm& n, cudaStream_t
     a.D = n.head_dim;
     a.w_type = n.w_type; a.tvec = a.rot.vec; a.eps = n.eps; a.inv_d = 1.0f / (float)n.head_dim;
     const int L = lanes_of(a.D);
-    const int64_t most = (int64_t)device_sm_count() * (n.x_type == ESB_F32 ? 2 : 3);
+    const int64_t most = (int64_t)device_sm_count() * kHnBlocks;
     a.work = split_heads(tokens, a.part[0].heads, a.part[1].heads, L, most * kHnWarps);
-    static HnKernel (*const pick[3][2])(int) = {{norm_kernel<ESB_F32, false>, norm_kernel<ESB_F32, true>},
-                                                {norm_kernel<ESB_F16, false>, norm_kernel<ESB_F16, true>},
-                                                {norm_kernel<ESB_BF16, false>, norm_kernel<ESB_BF16, true>}};
-    return launch_pdl(pick[n.x_type][vec](L), dim3((unsigned)blocks_of(a, most)), dim3(kHnThreads), 0, st, a);
+    const int mode = pair_mode(a.D, a.rot.dim, a.rot.inter, vec);
+    return launch_pdl(kernel_of(n.x_type, L, mode, false), dim3((unsigned)blocks_of(a, most)), dim3(kHnThreads), 0, st, a);
 }
 
 // A part of the sums for every block that there may be.
 size_t headnorm_grad_workspace_bytes(int64_t tokens, int64_t heads, int head_dim)
 {
     const int64_t rows = (tokens * heads + kHnWarps - 1) / kHnWarps + 1;
-    return sizeof(float) * 2 * (size_t)head_dim * (size_t)std::min<int64_t>(rows, (int64_t)kHnGradBlocks * device_sm_count());
+    return sizeof(float) * 2 * (size_t)head_dim * (size_t)std::min<int64_t>(rows, (int64_t)device_sm_count() * kHnBlocks);
 }
 
 cudaError_t launch_headnorm_grad(int64_t tokens, const esb_head_norm_grad& n, void* workspace, cudaStream_t st)
 {
     HeadArgs a = {};
-    bool vec = pairs_of_vectors(n.head_dim, n.rotation.dim, n.rotation.interleaved), sums = false;
+    bool vec = true, sums = false;
     for (int k = 0; k < 2; k++) {
         const esb_heads_grad& h = n.part[k];
         HeadPart& p = a.part[k];
@@ -320,13 +325,11 @@ cudaError_t launch_headnorm_grad(int64_t tokens, const esb_head_norm_grad& n, vo
     a.w_type = n.w_type; a.tvec = a.rot.vec; a.inv_d = 1.0f / (float)n.head_dim;
     a.partial = sums ? static_cast<float*>(workspace) : nullptr;
     const int L = lanes_of(a.D);
-    const int64_t most = (int64_t)kHnGradBlocks * device_sm_count();
+    const int64_t most = (int64_t)device_sm_count() * kHnBlocks;
     a.work = split_heads(tokens, a.part[0].heads, a.part[1].heads, L, most * kHnWarps);
     const int blocks = (int)blocks_of(a, most);
-    static HnKernel (*const pick[3][2])(int) = {{grad_kernel<ESB_F32, false>, grad_kernel<ESB_F32, true>},
-                                                {grad_kernel<ESB_F16, false>, grad_kernel<ESB_F16, true>},
-                                                {grad_kernel<ESB_BF16, false>, grad_kernel<ESB_BF16, true>}};
-    cudaError_t e = launch_pdl(pick[n.x_type][vec](L), dim3((unsigned)blocks), dim3(kHnThreads), 0, st, a);
+    const int mode = pair_mode(a.D, a.rot.dim, a.rot.inter, vec);
+    cudaError_t e = launch_pdl(kernel_of(n.x_type, L, mode, true), dim3((unsigned)blocks), dim3(kHnThreads), 0, st, a);
     if (e != cudaSuccess || !sums) return e;
     return launch_pdl(headnorm_dweight_kernel, dim3((unsigned)((2 * a.D + 31) / 32)), dim3(1024), 0, st,
                       static_cast<const float*>(a.partial), blocks, a.D, a.part[0].dweight, a.part[1].dweight);

@@ -11,7 +11,12 @@
 
 namespace esb {
 
-// The pairs that a lane holds: (first, first + i) of `count`.
+// How a lane's 8 pairs lie in memory: two vectors half a rotation apart, 16
+// values in a row (neighbouring pairs, or none), either by the lane (a part of
+// the head is not rotated), or no vectors at all.
+enum { kPairHalves, kPairRows, kPairMixed, kPairAny };
+
+// The pairs that a lane holds: (first, second) of `count` from pair j0 on.
 struct PairPlace {
     int j0, count;
     bool rows;                          // neighbours in memory: 16 values in a row
@@ -25,19 +30,41 @@ struct PairPlace {
     }
     __device__ __forceinline__ int first(int i, const RotArgs& r) const { return r.inter || j0 + i >= half ? 2 * (j0 + i) : j0 + i; }
     __device__ __forceinline__ int second(int i, const RotArgs& r) const { return r.inter || j0 + i >= half ? 2 * (j0 + i) + 1 : j0 + i + half; }
+    // the lane's two vectors
+    template <int MODE> __device__ __forceinline__ bool in_rows() const { return MODE == kPairRows || (MODE == kPairMixed && rows); }
+    template <int MODE> __device__ __forceinline__ int vec0() const { return in_rows<MODE>() ? 2 * j0 : j0; }
+    template <int MODE> __device__ __forceinline__ int vec1() const { return in_rows<MODE>() ? 2 * j0 + 8 : j0 + half; }
 };
 
+// 16 values in a row to 8 pairs, and back.
+__device__ __forceinline__ void rows_to_pairs(const float (&x)[8], const float (&y)[8], float (&a)[8], float (&b)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        a[i] = i < 4 ? x[(2 * i) & 7] : y[(2 * i) & 7];
+        b[i] = i < 4 ? x[(2 * i + 1) & 7] : y[(2 * i + 1) & 7];
+    }
+}
+__device__ __forceinline__ void pairs_to_rows(const float (&a)[8], const float (&b)[8], float (&x)[8], float (&y)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        x[i] = (i & 1) ? b[i / 2] : a[i / 2];
+        y[i] = (i & 1) ? b[4 + i / 2] : a[4 + i / 2];
+    }
+}
+
 // A lane's 16 values as they lie in memory.
-template <class T, bool VEC>
+template <class T, int MODE>
 struct RawPairs {
     Raw8<T> u, w;
+    // x: the head's first value
     __device__ __forceinline__ void load(const T* x, const PairPlace& p, const RotArgs& r, bool on)
     {
-        if constexpr (VEC) {
+        if constexpr (MODE != kPairAny) {
             const bool in = on && p.count > 0;
-            const int at = p.rows ? 2 * p.j0 : p.j0;
-            u.load(x + at, in ? 8 : 0, true);
-            w.load(x + (p.rows ? at + 8 : at + p.half), in ? 8 : 0, true);
+            u.load(x + p.vec0<MODE>(), in ? 8 : 0, true);
+            w.load(x + p.vec1<MODE>(), in ? 8 : 0, true);
         } else {
             uint32_t a[8], b[8];
 #pragma unroll
@@ -61,32 +88,31 @@ struct RawPairs {
     }
     __device__ __forceinline__ void values(const PairPlace& p, float (&a)[8], float (&b)[8]) const
     {
-        float x[8], y[8];
-        u.values(x);
-        w.values(y);
+        u.values(a);
+        w.values(b);
+        if (p.in_rows<MODE>()) {
+            float x[8], y[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const bool rows = VEC && p.rows;
-            a[i] = rows ? (i < 4 ? x[(2 * i) & 7] : y[(2 * i) & 7]) : x[i];
-            b[i] = rows ? (i < 4 ? x[(2 * i + 1) & 7] : y[(2 * i + 1) & 7]) : y[i];
+            for (int i = 0; i < 8; i++) { x[i] = a[i]; y[i] = b[i]; }
+            rows_to_pairs(x, y, a, b);
         }
     }
 };
 
-template <class T, bool VEC>
+template <class T, int MODE>
 __device__ __forceinline__ void store_pairs(T* y, const PairPlace& p, const RotArgs& r, const float (&a)[8], const float (&b)[8])
 {
-    if constexpr (VEC) {
+    if constexpr (MODE != kPairAny) {
         if (p.count <= 0) return;
-        float u[8], w[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            u[i] = p.rows ? ((i & 1) ? b[i / 2] : a[i / 2]) : a[i];
-            w[i] = p.rows ? ((i & 1) ? b[4 + i / 2] : a[4 + i / 2]) : b[i];
+        if (p.in_rows<MODE>()) {
+            float u[8], w[8];
+            pairs_to_rows(a, b, u, w);
+            store8<T>(y + 2 * p.j0, u);
+            store8<T>(y + 2 * p.j0 + 8, w);
+        } else {
+            store8<T>(y + p.j0, a);
+            store8<T>(y + p.j0 + p.half, b);
         }
-        const int at = p.rows ? 2 * p.j0 : p.j0;
-        store8<T>(y + at, u);
-        store8<T>(y + (p.rows ? at + 8 : at + p.half), w);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
@@ -134,45 +160,85 @@ struct HeadWork {
     int64_t tokens;
 };
 
-// Where a lane's group stands: item, head in it, and what that is.  All items of
-// the first part come before those of the second, so a warp changes what it
-// keeps of a part (weights, sums) once.  WARPS: of a block.
+// A warp's way through a part's items: where its lanes' group stands, one head
+// after the other.  The grid's warps take the items of both parts in turn, as
+// one row of them.
 template <int L, int WARPS>
 struct HeadWalk {
-    int64_t item, token;
-    int it, part, head;
-    bool on;
-    __device__ __forceinline__ void start(const HeadWork& a)
+    uint32_t row, rows, drow, token, tokens;    // there are fewer than 2^31 tokens
+    int chunk, dchunk, chunks, side, iter, heads, it, head;
+    bool on;                            // there is a head here for this group
+    __device__ __forceinline__ HeadWalk(const HeadWork& w, int k)
     {
-        item = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
+        const HeadSplit& s = w.part[k];
+        const int64_t warp = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5), warps = (int64_t)gridDim.x * WARPS;
+        int64_t first = warp;
+        if (k) {
+            const int64_t before = w.part[0].items % warps;
+            first = warp >= before ? warp - before : warp + warps - before;
+        }
+        chunks = s.chunks; side = s.side; iter = s.iter; heads = s.heads; tokens = (uint32_t)w.tokens;
+        rows = (uint32_t)(s.items / chunks);
+        row = (uint32_t)(first / chunks);
+        chunk = (int)(first - (int64_t)row * chunks);
+        drow = (uint32_t)(warps / chunks);
+        dchunk = (int)(warps - (int64_t)drow * chunks);
         it = 0;
-        place(a);
+        place();
     }
-    __device__ __forceinline__ void place(const HeadWork& a)
+    __device__ __forceinline__ void place()
     {
         const int group = (threadIdx.x & 31) / L;
-        part = item >= a.part[0].items;
-        const HeadSplit& s = a.part[part];
-        const int64_t i = part ? item - a.part[0].items : item, row = i / s.chunks;
-        const int side = s.side;
         token = row * (32 / L / side) + group / side;
-        head = ((int)(i - row * s.chunks) * s.iter + it) * side + group % side;
-        on = item < a.part[0].items + a.part[1].items && token < a.tokens && head < a.part[part].heads;
+        head = chunk * iter * side + group % side;
+        on = row < rows && token < tokens && head < heads;
     }
-    // the next head of the item, or the next item
-    __device__ __forceinline__ void next(const HeadWork& a)
+    __device__ __forceinline__ bool more() const { return row < rows; }
+    __device__ __forceinline__ void next()
     {
-        if (++it < a.part[part].iter) {
-            head += a.part[part].side;
-            on = on && head < a.part[part].heads;
+        if (++it < iter) {
+            head += side;
+            on = on && head < heads;
             return;
         }
         it = 0;
-        item += (int64_t)gridDim.x * WARPS;
-        place(a);
+        row += drow;
+        chunk += dchunk;
+        if (chunk >= chunks) { chunk -= chunks; row++; }
+        place();
     }
-    __device__ __forceinline__ bool more(const HeadWork& a) const { return item < a.part[0].items + a.part[1].items; }
 };
+// A place on it.
+struct HeadAt {
+    uint32_t token;
+    int head;
+    bool on, first, more;               // first: of an item
+    int64_t pos, slot;                  // of its token (in the first head of an item)
+    HeadAt() = default;
+    template <class W>
+    __device__ __forceinline__ explicit HeadAt(const W& w) : token(w.token), head(w.head), on(w.on), first(w.it == 0), more(w.more()), pos(0), slot(-1) {}
+};
+
+// 1 / sqrt(x): the hardware's, and one step that leaves two units in the last place.
+__device__ __forceinline__ float rsqrt_of(float x)
+{
+    float r;
+    asm("rsqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return x > 0.0f && x < __int_as_float(0x7f800000) ? fmaf(0.5f * r, fmaf(-x * r, r, 1.0f), r) : r;
+}
+
+// Pairs (a, b) turned: (a c - b s, b c + a s), two at a time; back: the other way.
+template <bool BACK>
+__device__ __forceinline__ void turn_pairs(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const Pair x = pair_of(a[i], a[i + 1]), y = pair_of(b[i], b[i + 1]), cc = pair_of(c[i], c[i + 1]);
+        const Pair sp = pair_of(s[i], s[i + 1]), sm = pair_of(-s[i], -s[i + 1]);
+        split(fma2(x, cc, mul2(y, BACK ? sp : sm)), a[i], a[i + 1]);
+        split(fma2(y, cc, mul2(x, BACK ? sm : sp)), b[i], b[i + 1]);
+    }
+}
 
 // Heads side by side and one after the other.  An item costs its heads and some
 // half of one for its token's cos and sin; the grid's last round should be full.
@@ -204,8 +270,13 @@ inline HeadWork split_heads(int64_t tokens, int heads0, int heads1, int L, int64
 
 inline int lanes_of(int D) { return D <= 64 ? 4 : D <= 128 ? 8 : 16; }
 
-// A lane's values are two vectors: whole eights of pairs on both sides of the rotation's end.
-inline bool pairs_of_vectors(int D, int rot_dim, bool interleaved) { return D % 16 == 0 && (interleaved || rot_dim % 16 == 0); }
+// How lanes hold pairs: by vectors where there are whole eights of pairs on both
+// sides of the rotation's end.
+inline int pair_mode(int D, int rot_dim, bool interleaved, bool vectors)
+{
+    if (!vectors || D % 16 != 0 || (!interleaved && rot_dim % 16 != 0)) return kPairAny;
+    return interleaved || rot_dim == 0 ? kPairRows : rot_dim == D ? kPairHalves : kPairMixed;
+}
 
 inline bool rows16(const void* p, int64_t ld, int type)
 {

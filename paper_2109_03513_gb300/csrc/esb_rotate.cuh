@@ -41,6 +41,16 @@ __device__ __forceinline__ float dot2_rn(float a, float c, float b, float s)
     return __fadd_rn(r, __fadd_rn(e, __fadd_rn(pe, qe)));
 }
 
+__device__ __forceinline__ Pair dot2_rn(const Pair& a, const Pair& c, const Pair& b, const Pair& s)
+{
+    const Pair minus = pair_of(-1.0f, -1.0f);
+    const Pair p = mul2(a, c), q = mul2(b, s);
+    const Pair pe = fma2(a, c, mul2(p, minus)), qe = fma2(b, s, mul2(q, minus));
+    const Pair r = add2(p, q), z = fma2(p, minus, r);
+    const Pair e = add2(fma2(fma2(z, minus, r), minus, p), fma2(z, minus, q));
+    return add2(r, add2(e, add2(pe, qe)));
+}
+
 // cos and sin of pair j of a position (NaN for a position that the table lacks).
 __device__ __forceinline__ void rot_at(const RotArgs& r, int64_t pos, int j, float& c, float& s)
 {
