@@ -102,6 +102,20 @@ __device__ __forceinline__ void copy4(uint32_t to, const void* from)
 __device__ __forceinline__ void copies_end_stage() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+template <int N>
+__device__ __forceinline__ void lds(uint32_t at, uint32_t (&w)[N])
+{
+    if constexpr (N == 1) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+    else asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ float lds_f32(uint32_t at)
+{
+    uint32_t w[1];
+    lds(at, w);
+    return __uint_as_float(w[0]);
+}
+
 // Eight codes to four pairs of fp16 numbers, codes i and i + 4 in pair i.
 // LIN, sets of one spacing (k = 2, 3): a number is its place among 0..7 with a
 // sign, and a place in bits 8..10 of an fp16 number is that many 2^-16 (below
@@ -346,12 +360,18 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     // where this lane's copies of a stage go
     const int copies = kAtPlaces * a.chunks;
     uint32_t to[W / 8];
+    bool mine[W / 8];
 #pragma unroll
     for (int i = 0; i < W / 8; i++) {
         const int c = lane + 32 * i;
-        to[i] = c < copies ? St::at(c / a.chunks, c % a.chunks) : 0xffffffffu;
+        mine[i] = c < copies;
+        to[i] = mine[i] ? St::at(c / a.chunks, c % a.chunks) : 0u;
     }
-    const uint32_t my_ring = smem_u32(ring) + warp * ST * St::kBytes;
+    const uint32_t my_ring = smem_u32(ring) + warp * ST * St::kBytes, ring_end = my_ring + ST * St::kBytes;
+    // and where it reads: rows g (and 8 further) of K, rows 2 t and 2 t + 1 of V
+    const uint32_t k_from = DP == 64 ? St::at(g, t >> 1) + (t & 1) * 8 : St::at(g, t);
+    const uint32_t v_in = DP == 64 ? (g & 3) * 4 : DP == 128 ? (g & 1) * 8 : 0, v_chunk = DP == 64 ? g >> 2 : DP == 128 ? g >> 1 : g;
+    const uint32_t v_from0 = St::kV + St::at(2 * t, v_chunk) + v_in, v_from1 = St::kV + St::at(2 * t + 1, v_chunk) + v_in;
 
     while (left > 0) {
         const Seq s = sequence(a, b);
@@ -373,29 +393,27 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             return i < stages ? __ldg(table + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size)) : -1;
         };
         int next_page = page_at(0, place0), issued = 0, issue_place = place0;
-        uint32_t issue_to = 0u, there = 0u;             // the ring's next stage; which of its stages hold a page that is there
+        uint32_t issue_to = my_ring, there = 0u;        // the ring's next stage; which of the last stages hold a page that is there
         auto issue = [&]() {
             const int page = next_page, p = issue_place;
             issue_place += kAtBlock;
             next_page = page_at(++issued, issue_place);
-            const uint32_t bit = 1u << issue_to;
-            there &= ~bit;
-            if (page >= 0 && page < a.npages) {
-                there |= bit;
+            there *= 2u;
+            if ((uint32_t)page < (uint32_t)a.npages) {
+                there++;
                 const int in = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
                 const uint64_t at = (uint64_t)(uint32_t)page * a.page16 + (uint32_t)(in * a.chunks);
-                const uint32_t base = my_ring + issue_to * St::kBytes;
                 const char *k = kg + at * 16, *v = vg + at * 16;
 #pragma unroll
                 for (int c = 0; c < W / 8; c++)
-                    if (to[c] != 0xffffffffu) {
-                        copy16(base + to[c], k + 512 * c);
-                        copy16(base + St::kV + to[c], v + 512 * c);
+                    if (mine[c]) {
+                        copy16(issue_to + to[c], k + 512 * c);
+                        copy16(issue_to + to[c] + St::kV, v + 512 * c);
                     }
-                copy4(base + St::kKs + 4 * lane, sg + (uint64_t)(uint32_t)page * a.page_lds + in);
+                copy4(issue_to + St::kKs + 4 * lane, sg + (uint64_t)(uint32_t)page * a.page_lds + in);
             }
             copies_end_stage();
-            issue_to = issue_to == ST - 1 ? 0u : issue_to + 1u;
+            issue_to = issue_to + St::kBytes == ring_end ? my_ring : issue_to + St::kBytes;
         };
 #pragma unroll
         for (int i = 0; i < ST - 1; i++) issue();
@@ -488,13 +506,13 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 #pragma unroll
                 for (int c = 0; c < 4; c++) o[i][nt][c] = 0.0f;
 
-        uint32_t use = 0u;
+        uint32_t use = my_ring;
         for (int i = 0, place = place0; i < stages; i++, place += kAtBlock) {
             copies_wait<ST - 2>();
             __syncwarp();                               // every lane's copies of this stage; all have read the one before
-            const bool here = there >> use & 1u;
-            const unsigned char* sm = ring + (warp * ST + use) * St::kBytes;
-            use = use == ST - 1 ? 0u : use + 1u;
+            const bool here = there >> (ST - 2) & 1u;
+            const uint32_t sm = use;
+            use = use + St::kBytes == ring_end ? my_ring : use + St::kBytes;
             issue();
             if (!here) continue;
 
@@ -510,20 +528,19 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                     for (int c = 0; c < 4; c++) part[h][nt][c] = 0.0f;
             {
                 uint32_t k0[WK], k1[WK];
-                auto words = [&](int row, uint32_t (&w)[WK]) {
-                    if constexpr (DP == 64) {
-                        const uint2 v = *reinterpret_cast<const uint2*>(sm + St::at(row, t >> 1) + (t & 1) * 8);
-                        w[0] = v.x; w[1] = v.y;
-                    } else {
+                auto words = [&](uint32_t at, uint32_t (&w)[WK]) {
+                    if constexpr (DP == 256) {
+                        uint32_t x[4], y[4];
+                        lds(at, x);
+                        lds(at ^ 64u, y);               // chunk t + 4
 #pragma unroll
-                        for (int h = 0; h < WK / 4; h++) {
-                            const uint4 v = *reinterpret_cast<const uint4*>(sm + St::at(row, t + 4 * h));
-                            w[4 * h] = v.x; w[4 * h + 1] = v.y; w[4 * h + 2] = v.z; w[4 * h + 3] = v.w;
-                        }
+                        for (int i = 0; i < 4; i++) { w[i] = x[i]; w[(4 + i) % WK] = y[i]; }
+                    } else {
+                        lds(at, w);
                     }
                 };
-                words(g, k0);
-                words(g + 8, k1);
+                words(sm + k_from, k0);
+                words(sm + k_from + 8 * St::kRow, k1);
 #pragma unroll
                 for (int k = 0; k < WK; k++) {
                     uint32_t x[4], y[4];
@@ -543,8 +560,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                             }
                 }
             }
-            const float* scales = reinterpret_cast<const float*>(sm + St::kKs);
-            const float ks0 = scales[g], ks1 = scales[g + 8], vs0 = scales[16 + g], vs1 = scales[24 + g];
+            const uint32_t scales = sm + St::kKs + 4 * g;
+            const float ks0 = lds_f32(scales), ks1 = lds_f32(scales + 32), vs0 = lds_f32(scales + 64), vs1 = lds_f32(scales + 96);
             // log2 of v's scales, where they have one
             const float lv0 = fmaxf(fminf(lg2(fabsf(vs0)), 100.0f), -100.0f), lv1 = fmaxf(fminf(lg2(fabsf(vs1)), 100.0f), -100.0f);
             const bool whole = place + kAtPlaces <= all_hi && place >= all_lo;
@@ -621,18 +638,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             // values: this lane's words of places 2 t, 2 t + 1, 2 t + 8, 2 t + 9
             uint32_t v[4][WV];
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const int row = 2 * t + (k & 1) + 8 * (k >> 1);
-                const unsigned char* vm = sm + St::kV;
-                if constexpr (DP == 64) v[k][0] = *reinterpret_cast<const uint32_t*>(vm + St::at(row, g >> 2) + (g & 3) * 4);
-                else if constexpr (DP == 128) {
-                    const uint2 x = *reinterpret_cast<const uint2*>(vm + St::at(row, g >> 1) + (g & 1) * 8);
-                    v[k][0] = x.x; v[k][1] = x.y;
-                } else {
-                    const uint4 x = *reinterpret_cast<const uint4*>(vm + St::at(row, g));
-                    v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
-                }
-            }
+            for (int k = 0; k < 4; k++) lds(sm + (k & 1 ? v_from1 : v_from0) + 8 * St::kRow * (k >> 1), v[k]);
             // a pair of places' codes of the same four values, the second place's above
             auto pair_codes = [](uint32_t x, uint32_t y, int upper) { return prmt(x, y, upper ? 0x7632u : 0x5410u); };
             if constexpr (WV == 1) {

@@ -1062,38 +1062,37 @@ def esb_headnorm(q: Optional[torch.Tensor], k: Optional[torch.Tensor], head_dim:
     if x0 is None:
         raise ValueError("q or k must be given")
     empty = _empty_on(stream)
-    a = esb_head_norm()
-    a.head_dim, a.eps = head_dim, eps
-    tokens, dtype = x0.shape[0], x0.dtype
-    outs, stats = [], []
-    wt = None
-    for part, name, x, w, y in ((a.part[0], "q", q, q_weight, qy), (a.part[1], "k", k, k_weight, ky)):
+    shape, dtype = x0.shape, x0.dtype
+    tokens, wt = shape[0], 0
+
+    def part(name, x, w, y):
+        nonlocal wt
         if x is None:
-            outs.append(None)
-            stats.append(None)
-            continue
-        a.x_type, part.ldx = _rows(x, name)
-        if x.shape[0] != tokens or x.dtype != dtype:
+            return esb_heads(), None, None
+        _, ldx = _rows(x, name)
+        size = x.shape
+        if size[0] != tokens or x.dtype != dtype:
             raise ValueError("q and k must have the same tokens and type")
-        part.x, part.heads = x.data_ptr(), _head_count(x, name, head_dim)
+        heads, wp = _head_count(x, name, head_dim), None
         if w is not None:
-            part.weight, a.w_type = _weight(w, head_dim)
-            if wt is not None and wt != w.dtype:
+            wp, t = _weight(w, head_dim)
+            if wt and wt != t + 1:
                 raise ValueError("q_weight and k_weight must have one type")
-            wt = w.dtype
+            wt = t + 1
         if y is None:
-            y = empty(x.shape, dtype=dtype, device=x.device)
-        part.ldy = _rows_like(y, name + "y", x.shape, dtype)
-        part.y = y.data_ptr()
-        outs.append(y)
-        r = None
-        if want_rstd:
-            r = empty((tokens, part.heads), dtype=torch.float32, device=x.device)
-            part.rstd = r.data_ptr()
-        stats.append(r)
-    a.rotation, a.positions = _turn(rotation, positions, tokens)
+            y = empty(size, dtype=dtype, device=x.device)
+            ldy = size[1]
+        else:
+            ldy = _rows_like(y, "qy, ky", size, dtype)
+        r = empty((tokens, heads), dtype=torch.float32, device=x.device) if want_rstd else None
+        return esb_heads(x.data_ptr(), ldx, y.data_ptr(), ldy, wp, None if r is None else r.data_ptr(), heads), y, r
+
+    qp, qy, qr = part("q", q, q_weight, qy)
+    kp, ky, kr = part("k", k, k_weight, ky)
+    rot, pos = _turn(rotation, positions, tokens)
+    a = esb_head_norm((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0), eps)
     _check(lib().esb_headnorm(tokens, ctypes.byref(a), _stream(stream)), "esb_headnorm")
-    return HeadNorm(*outs, *stats)
+    return HeadNorm(qy, ky, qr, kr)
 
 
 class HeadNormGrad(NamedTuple):
@@ -1115,55 +1114,56 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
     x0 = q if q is not None else k
     if x0 is None:
         raise ValueError("q or k must be given")
-    empty = _empty_on(stream)
-    a = esb_head_norm_grad()
-    a.head_dim = head_dim
-    tokens, dtype = x0.shape[0], x0.dtype
-    outs, sums = [], []
-    heads, wt = 0, None
-    for part, name, x, g, w, r, d in ((a.part[0], "q", q, gq, q_weight, q_rstd, dq), (a.part[1], "k", k, gk, k_weight, k_rstd, dk)):
+    empty, f32 = _empty_on(stream), torch.float32
+    dtype, tokens = x0.dtype, x0.shape[0]
+    total = wt = 0
+    # gradients of the weights, one after the other
+    sums = None if q_weight is None and k_weight is None else empty((2, head_dim), dtype=f32, device=x0.device)
+
+    def part(i, name, x, g, w, r, d):
+        nonlocal total, wt
         if x is None:
-            outs.append(None)
-            sums.append(None)
-            continue
-        a.x_type, part.ldx = _rows(x, name)
-        if x.shape[0] != tokens or x.dtype != dtype:
+            return esb_heads_grad(), None, None
+        _, ldx = _rows(x, name)
+        size = x.shape
+        if size[0] != tokens or x.dtype != dtype:
             raise ValueError("q and k must have the same tokens and type")
         if g is None or r is None:
-            raise ValueError(f"g{name} and {name}_rstd must be given")
-        part.x, part.heads = x.data_ptr(), _head_count(x, name, head_dim)
-        heads += part.heads
-        part.ldg = _rows_like(g, "g" + name, x.shape, dtype)
-        part.dy = g.data_ptr()
-        if r.shape != (tokens, part.heads) or not r.is_contiguous():
-            raise ValueError(f"{name}_rstd must be contiguous {(tokens, part.heads)} float32")
-        part.rstd = _vector(r.view(-1), name + "_rstd", tokens * part.heads, torch.float32)
-        dw = None
+            raise ValueError("the gradient and rstd of " + name + " must be given")
+        heads, wp, dw, dp = _head_count(x, name, head_dim), None, None, None
+        total += heads
+        ldg = _rows_like(g, "gq, gk", size, dtype)
+        if r.dtype != f32 or r.shape != (tokens, heads) or not r.is_cuda or not r.is_contiguous():
+            raise ValueError("rstd must be contiguous (tokens, heads) float32")
         if w is not None:
-            part.weight, a.w_type = _weight(w, head_dim)
-            if wt is not None and wt != w.dtype:
+            wp, t = _weight(w, head_dim)
+            if wt and wt != t + 1:
                 raise ValueError("q_weight and k_weight must have one type")
-            wt = w.dtype
-            dw = empty(head_dim, dtype=torch.float32, device=x.device)
-            part.dweight = dw.data_ptr()
-        sums.append(dw)
+            wt = t + 1
+            dw = sums[i]
+            dp = dw.data_ptr()
         if d is None:
-            d = empty(x.shape, dtype=dtype, device=x.device)
-        part.lddx = _rows_like(d, "d" + name, x.shape, dtype)
-        part.dx = d.data_ptr()
-        outs.append(d)
-    a.rotation, a.positions = _turn(rotation, positions, tokens)
+            d = empty(size, dtype=dtype, device=x.device)
+            ldd = size[1]
+        else:
+            ldd = _rows_like(d, "dq, dk", size, dtype)
+        return esb_heads_grad(g.data_ptr(), ldg, x.data_ptr(), ldx, r.data_ptr(), wp, d.data_ptr(), ldd, dp, heads), d, dw
+
+    qp, dq, dqw = part(0, "q", q, gq, q_weight, q_rstd, dq)
+    kp, dk, dkw = part(1, "k", k, gk, k_weight, k_rstd, dk)
+    rot, pos = _turn(rotation, positions, tokens)
+    a = esb_head_norm_grad((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0))
     wp, nb = None, 0
-    if any(s is not None for s in sums):
+    if sums is not None:
         if workspace is None:
-            nb = int(lib().esb_headnorm_backward_workspace_bytes(tokens, heads, head_dim))
+            nb = lib().esb_headnorm_backward_workspace_bytes(tokens, total, head_dim)
             workspace = empty(nb, dtype=torch.uint8, device=x0.device)
         else:
             _dev(workspace, "workspace")
             nb = workspace.numel() * workspace.element_size()
         wp = workspace.data_ptr()
     _check(lib().esb_headnorm_backward(tokens, ctypes.byref(a), wp, nb, _stream(stream)), "esb_headnorm_backward")
-    return HeadNormGrad(*outs, *sums)
+    return HeadNormGrad(dq, dk, dqw, dkw)
 
 
 class KvCache(NamedTuple):
@@ -1218,28 +1218,28 @@ def esb_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: to
     page * page_size + place, negative ones left out.  Where two slots are equal the row is not defined.  kq, vq: the
     numbers the codes stand for."""
     c = cache.c()
-    a = esb_append()
-    tokens = k.shape[0]
-    a.x_type, a.ldk = _rows(k, "k")
-    if k.shape[1] != c.heads * c.head_dim:
+    xt, ldk = _rows(k, "k")
+    shape = k.shape
+    tokens = shape[0]
+    if shape[1] != c.heads * c.head_dim:
         raise ValueError("k must have the cache's heads")
-    a.ldv = _rows_like(v, "v", k.shape, k.dtype)
-    a.k, a.v, a.slots = k.data_ptr(), v.data_ptr(), _vector(slots, "slots", tokens, torch.int64)
-    a.rule, a.rounding = rule, rounding
+    ldv = _rows_like(v, "v", shape, k.dtype)
+    kp = vp = pos = r = None
+    qt = ldkq = ldvq = 0
     if kq is not None:
-        a.q_type, a.ldkq = _rows(kq, "kq")
-        a.kq = kq.data_ptr()
-        if kq.shape != k.shape:
+        qt, ldkq = _rows(kq, "kq")
+        kp = kq.data_ptr()
+        if kq.shape != shape:
             raise ValueError("kq must have the shape of k")
     if vq is not None:
-        t, a.ldvq = _rows(vq, "vq")
-        if vq.shape != k.shape or (kq is not None and t != a.q_type):
+        t, ldvq = _rows(vq, "vq")
+        if vq.shape != shape or (kq is not None and t != qt):
             raise ValueError("vq must have the shape of v and the type of kq")
-        a.q_type, a.vq = t, vq.data_ptr()
-    r = None
+        qt, vp = t, vq.data_ptr()
     if rotation is not None:
-        r, a.positions = _turn(rotation, positions, tokens)
-        a.rotation = ctypes.addressof(r)
+        r, pos = _turn(rotation, positions, tokens)
+    a = esb_append(k.data_ptr(), v.data_ptr(), ldk, ldv, _vector(slots, "slots", tokens, torch.int64), pos,
+                   None if r is None else ctypes.addressof(r), kp, vp, ldkq, ldvq, xt, qt, rule, rounding)
     _check(lib().esb_cache_append(tokens, ctypes.byref(c), ctypes.byref(a), _stream(stream)), "esb_cache_append")
 
 
@@ -1254,43 +1254,36 @@ def esb_cache_attention(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, pag
     + 1] - 1 (None: one each; rows of no sequence are not written).  scale: 1 / sqrt(head_dim) unless given; window: places
     seen, the query's own among them (0: all)."""
     c = cache.c()
-    a = esb_attention()
     empty = _empty_on(stream)
-    a.q_type, a.ldq = _rows(q, "q")
-    tokens, cols = q.shape
-    a.q_heads = _head_count(q, "q", c.head_dim)
+    qt, ldq = _rows(q, "q")
+    shape = q.shape
+    tokens, cols = shape
+    heads = _head_count(q, "q", c.head_dim)
     seqs = lens.shape[0] if lens.dim() == 1 else -1
-    a.q, a.lens, a.seqs = q.data_ptr(), _vector(lens, "lens", seqs, torch.int32), seqs
-    if pages.dtype != torch.int32 or not pages.is_cuda or pages.dim() != 2 or pages.shape[0] != seqs or \
-            (pages.shape[1] > 1 and pages.stride(1) != 1):
+    lp = _vector(lens, "lens", seqs, torch.int32)
+    held = pages.shape
+    if pages.dtype != torch.int32 or not pages.is_cuda or len(held) != 2 or held[0] != seqs or (held[1] > 1 and pages.stride(1) != 1):
         raise ValueError("pages must be a 2-D CUDA int32 tensor with a contiguous row for each sequence")
-    a.max_pages, a.ld_pages = pages.shape[1], pages.stride(0) if seqs > 1 else pages.shape[1]
-    a.pages = pages.data_ptr()
+    sp = None
     if starts is not None:
-        a.starts = _vector(starts, "starts", seqs + 1, torch.int32)
+        sp = _vector(starts, "starts", seqs + 1, torch.int32)
     elif tokens != seqs:
         raise ValueError("q must have a row for each sequence, or starts")
-    a.scale = c.head_dim ** -0.5 if scale is None else scale
-    a.window = window
-    r = None
-    if rotation is not None:
-        r = rotation.c()
-        a.rotation = ctypes.addressof(r)
     if out is None:
         # rows of no sequence are not written
-        out = empty((tokens, cols), dtype=q.dtype, device=q.device)
-        a.out_type, a.ldo = a.q_type, cols
+        out = empty(shape, dtype=q.dtype, device=q.device)
+        ot, ldo = qt, cols
     else:
-        a.out_type, a.ldo = _rows(out, "out")
-        if out.shape != q.shape:
+        ot, ldo = _rows(out, "out")
+        if out.shape != shape:
             raise ValueError("out must have the shape of q")
-    a.out = out.data_ptr()
-    lse = None
-    if want_lse:
-        lse = empty((tokens, a.q_heads), dtype=torch.float32, device=q.device)
-        a.lse = lse.data_ptr()
+    lse = empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
+    r = None if rotation is None else rotation.c()
+    a = esb_attention(q.data_ptr(), ldq, out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), sp, lp, pages.data_ptr(),
+                      pages.stride(0) if seqs > 1 else held[1], None if r is None else ctypes.addressof(r), seqs, held[1], heads,
+                      window, qt, ot, c.head_dim ** -0.5 if scale is None else scale)
     if workspace is None:
-        nb = int(lib().esb_cache_attention_workspace_bytes(tokens, seqs, a.q_heads, c.heads, c.head_dim, a.q_type))
+        nb = lib().esb_cache_attention_workspace_bytes(tokens, seqs, heads, c.heads, c.head_dim, qt)
         workspace = empty(nb, dtype=torch.uint8, device=q.device)
     else:
         _dev(workspace, "workspace")
