@@ -55,9 +55,7 @@ struct AttnArgs {
 namespace {
 
 constexpr int kAtWarps = 4, kAtThreads = 32 * kAtWarps;
-constexpr int kAtPlaces = 16;                           // of a stage
-constexpr int kAtBlock = kAtPlaces * kAtWarps;          // places of a block of work
-constexpr int kAtMinBlocks = 2;                         // of a thread block, while there is enough work
+constexpr int kAtPlaces = 16;                           // of a part of a stage, the matrix instruction's rows
 
 // ------------------------------------------------------------ instructions
 
@@ -88,7 +86,7 @@ __device__ __forceinline__ float ex2(float x)
 __device__ __forceinline__ float lg2(float x)
 {
     float r;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 __device__ __forceinline__ void copy16(uint32_t to, const void* from)
@@ -164,11 +162,14 @@ template <int DP> struct Stage {
 
 template <int DP, int NT, int NP> struct Shape {
     static constexpr int R = 8 * NT, kSteps = DP / 16;
-    static constexpr int kStages = DP == 256 ? 4 : 6;
+    static constexpr int kParts = NT == 1 ? 2 : 1;      // of a stage: few rows share a stage's fixed work over more places
+    static constexpr int kBlock = kAtPlaces * kParts * kAtWarps;    // places of a block of work
+    static constexpr int kMinBlocks = NT == 1 ? 1 : 2;  // of a thread block, while there is enough work
+    static constexpr int kStages = DP == 256 ? (NT == 1 ? 3 : 4) : NT == 1 ? 3 : 6;
     static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
-    static constexpr int kSm = NT == 1 ? (DP == 256 ? 3 : 4) : (NT == 2 && DP <= 128 && NP == 1 ? 3 : 2);
+    static constexpr int kSm = NT == 1 ? (DP == 256 ? 2 : 3) : (NT == 2 && DP <= 128 && NP == 1 ? 3 : 2);
     static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
-    static constexpr int kRing = kAtWarps * kStages * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;
+    static constexpr int kRing = kAtWarps * kStages * kParts * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;
     static constexpr int kSums = kAtWarps * R * 8;      // maxima and sums of the warps
     static constexpr int kBytes = (kRing > kMerge ? kRing : kMerge) + kQueryBytes + kSums + 4 * R;
     static constexpr int kSlot = R * (DP + 2);          // floats of a part of a tile
@@ -194,19 +195,19 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b)
     s.seen = s.len < held ? s.len : (int)held;
     return s;
 }
-template <int R> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (int)(((int64_t)s.nq * a.group + R - 1) / R); }
+template <class Sh> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (int)(((int64_t)s.nq * a.group + Sh::R - 1) / Sh::R); }
 
 struct Tile {
-    int lo, hi, blocks;                 // places lo .. hi - 1, lo a multiple of 16; blocks of work (one where there are none)
+    int lo, hi, blocks;                 // places lo .. hi - 1, lo at a stage's start; blocks of work (one where there are none)
 };
-template <int R> __device__ __forceinline__ Tile tile_of(const AttnArgs& a, const Seq& s, int i)
+template <class Sh> __device__ __forceinline__ Tile tile_of(const AttnArgs& a, const Seq& s, int i)
 {
     Tile t;
-    const int64_t rows = (int64_t)s.nq * a.group, first = (int64_t)i * R, last = min(first + R, rows) - 1;
+    const int64_t rows = (int64_t)s.nq * a.group, first = (int64_t)i * Sh::R, last = min(first + Sh::R, rows) - 1;
     const int64_t p0 = (int64_t)s.len - s.nq + first / a.group, p1 = (int64_t)s.len - s.nq + last / a.group;
     t.hi = (int)max((int64_t)0, min(p1 + 1, (int64_t)s.seen));
-    t.lo = a.window > 0 ? (int)max((int64_t)0, p0 - a.window + 1) & ~(kAtPlaces - 1) : 0;
-    t.blocks = t.hi > t.lo ? (t.hi - t.lo + kAtBlock - 1) / kAtBlock : 1;
+    t.lo = a.window > 0 ? (int)max((int64_t)0, p0 - a.window + 1) & ~(kAtPlaces * Sh::kParts - 1) : 0;
+    t.blocks = t.hi > t.lo ? (t.hi - t.lo + Sh::kBlock - 1) / Sh::kBlock : 1;
     return t;
 }
 
@@ -224,7 +225,7 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh)
 }
 
 // Work of sequences b0 + thread (0 past the end), long ones by the whole block.
-template <int R>
+template <class Sh>
 __device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* sh)
 {
     const int b = b0 + threadIdx.x;
@@ -232,10 +233,10 @@ __device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* s
     bool many = false;
     if (b < a.seqs) {
         const Seq s = sequence(a, b);
-        const int n = tiles_of<R>(a, s);
+        const int n = tiles_of<Sh>(a, s);
         many = n > 8;
         if (!many)
-            for (int i = 0; i < n; i++) w += tile_of<R>(a, s, i).blocks;
+            for (int i = 0; i < n; i++) w += tile_of<Sh>(a, s, i).blocks;
     }
     if (a.starts && __syncthreads_or(many)) {
         __shared__ unsigned list[kAtWarps];
@@ -245,9 +246,9 @@ __device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* s
         for (int k = 0; k < kAtThreads; k++) {
             if (!(list[k >> 5] >> (k & 31) & 1u)) continue;
             const Seq s = sequence(a, b0 + k);
-            const int n = tiles_of<R>(a, s);
+            const int n = tiles_of<Sh>(a, s);
             int64_t part = 0;
-            for (int i = threadIdx.x; i < n; i += kAtThreads) part += tile_of<R>(a, s, i).blocks;
+            for (int i = threadIdx.x; i < n; i += kAtThreads) part += tile_of<Sh>(a, s, i).blocks;
             part = block_sum(part, sh);
             if (threadIdx.x == k) w = part;
         }
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 {
     using Sh = Shape<DP, NT, NP>;
     using St = Stage<DP>;
-    constexpr int R = Sh::R, STEPS = Sh::kSteps, W = DP / 8, WK = W / 4, WV = W / 8, ST = Sh::kStages;
+    constexpr int R = Sh::R, STEPS = Sh::kSteps, W = DP / 8, WK = W / 4, WV = W / 8, ST = Sh::kStages, SUB = Sh::kParts, BLOCK = Sh::kBlock, BYTES = SUB * St::kBytes;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int64_t sh[kAtWarps + 2];
     unsigned char* ring = smem;
@@ -319,37 +320,37 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     int64_t left = 0, rest = 0;
     int b = 0, head = 0, tile = 0;
     {
-        int64_t w = work_of<R>(a, 0, sh), total = 0;
+        int64_t w = work_of<Sh>(a, 0, sh), total = 0;
         if (a.seqs <= kAtThreads) total = block_sum(w, sh);
         else
-            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) total += block_sum(b0 ? work_of<R>(a, b0, sh) : w, sh);
-        const int64_t least = total / kAtMinBlocks, n = least < 1 ? 1 : (least < gridDim.x ? least : gridDim.x);
+            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) total += block_sum(b0 ? work_of<Sh>(a, b0, sh) : w, sh);
+        const int64_t least = total / Sh::kMinBlocks, n = least < 1 ? 1 : (least < gridDim.x ? least : gridDim.x);
         if (me < n && total > 0) {
             int64_t at = total * me / n;
             left = total * (me + 1) / n - at;
             for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) {
-                if (b0) w = work_of<R>(a, b0, sh);
+                if (b0) w = work_of<Sh>(a, b0, sh);
                 int64_t sum;
                 const Found f = find(w, at, sh, sum);
                 if (f.who >= 0) { b = b0 + f.who; rest = f.rest; break; }
                 at -= sum;
             }
             const Seq s = sequence(a, b);
-            const int n_tiles = tiles_of<R>(a, s);
+            const int n_tiles = tiles_of<Sh>(a, s);
             if (n_tiles == 1) {
-                const int per = tile_of<R>(a, s, 0).blocks;
+                const int per = tile_of<Sh>(a, s, 0).blocks;
                 head = (int)(rest / per);
                 rest -= (int64_t)head * per;
             } else {
                 int64_t per = 0;
-                for (int i = threadIdx.x; i < n_tiles; i += kAtThreads) per += tile_of<R>(a, s, i).blocks;
+                for (int i = threadIdx.x; i < n_tiles; i += kAtThreads) per += tile_of<Sh>(a, s, i).blocks;
                 per = block_sum(per, sh);
                 head = (int)(rest / per);
                 rest -= (int64_t)head * per;
                 for (int i0 = 0; i0 < n_tiles; i0 += kAtThreads) {
                     const int i = i0 + threadIdx.x;
                     int64_t sum;
-                    const Found f = find(i < n_tiles ? tile_of<R>(a, s, i).blocks : 0, rest, sh, sum);
+                    const Found f = find(i < n_tiles ? tile_of<Sh>(a, s, i).blocks : 0, rest, sh, sum);
                     if (f.who >= 0) { tile = i0 + f.who; rest = f.rest; break; }
                     rest -= sum;
                 }
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         mine[i] = c < copies;
         to[i] = mine[i] ? St::at(c / a.chunks, c % a.chunks) : 0u;
     }
-    const uint32_t my_ring = smem_u32(ring) + warp * ST * St::kBytes, ring_end = my_ring + ST * St::kBytes;
+    const uint32_t my_ring = smem_u32(ring) + warp * ST * BYTES, ring_end = my_ring + ST * BYTES;
     // and where it reads: rows g (and 8 further) of K, rows 2 t and 2 t + 1 of V
     const uint32_t k_from = DP == 64 ? St::at(g, t >> 1) + (t & 1) * 8 : St::at(g, t);
     const uint32_t v_in = DP == 64 ? (g & 3) * 4 : DP == 128 ? (g & 1) * 8 : 0, v_chunk = DP == 64 ? g >> 2 : DP == 128 ? g >> 1 : g;
@@ -375,45 +376,59 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 
     while (left > 0) {
         const Seq s = sequence(a, b);
-        const Tile tl = tile_of<R>(a, s, tile);
+        const Tile tl = tile_of<Sh>(a, s, tile);
         const int blocks = (int)min((int64_t)tl.blocks - rest, left), first_block = (int)rest;
         const int64_t rows = (int64_t)s.nq * a.group, row0 = (int64_t)tile * R;
         const int n_rows = (int)min((int64_t)R, rows - row0);
 
         __syncthreads();                                // the last tile's shared memory has been read
         const int32_t* table = a.pages + (int64_t)b * a.ld_pages;
-        const int place0 = tl.lo + (first_block * kAtWarps + warp) * kAtPlaces;
-        const int end = min(tl.hi, tl.lo + (first_block + blocks) * kAtBlock);
-        const int stages = end > place0 ? (end - place0 + kAtBlock - 1) / kAtBlock : 0;
+        const int place0 = tl.lo + (first_block * kAtWarps + warp) * (kAtPlaces * SUB);
+        const int end = min(tl.hi, tl.lo + (first_block + blocks) * BLOCK);
+        const int stages = end > place0 ? (end - place0 + BLOCK - 1) / BLOCK : 0;
         const int64_t head_row = (int64_t)head * a.page_size;
         const char* kg = reinterpret_cast<const char*>(a.kc) + (head_row * a.chunks + lane) * 16;
         const char* vg = reinterpret_cast<const char*>(a.vc) + (head_row * a.chunks + lane) * 16;
         const float* sg = (lane < 16 ? a.ks : a.vs) + head_row + (lane & 15);
-        auto page_at = [&](int i, int p) {
-            return i < stages ? __ldg(table + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size)) : -1;
+        // pages of the next stage that is copied; its second part's, where that may be another page
+        const bool one_page = SUB == 1 || a.page_size % (kAtPlaces * SUB) == 0;
+        auto page_at = [&](int p) {
+            return p < end ? __ldg(table + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size)) : -1;
         };
-        int next_page = page_at(0, place0), issued = 0, issue_place = place0;
-        uint32_t issue_to = my_ring, there = 0u;        // the ring's next stage; which of the last stages hold a page that is there
+        int issue_place = place0, next_page[SUB];
+        auto look = [&]() {
+            next_page[0] = page_at(issue_place);
+            if constexpr (SUB == 2) next_page[SUB - 1] = one_page ? next_page[0] : page_at(issue_place + kAtPlaces);
+        };
+        look();
+        uint32_t issue_to = my_ring, there = 0u;        // the ring's next stage; which of the last parts hold a page that is there
         auto issue = [&]() {
-            const int page = next_page, p = issue_place;
-            issue_place += kAtBlock;
-            next_page = page_at(++issued, issue_place);
-            there *= 2u;
-            if ((uint32_t)page < (uint32_t)a.npages) {
+            int pages[SUB];
+#pragma unroll
+            for (int h = 0; h < SUB; h++) pages[h] = next_page[h];
+            int p = issue_place;
+            issue_place += BLOCK;
+            look();
+#pragma unroll
+            for (int h = 0; h < SUB; h++, p += kAtPlaces) {
+                const uint32_t page = (uint32_t)pages[h];
+                there *= 2u;
+                if (page >= (uint32_t)a.npages) continue;
                 there++;
                 const int in = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
-                const uint64_t at = (uint64_t)(uint32_t)page * a.page16 + (uint32_t)(in * a.chunks);
+                const uint64_t at = (uint64_t)page * a.page16 + (uint32_t)(in * a.chunks);
                 const char *k = kg + at * 16, *v = vg + at * 16;
+                const uint32_t dst = issue_to + h * St::kBytes;
 #pragma unroll
                 for (int c = 0; c < W / 8; c++)
                     if (mine[c]) {
-                        copy16(issue_to + to[c], k + 512 * c);
-                        copy16(issue_to + to[c] + St::kV, v + 512 * c);
+                        copy16(dst + to[c], k + 512 * c);
+                        copy16(dst + to[c] + St::kV, v + 512 * c);
                     }
-                copy4(issue_to + St::kKs + 4 * lane, sg + (uint64_t)(uint32_t)page * a.page_lds + in);
+                copy4(dst + St::kKs + 4 * lane, sg + (uint64_t)page * a.page_lds + in);
             }
             copies_end_stage();
-            issue_to = issue_to + St::kBytes == ring_end ? my_ring : issue_to + St::kBytes;
+            issue_to = issue_to + BYTES == ring_end ? my_ring : issue_to + BYTES;
         };
 #pragma unroll
         for (int i = 0; i < ST - 1; i++) issue();
@@ -507,26 +522,25 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 for (int c = 0; c < 4; c++) o[i][nt][c] = 0.0f;
 
         uint32_t use = my_ring;
-        for (int i = 0, place = place0; i < stages; i++, place += kAtBlock) {
+        for (int i = 0, place = place0; i < stages; i++, place += BLOCK) {
             copies_wait<ST - 2>();
             __syncwarp();                               // every lane's copies of this stage; all have read the one before
-            const bool here = there >> (ST - 2) & 1u;
-            const uint32_t sm = use;
-            use = use + St::kBytes == ring_end ? my_ring : use + St::kBytes;
+            const uint32_t here = there >> (SUB * (ST - 2)) & ((1u << SUB) - 1u), sm = use;
+            use = use + BYTES == ring_end ? my_ring : use + BYTES;
             issue();
-            if (!here) continue;
+            if (here == 0u) continue;
 
-            // scores: rows g and g + 8 of the stage
-            // (two chains of products where a warp has few columns)
-            constexpr int CH = NT == 1 ? 2 : 1;
-            float sc[NT][4], part[CH][NT][4];
+            // scores: rows g and g + 8 of each part (two chains of products where a warp has few columns)
+            constexpr int CH = NT == 1 && SUB == 1 ? 2 : 1;
+            float part[SUB][CH][NT][4];
 #pragma unroll
-            for (int h = 0; h < CH; h++)
+            for (int sub = 0; sub < SUB; sub++) {
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
+                for (int h = 0; h < CH; h++)
 #pragma unroll
-                    for (int c = 0; c < 4; c++) part[h][nt][c] = 0.0f;
-            {
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int c = 0; c < 4; c++) part[sub][h][nt][c] = 0.0f;
                 uint32_t k0[WK], k1[WK];
                 auto words = [&](uint32_t at, uint32_t (&w)[WK]) {
                     if constexpr (DP == 256) {
@@ -539,8 +553,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         lds(at, w);
                     }
                 };
-                words(sm + k_from, k0);
-                words(sm + k_from + 8 * St::kRow, k1);
+                words(sm + sub * St::kBytes + k_from, k0);
+                words(sm + sub * St::kBytes + k_from + 8 * St::kRow, k1);
 #pragma unroll
                 for (int k = 0; k < WK; k++) {
                     uint32_t x[4], y[4];
@@ -556,55 +570,76 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                                 uint2 q;
                                 if constexpr (Sh::kQueryRegs) q = qr[at];
                                 else q = qf[at * 32 + lane];
-                                mma16(part[h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
+                                mma16(part[sub][h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
                             }
                 }
             }
-            const uint32_t scales = sm + St::kKs + 4 * g;
-            const float ks0 = lds_f32(scales), ks1 = lds_f32(scales + 32), vs0 = lds_f32(scales + 64), vs1 = lds_f32(scales + 96);
-            // log2 of v's scales, where they have one
-            const float lv0 = fmaxf(fminf(lg2(fabsf(vs0)), 100.0f), -100.0f), lv1 = fmaxf(fminf(lg2(fabsf(vs1)), 100.0f), -100.0f);
-            const bool whole = place + kAtPlaces <= all_hi && place >= all_lo;
-            bool raise = false;
+            const bool whole = place + kAtPlaces * SUB <= all_hi && place >= all_lo && here == (1u << SUB) - 1u;
+            float sc[SUB][NT][4], vs[SUB][2];
+            float over = ninf;                          // how far scores (with their values' scales) pass the maximum
             // scores less the maximum (what is not seen: -inf, whatever the maximum is)
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    float x = part[0][nt][c], y = part[0][nt][2 + c];
-                    if constexpr (CH == 2) {
-                        x += part[CH - 1][nt][c];
-                        y += part[CH - 1][nt][2 + c];
-                    }
-                    part[0][nt][c] = x * ks0;
-                    part[0][nt][2 + c] = y * ks1;
-                    x = fmaf(part[0][nt][c], fq[nt][c], -M[nt][c]);
-                    y = fmaf(part[0][nt][2 + c], fq[nt][c], -M[nt][c]);
-                    if (!whole) {
-                        if (place + g >= qhi[nt][c] || place + g < qlo[nt][c]) x = ninf;
-                        if (place + g + 8 >= qhi[nt][c] || place + g + 8 < qlo[nt][c]) y = ninf;
-                    }
-                    raise |= fmaxf(x + lv0, y + lv1) > 8.0f;
-                    sc[nt][c] = x;
-                    sc[nt][2 + c] = y;
-                }
-            if (__any_sync(0xffffffffu, raise)) {
+            for (int sub = 0; sub < SUB; sub++) {
+                const uint32_t scales = sm + sub * St::kBytes + St::kKs + 4 * g;
+                const float ks0 = lds_f32(scales), ks1 = lds_f32(scales + 32);
+                vs[sub][0] = lds_f32(scales + 64);
+                vs[sub][1] = lds_f32(scales + 96);
+                // log2 of v's scales, where they have one
+                const float lv0 = fmaxf(fminf(lg2(fabsf(vs[sub][0])), 100.0f), -100.0f), lv1 = fmaxf(fminf(lg2(fabsf(vs[sub][1])), 100.0f), -100.0f);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                     for (int c = 0; c < 2; c++) {
-                        const float x = sc[nt][c] == ninf ? ninf : part[0][nt][c] * fq[nt][c];
-                        const float y = sc[nt][2 + c] == ninf ? ninf : part[0][nt][2 + c] * fq[nt][c];
-                        float m = fmaxf(x + lv0, y + lv1);
+                        float x = part[sub][0][nt][c], y = part[sub][0][nt][2 + c];
+                        if constexpr (CH == 2) {
+                            x += part[sub][CH - 1][nt][c];
+                            y += part[sub][CH - 1][nt][2 + c];
+                        }
+                        part[sub][0][nt][c] = x * ks0;
+                        part[sub][0][nt][2 + c] = y * ks1;
+                        x = fmaf(part[sub][0][nt][c], fq[nt][c], -M[nt][c]);
+                        y = fmaf(part[sub][0][nt][2 + c], fq[nt][c], -M[nt][c]);
+                        if (!whole) {
+                            const int at = place + sub * kAtPlaces + g;
+                            const bool on = here >> (SUB - 1 - sub) & 1u;
+                            if (!on || at >= qhi[nt][c] || at < qlo[nt][c]) x = ninf;
+                            if (!on || at + 8 >= qhi[nt][c] || at + 8 < qlo[nt][c]) y = ninf;
+                        }
+                        over = fmaxf(over, fmaxf(x + lv0, y + lv1));
+                        sc[sub][nt][c] = x;
+                        sc[sub][nt][2 + c] = y;
+                    }
+            }
+            if (__any_sync(0xffffffffu, over > 8.0f)) {
+                float lv[SUB][2];
+#pragma unroll
+                for (int sub = 0; sub < SUB; sub++)
+#pragma unroll
+                    for (int c = 0; c < 2; c++) lv[sub][c] = fmaxf(fminf(lg2(fabsf(vs[sub][c])), 100.0f), -100.0f);
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int c = 0; c < 2; c++) {
+                        float m = M[nt][c];
+#pragma unroll
+                        for (int sub = 0; sub < SUB; sub++) {
+                            float &x = sc[sub][nt][c], &y = sc[sub][nt][2 + c];
+                            x = x == ninf ? ninf : part[sub][0][nt][c] * fq[nt][c];
+                            y = y == ninf ? ninf : part[sub][0][nt][2 + c] * fq[nt][c];
+                            m = fmaxf(m, fmaxf(x + lv[sub][0], y + lv[sub][1]));
+                        }
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                        m = fmaxf(m, M[nt][c]);
                         const float f = m > M[nt][c] ? ex2(M[nt][c] - m) : 1.0f;
                         M[nt][c] = m;
                         L[nt][c] *= f;
-                        sc[nt][c] = x == ninf ? ninf : x - m;
-                        sc[nt][2 + c] = y == ninf ? ninf : y - m;
+#pragma unroll
+                        for (int sub = 0; sub < SUB; sub++) {
+                            float &x = sc[sub][nt][c], &y = sc[sub][nt][2 + c];
+                            x = x == ninf ? ninf : x - m;
+                            y = y == ninf ? ninf : y - m;
+                        }
 #pragma unroll
                         for (int k = 0; k < DP / 16; k++) {
                             o[k][nt][c] *= f;
@@ -612,69 +647,72 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         }
                     }
             }
-            // weights, turned into the second product's operand
-            uint32_t p0[NT][NP], p1[NT][NP];
 #pragma unroll
-            for (int nt = 0; nt < NT; nt++) {
-                float w[4];
+            for (int sub = 0; sub < SUB; sub++) {
+                // weights, turned into the second product's operand
+                uint32_t p0[NT][NP], p1[NT][NP];
 #pragma unroll
-                for (int c = 0; c < 4; c++) {
-                    const float e = ex2(sc[nt][c]);
-                    L[nt][c & 1] += e;
-                    w[c] = e * (c < 2 ? vs0 : vs1);
-                    if (!whole && sc[nt][c] == ninf) w[c] = 0.0f;  // a scale that is not seen may be NaN
-                }
-                const uint32_t h0 = pack2<__half>(w[0], w[1]), h1 = pack2<__half>(w[2], w[3]);
-                p0[nt][0] = transposed(h0);
-                p1[nt][0] = transposed(h1);
-                if constexpr (NP == 2) {
-                    float x[4];
-                    unpack2<__half>(h0, x[0], x[1]);
-                    unpack2<__half>(h1, x[2], x[3]);
-                    p0[nt][NP - 1] = transposed(pack2<__half>(w[0] - x[0], w[1] - x[1]));
-                    p1[nt][NP - 1] = transposed(pack2<__half>(w[2] - x[2], w[3] - x[3]));
-                }
-            }
-            // values: this lane's words of places 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-            uint32_t v[4][WV];
+                for (int nt = 0; nt < NT; nt++) {
+                    float w[4];
 #pragma unroll
-            for (int k = 0; k < 4; k++) lds(sm + (k & 1 ? v_from1 : v_from0) + 8 * St::kRow * (k >> 1), v[k]);
-            // a pair of places' codes of the same four values, the second place's above
-            auto pair_codes = [](uint32_t x, uint32_t y, int upper) { return prmt(x, y, upper ? 0x7632u : 0x5410u); };
-            if constexpr (WV == 1) {
-                // rows g: values 0..3 of the word, rows g + 8: values 4..7
-                uint32_t x0[4], x1[4], y0[4], y1[4];
-                decode8<LIN>(pair_codes(v[0][0], v[1][0], 0), a.vlut, x0);
-                decode8<LIN>(pair_codes(v[2][0], v[3][0], 0), a.vlut, x1);
-                decode8<LIN>(pair_codes(v[0][0], v[1][0], 1), a.vlut, y0);
-                decode8<LIN>(pair_codes(v[2][0], v[3][0], 1), a.vlut, y1);
-#pragma unroll
-                for (int k = 0; k < 4; k++)
-#pragma unroll
-                    for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                        for (int p = 0; p < NP; p++) mma16(o[k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
-            } else {
-                // rows g: the first word's values, rows g + 8: the second's
-#pragma unroll
-                for (int wp = 0; wp < WV / 2; wp++)
-#pragma unroll
-                    for (int up = 0; up < 2; up++) {
-                        uint32_t x0[4], x1[4], y0[4], y1[4];
-                        constexpr int LAST = WV - 1;
-                        const int second = 2 * wp + 1 < LAST ? 2 * wp + 1 : LAST;
-                        decode8<LIN>(pair_codes(v[0][2 * wp], v[1][2 * wp], up), a.vlut, x0);
-                        decode8<LIN>(pair_codes(v[2][2 * wp], v[3][2 * wp], up), a.vlut, x1);
-                        decode8<LIN>(pair_codes(v[0][second], v[1][second], up), a.vlut, y0);
-                        decode8<LIN>(pair_codes(v[2][second], v[3][second], up), a.vlut, y1);
-#pragma unroll
-                        for (int k = 0; k < 4; k++)
-#pragma unroll
-                            for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                for (int p = 0; p < NP; p++)
-                                    mma16(o[8 * wp + 4 * up + k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                    for (int c = 0; c < 4; c++) {
+                        const float e = ex2(sc[sub][nt][c]);
+                        L[nt][c & 1] += e;
+                        w[c] = e * vs[sub][c >> 1];
+                        if (!whole && sc[sub][nt][c] == ninf) w[c] = 0.0f;   // a scale that is not seen may be NaN
                     }
+                    const uint32_t h0 = pack2<__half>(w[0], w[1]), h1 = pack2<__half>(w[2], w[3]);
+                    p0[nt][0] = transposed(h0);
+                    p1[nt][0] = transposed(h1);
+                    if constexpr (NP == 2) {
+                        float x[4];
+                        unpack2<__half>(h0, x[0], x[1]);
+                        unpack2<__half>(h1, x[2], x[3]);
+                        p0[nt][NP - 1] = transposed(pack2<__half>(w[0] - x[0], w[1] - x[1]));
+                        p1[nt][NP - 1] = transposed(pack2<__half>(w[2] - x[2], w[3] - x[3]));
+                    }
+                }
+                // values: this lane's words of places 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+                uint32_t v[4][WV];
+#pragma unroll
+                for (int k = 0; k < 4; k++) lds(sm + sub * St::kBytes + (k & 1 ? v_from1 : v_from0) + 8 * St::kRow * (k >> 1), v[k]);
+                // a pair of places' codes of the same four values, the second place's above
+                auto pair_codes = [](uint32_t x, uint32_t y, int upper) { return prmt(x, y, upper ? 0x7632u : 0x5410u); };
+                if constexpr (WV == 1) {
+                    // rows g: values 0..3 of the word, rows g + 8: values 4..7
+                    uint32_t x0[4], x1[4], y0[4], y1[4];
+                    decode8<LIN>(pair_codes(v[0][0], v[1][0], 0), a.vlut, x0);
+                    decode8<LIN>(pair_codes(v[2][0], v[3][0], 0), a.vlut, x1);
+                    decode8<LIN>(pair_codes(v[0][0], v[1][0], 1), a.vlut, y0);
+                    decode8<LIN>(pair_codes(v[2][0], v[3][0], 1), a.vlut, y1);
+#pragma unroll
+                    for (int k = 0; k < 4; k++)
+#pragma unroll
+                        for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                            for (int p = 0; p < NP; p++) mma16(o[k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                } else {
+                    // rows g: the first word's values, rows g + 8: the second's
+#pragma unroll
+                    for (int wp = 0; wp < WV / 2; wp++)
+#pragma unroll
+                        for (int up = 0; up < 2; up++) {
+                            uint32_t x0[4], x1[4], y0[4], y1[4];
+                            constexpr int LAST = WV - 1;
+                            const int second = 2 * wp + 1 < LAST ? 2 * wp + 1 : LAST;
+                            decode8<LIN>(pair_codes(v[0][2 * wp], v[1][2 * wp], up), a.vlut, x0);
+                            decode8<LIN>(pair_codes(v[2][2 * wp], v[3][2 * wp], up), a.vlut, x1);
+                            decode8<LIN>(pair_codes(v[0][second], v[1][second], up), a.vlut, y0);
+                            decode8<LIN>(pair_codes(v[2][second], v[3][second], up), a.vlut, y1);
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+#pragma unroll
+                                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                                    for (int p = 0; p < NP; p++)
+                                        mma16(o[8 * wp + 4 * up + k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                        }
+                }
             }
         }
         copies_wait<0>();
@@ -758,7 +796,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         left -= blocks;
         rest = 0;
         if (ends) {
-            if (++tile >= tiles_of<R>(a, s)) {
+            if (++tile >= tiles_of<Sh>(a, s)) {
                 tile = 0;
                 if (++head >= a.heads) {
                     head = 0;
