@@ -65,6 +65,9 @@ cudaError_t launch_attention(int64_t tokens, const esb_kv_cache& c, const esb_at
     a.page_shift = -1;
     for (int i = 4; i < 31; i++)
         if (c.page_size == 1 << i) a.page_shift = i;
+    a.group_shift = -1;
+    for (int i = 0; i < 24; i++)
+        if (a.group == 1 << i) a.group_shift = i;
     a.window = n.window; a.q_type = n.q_type; a.out_type = n.out_type;
     a.qvec = rows16(n.q, n.ldq, n.q_type); a.ovec = rows16(n.out, n.ldo, n.out_type);
     a.scale2 = (float)((double)n.scale * 1.4426950408889634) * (lin ? (float)(1 << (16 - c.k_fmt.k)) : 1.0f);

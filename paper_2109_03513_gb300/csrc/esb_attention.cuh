@@ -22,6 +22,7 @@
 // the workspace, and a second kernel joins them in their order.
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -44,12 +45,12 @@ struct AttnArgs {
     int64_t npages;
     uint32_t page16, page_lds;                          // a page in 16 bytes of codes, and in scales
     uint2 klut, vlut;                                   // high bytes of the fp16 numbers of codes 0..7; LIN: x = what turns a code into its place
-    int seqs, max_pages, heads, group, D, chunks, page_size, page_shift, window;
+    int seqs, max_pages, heads, group, group_shift, D, chunks, page_size, page_shift, window;
     int q_type, out_type, qvec, ovec;
     float scale2, vunit;                                // scale log2(e) and K's unit; V's unit
     RotArgs rot;
     float* partial;                                     // slots of R x (DP + 2) floats
-    int4* head;                                         // slots
+    int4* head;                                         // of each part: (the last part of the tile that begins in it and goes on) + 1, sequence, head, tile
 };
 
 namespace {
@@ -195,7 +196,14 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b)
     s.seen = s.len < held ? s.len : (int)held;
     return s;
 }
-template <class Sh> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (int)(((int64_t)s.nq * a.group + Sh::R - 1) / Sh::R); }
+// Rows of a sequence's tiles: below 2^31.
+__device__ __forceinline__ uint32_t token_of(const AttnArgs& a, uint32_t row) { return a.group_shift >= 0 ? row >> a.group_shift : row / (uint32_t)a.group; }
+// Most quotients of 64 bits are of numbers of 32.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
+{
+    return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+template <class Sh> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (s.nq * a.group + Sh::R - 1) / Sh::R; }
 
 struct Tile {
     int lo, hi, blocks;                 // places lo .. hi - 1, lo at a stage's start; blocks of work (one where there are none)
@@ -203,8 +211,8 @@ struct Tile {
 template <class Sh> __device__ __forceinline__ Tile tile_of(const AttnArgs& a, const Seq& s, int i)
 {
     Tile t;
-    const int64_t rows = (int64_t)s.nq * a.group, first = (int64_t)i * Sh::R, last = min(first + Sh::R, rows) - 1;
-    const int64_t p0 = (int64_t)s.len - s.nq + first / a.group, p1 = (int64_t)s.len - s.nq + last / a.group;
+    const uint32_t rows = (uint32_t)(s.nq * a.group), first = (uint32_t)i * Sh::R, last = min(first + Sh::R, rows) - 1u;
+    const int64_t p0 = (int64_t)s.len - s.nq + token_of(a, first), p1 = (int64_t)s.len - s.nq + token_of(a, last);
     t.hi = (int)max((int64_t)0, min(p1 + 1, (int64_t)s.seen));
     t.lo = a.window > 0 ? (int)max((int64_t)0, p0 - a.window + 1) & ~(kAtPlaces * Sh::kParts - 1) : 0;
     t.blocks = t.hi > t.lo ? (t.hi - t.lo + Sh::kBlock - 1) / Sh::kBlock : 1;
@@ -313,11 +321,12 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const float ninf = __int_as_float(0xff800000);
     griddep_wait();
+    griddep_launch_dependents();        // every block runs at once, so those of the join only fill what is left
 
     // this block's part of the work: sequence, head, tile and block of places
     const int me = blockIdx.x;
-    int4 slot_head[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
-    int64_t left = 0, rest = 0;
+    int4 goes_on = make_int4(0, 0, 0, 0);
+    int64_t left = 0, rest = 0, at_block = 0, share = 1, larger = 0;    // the first `larger` blocks have one more than `share`
     int b = 0, head = 0, tile = 0;
     {
         int64_t w = work_of<Sh>(a, 0, sh), total = 0;
@@ -326,8 +335,11 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) total += block_sum(b0 ? work_of<Sh>(a, b0, sh) : w, sh);
         const int64_t least = total / Sh::kMinBlocks, n = least < 1 ? 1 : (least < gridDim.x ? least : gridDim.x);
         if (me < n && total > 0) {
-            int64_t at = total * me / n;
-            left = total * (me + 1) / n - at;
+            share = quotient(total, n);
+            larger = total - share * n;
+            int64_t at = share * me + min((int64_t)me, larger);
+            left = share + (me < larger ? 1 : 0);
+            at_block = at;
             for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) {
                 if (b0) w = work_of<Sh>(a, b0, sh);
                 int64_t sum;
@@ -339,13 +351,13 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             const int n_tiles = tiles_of<Sh>(a, s);
             if (n_tiles == 1) {
                 const int per = tile_of<Sh>(a, s, 0).blocks;
-                head = (int)(rest / per);
+                head = (int)quotient(rest, per);
                 rest -= (int64_t)head * per;
             } else {
                 int64_t per = 0;
                 for (int i = threadIdx.x; i < n_tiles; i += kAtThreads) per += tile_of<Sh>(a, s, i).blocks;
                 per = block_sum(per, sh);
-                head = (int)(rest / per);
+                head = (int)quotient(rest, per);
                 rest -= (int64_t)head * per;
                 for (int i0 = 0; i0 < n_tiles; i0 += kAtThreads) {
                     const int i = i0 + threadIdx.x;
@@ -378,8 +390,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         const Seq s = sequence(a, b);
         const Tile tl = tile_of<Sh>(a, s, tile);
         const int blocks = (int)min((int64_t)tl.blocks - rest, left), first_block = (int)rest;
-        const int64_t rows = (int64_t)s.nq * a.group, row0 = (int64_t)tile * R;
-        const int n_rows = (int)min((int64_t)R, rows - row0);
+        const uint32_t row0 = (uint32_t)tile * R;
+        const int n_rows = (int)min((uint32_t)R, (uint32_t)(s.nq * a.group) - row0);
 
         __syncthreads();                                // the last tile's shared memory has been read
         const int32_t* table = a.pages + (int64_t)b * a.ld_pages;
@@ -438,7 +450,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         for (int nt = warp; nt < NT; nt += kAtWarps) {
             const int r = nt * 8 + g;
             const bool on = r < n_rows;
-            const int64_t row = row0 + (on ? r : 0), token = row / a.group;
+            const uint32_t row = row0 + (on ? r : 0), token = token_of(a, row);
             const int64_t at = (s.row0 + token) * a.ldq + ((int64_t)head * a.group + (row - token * a.group)) * a.D;
             const int64_t pos = (int64_t)s.len - s.nq + token;
             float v[WK][8];
@@ -502,7 +514,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 #pragma unroll
             for (int c = 0; c < 2; c++) {
                 const int r = nt * 8 + 2 * t + c;
-                const int64_t pos = (int64_t)s.len - s.nq + (row0 + r) / a.group;
+                const int64_t pos = (int64_t)s.len - s.nq + token_of(a, row0 + r);
                 fq[nt][c] = qscale[r];
                 M[nt][c] = ninf;
                 L[nt][c] = 0.0f;
@@ -510,7 +522,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 qlo[nt][c] = a.window > 0 ? (int)max((int64_t)0, pos - a.window + 1) : 0;
             }
         // stages between these are seen by every row
-        const int64_t p0 = (int64_t)s.len - s.nq + row0 / a.group, p1 = (int64_t)s.len - s.nq + (row0 + n_rows - 1) / a.group;
+        const int64_t p0 = (int64_t)s.len - s.nq + token_of(a, row0), p1 = (int64_t)s.len - s.nq + token_of(a, row0 + n_rows - 1);
         const int all_hi = (int)max((int64_t)0, min(p0 + 1, (int64_t)s.seen)), all_lo = a.window > 0 ? (int)max((int64_t)0, p1 - a.window + 1) : 0;
 
         float o[DP / 16][NT][4];
@@ -772,7 +784,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 for (int k = 0; k < 8; k++) y[k] = x.x == ninf ? y[k] : fmaf(f[w], from[k], y[k]);
             }
             if (begins && ends) {
-                const int64_t row = row0 + r, token = row / a.group;
+                const uint32_t row = row0 + r, token = token_of(a, row);
                 const int64_t qh = (int64_t)head * a.group + (row - token * a.group);
                 const float inv = l == 0.0f ? 0.0f : __fdiv_rn(a.vunit, l);
 #pragma unroll
@@ -788,11 +800,12 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 }
             }
         }
-        if (!(begins && ends)) {
-            const int4 h = make_int4(ends ? 3 : 1, b, head, tile);
-            if (begins) slot_head[1] = h;
-            else slot_head[0] = h;
+        if (begins && !ends) {
+            const int64_t end_block = at_block + tl.blocks - 1, few = (share + 1) * larger;
+            const int64_t last = end_block < few ? quotient(end_block, share + 1) : larger + quotient(end_block - few, share);
+            goes_on = make_int4((int)last + 1, b, head, tile);
         }
+        at_block += blocks;
         left -= blocks;
         rest = 0;
         if (ends) {
@@ -808,36 +821,24 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             }
         }
     }
-    if (threadIdx.x < 2) a.head[2 * me + threadIdx.x] = slot_head[threadIdx.x];
+    if (threadIdx.x == 0) a.head[me] = goes_on;
 }
 
 // Joins the parts of a tile that begins in part `x` of the work and goes on in
 // the following ones.
 template <int DP, int R>
-__global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a, int parts)
+__global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a)
 {
     constexpr int SLOT = R * (DP + 2);
     griddep_wait();
     const int p0 = blockIdx.x;
-    const int4 h = a.head[2 * p0 + 1];
-    if (!(h.x & 1)) return;
+    const int4 h = a.head[p0];
+    if (h.x == 0) return;
     const Seq s = sequence(a, h.y);
-    const int64_t row = (int64_t)h.w * R + blockIdx.y, rows = (int64_t)s.nq * a.group;
-    if (row >= rows) return;
     const int r = blockIdx.y;
-    // the part that ends the tile
-    __shared__ int last;
-    if (threadIdx.x == 0) last = parts - 1;
-    __syncthreads();
-    for (int base = p0 + 1; base < parts; base += 128) {
-        const int p = base + threadIdx.x;
-        if (p < parts && (a.head[2 * p].x & 3) == 3) atomicMin(&last, p);
-        __syncthreads();
-        const bool found = last < base + 128;
-        __syncthreads();
-        if (found) break;
-    }
-    const int n = last - p0 + 1;
+    const uint32_t row = (uint32_t)h.w * R + r;
+    if (row >= (uint32_t)(s.nq * a.group)) return;
+    const int n = h.x - p0;             // parts
     auto slot = [&](int i) { return a.partial + (int64_t)(i == 0 ? 2 * p0 + 1 : 2 * (p0 + i)) * SLOT; };
     __shared__ float wm[4];
     const float ninf = __int_as_float(0xff800000);
@@ -875,7 +876,8 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a, i
         const float* p = parts_of[k][threadIdx.x % T];
         y[0] += p[0]; y[1] += p[1]; y[2] += p[2]; y[3] += p[3]; l += p[4];
     }
-    const int64_t token = row / a.group, qh = (int64_t)h.z * a.group + (row - token * a.group);
+    const uint32_t token = token_of(a, row);
+    const int64_t qh = (int64_t)h.z * a.group + (row - token * a.group);
     const float inv = l == 0.0f ? 0.0f : __fdiv_rn(a.vunit, l);
     const int64_t at = (s.row0 + token) * a.ldo + qh * a.D + d;
 #pragma unroll
@@ -896,17 +898,17 @@ cudaError_t run_attention(const AttnArgs& in, void* workspace, cudaStream_t st)
     AttnArgs a = in;
     const int parts = device_sm_count() * Sh::kSm;
     a.head = static_cast<int4*>(workspace);
-    a.partial = reinterpret_cast<float*>(a.head + 2 * parts);
+    a.partial = reinterpret_cast<float*>(a.head + parts);
     cudaError_t e = cudaFuncSetAttribute(attention_kernel<DP, NT, NP, LIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
     if (e != cudaSuccess) return e;
     e = launch_pdl(attention_kernel<DP, NT, NP, LIN>, dim3((unsigned)parts), dim3(kAtThreads), Sh::kBytes, st, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(attention_join_kernel<DP, Sh::R>, dim3((unsigned)parts, Sh::R), dim3(128), 0, st, a, parts);
+    return launch_pdl(attention_join_kernel<DP, Sh::R>, dim3((unsigned)parts, (unsigned)(a.starts ? Sh::R : std::min(a.group, Sh::R))), dim3(128), 0, st, a);
 }
 template <int DP, int NT, int NP> size_t workspace_of()
 {
     using Sh = Shape<DP, NT, NP>;
-    return (size_t)(device_sm_count() * Sh::kSm) * 2 * (sizeof(int4) + sizeof(float) * Sh::kSlot);
+    return (size_t)(device_sm_count() * Sh::kSm) * (sizeof(int4) + 2 * sizeof(float) * Sh::kSlot);
 }
 
 // One of a head size's shapes: NT eights of rows, NP planes of queries and weights.

@@ -284,6 +284,7 @@ esb_status esb_cache_attention(int64_t tokens, const esb_kv_cache* c, const esb_
     if (r != ESB_OK) return r;
     if (a->q_heads <= 0 || a->q_heads % c->heads != 0) return ESB_ERR_UNSUPPORTED;
     if (tokens >= 1ll << 31 || a->q_heads >= 1 << 23 || (int64_t)a->max_pages * c->page_size > 1 << 30) return ESB_ERR_RANGE;
+    if (tokens * (a->q_heads / c->heads) >= (1ll << 31) - 64) return ESB_ERR_RANGE;
     r = rotation_ok(a->rotation, c->head_dim, false, nullptr);
     if (r != ESB_OK) return r;
     if (tokens == 0 || a->seqs == 0) return ESB_OK;
