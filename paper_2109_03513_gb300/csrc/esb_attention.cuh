@@ -447,56 +447,47 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 
         // queries: rotated, scaled, each row by a power of two that puts its
         // largest below 2^15, as operands of the matrix instruction
-        for (int nt = warp; nt < NT; nt += kAtWarps) {
-            const int r = nt * 8 + g;
-            const bool on = r < n_rows;
-            const uint32_t row = row0 + (on ? r : 0), token = token_of(a, row);
+        // (a thread for each eight values, which are a word of K's codes)
+        for (int i = threadIdx.x; i < R * W; i += kAtThreads) {
+            const int r = i / W, word = i % W, d = 8 * word;
+            const bool on = r < n_rows && d < a.D;
+            const uint32_t row = row0 + (r < n_rows ? r : 0), token = token_of(a, row);
             const int64_t at = (s.row0 + token) * a.ldq + ((int64_t)head * a.group + (row - token * a.group)) * a.D;
             const int64_t pos = (int64_t)s.len - s.nq + token;
-            float v[WK][8];
-            float big = 0.0f;
+            float v[8], big = 0.0f;
 #pragma unroll
-            for (int k = 0; k < WK; k++) {
-                const int word = DP == 256 ? (k < 4 ? 4 * t + k : 16 + 4 * t + k - 4) : WK * t + k, d = 8 * word;
-                if (on && d < a.D) {
-                    if (a.rot.dim) {
-                        if (a.q_type == ESB_F32) rotated8(static_cast<const float*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
-                        else if (a.q_type == ESB_F16) rotated8(static_cast<const __half*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
-                        else rotated8(static_cast<const __nv_bfloat16*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v[k]);
-                    } else {
-                        load8_any(a.q, a.q_type, at + d, a.D - d, a.qvec, v[k]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; i++) v[k][i] = 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; i++) big = fmaxf(big, fabsf(v[k][i]));
+            for (int e = 0; e < 8; e++) v[e] = 0.0f;
+            if (on) {
+                if (!a.rot.dim) load8_any(a.q, a.q_type, at + d, a.D - d, a.qvec, v);
+                else if (a.q_type == ESB_F32) rotated8(static_cast<const float*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v);
+                else if (a.q_type == ESB_F16) rotated8(static_cast<const __half*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v);
+                else rotated8(static_cast<const __nv_bfloat16*>(a.q) + at, a.D, d, a.qvec, a.rot, pos, v);
             }
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+#pragma unroll
+            for (int e = 0; e < 8; e++) big = fmaxf(big, fabsf(v[e]));
+#pragma unroll
+            for (int o = W / 2; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
             // 2^e takes the largest to 2^14 .. 2^15; the ends of fp32 stay in range
             const int e = big > 0.0f && big < __int_as_float(0x7f800000) ? 14 - max(-112, min(126, ((int)(__float_as_uint(big) >> 23) - 127))) : 0;
             const float up = __uint_as_float((uint32_t)(e / 2 + 127) << 23), up2 = __uint_as_float((uint32_t)(e - e / 2 + 127) << 23);
-            if (t == 0) qscale[r] = a.scale2 * __uint_as_float((uint32_t)(127 - e / 2) << 23) * __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+            if (word == 0) qscale[r] = a.scale2 * __uint_as_float((uint32_t)(127 - e / 2) << 23) * __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
 #pragma unroll
-            for (int k = 0; k < WK; k++) {
+            for (int x = 0; x < 8; x++) v[x] = v[x] * up * up2;
+            // the lane and step that take this word: quads' words as K's are read
+            const int to_t = DP == 64 ? word >> 1 : (word & 15) >> 2, k = DP == 64 ? word & 1 : (word & 3) + 4 * (word >> 4);
+            uint2* q = qf + (((r >> 3) * NP) * STEPS + 2 * k) * 32 + (r & 7) * 4 + to_t;
 #pragma unroll
-                for (int i = 0; i < 8; i++) v[k][i] = v[k][i] * up * up2;
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    uint2 hi, lo;
-                    hi.x = pack2<__half>(v[k][2 * h], v[k][2 * h + 4]);
-                    hi.y = pack2<__half>(v[k][2 * h + 1], v[k][2 * h + 5]);
-                    qf[((nt * NP) * STEPS + 2 * k + h) * 32 + lane] = hi;
-                    if constexpr (NP == 2) {
-                        float x[4];
-                        unpack2<__half>(hi.x, x[0], x[1]);
-                        unpack2<__half>(hi.y, x[2], x[3]);
-                        lo.x = pack2<__half>(v[k][2 * h] - x[0], v[k][2 * h + 4] - x[1]);
-                        lo.y = pack2<__half>(v[k][2 * h + 1] - x[2], v[k][2 * h + 5] - x[3]);
-                        qf[((nt * NP + 1) * STEPS + 2 * k + h) * 32 + lane] = lo;
-                    }
+            for (int h = 0; h < 2; h++) {
+                uint2 hi;
+                hi.x = pack2<__half>(v[2 * h], v[2 * h + 4]);
+                hi.y = pack2<__half>(v[2 * h + 1], v[2 * h + 5]);
+                q[h * 32] = hi;
+                if constexpr (NP == 2) {
+                    float x[4];
+                    unpack2<__half>(hi.x, x[0], x[1]);
+                    unpack2<__half>(hi.y, x[2], x[3]);
+                    q[(STEPS + h) * 32] = make_uint2(pack2<__half>(v[2 * h] - x[0], v[2 * h + 4] - x[1]),
+                                                     pack2<__half>(v[2 * h + 1] - x[2], v[2 * h + 5] - x[3]));
                 }
             }
         }
