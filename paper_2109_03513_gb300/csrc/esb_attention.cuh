@@ -23,6 +23,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -890,8 +891,17 @@ cudaError_t run_attention(const AttnArgs& in, void* workspace, cudaStream_t st)
     const int parts = device_sm_count() * Sh::kSm;
     a.head = static_cast<int4*>(workspace);
     a.partial = reinterpret_cast<float*>(a.head + parts);
-    cudaError_t e = cudaFuncSetAttribute(attention_kernel<DP, NT, NP, LIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
+    // once for a device
+    static std::atomic<unsigned long long> configured{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0ull;
+    if (!(configured.load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(attention_kernel<DP, NT, NP, LIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes);
+        if (e != cudaSuccess) return e;
+        configured.fetch_or(bit, std::memory_order_relaxed);
+    }
     e = launch_pdl(attention_kernel<DP, NT, NP, LIN>, dim3((unsigned)parts), dim3(kAtThreads), Sh::kBytes, st, a);
     if (e != cudaSuccess) return e;
     return launch_pdl(attention_join_kernel<DP, Sh::R>, dim3((unsigned)parts, (unsigned)(a.starts ? Sh::R : std::min(a.group, Sh::R))), dim3(128), 0, st, a);

@@ -3,11 +3,15 @@ head of a decoder, as it answers (4-bit weights with group scales, 8-bit
 activations) and as it is trained (fake-quantised weights and activations,
 straight-through gradients).
 
-There is no attention here: a layer is norm -> up -> relu -> down with a
-residual stream, a token's answer depends on that token alone.  It runs the
-library's language-model operators together, in the order in which a decoding
-or training step calls them; PyTorch adds the embedding lookup, the rectifier
-and, in training, the dense products of the fake-quantised values.
+The model that is trained has no attention: a layer is norm -> up -> relu ->
+down with a residual stream, a token's answer depends on that token alone.  It
+runs the library's language-model operators together, in the order in which a
+decoding or training step calls them; PyTorch adds the embedding lookup, the
+rectifier and, in training, the dense products of the fake-quantised values.
+
+Decoder answers with attention as well: before each such layer the heads'
+norms and rotation, the 4-bit cache and attention over it, with 4-bit
+projections around them.  It takes prompts and single tokens alike.
 
     python -m paper_2109_03513_gb300.lmrun        # trains on a fixed next-token rule, then answers
 """
@@ -120,6 +124,53 @@ class Serving:
         o = esb.esb_rmsnorm(stream, self.norms["norm"], c.eps, residual=out, fmt=X_FMT)
         logits = esb.esb_matvec_groups(o.coded, w["head"], y_dtype=torch.float32)
         return esb.esb_logprobs(logits, targets, top=top)
+
+
+class Decoder:
+    """Serving of layers with attention (random weights): norm -> q, k, v -> norms of heads and rotation -> append ->
+    attention -> output projection, then the feed-forward layer.  Sequences grow in pages of a shared cache; step()
+    takes some new tokens of each, a prompt's or one."""
+
+    def __init__(self, cfg: Config, heads: int = 4, kv_heads: int = 2, head_dim: int = 64, pages: int = 64, page_size: int = 16,
+                 most: int = 4096, k_fmt: esb.Fmt = esb.Fmt(4, 2), v_fmt: esb.Fmt = esb.Fmt(4, 2), seed: int = 0, device="cuda"):
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        self.ffn = Model(cfg, seed, device).serving()
+        self.cfg, self.heads, self.kv_heads, self.head_dim, self.page_size = cfg, heads, kv_heads, head_dim, page_size
+        self.rotation = esb.rotation(head_dim, most, device=device)
+        self.caches = [esb.kv_cache(pages, kv_heads, page_size, head_dim, k_fmt, v_fmt, device) for _ in range(cfg.layers)]
+        rows = (heads + 2 * kv_heads) * head_dim
+
+        def coded(n, k):
+            return esb.esb_project_groups(torch.randn(n, k, generator=g, device=device) * k ** -0.5, W_FMT, GROUP)[0]
+
+        self.qkv = [coded(rows, cfg.width) for _ in range(cfg.layers)]
+        self.out = [coded(cfg.width, heads * head_dim) for _ in range(cfg.layers)]
+        self.norms = [[1 + 0.1 * torch.randn(n, generator=g, device=device) for n in (cfg.width, head_dim, head_dim)] for _ in range(cfg.layers)]
+
+    def step(self, tokens: torch.Tensor, starts: torch.Tensor, lens: torch.Tensor, pages: torch.Tensor) -> torch.Tensor:
+        """Logits (n, vocab) of new tokens (n,): sequence i's are rows starts[i] .. starts[i + 1] - 1, lens[i] its places
+        with them, pages[i] the cache's pages it has (int32 each)."""
+        c, f, d = self.cfg, self.ffn, self.head_dim
+        n = tokens.numel()
+        seq = torch.bucketize(torch.arange(n, device=tokens.device), starts[1:], right=True)
+        positions = lens[seq].long() - starts[seq + 1] + torch.arange(n, device=tokens.device)
+        slots = pages[seq, positions // self.page_size].long() * self.page_size + positions % self.page_size
+        stream, out, nq, nk = f.embed[tokens], None, self.heads * d, self.kv_heads * d
+        for i in range(c.layers):
+            wx, wq, wk = self.norms[i]
+            o = esb.esb_rmsnorm(stream, wx, c.eps, residual=out, fmt=X_FMT, want_y=False)
+            stream = o.h if out is not None else stream
+            qkv = esb.esb_matvec_groups(o.coded, self.qkv[i])
+            hn = esb.esb_headnorm(qkv[:, :nq], qkv[:, nq:nq + nk], d, wq, wk, c.eps, rotation=self.rotation, positions=positions)
+            esb.esb_cache_append(self.caches[i], hn.k, qkv[:, nq + nk:], slots)
+            a, _ = esb.esb_cache_attention(hn.q, self.caches[i], lens, pages, starts=starts)
+            out = esb.esb_matvec_groups(esb.esb_project_groups(a, X_FMT, 0)[0], self.out[i])
+            o = esb.esb_rmsnorm(stream, f.norms[f"norm{i}"], c.eps, residual=out, fmt=X_FMT, want_y=False)
+            u = torch.relu_(esb.esb_matvec_groups(o.coded, f.w[f"up{i}"]))
+            stream, out = o.h, esb.esb_matvec_groups(esb.esb_project_groups(u, X_FMT, 0)[0], f.w[f"down{i}"])
+        o = esb.esb_rmsnorm(stream, f.norms["norm"], c.eps, residual=out, fmt=X_FMT)
+        return esb.esb_matvec_groups(o.coded, f.w["head"], y_dtype=torch.float32)
 
 
 def main(steps: int = 200, seed: int = 0) -> float:
