@@ -862,7 +862,8 @@ typedef struct esb_kv_cache {
  *   positions  [device] tokens (with rotation)
  *   rotation   [host] or NULL
  *   kq, vq     [device] the numbers the codes stand for, tokens x (heads *
- *              head_dim) of q_type, or NULL; rows of tokens left out are not written
+ *              head_dim) of q_type, or NULL; rows of tokens left out are not
+ *              written.  They may not lie on k or v
  * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes), RANGE, ALIGN, CUDA. */
 typedef struct esb_append {
     const void *k, *v;         /* [device] tokens x (heads * head_dim) of x_type */
@@ -893,8 +894,8 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
  * sees makes its numbers NaN; what it does not see has no effect, whatever it is.
  * Products are of fp16 numbers, sums fp32: codes take part as they are; queries
  * and weights (probabilities times a value's scale) with 11 significant bits
- * where queries are bf16, else with 22.  v's scales are exact between 2^-100 and
- * 2^100.
+ * where queries are bf16, else with 22, where v's scales lie between 2^-100 and
+ * 2^100 and, of the places that a query sees, within a factor of 2^100.
  *   workspace  [device] >= esb_cache_attention_workspace_bytes bytes, 16-byte
  *              aligned; nothing is kept in it between calls
  * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes, q_heads not a multiple of

@@ -73,6 +73,22 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The instruction's sums are truncated, not rounded: where queries and weights
+// have 22 bits, a place's products are summed on their own and added in fp32.
+__device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b0)[2], const uint32_t (&b1)[2])
+{
+    float x[4];
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0[1]), "r"(b1[1]), "f"(0.0f));
+    mma16(x, a0, a1, a2, a3, b0[0], b1[0]);
+#pragma unroll
+    for (int i = 0; i < 4; i++) d[i] += x[i];
+}
+__device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b0)[1], const uint32_t (&b1)[1])
+{
+    mma16(d, a0, a1, a2, a3, b0[0], b1[0]);
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t a)
 {
     uint32_t r;
@@ -233,15 +249,17 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh)
     return v;
 }
 
-// Work of sequences b0 + thread (0 past the end), long ones by the whole block.
+// Work of sequence first + thread * step, for the first `count` threads; those
+// with many tiles by the whole block.
+// (One copy of it: a block runs this once, out of a cold instruction cache.)
 template <class Sh>
-__device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* sh)
+__device__ __noinline__ int64_t work_of(const AttnArgs& a, int64_t first, int64_t step, int count, int64_t* sh)
 {
-    const int b = b0 + threadIdx.x;
+    const int64_t b = first + threadIdx.x * step;
     int64_t w = 0;
     bool many = false;
-    if (b < a.seqs) {
-        const Seq s = sequence(a, b);
+    if ((int)threadIdx.x < count && b < a.seqs) {
+        const Seq s = sequence(a, (int)b);
         const int n = tiles_of<Sh>(a, s);
         many = n > 8;
         if (!many)
@@ -254,7 +272,7 @@ __device__ __forceinline__ int64_t work_of(const AttnArgs& a, int b0, int64_t* s
         __syncthreads();
         for (int k = 0; k < kAtThreads; k++) {
             if (!(list[k >> 5] >> (k & 31) & 1u)) continue;
-            const Seq s = sequence(a, b0 + k);
+            const Seq s = sequence(a, (int)(first + k * step));
             const int n = tiles_of<Sh>(a, s);
             int64_t part = 0;
             for (int i = threadIdx.x; i < n; i += kAtThreads) part += tile_of<Sh>(a, s, i).blocks;
@@ -272,7 +290,7 @@ struct Found {
     int who;
     int64_t rest;
 };
-__device__ __forceinline__ Found find(int64_t w, int64_t at, int64_t* sh, int64_t& total)
+__device__ __noinline__ Found find(int64_t w, int64_t at, int64_t* sh, int64_t& total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t p = w;
@@ -307,7 +325,7 @@ __device__ __forceinline__ Found find(int64_t w, int64_t at, int64_t* sh, int64_
 // ------------------------------------------------------------------ kernel
 
 template <int DP, int NT, int NP, bool LIN>
-__global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_kernel(const __grid_constant__ AttnArgs a)
 {
     using Sh = Shape<DP, NT, NP>;
     using St = Stage<DP>;
@@ -330,10 +348,12 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     int64_t left = 0, rest = 0, at_block = 0, share = 1, larger = 0;    // the first `larger` blocks have one more than `share`
     int b = 0, head = 0, tile = 0;
     {
-        int64_t w = work_of<Sh>(a, 0, sh), total = 0;
-        if (a.seqs <= kAtThreads) total = block_sum(w, sh);
-        else
-            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) total += block_sum(b0 ? work_of<Sh>(a, b0, sh) : w, sh);
+        // each thread sums a run of sequences
+        const int run = (a.seqs + kAtThreads - 1) / kAtThreads;
+        int64_t w = 0;
+#pragma unroll 1
+        for (int i = 0; i < run; i++) w += work_of<Sh>(a, i, run, kAtThreads, sh);
+        const int64_t total = block_sum(w, sh);
         const int64_t least = total / Sh::kMinBlocks, n = least < 1 ? 1 : (least < gridDim.x ? least : gridDim.x);
         if (me < n && total > 0) {
             share = quotient(total, n);
@@ -341,12 +361,14 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             int64_t at = share * me + min((int64_t)me, larger);
             left = share + (me < larger ? 1 : 0);
             at_block = at;
-            for (int b0 = 0; b0 < a.seqs; b0 += kAtThreads) {
-                if (b0) w = work_of<Sh>(a, b0, sh);
-                int64_t sum;
-                const Found f = find(w, at, sh, sum);
-                if (f.who >= 0) { b = b0 + f.who; rest = f.rest; break; }
-                at -= sum;
+            int64_t sum;
+            Found f = find(w, at, sh, sum);
+            b = f.who * run;
+            rest = f.rest;
+            for (int i = 0; run > 1 && i < run; i += kAtThreads) {
+                f = find(work_of<Sh>(a, b + i, 1, min(run - i, kAtThreads), sh), rest, sh, sum);
+                if (f.who >= 0) { b += i + f.who; rest = f.rest; break; }
+                rest -= sum;
             }
             const Seq s = sequence(a, b);
             const int n_tiles = tiles_of<Sh>(a, s);
@@ -534,8 +556,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             issue();
             if (here == 0u) continue;
 
-            // scores: rows g and g + 8 of each part (two chains of products where a warp has few columns)
-            constexpr int CH = NT == 1 && SUB == 1 ? 2 : 1;
+            // scores: rows g and g + 8 of each part (the planes' sums apart)
+            constexpr int CH = NP == 2 || (NT == 1 && SUB == 1) ? 2 : 1;
             float part[SUB][CH][NT][4];
 #pragma unroll
             for (int sub = 0; sub < SUB; sub++) {
@@ -574,7 +596,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                                 uint2 q;
                                 if constexpr (Sh::kQueryRegs) q = qr[at];
                                 else q = qf[at * 32 + lane];
-                                mma16(part[sub][h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
+                                mma16(part[sub][NP == 2 ? p : h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
                             }
                 }
             }
@@ -693,8 +715,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                     for (int k = 0; k < 4; k++)
 #pragma unroll
                         for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                            for (int p = 0; p < NP; p++) mma16(o[k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                        mma16_add(o[k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt], p1[nt]);
                 } else {
                     // rows g: the first word's values, rows g + 8: the second's
 #pragma unroll
@@ -712,9 +733,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                             for (int k = 0; k < 4; k++)
 #pragma unroll
                                 for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                                    for (int p = 0; p < NP; p++)
-                                        mma16(o[8 * wp + 4 * up + k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt][p], p1[nt][p]);
+                                mma16_add(o[8 * wp + 4 * up + k][nt], x0[k], y0[k], x1[k], y1[k], p0[nt], p1[nt]);
                         }
                 }
             }

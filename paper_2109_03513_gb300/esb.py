@@ -1037,6 +1037,12 @@ def _turn(rot: Optional[Rotation], positions, tokens: int) -> tuple[esb_rotation
     return rot.c(), _vector(positions, "positions", tokens, torch.int64)
 
 
+def _on_current(t: torch.Tensor):
+    """A launch goes to the current device: memory of another would be read across."""
+    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
+        raise ValueError("tensors must be on the current device")
+
+
 def _head_count(t: torch.Tensor, name: str, head_dim: int) -> int:
     if head_dim <= 0 or t.shape[1] % head_dim:
         raise ValueError(f"{name} must have whole heads of head_dim values a row")
@@ -1090,6 +1096,7 @@ def esb_headnorm(q: Optional[torch.Tensor], k: Optional[torch.Tensor], head_dim:
     qp, qy, qr = part("q", q, q_weight, qy)
     kp, ky, kr = part("k", k, k_weight, ky)
     rot, pos = _turn(rotation, positions, tokens)
+    _on_current(x0)
     a = esb_head_norm((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0), eps)
     _check(lib().esb_headnorm(tokens, ctypes.byref(a), _stream(stream)), "esb_headnorm")
     return HeadNorm(qy, ky, qr, kr)
@@ -1152,6 +1159,7 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
     qp, dq, dqw = part(0, "q", q, gq, q_weight, q_rstd, dq)
     kp, dk, dkw = part(1, "k", k, gk, k_weight, k_rstd, dk)
     rot, pos = _turn(rotation, positions, tokens)
+    _on_current(x0)
     a = esb_head_norm_grad((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0))
     wp, nb = None, 0
     if sums is not None:
@@ -1238,6 +1246,7 @@ def esb_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: to
         qt, vp = t, vq.data_ptr()
     if rotation is not None:
         r, pos = _turn(rotation, positions, tokens)
+    _on_current(k)
     a = esb_append(k.data_ptr(), v.data_ptr(), ldk, ldv, _vector(slots, "slots", tokens, torch.int64), pos,
                    None if r is None else ctypes.addressof(r), kp, vp, ldkq, ldvq, xt, qt, rule, rounding)
     _check(lib().esb_cache_append(tokens, ctypes.byref(c), ctypes.byref(a), _stream(stream)), "esb_cache_append")
@@ -1279,6 +1288,7 @@ def esb_cache_attention(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, pag
             raise ValueError("out must have the shape of q")
     lse = empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
     r = None if rotation is None else rotation.c()
+    _on_current(q)
     a = esb_attention(q.data_ptr(), ldq, out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), sp, lp, pages.data_ptr(),
                       pages.stride(0) if seqs > 1 else held[1], None if r is None else ctypes.addressof(r), seqs, held[1], heads,
                       window, qt, ot, c.head_dim ** -0.5 if scale is None else scale)

@@ -550,6 +550,29 @@ def test_attention_offsets_past_32_bits():
     assert torch.equal(kc[2, :, 5], c.k_codes[2, :, 5])
 
 
+@pytest.mark.parametrize("seqs", [128, 129, 1500, 17000])
+def test_attention_of_many_sequences(seqs):
+    # more sequences than threads that look for a block's part of them, some without queries, some with many
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seqs)
+    c = make_cache(50, 1, 16, 64, 2, 2, 3)
+    lens = torch.randint(0, 60, (seqs,), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randint(0, 50, (seqs, 4), generator=g, device="cuda", dtype=torch.int32)
+    q = rand((seqs, 64), 8, BF)
+    out, lse = esb.esb_cache_attention(q, c, lens, t, want_lse=True)
+    pick = torch.cat([torch.arange(0, seqs, max(1, seqs // 40), device="cuda"), torch.tensor([seqs - 1], device="cuda")])
+    check_attention(q[pick], c, lens[pick], t[pick], out[pick], lse[pick])
+    # the same as several queries of some
+    counts = torch.randint(0, 3, (seqs,), generator=g, device="cuda")
+    counts[seqs // 2], counts[seqs // 3] = 300, 90
+    starts = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), counts.cumsum(0)]).int()
+    q = rand((int(starts[-1]), 64), 9, BF)
+    out, lse = esb.esb_cache_attention(q, c, lens, t, starts=starts, want_lse=True)
+    for i in pick.tolist() + [seqs // 2, seqs // 3]:
+        a, b = int(starts[i]), int(starts[i + 1])
+        check_attention(q[a:b], c, lens[i:i + 1], t[i:i + 1], out[a:b], lse[a:b], starts=i32([0, b - a]))
+
+
 def test_attention_nothing_to_do_and_refusals():
     c = esb.kv_cache(2, 1, 16, 64)
     q = rand((2, 64), 1)
