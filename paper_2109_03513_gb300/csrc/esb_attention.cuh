@@ -185,7 +185,7 @@ template <int DP, int NT, int NP> struct Shape {
     static constexpr int kMinBlocks = NT == 1 ? 1 : 2;  // of a thread block, while there is enough work
     static constexpr int kStages = DP == 256 ? (NT == 1 ? 3 : 4) : NT == 1 ? 3 : 6;
     static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
-    static constexpr int kSm = NT == 1 ? (DP == 256 ? 2 : 3) : (NT == 2 && DP <= 128 && NP == 1 ? 3 : 2);
+    static constexpr int kSm = NT > 1 || DP == 256 ? 2 : DP == 64 ? 4 : 3;    // blocks on an SM
     static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
     static constexpr int kRing = kAtWarps * kStages * kParts * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;
     static constexpr int kSums = kAtWarps * R * 8;      // maxima and sums of the warps

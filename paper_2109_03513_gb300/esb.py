@@ -1125,7 +1125,7 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
     dtype, tokens = x0.dtype, x0.shape[0]
     total = wt = 0
     # gradients of the weights, one after the other
-    sums = None if q_weight is None and k_weight is None else empty((2, head_dim), dtype=f32, device=x0.device)
+    sums = None if q_weight is None and k_weight is None else empty((2, head_dim), dtype=f32, device=x0.device).unbind(0)
 
     def part(i, name, x, g, w, r, d):
         nonlocal total, wt
@@ -1206,7 +1206,7 @@ class KvCache(NamedTuple):
         if pages and (cst[3] != 1 or (cst[2] != words and size > 1) or (cst[1] != size * words and heads > 1) or
                       (sst[2] != 1 and size > 1) or (sst[1] != size and heads > 1)):
             raise ValueError("a page's codes and scales must be contiguous")
-        return esb_kv_cache(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, ld, lds, heads, size, d, kf.c(), vf.c())
+        return esb_kv_cache(kc.data_ptr(), vc.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, ld, lds, heads, size, d, (kf.b, kf.k, kf.signed), (vf.b, vf.k, vf.signed))
 
 
 def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, k_fmt: Fmt = Fmt(4, 2), v_fmt: Fmt = Fmt(4, 2),
