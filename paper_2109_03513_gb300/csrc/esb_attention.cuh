@@ -17,9 +17,18 @@
 // so far (up to 2^8; it is raised when a u passes that), the weight 2^(score -
 // M) v_scale is of order 1 whatever the scales are, and is rounded to fp16.
 //
-// The work, blocks of 64 places of all tiles in a row, is cut into equal parts,
-// one for each thread block, wherever that cuts a tile; parts of tiles go to
-// the workspace, and a second kernel joins them in their order.
+// The work, blocks of places (a stage of each of four warps) of all tiles in a
+// row, is cut into equal parts, one for each thread block, wherever that cuts a
+// tile; parts of tiles go to the workspace, and a second kernel joins them in
+// their order.
+//
+// 4 x 131072 places, 8 heads of 128, 4 queries each (570 MB): 150 us, 3.8 TB/s,
+// 56% of the copy rate.  16 places take 370 instructions of a warp, 264 of them on
+// the pipe of integer and permute work, which does 64 lanes a clock and is three
+// quarters busy.  A prompt's 512 tokens over 4096 places, four of them (129 GFLOP):
+// 660 us, 195 TFLOP/s; its tiles' sums leave two warps a scheduler, which wait for
+// fixed latencies.  One sequence of 2048 places: 12 us, two kernels' starts,
+// look-ups and loads one after the other.
 #pragma once
 
 #include <algorithm>
@@ -140,7 +149,8 @@ __device__ __forceinline__ float lds_f32(uint32_t at)
 // places are put in order for four codes at once, then spread; a shift to the
 // left is a multiplication, on the pipe that has nothing to do.
 // Ten instructions a word (thirteen with the table), nine and twelve of them on
-// the pipe that bounds the kernel.
+// the pipe that bounds the kernel.  (Signs spread by a second permute and tables
+// for all sets: fourteen, and 4 x 131072 places in 237 us where these took 186.)
 template <bool LIN>
 __device__ __forceinline__ void decode8(uint32_t w, const uint2& lut, uint32_t (&r)[4])
 {
@@ -180,12 +190,14 @@ template <int DP> struct Stage {
 
 template <int DP, int NT, int NP> struct Shape {
     static constexpr int R = 8 * NT, kSteps = DP / 16;
-    static constexpr int kParts = NT == 1 ? 2 : 1;      // of a stage: few rows share a stage's fixed work over more places
+    static constexpr int kParts = NT == 1 ? 2 : 1;      // of a stage: few rows share its fixed work over more places (169 us, 180 with one, for 4 x 131072 then)
     static constexpr int kBlock = kAtPlaces * kParts * kAtWarps;    // places of a block of work
     static constexpr int kMinBlocks = NT == 1 ? 1 : 2;  // of a thread block, while there is enough work
     static constexpr int kStages = DP == 256 ? (NT == 1 ? 3 : 4) : NT == 1 ? 3 : 6;
     static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
-    static constexpr int kSm = NT > 1 || DP == 256 ? 2 : DP == 64 ? 4 : 3;    // blocks on an SM
+    // Blocks on an SM.  Tiles of 16 rows: 49 us for 24 x 10000 places, 55 with three blocks, whose registers spill;
+    // heads of 64: 37 us for 48 windows of 1000, 39.5 with three.
+    static constexpr int kSm = NT > 1 || DP == 256 ? 2 : DP == 64 ? 4 : 3;
     static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
     static constexpr int kRing = kAtWarps * kStages * kParts * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;
     static constexpr int kSums = kAtWarps * R * 8;      // maxima and sums of the warps

@@ -278,6 +278,9 @@ inline int pair_mode(int D, int rot_dim, bool interleaved, bool vectors)
     return interleaved || rot_dim == 0 ? kPairRows : rot_dim == D ? kPairHalves : kPairMixed;
 }
 
+// Whole eights of a table's cosines and sines are vectors.
+inline bool table_vectors(const RotArgs& r) { return r.dim % 8 == 0 && r.ld % 4 == 0 && (reinterpret_cast<uintptr_t>(r.table) & 15u) == 0; }
+
 inline bool rows16(const void* p, int64_t ld, int type)
 {
     return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * type_bytes(type) % 16 == 0;
