@@ -613,9 +613,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 }
             }
             const bool whole = place + kAtPlaces * SUB <= all_hi && place >= all_lo && here == (1u << SUB) - 1u;
-            float sc[SUB][NT][4], vs[SUB][2];
-            float over = ninf;                          // how far scores (with their values' scales) pass the maximum
-            // scores less the maximum (what is not seen: -inf, whatever the maximum is)
+            float sc[SUB][NT][4], vs[SUB][2], lv[SUB][2];
+            // scores less the maximum
 #pragma unroll
             for (int sub = 0; sub < SUB; sub++) {
                 const uint32_t scales = sm + sub * St::kBytes + St::kKs + 4 * g;
@@ -623,7 +622,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 vs[sub][0] = lds_f32(scales + 64);
                 vs[sub][1] = lds_f32(scales + 96);
                 // log2 of v's scales, where they have one
-                const float lv0 = fmaxf(fminf(lg2(fabsf(vs[sub][0])), 100.0f), -100.0f), lv1 = fmaxf(fminf(lg2(fabsf(vs[sub][1])), 100.0f), -100.0f);
+#pragma unroll
+                for (int c = 0; c < 2; c++) lv[sub][c] = fmaxf(fminf(lg2(fabsf(vs[sub][c])), 100.0f), -100.0f);
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -635,25 +635,35 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         }
                         part[sub][0][nt][c] = x * ks0;
                         part[sub][0][nt][2 + c] = y * ks1;
-                        x = fmaf(part[sub][0][nt][c], fq[nt][c], -M[nt][c]);
-                        y = fmaf(part[sub][0][nt][2 + c], fq[nt][c], -M[nt][c]);
-                        if (!whole) {
-                            const int at = place + sub * kAtPlaces + g;
-                            const bool on = here >> (SUB - 1 - sub) & 1u;
-                            if (!on || at >= qhi[nt][c] || at < qlo[nt][c]) x = ninf;
-                            if (!on || at + 8 >= qhi[nt][c] || at + 8 < qlo[nt][c]) y = ninf;
-                        }
-                        over = fmaxf(over, fmaxf(x + lv0, y + lv1));
-                        sc[sub][nt][c] = x;
-                        sc[sub][nt][2 + c] = y;
+                        sc[sub][nt][c] = fmaf(part[sub][0][nt][c], fq[nt][c], -M[nt][c]);
+                        sc[sub][nt][2 + c] = fmaf(part[sub][0][nt][2 + c], fq[nt][c], -M[nt][c]);
                     }
             }
-            if (__any_sync(0xffffffffu, over > 8.0f)) {
-                float lv[SUB][2];
+            // what is not seen: -inf, whatever the maximum is (apart from the rest,
+            // which whole stages have to themselves)
+            uint32_t unseen = 0u;
+            if (!whole) {
 #pragma unroll
                 for (int sub = 0; sub < SUB; sub++)
 #pragma unroll
-                    for (int c = 0; c < 2; c++) lv[sub][c] = fmaxf(fminf(lg2(fabsf(vs[sub][c])), 100.0f), -100.0f);
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            const int at = place + sub * kAtPlaces + g + 8 * (c >> 1);
+                            if (!(here >> (SUB - 1 - sub) & 1u) || at >= qhi[nt][c & 1] || at < qlo[nt][c & 1]) {
+                                unseen |= 1u << ((sub * NT + nt) * 4 + c);
+                                sc[sub][nt][c] = ninf;
+                            }
+                        }
+            }
+            float over = ninf;                          // how far scores (with their values' scales) pass the maximum
+#pragma unroll
+            for (int sub = 0; sub < SUB; sub++)
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                    for (int c = 0; c < 2; c++) over = fmaxf(over, fmaxf(sc[sub][nt][c] + lv[sub][0], sc[sub][nt][2 + c] + lv[sub][1]));
+            if (__any_sync(0xffffffffu, over > 8.0f)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -685,20 +695,33 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         }
                     }
             }
+            // weights; a scale that is not seen may be NaN
 #pragma unroll
-            for (int sub = 0; sub < SUB; sub++) {
-                // weights, turned into the second product's operand
-                uint32_t p0[NT][NP], p1[NT][NP];
+            for (int sub = 0; sub < SUB; sub++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++) {
-                    float w[4];
+                for (int nt = 0; nt < NT; nt++)
 #pragma unroll
                     for (int c = 0; c < 4; c++) {
                         const float e = ex2(sc[sub][nt][c]);
                         L[nt][c & 1] += e;
-                        w[c] = e * vs[sub][c >> 1];
-                        if (!whole && sc[sub][nt][c] == ninf) w[c] = 0.0f;   // a scale that is not seen may be NaN
+                        sc[sub][nt][c] = e * vs[sub][c >> 1];
                     }
+            if (!whole) {
+#pragma unroll
+                for (int sub = 0; sub < SUB; sub++)
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int c = 0; c < 4; c++)
+                            if (unseen >> ((sub * NT + nt) * 4 + c) & 1u) sc[sub][nt][c] = 0.0f;
+            }
+#pragma unroll
+            for (int sub = 0; sub < SUB; sub++) {
+                // turned into the second product's operand
+                uint32_t p0[NT][NP], p1[NT][NP];
+#pragma unroll
+                for (int nt = 0; nt < NT; nt++) {
+                    const float (&w)[4] = sc[sub][nt];
                     const uint32_t h0 = pack2<__half>(w[0], w[1]), h1 = pack2<__half>(w[2], w[3]);
                     p0[nt][0] = transposed(h0);
                     p1[nt][0] = transposed(h1);
