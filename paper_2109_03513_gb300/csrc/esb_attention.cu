@@ -62,9 +62,6 @@ cudaError_t launch_attention(int64_t tokens, const esb_kv_cache& c, const esb_at
     a.vunit = lin ? (float)(1 << (16 - c.v_fmt.k)) : 1.0f;
     a.seqs = n.seqs; a.max_pages = n.max_pages; a.heads = c.heads; a.group = n.q_heads / c.heads; a.D = c.head_dim;
     a.chunks = (c.head_dim + 31) / 32; a.page_size = c.page_size;
-    a.page_shift = -1;
-    for (int i = 4; i < 31; i++)
-        if (c.page_size == 1 << i) a.page_shift = i;
     a.group_shift = -1;
     for (int i = 0; i < 24; i++)
         if (a.group == 1 << i) a.group_shift = i;

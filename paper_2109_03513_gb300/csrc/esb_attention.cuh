@@ -55,7 +55,7 @@ struct AttnArgs {
     int64_t npages;
     uint32_t page16, page_lds;                          // a page in 16 bytes of codes, and in scales
     uint2 klut, vlut;                                   // high bytes of the fp16 numbers of codes 0..7; LIN: x = what turns a code into its place
-    int seqs, max_pages, heads, group, group_shift, D, chunks, page_size, page_shift, window;
+    int seqs, max_pages, heads, group, group_shift, D, chunks, page_size, window;
     int q_type, out_type, qvec, ovec;
     float scale2, vunit;                                // scale log2(e) and K's unit; V's unit
     RotArgs rot;
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     __shared__ int64_t sh[kAtWarps + 2];
     unsigned char* ring = smem;
     float* merge = reinterpret_cast<float*>(smem);
-    uint2* qf = reinterpret_cast<uint2*>(smem + (Sh::kRing > Sh::kMerge ? Sh::kRing : Sh::kMerge));
+    uint4* qf = reinterpret_cast<uint4*>(smem + (Sh::kRing > Sh::kMerge ? Sh::kRing : Sh::kMerge));
     float2* sums = reinterpret_cast<float2*>(reinterpret_cast<unsigned char*>(qf) + Sh::kQueryBytes);
     float* qscale = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(sums) + Sh::kSums);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
@@ -437,33 +437,42 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         const char* kg = reinterpret_cast<const char*>(a.kc) + (head_row * a.chunks + lane) * 16;
         const char* vg = reinterpret_cast<const char*>(a.vc) + (head_row * a.chunks + lane) * 16;
         const float* sg = (lane < 16 ? a.ks : a.vs) + head_row + (lane & 15);
-        // pages of the next stage that is copied; its second part's, where that may be another page
+        // The next stage that is copied: its places' page in the table and place in
+        // it, and the page's number; the second part's, where that may be another page.
         const bool one_page = SUB == 1 || a.page_size % (kAtPlaces * SUB) == 0;
-        auto page_at = [&](int p) {
-            return p < end ? __ldg(table + (a.page_shift >= 0 ? p >> a.page_shift : p / a.page_size)) : -1;
-        };
-        int issue_place = place0, next_page[SUB];
+        int look_place = place0, entry = place0 / a.page_size, in = place0 - entry * a.page_size;
+        const int step_entry = BLOCK / a.page_size, step_in = BLOCK - step_entry * a.page_size;
+        int next_page[SUB], next_in[SUB];
         auto look = [&]() {
-            next_page[0] = page_at(issue_place);
-            if constexpr (SUB == 2) next_page[SUB - 1] = one_page ? next_page[0] : page_at(issue_place + kAtPlaces);
+            next_in[0] = in;
+            next_page[0] = look_place < end ? __ldg(table + entry) : -1;
+            if constexpr (SUB == 2) {
+                next_page[SUB - 1] = next_page[0];
+                next_in[SUB - 1] = in + kAtPlaces;
+                if (!one_page && in + kAtPlaces == a.page_size) {
+                    next_page[SUB - 1] = look_place + kAtPlaces < end ? __ldg(table + entry + 1) : -1;
+                    next_in[SUB - 1] = 0;
+                }
+            }
+            look_place += BLOCK;
+            entry += step_entry;
+            in += step_in;
+            if (in >= a.page_size) { in -= a.page_size; entry++; }
         };
         look();
         uint32_t issue_to = my_ring, there = 0u;        // the ring's next stage; which of the last parts hold a page that is there
         auto issue = [&]() {
-            int pages[SUB];
+            int pages[SUB], ins[SUB];
 #pragma unroll
-            for (int h = 0; h < SUB; h++) pages[h] = next_page[h];
-            int p = issue_place;
-            issue_place += BLOCK;
+            for (int h = 0; h < SUB; h++) { pages[h] = next_page[h]; ins[h] = next_in[h]; }
             look();
 #pragma unroll
-            for (int h = 0; h < SUB; h++, p += kAtPlaces) {
+            for (int h = 0; h < SUB; h++) {
                 const uint32_t page = (uint32_t)pages[h];
                 there *= 2u;
                 if (page >= (uint32_t)a.npages) continue;
                 there++;
-                const int in = a.page_shift >= 0 ? p & (a.page_size - 1) : p % a.page_size;
-                const uint64_t at = (uint64_t)page * a.page16 + (uint32_t)(in * a.chunks);
+                const uint64_t at = (uint64_t)page * a.page16 + (uint32_t)(ins[h] * a.chunks);
                 const char *k = kg + at * 16, *v = vg + at * 16;
                 const uint32_t dst = issue_to + h * St::kBytes;
 #pragma unroll
@@ -472,7 +481,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         copy16(dst + to[c], k + 512 * c);
                         copy16(dst + to[c] + St::kV, v + 512 * c);
                     }
-                copy4(dst + St::kKs + 4 * lane, sg + (uint64_t)page * a.page_lds + in);
+                copy4(dst + St::kKs + 4 * lane, sg + (uint64_t)page * a.page_lds + ins[h]);
             }
             copies_end_stage();
             issue_to = issue_to + BYTES == ring_end ? my_ring : issue_to + BYTES;
@@ -510,27 +519,24 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             for (int x = 0; x < 8; x++) v[x] = v[x] * up * up2;
             // the lane and step that take this word: quads' words as K's are read
             const int to_t = DP == 64 ? word >> 1 : (word & 15) >> 2, k = DP == 64 ? word & 1 : (word & 3) + 4 * (word >> 4);
-            uint2* q = qf + (((r >> 3) * NP) * STEPS + 2 * k) * 32 + (r & 7) * 4 + to_t;
+            uint4* q = qf + ((r >> 3) * NP * WK + k) * 32 + (r & 7) * 4 + to_t;
+            // values x and x + 4 are a pair, as decoded codes are
+            uint32_t hi[4], lo[4];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                uint2 hi;
-                hi.x = pack2<__half>(v[2 * h], v[2 * h + 4]);
-                hi.y = pack2<__half>(v[2 * h + 1], v[2 * h + 5]);
-                q[h * 32] = hi;
-                if constexpr (NP == 2) {
-                    float x[4];
-                    unpack2<__half>(hi.x, x[0], x[1]);
-                    unpack2<__half>(hi.y, x[2], x[3]);
-                    q[(STEPS + h) * 32] = make_uint2(pack2<__half>(v[2 * h] - x[0], v[2 * h + 4] - x[1]),
-                                                     pack2<__half>(v[2 * h + 1] - x[2], v[2 * h + 5] - x[3]));
-                }
+            for (int x = 0; x < 4; x++) {
+                hi[x] = pack2<__half>(v[x], v[x + 4]);
+                float y, z;
+                unpack2<__half>(hi[x], y, z);
+                lo[x] = pack2<__half>(v[x] - y, v[x + 4] - z);
             }
+            q[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if constexpr (NP == 2) q[WK * 32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         __syncthreads();
-        uint2 qr[Sh::kQueryRegs ? NT * NP * STEPS : 1];
+        uint4 qr[Sh::kQueryRegs ? NT * NP * WK : 1];
         if constexpr (Sh::kQueryRegs) {
 #pragma unroll
-            for (int i = 0; i < NT * NP * STEPS; i++) qr[i] = qf[i * 32 + lane];
+            for (int i = 0; i < NT * NP * WK; i++) qr[i] = qf[i * 32 + lane];
         }
         // this lane's columns: rows 2 t and 2 t + 1 of every eight
         float fq[NT][2], M[NT][2], L[NT][2];
@@ -599,17 +605,16 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                     decode8<LIN>(k0[k], a.klut, x);
                     decode8<LIN>(k1[k], a.klut, y);
 #pragma unroll
-                    for (int h = 0; h < 2; h++)
+                    for (int nt = 0; nt < NT; nt++)
 #pragma unroll
-                        for (int nt = 0; nt < NT; nt++)
-#pragma unroll
-                            for (int p = 0; p < NP; p++) {
-                                const int at = (nt * NP + p) * STEPS + 2 * k + h;
-                                uint2 q;
-                                if constexpr (Sh::kQueryRegs) q = qr[at];
-                                else q = qf[at * 32 + lane];
-                                mma16(part[sub][NP == 2 ? p : h % CH][nt], x[2 * h], y[2 * h], x[2 * h + 1], y[2 * h + 1], q.x, q.y);
-                            }
+                        for (int p = 0; p < NP; p++) {
+                            const int at = (nt * NP + p) * WK + k;
+                            uint4 q;
+                            if constexpr (Sh::kQueryRegs) q = qr[at];
+                            else q = qf[at * 32 + lane];
+                            mma16(part[sub][NP == 2 ? p : 0][nt], x[0], y[0], x[1], y[1], q.x, q.y);
+                            mma16(part[sub][NP == 2 ? p : CH - 1][nt], x[2], y[2], x[3], y[3], q.z, q.w);
+                        }
                 }
             }
             const bool whole = place + kAtPlaces * SUB <= all_hi && place >= all_lo && here == (1u << SUB) - 1u;
