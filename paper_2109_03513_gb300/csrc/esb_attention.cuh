@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 {
     using Sh = Shape<DP, NT, NP>;
     using St = Stage<DP>;
-    constexpr int R = Sh::R, STEPS = Sh::kSteps, W = DP / 8, WK = W / 4, WV = W / 8, ST = Sh::kStages, SUB = Sh::kParts, BLOCK = Sh::kBlock, BYTES = SUB * St::kBytes;
+    constexpr int R = Sh::R, W = DP / 8, WK = W / 4, WV = W / 8, ST = Sh::kStages, SUB = Sh::kParts, BLOCK = Sh::kBlock, BYTES = SUB * St::kBytes;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ int64_t sh[kAtWarps + 2];
     unsigned char* ring = smem;
@@ -604,6 +604,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                     uint32_t x[4], y[4];
                     decode8<LIN>(k0[k], a.klut, x);
                     decode8<LIN>(k1[k], a.klut, y);
+                    // both steps of a word: products that follow one another have other sums
+                    uint2 second[NT][NP];
 #pragma unroll
                     for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -613,8 +615,13 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                             if constexpr (Sh::kQueryRegs) q = qr[at];
                             else q = qf[at * 32 + lane];
                             mma16(part[sub][NP == 2 ? p : 0][nt], x[0], y[0], x[1], y[1], q.x, q.y);
-                            mma16(part[sub][NP == 2 ? p : CH - 1][nt], x[2], y[2], x[3], y[3], q.z, q.w);
+                            second[nt][p] = make_uint2(q.z, q.w);
                         }
+#pragma unroll
+                    for (int nt = 0; nt < NT; nt++)
+#pragma unroll
+                        for (int p = 0; p < NP; p++)
+                            mma16(part[sub][NP == 2 ? p : CH - 1][nt], x[2], y[2], x[3], y[3], second[nt][p].x, second[nt][p].y);
                 }
             }
             const bool whole = place + kAtPlaces * SUB <= all_hi && place >= all_lo && here == (1u << SUB) - 1u;
