@@ -672,9 +672,12 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 #pragma unroll
             for (int sub = 0; sub < SUB; sub++)
 #pragma unroll
-                for (int nt = 0; nt < NT; nt++)
+                for (int row = 0; row < 2; row++) {
+                    float m = sc[sub][0][2 * row];
 #pragma unroll
-                    for (int c = 0; c < 2; c++) over = fmaxf(over, fmaxf(sc[sub][nt][c] + lv[sub][0], sc[sub][nt][2 + c] + lv[sub][1]));
+                    for (int i = 1; i < 2 * NT; i++) m = fmaxf(m, sc[sub][i >> 1][2 * row + (i & 1)]);
+                    over = fmaxf(over, m + lv[sub][row]);
+                }
             if (__any_sync(0xffffffffu, over > 8.0f)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
