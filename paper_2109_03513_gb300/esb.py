@@ -1049,6 +1049,17 @@ def _head_count(t: torch.Tensor, name: str, head_dim: int) -> int:
     return t.shape[1] // head_dim
 
 
+def _heads(t: torch.Tensor, name: str, tokens: int, cols: int, dtype, head_dim: int) -> tuple[int, int]:
+    """(row stride, columns) of tokens' heads: this type, whole heads a row, and so many columns where cols is not 0."""
+    st, shape = t.stride(), t.shape
+    if t.dtype != dtype or not t.is_cuda or len(st) != 2 or shape[0] != tokens or (st[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name} must be a 2-D CUDA tensor of {tokens} contiguous rows, {dtype}")
+    n = shape[1]
+    if n != cols if cols else n % head_dim:
+        raise ValueError(f"{name} must have " + (f"{cols} columns" if cols else "whole heads of head_dim values a row"))
+    return st[0] if tokens != 1 else n or 1, n
+
+
 class HeadNorm(NamedTuple):
     """What esb_headnorm wrote: queries, keys, and 1 / rms of each token's heads (tokens, heads) (None where not wanted)."""
     q: Optional[torch.Tensor]
@@ -1065,41 +1076,48 @@ def esb_headnorm(q: Optional[torch.Tensor], k: Optional[torch.Tensor], head_dim:
     """RMS norm of every head of queries and keys (tokens, heads * head_dim) and the rotation by the tokens' positions
     (tokens,) int64 -> HeadNorm.  One of q and k may be None; qy, ky may be q, k."""
     x0 = q if q is not None else k
-    if x0 is None:
-        raise ValueError("q or k must be given")
-    empty = _empty_on(stream)
-    shape, dtype = x0.shape, x0.dtype
-    tokens, wt = shape[0], 0
-
-    def part(name, x, w, y):
-        nonlocal wt
-        if x is None:
-            return esb_heads(), None, None
-        _, ldx = _rows(x, name)
-        size = x.shape
-        if size[0] != tokens or x.dtype != dtype:
-            raise ValueError("q and k must have the same tokens and type")
-        heads, wp = _head_count(x, name, head_dim), None
-        if w is not None:
-            wp, t = _weight(w, head_dim)
-            if wt and wt != t + 1:
+    if x0 is None or head_dim <= 0 or x0.dim() != 2:
+        raise ValueError("q or k must be given, 2-D, and head_dim be positive")
+    empty, f32 = _empty_on(stream), torch.float32
+    dtype, tokens = x0.dtype, x0.shape[0]
+    xt, wt = _TYPES.get(dtype), None
+    if xt is None:
+        raise ValueError("q and k must be float32, float16 or bfloat16")
+    qp = kp = qr = kr = None
+    if q is not None:
+        ld, cols = _heads(q, "q", tokens, 0, dtype, head_dim)
+        wp = None
+        if q_weight is not None:
+            wp, wt = _weight(q_weight, head_dim)
+        if qy is None:
+            qy = empty((tokens, cols), dtype=dtype, device=q.device)
+        ldy, _ = _heads(qy, "qy", tokens, cols, dtype, head_dim)
+        rp = None
+        if want_rstd:
+            qr = empty((tokens, cols // head_dim), dtype=f32, device=q.device)
+            rp = qr.data_ptr()
+        qp = esb_heads(q.data_ptr(), ld, qy.data_ptr(), ldy, wp, rp, cols // head_dim)
+    if k is not None:
+        ld, cols = _heads(k, "k", tokens, 0, dtype, head_dim)
+        wp = None
+        if k_weight is not None:
+            wp, t = _weight(k_weight, head_dim)
+            if wt is not None and wt != t:
                 raise ValueError("q_weight and k_weight must have one type")
-            wt = t + 1
-        if y is None:
-            y = empty(size, dtype=dtype, device=x.device)
-            ldy = size[1]
-        else:
-            ldy = _rows_like(y, "qy, ky", size, dtype)
-        r = empty((tokens, heads), dtype=torch.float32, device=x.device) if want_rstd else None
-        return esb_heads(x.data_ptr(), ldx, y.data_ptr(), ldy, wp, None if r is None else r.data_ptr(), heads), y, r
-
-    qp, qy, qr = part("q", q, q_weight, qy)
-    kp, ky, kr = part("k", k, k_weight, ky)
+            wt = t
+        if ky is None:
+            ky = empty((tokens, cols), dtype=dtype, device=k.device)
+        ldy, _ = _heads(ky, "ky", tokens, cols, dtype, head_dim)
+        rp = None
+        if want_rstd:
+            kr = empty((tokens, cols // head_dim), dtype=f32, device=k.device)
+            rp = kr.data_ptr()
+        kp = esb_heads(k.data_ptr(), ld, ky.data_ptr(), ldy, wp, rp, cols // head_dim)
     rot, pos = _turn(rotation, positions, tokens)
     _on_current(x0)
-    a = esb_head_norm((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0), eps)
+    a = esb_head_norm((qp or esb_heads(), kp or esb_heads()), pos, rot, head_dim, xt, wt or 0, eps)
     _check(lib().esb_headnorm(tokens, ctypes.byref(a), _stream(stream)), "esb_headnorm")
-    return HeadNorm(qy, ky, qr, kr)
+    return HeadNorm(None if q is None else qy, None if k is None else ky, qr, kr)
 
 
 class HeadNormGrad(NamedTuple):
@@ -1119,48 +1137,58 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
     """Gradient of esb_headnorm from gq, gk (of its queries and keys), its inputs and its rstd -> HeadNormGrad.  A
     weight's gradient is computed where there is the weight."""
     x0 = q if q is not None else k
-    if x0 is None:
-        raise ValueError("q or k must be given")
+    if x0 is None or head_dim <= 0 or x0.dim() != 2:
+        raise ValueError("q or k must be given, 2-D, and head_dim be positive")
     empty, f32 = _empty_on(stream), torch.float32
     dtype, tokens = x0.dtype, x0.shape[0]
-    total = wt = 0
-    # gradients of the weights, one after the other
-    sums = None if q_weight is None and k_weight is None else empty((2, head_dim), dtype=f32, device=x0.device).unbind(0)
-
-    def part(i, name, x, g, w, r, d):
-        nonlocal total, wt
-        if x is None:
-            return esb_heads_grad(), None, None
-        _, ldx = _rows(x, name)
-        size = x.shape
-        if size[0] != tokens or x.dtype != dtype:
-            raise ValueError("q and k must have the same tokens and type")
-        if g is None or r is None:
-            raise ValueError("the gradient and rstd of " + name + " must be given")
-        heads, wp, dw, dp = _head_count(x, name, head_dim), None, None, None
+    xt, wt, total = _TYPES.get(dtype), None, 0
+    if xt is None:
+        raise ValueError("q and k must be float32, float16 or bfloat16")
+    sums = None
+    if q_weight is not None or k_weight is not None:
+        sums = empty((2, head_dim), dtype=f32, device=x0.device)
+    qp = kp = dqw = dkw = None
+    if q is not None:
+        if gq is None or q_rstd is None:
+            raise ValueError("gq and q_rstd must be given")
+        ld, cols = _heads(q, "q", tokens, 0, dtype, head_dim)
+        ldg, _ = _heads(gq, "gq", tokens, cols, dtype, head_dim)
+        total = cols // head_dim
+        if q_rstd.dtype != f32 or q_rstd.shape != (tokens, total) or not q_rstd.is_cuda or not q_rstd.is_contiguous():
+            raise ValueError("q_rstd must be contiguous (tokens, heads) float32")
+        if dq is None:
+            dq = empty((tokens, cols), dtype=dtype, device=q.device)
+        ldd, _ = _heads(dq, "dq", tokens, cols, dtype, head_dim)
+        wp = dp = None
+        if q_weight is not None:
+            wp, wt = _weight(q_weight, head_dim)
+            dqw = sums[0]
+            dp = sums.data_ptr()
+        qp = esb_heads_grad(gq.data_ptr(), ldg, q.data_ptr(), ld, q_rstd.data_ptr(), wp, dq.data_ptr(), ldd, dp, total)
+    if k is not None:
+        if gk is None or k_rstd is None:
+            raise ValueError("gk and k_rstd must be given")
+        ld, cols = _heads(k, "k", tokens, 0, dtype, head_dim)
+        ldg, _ = _heads(gk, "gk", tokens, cols, dtype, head_dim)
+        heads = cols // head_dim
         total += heads
-        ldg = _rows_like(g, "gq, gk", size, dtype)
-        if r.dtype != f32 or r.shape != (tokens, heads) or not r.is_cuda or not r.is_contiguous():
-            raise ValueError("rstd must be contiguous (tokens, heads) float32")
-        if w is not None:
-            wp, t = _weight(w, head_dim)
-            if wt and wt != t + 1:
+        if k_rstd.dtype != f32 or k_rstd.shape != (tokens, heads) or not k_rstd.is_cuda or not k_rstd.is_contiguous():
+            raise ValueError("k_rstd must be contiguous (tokens, heads) float32")
+        if dk is None:
+            dk = empty((tokens, cols), dtype=dtype, device=k.device)
+        ldd, _ = _heads(dk, "dk", tokens, cols, dtype, head_dim)
+        wp = dp = None
+        if k_weight is not None:
+            wp, t = _weight(k_weight, head_dim)
+            if wt is not None and wt != t:
                 raise ValueError("q_weight and k_weight must have one type")
-            wt = t + 1
-            dw = sums[i]
-            dp = dw.data_ptr()
-        if d is None:
-            d = empty(size, dtype=dtype, device=x.device)
-            ldd = size[1]
-        else:
-            ldd = _rows_like(d, "dq, dk", size, dtype)
-        return esb_heads_grad(g.data_ptr(), ldg, x.data_ptr(), ldx, r.data_ptr(), wp, d.data_ptr(), ldd, dp, heads), d, dw
-
-    qp, dq, dqw = part(0, "q", q, gq, q_weight, q_rstd, dq)
-    kp, dk, dkw = part(1, "k", k, gk, k_weight, k_rstd, dk)
+            wt = t
+            dkw = sums[1]
+            dp = sums.data_ptr() + 4 * head_dim
+        kp = esb_heads_grad(gk.data_ptr(), ldg, k.data_ptr(), ld, k_rstd.data_ptr(), wp, dk.data_ptr(), ldd, dp, heads)
     rot, pos = _turn(rotation, positions, tokens)
     _on_current(x0)
-    a = esb_head_norm_grad((qp, kp), pos, rot, head_dim, _TYPES[dtype], max(wt - 1, 0))
+    a = esb_head_norm_grad((qp or esb_heads_grad(), kp or esb_heads_grad()), pos, rot, head_dim, xt, wt or 0)
     wp, nb = None, 0
     if sums is not None:
         if workspace is None:
@@ -1171,7 +1199,7 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
             nb = workspace.numel() * workspace.element_size()
         wp = workspace.data_ptr()
     _check(lib().esb_headnorm_backward(tokens, ctypes.byref(a), wp, nb, _stream(stream)), "esb_headnorm_backward")
-    return HeadNormGrad(dq, dk, dqw, dkw)
+    return HeadNormGrad(None if q is None else dq, None if k is None else dk, dqw, dkw)
 
 
 class KvCache(NamedTuple):
