@@ -802,8 +802,8 @@ typedef struct esb_head_norm {
     int32_t x_type, w_type;
     float eps;                 /* >= 0, finite */
 } esb_head_norm;
-/* Errors: INVALID_ARG, UNSUPPORTED (head_dim, rotation's dim), RANGE (tokens or
- * heads of 2^31 and more), ALIGN, CUDA. */
+/* Errors: INVALID_ARG, UNSUPPORTED (head_dim, rotation's dim), RANGE (2^31
+ * tokens, 2^23 heads and more), ALIGN, CUDA. */
 esb_status esb_headnorm(int64_t tokens, const esb_head_norm* a, void* stream);
 
 /* Its gradient, from x and rstd of the forward pass: with g the rotation of dy
@@ -841,7 +841,8 @@ esb_status esb_headnorm_backward(int64_t tokens, const esb_head_norm_grad* a, vo
  *   value = scale q(code),  b = 4, signed, 0 <= k <= 3
  * A page is `heads` times page_size rows of words, then the next head; pages
  * are page_ld words (a multiple of 4, below 2^34) and page_lds scales (below
- * 2^32) apart. */
+ * 2^32) apart.  page_size <= 2^24, heads < 2^23, their product < 2^31, pages <=
+ * 2^31. */
 typedef struct esb_kv_cache {
     uint32_t *k_codes, *v_codes;   /* [device] 16-byte aligned */
     float *k_scales, *v_scales;    /* [device] pages of heads x page_size floats */
@@ -899,7 +900,8 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
  *   workspace  [device] >= esb_cache_attention_workspace_bytes bytes, 16-byte
  *              aligned; nothing is kept in it between calls
  * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes, q_heads not a multiple of
- * heads), RANGE, ALIGN, CUDA. */
+ * heads), RANGE (2^31 - 64 tokens times heads that share one, 2^30 places of a
+ * page table, and more), ALIGN, CUDA. */
 typedef struct esb_attention {
     const void* q;             /* [device] tokens x (q_heads * head_dim) of q_type */
     int64_t ldq;

@@ -22,11 +22,11 @@
 // tile; parts of tiles go to the workspace, and a second kernel joins them in
 // their order.
 //
-// 4 x 131072 places, 8 heads of 128, 4 queries each (570 MB): 150 us, 3.8 TB/s,
-// 56% of the copy rate.  16 places take 370 instructions of a warp, 264 of them on
-// the pipe of integer and permute work, which does 64 lanes a clock and is three
-// quarters busy.  A prompt's 512 tokens over 4096 places, four of them (129 GFLOP):
-// 660 us, 195 TFLOP/s; its tiles' sums leave two warps a scheduler, which wait for
+// 4 x 131072 places, 8 heads of 128, 4 queries each (570 MB): 137 us, 4.2 TB/s,
+// 62% of the copy rate.  More than half of the instructions go to the pipe of
+// integer and permute work, which does 64 lanes a clock and is some three quarters
+// busy.  A prompt's 512 tokens over 4096 places, four of them (129 GFLOP):
+// 630 us, 205 TFLOP/s; its tiles' sums leave two warps a scheduler, which wait for
 // fixed latencies.  One sequence of 2048 places: 12 us, two kernels' starts,
 // look-ups and loads one after the other.
 #pragma once

@@ -39,9 +39,10 @@ esb_status cache_ok(const esb_kv_cache* c)
         if (esb_format_check(f) != ESB_OK || f.b != 4 || !f.is_signed) return ESB_ERR_UNSUPPORTED;
     if (!head_ok(c->head_dim) || c->page_size <= 0 || c->page_size % 16 != 0) return ESB_ERR_UNSUPPORTED;
     if (c->pages < 0 || c->heads <= 0) return ESB_ERR_INVALID_ARG;
-    if (c->heads >= 1 << 23 || c->page_size > 1 << 30 || c->pages > 1ll << 31 || c->page_ld >= 1ll << 34 || c->page_lds >= 1ll << 32)
-        return ESB_ERR_RANGE;
     const int64_t rows = (int64_t)c->heads * c->page_size;
+    if (c->heads >= 1 << 23 || c->page_size > 1 << 24 || rows >= 1ll << 31 || c->pages > 1ll << 31 || c->page_ld >= 1ll << 34 ||
+        c->page_lds >= 1ll << 32)
+        return ESB_ERR_RANGE;
     if (c->pages > 0 && (!c->k_codes || !c->v_codes || !c->k_scales || !c->v_scales)) return ESB_ERR_INVALID_ARG;
     if (c->pages > 1 && (c->page_ld < rows * esb_row_words(c->head_dim, 4) || c->page_lds < rows)) return ESB_ERR_INVALID_ARG;
     return aligned(c->k_codes, 16) && aligned(c->v_codes, 16) && (c->pages <= 1 || c->page_ld % 4 == 0) && aligned(c->k_scales, 4) &&

@@ -81,7 +81,8 @@ def cache(**kw):
 BAD_CACHES = [
     (UNS, dict(k_fmt=esb.Fmt(8, 6).c())), (UNS, dict(v_fmt=esb.Fmt(4, 2, False).c())), (UNS, dict(k_fmt=esb.esb_format(4, 4, 1))),
     (UNS, dict(head_dim=63)), (UNS, dict(head_dim=264)), (UNS, dict(page_size=0)), (UNS, dict(page_size=24)), (INV, dict(pages=-1)),
-    (INV, dict(heads=0)), (RNG, dict(heads=1 << 23)), (RNG, dict(pages=1 << 40)), (INV, dict(k_codes=None)), (INV, dict(v_codes=None)),
+    (INV, dict(heads=0)), (RNG, dict(heads=1 << 23)), (RNG, dict(page_size=(1 << 24) + 16)), (RNG, dict(heads=1 << 20, page_size=2048)),
+    (RNG, dict(page_ld=1 << 34)), (RNG, dict(page_lds=1 << 32)), (RNG, dict(pages=1 << 40)), (INV, dict(k_codes=None)), (INV, dict(v_codes=None)),
     (INV, dict(k_scales=None)), (INV, dict(v_scales=None)), (INV, dict(page_ld=252)), (INV, dict(page_lds=31)), (ALN, dict(k_codes=264)),
     (ALN, dict(v_codes=ODD)), (ALN, dict(page_ld=258)), (ALN, dict(k_scales=ODD)), (ALN, dict(v_scales=258)),
 ]
@@ -114,7 +115,7 @@ def attend(lib, tokens=3, null=False, c=None, r=None, ws=P, nb=1 << 40, **kw):
 @pytest.mark.parametrize("want,kw", [
     (INV, dict(null=True)), (INV, dict(tokens=-1)), (RNG, dict(tokens=1 << 31)), (INV, dict(seqs=-1)), (INV, dict(max_pages=-1)),
     (INV, dict(window=-1)), (INV, dict(scale=float("nan"))), (INV, dict(scale=float("inf"))), (INV, dict(q_type=3)), (INV, dict(out_type=-1)),
-    (UNS, dict(q_heads=3)), (UNS, dict(q_heads=0)), (RNG, dict(q_heads=1 << 24)), (RNG, dict(max_pages=(1 << 26) + 1)),
+    (UNS, dict(q_heads=3)), (UNS, dict(q_heads=0)), (RNG, dict(q_heads=1 << 24)), (RNG, dict(tokens=1 << 30)), (RNG, dict(max_pages=(1 << 26) + 1)),
     (UNS, dict(r=turn(dim=7))), (INV, dict(r=turn(table=None))), (INV, dict(q=None)), (INV, dict(out=None)), (INV, dict(lens=None)),
     (INV, dict(pages=None)), (INV, dict(ldq=255)), (INV, dict(ldo=255)), (INV, dict(ld_pages=4)), (INV, dict(seqs=2)),
     (ALN, dict(q=ODD)), (ALN, dict(out=ODD)), (ALN, dict(lse=ODD)), (ALN, dict(starts=ODD)), (ALN, dict(lens=ODD)), (ALN, dict(pages=ODD)),
