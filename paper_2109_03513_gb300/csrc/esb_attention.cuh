@@ -196,7 +196,7 @@ template <int DP, int NT, int NP> struct Shape {
     static constexpr int kStages = DP == 256 ? (NT == 1 ? 3 : 4) : NT == 1 ? 3 : 6;
     static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
     // Blocks on an SM.  Tiles of 16 rows: 49 us for 24 x 10000 places, 55 with three blocks, whose registers spill;
-    // heads of 64: 37 us for 48 windows of 1000, 39.5 with three.
+    // heads of 64: 37 us for 48 windows of 1000, 39.5 with three; of 128: 137 us for 4 x 131072 places, 148 with four.
     static constexpr int kSm = NT > 1 || DP == 256 ? 2 : DP == 64 ? 4 : 3;
     static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
     static constexpr int kRing = kAtWarps * kStages * kParts * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;

@@ -573,6 +573,31 @@ def test_attention_of_many_sequences(seqs):
         check_attention(q[a:b], c, lens[i:i + 1], t[i:i + 1], out[a:b], lse[a:b], starts=i32([0, b - a]))
 
 
+def test_rows_past_32_bits():
+    # tokens' rows more than 2^31 values apart, into and out of each operator
+    d, n, ld = 64, 3, (1 << 31) + 8
+    store = torch.empty((n - 1) * ld + 2 * d, dtype=BF, device="cuda")
+    far = torch.as_strided(store, (n, 2 * d), (ld, 1))
+    x = rand((n, 2 * d), 1, BF)
+    far.copy_(x)
+    r, pos = esb.rotation(d, 10), ints(0, 10, (n,), 2)
+    want = esb.esb_headnorm(x, None, d, rotation=r, positions=pos, want_rstd=True)
+    assert torch.equal(esb.esb_headnorm(far, None, d, rotation=r, positions=pos).q, want.q)
+    g = rand((n, 2 * d), 3, BF)
+    dw = 1 + rand((d,), 4, std=0.1)
+    b = esb.esb_headnorm_backward(g, None, x, None, d, dw, None, want.q_rstd, None, rotation=r, positions=pos)
+    bf = esb.esb_headnorm_backward(g, None, far, None, d, dw, None, want.q_rstd, None, rotation=r, positions=pos)
+    assert torch.equal(b.dq, bf.dq) and torch.equal(b.dq_weight, bf.dq_weight)
+    slots = torch.tensor([3, 20, 4], device="cuda")
+    near, wide = esb.kv_cache(2, 2, 16, d), esb.kv_cache(2, 2, 16, d)
+    esb.esb_cache_append(near, x, x, slots, rotation=r, positions=pos)
+    esb.esb_cache_append(wide, far, far, slots, rotation=r, positions=pos)
+    assert torch.equal(near.k_codes, wide.k_codes) and torch.equal(near.v_codes, wide.v_codes) and torch.equal(near.k_scales, wide.k_scales)
+    t, lens = i32([[0, 1]] * n), i32([32, 5, 21])
+    a, _ = esb.esb_cache_attention(x, near, lens, t)
+    assert torch.equal(esb.esb_cache_attention(far, near, lens, t, out=far)[0], a)   # the output on the queries' own rows
+
+
 def test_attention_nothing_to_do_and_refusals():
     c = esb.kv_cache(2, 1, 16, 64)
     q = rand((2, 64), 1)
@@ -591,6 +616,29 @@ def test_attention_nothing_to_do_and_refusals():
                  lambda: esb.esb_cache_append(c, q, q, i32([0, 1])), lambda: esb.esb_headnorm(q, None, 60)):
         with pytest.raises((ValueError, esb.EsbError)):
             call()
+
+
+def test_attention_calls_share_a_workspace_one_after_the_other():
+    # a call's parts are joined before the next call writes its own, whatever the shapes; two streams have a workspace each
+    c, small = make_cache(300, 4, 64, 128, 2, 1, 3), make_cache(40, 2, 16, 64, 0, 2, 4)
+    t, ts = tables([9000, 5000, 100], 64, 300, 1), tables([300, 20], 16, 40, 2)
+    n, ns, starts = i32([9000, 5000, 100]), i32([300, 20]), i32([0, 12, 20])
+    q, qs, qf = rand((3, 16 * 128), 1, BF), rand((20, 6 * 64), 2, HF), rand((3, 8 * 128), 3)
+    nb = 1 << 26
+    calls = [lambda w, s: esb.esb_cache_attention(q, c, n, t, want_lse=True, workspace=w, stream=s),
+             lambda w, s: esb.esb_cache_attention(qs, small, ns, ts, starts=starts, want_lse=True, workspace=w, stream=s),
+             lambda w, s: esb.esb_cache_attention(qf, c, n, t, want_lse=True, window=3000, workspace=w, stream=s)]
+    want = [f(None, None) for f in calls]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.full((nb,), 255, dtype=torch.uint8, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    got = [[f(w, s) for _ in range(8) for f in calls] for w, s in zip(spaces, streams)]
+    torch.cuda.synchronize()
+    for outs in got:
+        for i, (o1, l1) in enumerate(outs):
+            assert torch.equal(o1, want[i % 3][0]) and torch.equal(l1, want[i % 3][1]), i
+    with pytest.raises(esb.EsbError):
+        calls[0](spaces[0][:1000], None)
 
 
 def test_attention_repeats_on_another_stream_and_in_a_graph():
