@@ -905,7 +905,7 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
 typedef struct esb_attention {
     const void* q;             /* [device] tokens x (q_heads * head_dim) of q_type */
     int64_t ldq;
-    void* out;                 /* [device] the same of out_type */
+    void* out;                 /* [device] the same of out_type; may lie on q with the same type and stride */
     int64_t ldo;
     float* lse;
     const int32_t *starts, *lens, *pages;
