@@ -262,7 +262,7 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh)
 }
 
 // Work of sequence first + thread * step, for the first `count` threads; those
-// with many tiles by the whole block.
+// with many tiles by the whole block.  A single query's tiles see the same places.
 // (One copy of it: a block runs this once, out of a cold instruction cache.)
 template <class Sh>
 __device__ __noinline__ int64_t work_of(const AttnArgs& a, int64_t first, int64_t step, int count, int64_t* sh)
@@ -273,11 +273,12 @@ __device__ __noinline__ int64_t work_of(const AttnArgs& a, int64_t first, int64_
     if ((int)threadIdx.x < count && b < a.seqs) {
         const Seq s = sequence(a, (int)b);
         const int n = tiles_of<Sh>(a, s);
-        many = n > 8;
-        if (!many)
+        many = s.nq > 1 && n > 8;
+        if (s.nq == 1) w = (int64_t)n * tile_of<Sh>(a, s, 0).blocks;
+        else if (!many)
             for (int i = 0; i < n; i++) w += tile_of<Sh>(a, s, i).blocks;
     }
-    if (a.starts && __syncthreads_or(many)) {
+    if (a.starts && __syncthreads_or(many)) {          // else every sequence has one query
         __shared__ unsigned list[kAtWarps];
         const unsigned m = __ballot_sync(0xffffffffu, many);
         if ((threadIdx.x & 31) == 0) list[threadIdx.x >> 5] = m;
