@@ -36,6 +36,7 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "esb_attention_plan.h"
 #include "esb_internal.h"
 #include "esb_rotate.cuh"
 #include "esb_rows.cuh"
@@ -234,18 +235,11 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
 }
 template <class Sh> __device__ __forceinline__ int tiles_of(const AttnArgs& a, const Seq& s) { return (s.nq * a.group + Sh::R - 1) / Sh::R; }
 
-struct Tile {
-    int lo, hi, blocks;                 // places lo .. hi - 1, lo at a stage's start; blocks of work (one where there are none)
-};
 template <class Sh> __device__ __forceinline__ Tile tile_of(const AttnArgs& a, const Seq& s, int i)
 {
-    Tile t;
     const uint32_t rows = (uint32_t)(s.nq * a.group), first = (uint32_t)i * Sh::R, last = min(first + Sh::R, rows) - 1u;
     const int64_t p0 = (int64_t)s.len - s.nq + token_of(a, first), p1 = (int64_t)s.len - s.nq + token_of(a, last);
-    t.hi = (int)max((int64_t)0, min(p1 + 1, (int64_t)s.seen));
-    t.lo = a.window > 0 ? (int)max((int64_t)0, p0 - a.window + 1) & ~(kAtPlaces * Sh::kParts - 1) : 0;
-    t.blocks = t.hi > t.lo ? (t.hi - t.lo + Sh::kBlock - 1) / Sh::kBlock : 1;
-    return t;
+    return tile_places(p0, p1, s.seen, a.window, kAtPlaces * Sh::kParts, Sh::kBlock);
 }
 
 __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* sh)
@@ -431,8 +425,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 
         __syncthreads();                                // the last tile's shared memory has been read
         const int32_t* table = a.pages + (int64_t)b * a.ld_pages;
-        const int place0 = tl.lo + (first_block * kAtWarps + warp) * (kAtPlaces * SUB);
-        const int end = min(tl.hi, tl.lo + (first_block + blocks) * BLOCK);
+        const int place0 = first_place(tl, first_block, warp, kAtWarps, kAtPlaces * SUB), end = end_place(tl, first_block, blocks, BLOCK);
         const int stages = end > place0 ? (end - place0 + BLOCK - 1) / BLOCK : 0;
         const int64_t head_row = (int64_t)head * a.page_size;
         const char* kg = reinterpret_cast<const char*>(a.kc) + (head_row * a.chunks + lane) * 16;
