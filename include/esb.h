@@ -776,7 +776,7 @@ esb_status esb_logprobs_backward(const void* x, int32_t x_type, int64_t rows, in
  * (2 i, 2 i + 1) if interleaved: (a, b) -> (a c - b s, b c + a s). */
 typedef struct esb_rotation {
     const float* table;        /* [device] positions rows of dim floats, stride ld: cos of the dim/2 angles, then their sines */
-    int64_t positions, ld;
+    int64_t positions, ld;     /* at least one position, where there are tokens */
     int32_t dim;               /* even, at most the head's values; 0: no rotation */
     int32_t interleaved;
 } esb_rotation;

@@ -24,12 +24,15 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 // Rows of a type start on that type's boundary.
 bool typed(const void* p, int32_t t) { return aligned(p, t == ESB_F32 ? 4 : 2); }
 bool head_ok(int32_t d) { return d >= 8 && d <= 256 && d % 8 == 0; }
-// A rotation that there may be (`used`: for tokens with these positions).
-esb_status rotation_ok(const esb_rotation* r, int32_t head_dim, bool used, const int64_t* positions)
+// A rotation that there may be, for tokens with these positions (or, not given,
+// with those of their sequences).  A kernel reads row 0 for a position that the
+// table lacks.
+esb_status rotation_ok(const esb_rotation* r, int32_t head_dim, int64_t tokens, const int64_t* positions, bool given = true)
 {
     if (!r || r->dim == 0) return ESB_OK;
     if (r->dim < 0 || r->dim % 2 != 0 || r->dim > head_dim) return ESB_ERR_UNSUPPORTED;
-    if (!r->table || r->positions < 0 || r->ld < r->dim || (used && !positions)) return ESB_ERR_INVALID_ARG;
+    if (!r->table || r->positions < 0 || r->ld < r->dim) return ESB_ERR_INVALID_ARG;
+    if (tokens > 0 && (r->positions == 0 || (given && !positions))) return ESB_ERR_INVALID_ARG;
     return aligned(r->table, 4) && aligned(positions, 8) ? ESB_OK : ESB_ERR_ALIGN;
 }
 esb_status cache_ok(const esb_kv_cache* c)
@@ -181,7 +184,7 @@ esb_status esb_headnorm(int64_t tokens, const esb_head_norm* a, void* stream)
     if (!a || tokens < 0 || !(std::isfinite(a->eps) && a->eps >= 0.0f) || !type_ok(a->x_type)) return ESB_ERR_INVALID_ARG;
     if (!head_ok(a->head_dim)) return ESB_ERR_UNSUPPORTED;
     if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
-    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens > 0, a->positions);
+    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens, a->positions);
     if (r != ESB_OK) return r;
     int64_t heads = 0;
     for (const esb_heads& h : a->part) {
@@ -209,7 +212,7 @@ esb_status esb_headnorm_backward(int64_t tokens, const esb_head_norm_grad* a, vo
     if (!a || tokens < 0 || !type_ok(a->x_type)) return ESB_ERR_INVALID_ARG;
     if (!head_ok(a->head_dim)) return ESB_ERR_UNSUPPORTED;
     if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
-    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens > 0, a->positions);
+    const esb_status r = rotation_ok(&a->rotation, a->head_dim, tokens, a->positions);
     if (r != ESB_OK) return r;
     int64_t heads = 0;
     bool sums = false;
@@ -250,7 +253,7 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* c, const esb_app
     esb_status r = cache_ok(c);
     if (r != ESB_OK) return r;
     if (tokens >= 1ll << 31) return ESB_ERR_RANGE;
-    r = rotation_ok(a->rotation, c->head_dim, tokens > 0, a->positions);
+    r = rotation_ok(a->rotation, c->head_dim, tokens, a->positions);
     if (r != ESB_OK) return r;
     if (tokens == 0) return ESB_OK;
     const int64_t cols = (int64_t)c->heads * c->head_dim;
@@ -286,7 +289,7 @@ esb_status esb_cache_attention(int64_t tokens, const esb_kv_cache* c, const esb_
     if (a->q_heads <= 0 || a->q_heads % c->heads != 0) return ESB_ERR_UNSUPPORTED;
     if (tokens >= 1ll << 31 || a->q_heads >= 1 << 23 || (int64_t)a->max_pages * c->page_size > 1 << 30) return ESB_ERR_RANGE;
     if (tokens * (a->q_heads / c->heads) >= (1ll << 31) - 64) return ESB_ERR_RANGE;
-    r = rotation_ok(a->rotation, c->head_dim, false, nullptr);
+    r = rotation_ok(a->rotation, c->head_dim, a->seqs > 0 ? tokens : 0, nullptr, false);
     if (r != ESB_OK) return r;
     if (tokens == 0 || a->seqs == 0) return ESB_OK;
     const int64_t cols = (int64_t)a->q_heads * c->head_dim;
