@@ -895,8 +895,11 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
  * sees makes its numbers NaN; what it does not see has no effect, whatever it is.
  * Products are of fp16 numbers, sums fp32: codes take part as they are; queries
  * and weights (probabilities times a value's scale) with 11 significant bits
- * where queries are bf16, else with 22, where v's scales lie between 2^-100 and
- * 2^100 and, of the places that a query sees, within a factor of 2^100.
+ * where queries are bf16, else with 22, but no finer than a fixed step: a query's
+ * value is off by no more than 2^-11 (2^-22) of itself or 2^-39 of the head's
+ * largest, a weight by no more than 2^-11 (2^-22) of itself or 2^-32 (2^-43) of
+ * the query's largest.  That is where v's scales are 0 or lie between 2^-80 and
+ * 2^80; the sum of the probabilities has no such step.
  *   workspace  [device] >= esb_cache_attention_workspace_bytes bytes, 16-byte
  *              aligned; nothing is kept in it between calls
  * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes, q_heads not a multiple of

@@ -59,7 +59,7 @@ cudaError_t launch_attention(int64_t tokens, const esb_kv_cache& c, const esb_at
     // places of k = 2 are their codes with the top bit changed; a place counts 2^-16, and stands for 2^-k
     a.klut = lin ? make_uint2(c.k_fmt.k == 2 ? 0x04040404u : 0u, 0u) : lut_of(c.k_fmt.k);
     a.vlut = lin ? make_uint2(c.v_fmt.k == 2 ? 0x04040404u : 0u, 0u) : lut_of(c.v_fmt.k);
-    a.vunit = lin ? (float)(1 << (16 - c.v_fmt.k)) : 1.0f;
+    a.vunit = (lin ? (float)(1 << (16 - c.v_fmt.k)) : 1.0f) / kWeightUp;
     a.seqs = n.seqs; a.max_pages = n.max_pages; a.heads = c.heads; a.group = n.q_heads / c.heads; a.D = c.head_dim;
     a.chunks = (c.head_dim + 31) / 32; a.page_size = c.page_size;
     a.group_shift = -1;

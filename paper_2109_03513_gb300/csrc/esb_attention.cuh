@@ -15,7 +15,11 @@
 //
 // Weights carry v's scale: with u = score + log2(v's scale) and M the largest u
 // so far (up to 2^8; it is raised when a u passes that), the weight 2^(score -
-// M) v_scale is of order 1 whatever the scales are, and is rounded to fp16.
+// M) v_scale is of order 1 whatever the scales are.  It is rounded to fp16 as
+// 2^7 times that, so that the largest lies in 2^7 .. 2^15 and fp16's fixed steps
+// of 2^-24, of which a long rest behind one large weight is made, are 2^-31 of it
+// or less.  With two planes the second holds 2^11 times what the first leaves,
+// in steps of 2^-35 (2^-42 of the largest), and is summed apart.
 //
 // The work, blocks of places (a stage of each of four warps) of all tiles in a
 // row, is cut into equal parts, one for each thread block, wherever that cuts a
@@ -58,7 +62,7 @@ struct AttnArgs {
     uint2 klut, vlut;                                   // high bytes of the fp16 numbers of codes 0..7; LIN: x = what turns a code into its place
     int seqs, max_pages, heads, group, group_shift, D, chunks, page_size, window;
     int q_type, out_type, qvec, ovec;
-    float scale2, vunit;                                // scale log2(e) and K's unit; V's unit
+    float scale2, vunit;                                // scale log2(e) and K's unit; V's unit, and the weights'
     RotArgs rot;
     float* partial;                                     // slots of R x (DP + 2) floats
     int4* head;                                         // of each part: (the last part of the tile that begins in it and goes on) + 1, sequence, head, tile
@@ -83,6 +87,10 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// What a weight is multiplied by before it is rounded to fp16, and what its first
+// plane's remainder is before that is.
+constexpr float kWeightUp = 128.0f, kLowUp = 2048.0f;
+
 // The instruction's sums are truncated, not rounded: where queries and weights
 // have 22 bits, a place's products are summed on their own and added in fp32.
 __device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b0)[2], const uint32_t (&b1)[2])
@@ -91,6 +99,8 @@ __device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                  : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0[1]), "r"(b1[1]), "f"(0.0f));
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] *= 1.0f / kLowUp;
     mma16(x, a0, a1, a2, a3, b0[0], b1[0]);
 #pragma unroll
     for (int i = 0; i < 4; i++) d[i] += x[i];
@@ -627,9 +637,12 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 const float ks0 = lds_f32(scales), ks1 = lds_f32(scales + 32);
                 vs[sub][0] = lds_f32(scales + 64);
                 vs[sub][1] = lds_f32(scales + 96);
-                // log2 of v's scales, where they have one
+                // log2 of v's scales, where they have one (2^30 places have a sum below 2^128: 2^(8 + 90) each)
 #pragma unroll
-                for (int c = 0; c < 2; c++) lv[sub][c] = fmaxf(fminf(lg2(fabsf(vs[sub][c])), 100.0f), -100.0f);
+                for (int c = 0; c < 2; c++) {
+                    lv[sub][c] = fmaxf(fminf(lg2(fabsf(vs[sub][c])), 100.0f), -90.0f);
+                    vs[sub][c] *= kWeightUp;
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; nt++)
 #pragma unroll
@@ -738,8 +751,10 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         float x[4];
                         unpack2<__half>(h0, x[0], x[1]);
                         unpack2<__half>(h1, x[2], x[3]);
-                        p0[nt][NP - 1] = transposed(pack2<__half>(w[0] - x[0], w[1] - x[1]));
-                        p1[nt][NP - 1] = transposed(pack2<__half>(w[2] - x[2], w[3] - x[3]));
+#pragma unroll
+                        for (int c = 0; c < 4; c++) x[c] = (w[c] - x[c]) * kLowUp;
+                        p0[nt][NP - 1] = transposed(pack2<__half>(x[0], x[1]));
+                        p1[nt][NP - 1] = transposed(pack2<__half>(x[2], x[3]));
                     }
                 }
                 // values: this lane's words of places 2 t, 2 t + 1, 2 t + 8, 2 t + 9

@@ -1,11 +1,13 @@
 """A decoder's attention at its edges: many queries on one head of the cache,
-lengths far past the page table."""
+lengths far past the page table, one place far ahead of a long rest."""
+import math
+
 import pytest
 import torch
 
 from paper_2109_03513_gb300 import esb
-from test_gpu_attention import check_attention, i32, ints, make_cache, tables
-from test_gpu_lm import TYPES, rand
+from test_gpu_attention import BF, FL, cached64, check_attention, i32, ints, make_cache, tables
+from test_gpu_lm import TYPES, U, close, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +53,48 @@ def test_lengths_far_past_the_page_table(m, dtype):
         if window in (1, 40):
             for i in (0, 2, 3):
                 assert (out[m * i:m * (i + 1)] == 0).all()
+
+
+LN2 = math.log(2.0)
+AHEAD = [(4096, 14.0, 1.0), (4096, 18.0, 1.0), (131072, 10.0, 1.0), (131072, 14.0, 1.0), (131072, 17.0, 1.0), (131072, 20.0, 1.0),
+         (131072, 17 * LN2 - math.log(1.3), 0.0), (131072, 20 * LN2 - math.log(1.3), 0.0), (131072, 25.05 * LN2, 0.0)]
+
+
+@pytest.mark.parametrize("n,gap,spread", AHEAD)
+@pytest.mark.parametrize("d,group,kk,vk", [(64, 2, 2, 2), (64, 20, 0, 2), (128, 4, 2, 2), (128, 12, 2, 1), (256, 1, 2, 2), (256, 12, 1, 3)])
+@pytest.mark.parametrize("dtype", [FL, BF])
+def test_a_few_places_far_ahead_of_the_others(n, gap, spread, d, group, kk, vk, dtype):
+    # The first places (some for each warp of a block) score `gap` more than the rest, and have zero codes in half of their
+    # values: what stands there is the rest's.  Scores are one product each, so that they are exact but for a few roundings.
+    page, seqs = 64, 700
+    k = torch.zeros((n, d), device="cuda")
+    k[:, 0] = spread * rand((n,), 1) + 0.5
+    v = torch.exp(0.3 * rand((n, 1), 2)).expand(n, d).clone()
+    first = torch.arange(0, 128, 16, device="cuda")
+    k[first, 0] = gap + 0.5
+    v[first, :d // 2] = 0
+    c = esb.kv_cache(n // page, 1, page, d, esb.Fmt(4, kk), esb.Fmt(4, vk))
+    esb.esb_cache_append(c, k, v, torch.arange(n, device="cuda"))
+    # sequences that share the pages: enough of them that a tile's work is one block's, or two blocks'
+    t = torch.arange(n // page, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    q = torch.zeros((seqs, group, d), dtype=dtype, device="cuda")
+    q[:, :, 0] = 1
+    out, lse = esb.esb_cache_attention(q.flatten(1), c, i32([n] * seqs), t, scale=1.0, out=torch.empty((seqs, group * d), device="cuda"), want_lse=True)
+    at = torch.arange(n // page, device="cuda")
+    (k64, _), (v64, vs) = cached64(c, "k", at), cached64(c, "v", at)
+    s, v64, vs = k64[0, :, 0], v64[0], vs[0]
+    mx = s.max()
+    e = torch.exp(s - mx)
+    pr = (e / e.sum())[:, None]
+    want = (pr * v64).sum(0)
+    # a weight: a product and a few sums of fp32 numbers as large as the score and the largest one, and 2^x
+    eta = (8 * U * (s.abs() + mx.abs()) + 2.0 ** -21)[:, None]
+    # its own roundings, as documented: 11 (22) bits, and a part of the query's largest weight
+    bits, floor = (2.0 ** -11, 2.0 ** -32) if dtype == BF else (2.0 ** -22, 2.0 ** -43)
+    # a block's warp adds 16 places of every 64, each time off by 2^-23; instructions', warps' and parts' sums beside that
+    sums = (n / 64 + 160) * 2 * U
+    bound = (pr * (eta + bits) * v64.abs()).sum(0) + floor * (pr[:, 0] * vs).max() * (v64 / vs[:, None]).abs().sum(0) + \
+        want.abs() * ((pr * eta).sum() + sums) + (pr * v64.abs()).sum(0) * sums
+    close(out.unflatten(1, (group, d)), want.expand(seqs, group, d), bound.expand(seqs, group, d), FL)
+    wl = mx + torch.log(e.sum())
+    assert (lse.double() - wl).abs().max() <= (pr * eta).sum() * 1.01 + sums + 8 * U * (wl.abs() + mx.abs())
