@@ -72,6 +72,9 @@ namespace {
 
 constexpr int kAtWarps = 4, kAtThreads = 32 * kAtWarps;
 constexpr int kAtPlaces = 16;                           // of a part of a stage, the matrix instruction's rows
+// The maximum of no scores: the least finite number, from which a score of -inf
+// (a seen place's, or one that is not seen) is still -inf away, not NaN.
+constexpr int kNone = (int)0xff7fffffu;
 
 // ------------------------------------------------------------ instructions
 
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     float2* sums = reinterpret_cast<float2*>(reinterpret_cast<unsigned char*>(qf) + Sh::kQueryBytes);
     float* qscale = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(sums) + Sh::kSums);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const float ninf = __int_as_float(0xff800000);
+    const float ninf = __int_as_float(0xff800000), none = __int_as_float(kNone);
     griddep_wait();
     griddep_launch_dependents();        // every block runs at once, so those of the join only fill what is left
 
@@ -552,7 +555,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 const int r = nt * 8 + 2 * t + c;
                 const int64_t pos = (int64_t)s.len - s.nq + token_of(a, row0 + r);
                 fq[nt][c] = qscale[r];
-                M[nt][c] = ninf;
+                M[nt][c] = none;
                 L[nt][c] = 0.0f;
                 qhi[nt][c] = r < n_rows ? (int)max((int64_t)0, min(pos + 1, (int64_t)s.seen)) : 0;
                 qlo[nt][c] = a.window > 0 ? (int)max((int64_t)0, pos - a.window + 1) : 0;
@@ -658,8 +661,8 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                         sc[sub][nt][2 + c] = fmaf(part[sub][0][nt][2 + c], fq[nt][c], -M[nt][c]);
                     }
             }
-            // what is not seen: -inf, whatever the maximum is (apart from the rest,
-            // which whole stages have to themselves)
+            // what is not seen: -inf (apart from the rest, which whole stages have to
+            // themselves)
             uint32_t unseen = 0u;
             if (!whole) {
 #pragma unroll
@@ -838,7 +841,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
         for (int i = threadIdx.x; i < n_rows * (DP / 8); i += kAtThreads) {
             const int r = i / (DP / 8), d = (i - r * (DP / 8)) * 8;
             if (d >= a.D) continue;
-            float m = ninf, l = 0.0f, f[kAtWarps], y[8];
+            float m = none, l = 0.0f, f[kAtWarps], y[8];
 #pragma unroll
             for (int w = 0; w < kAtWarps; w++) m = fmaxf(m, sums[w * R + r].x);
 #pragma unroll
@@ -846,12 +849,11 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
 #pragma unroll
             for (int w = 0; w < kAtWarps; w++) {
                 const float2 x = sums[w * R + r];
-                f[w] = x.x == ninf ? 0.0f : ex2(x.x - m);
-                // a sum that is NaN without a maximum stays NaN
-                l += x.x == ninf ? (x.y == x.y ? 0.0f : x.y) : f[w] * x.y;
+                f[w] = ex2(x.x - m);
+                l = fmaf(f[w], x.y, l);
                 const float* from = merge + (w * R + r) * DP + d;
 #pragma unroll
-                for (int k = 0; k < 8; k++) y[k] = x.x == ninf ? y[k] : fmaf(f[w], from[k], y[k]);
+                for (int k = 0; k < 8; k++) y[k] = fmaf(f[w], from[k], y[k]);
             }
             if (begins && ends) {
                 const uint32_t row = row0 + r, token = token_of(a, row);
@@ -861,7 +863,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
                 for (int k = 0; k < 8; k++) y[k] = l == 0.0f ? 0.0f : (l == l ? y[k] * inv : l);
                 store8_any(a.out, a.out_type, (s.row0 + token) * a.ldo + qh * a.D + d, a.D - d, a.ovec, y);
                 if (a.lse && d == 0)
-                    a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : (m == ninf ? l : m * 0.69314718f + logf(l));
+                    a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : m * 0.69314718f + logf(l);
             } else {
                 store8<float>(slot + (int64_t)r * DP + d, y);
                 if (d == 0) {
@@ -912,7 +914,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a)
     auto slot = [&](int i) { return a.partial + (int64_t)(i == 0 ? 2 * p0 + 1 : 2 * (p0 + i)) * SLOT; };
     __shared__ float wm[4];
     const float ninf = __int_as_float(0xff800000);
-    float m = ninf;
+    float m = __int_as_float(kNone);
     for (int i = threadIdx.x; i < n; i += 128) m = fmaxf(m, slot(i)[R * DP + r]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -928,10 +930,6 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a)
         const float* p = slot(i);
         const float pm = p[R * DP + r], pl = p[R * DP + R + r];
         const float4 v = *reinterpret_cast<const float4*>(p + r * DP + d);
-        if (pm == ninf) {
-            l += pl == pl ? 0.0f : pl;
-            continue;
-        }
         const float f = ex2(pm - m);
         l = fmaf(f, pl, l);
         y[0] = fmaf(f, v.x, y[0]); y[1] = fmaf(f, v.y, y[1]); y[2] = fmaf(f, v.z, y[2]); y[3] = fmaf(f, v.w, y[3]);
@@ -958,7 +956,7 @@ __global__ void __launch_bounds__(128) attention_join_kernel(const AttnArgs a)
         else static_cast<__nv_bfloat16*>(a.out)[at + k] = from_f32<__nv_bfloat16>(v);
     }
     if (a.lse && d == 0)
-        a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : (m == ninf ? l : m * 0.69314718f + logf(l));
+        a.lse[(s.row0 + token) * ((int64_t)a.heads * a.group) + qh] = l == 0.0f ? ninf : m * 0.69314718f + logf(l);
 }
 
 template <int DP, int NT, int NP, bool LIN>

@@ -1,5 +1,6 @@
 """A decoder's attention at its edges: many queries on one head of the cache,
-lengths far past the page table, one place far ahead of a long rest."""
+lengths far past the page table, some places far ahead of a long rest,
+scores past fp32's range."""
 import math
 
 import pytest
@@ -98,3 +99,30 @@ def test_a_few_places_far_ahead_of_the_others(n, gap, spread, d, group, kk, vk, 
     close(out.unflatten(1, (group, d)), want.expand(seqs, group, d), bound.expand(seqs, group, d), FL)
     wl = mx + torch.log(e.sum())
     assert (lse.double() - wl).abs().max() <= (pr * eta).sum() * 1.01 + sums + 8 * U * (wl.abs() + mx.abs())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_past_the_least_fp32_number_weigh_nothing(d, dtype):
+    # such a place is the first that its warp of a block sees, or the only one, or all that a whole warp sees
+    group, page, n = 2, 16, 300
+    c = make_cache(19, 1, page, d, 2, 2, 3)
+    x = torch.zeros((n, d), device="cuda")
+    x[:] = -1.0
+    away = torch.zeros(n, dtype=torch.bool, device="cuda")
+    away[torch.tensor([0, 16, 17, 32, 64, 100, 128], device="cuda")] = True
+    away[150:256] = True
+    near = rand((n, d), 4).abs() * -1.0
+    k = torch.where(away[:, None], x, near)
+    esb.esb_cache_append(c, k, rand((n, d), 5), torch.arange(n, device="cuda"))
+    t = torch.arange(19, dtype=torch.int32, device="cuda")[None]
+    q = rand((1, group * d), 8, dtype).abs() + 0.25
+    for big in (3e38, float("inf")):
+        c.k_scales.view(-1)[:n][away] = big
+        for length in (17, 18, 33, 65, 129, 300):
+            lens = i32([length])
+            out, lse = esb.esb_cache_attention(q, c, lens, t, want_lse=True)
+            # the same without these places: their keys far below the others
+            near_c = c._replace(k_scales=c.k_scales.clone())
+            near_c.k_scales.view(-1)[:n][away] = 1e3
+            check_attention(q, near_c, lens, t, out, lse)
