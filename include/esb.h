@@ -900,7 +900,7 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
  * value is off by no more than 2^-11 (2^-22) of itself or 2^-39 of the head's
  * largest, a weight by no more than 2^-11 (2^-22) of itself or 2^-32 (2^-43) of
  * the query's largest.  That is where v's scales are 0 or lie between 2^-80 and
- * 2^80; the sum of the probabilities has no such step.
+ * 2^80, and k's are below 2^96; the sum of the probabilities has no such step.
  *   workspace  [device] >= esb_cache_attention_workspace_bytes bytes, 16-byte
  *              aligned; nothing is kept in it between calls
  * Errors: INVALID_ARG, UNSUPPORTED (formats, sizes, q_heads not a multiple of
@@ -917,7 +917,7 @@ typedef struct esb_attention {
     const esb_rotation* rotation;   /* [host] or NULL */
     int32_t seqs, max_pages, q_heads, window;
     int32_t q_type, out_type;
-    float scale;
+    float scale;               /* finite; times a head's largest query value it is below 2^126 */
 } esb_attention;
 size_t esb_cache_attention_workspace_bytes(int64_t tokens, int32_t seqs, int32_t q_heads, int32_t heads, int32_t head_dim,
                                            int32_t q_type);

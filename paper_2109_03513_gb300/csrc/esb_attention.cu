@@ -67,7 +67,8 @@ cudaError_t launch_attention(int64_t tokens, const esb_kv_cache& c, const esb_at
         if (a.group == 1 << i) a.group_shift = i;
     a.window = n.window; a.q_type = n.q_type; a.out_type = n.out_type;
     a.qvec = rows16(n.q, n.ldq, n.q_type); a.ovec = rows16(n.out, n.ldo, n.out_type);
-    a.scale2 = (float)((double)n.scale * 1.4426950408889634) * (lin ? (float)(1 << (16 - c.k_fmt.k)) : 1.0f);
+    a.scale2 = (float)std::frexp((double)n.scale * 1.4426950408889634, &a.scale_up);
+    a.scale_up += lin ? 16 - c.k_fmt.k : 0;
     a.rot = make_rot(n.rotation, c.head_dim);
     const int p = planes(n.q_type);
     if (a.D <= 64) return attention_run_64(a, eights_of(tokens, n.seqs, a.group, attention_most_64(p)), p, lin, workspace, st);

@@ -62,7 +62,8 @@ struct AttnArgs {
     uint2 klut, vlut;                                   // high bytes of the fp16 numbers of codes 0..7; LIN: x = what turns a code into its place
     int seqs, max_pages, heads, group, group_shift, D, chunks, page_size, window;
     int q_type, out_type, qvec, ovec;
-    float scale2, vunit;                                // scale log2(e) and K's unit; V's unit, and the weights'
+    float scale2, vunit;                                // scale log2(e) and K's unit, below 1 and times 2^scale_up; V's unit, and the weights'
+    int scale_up;
     RotArgs rot;
     float* partial;                                     // slots of R x (DP + 2) floats
     int4* head;                                         // of each part: (the last part of the tile that begins in it and goes on) + 1, sequence, head, tile
@@ -521,7 +522,9 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
             // 2^e takes the largest to 2^14 .. 2^15; the ends of fp32 stay in range
             const int e = big > 0.0f && big < __int_as_float(0x7f800000) ? 14 - max(-112, min(126, ((int)(__float_as_uint(big) >> 23) - 127))) : 0;
             const float up = __uint_as_float((uint32_t)(e / 2 + 127) << 23), up2 = __uint_as_float((uint32_t)(e - e / 2 + 127) << 23);
-            if (word == 0) qscale[r] = a.scale2 * __uint_as_float((uint32_t)(127 - e / 2) << 23) * __uint_as_float((uint32_t)(127 - (e - e / 2)) << 23);
+            // what takes a product back to its score: finite, so that a product of 0 is one of 0
+            const int back = max(-252, min(127, a.scale_up - e));
+            if (word == 0) qscale[r] = a.scale2 * __uint_as_float((uint32_t)(127 + back / 2) << 23) * __uint_as_float((uint32_t)(127 + back - back / 2) << 23);
 #pragma unroll
             for (int x = 0; x < 8; x++) v[x] = v[x] * up * up2;
             // the lane and step that take this word: quads' words as K's are read

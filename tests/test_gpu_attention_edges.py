@@ -1,6 +1,6 @@
 """A decoder's attention at its edges: many queries on one head of the cache,
 lengths far past the page table, some places far ahead of a long rest,
-scores past fp32's range."""
+scores past fp32's range, scales of any size."""
 import math
 
 import pytest
@@ -126,3 +126,21 @@ def test_scores_past_the_least_fp32_number_weigh_nothing(d, dtype):
             near_c = c._replace(k_scales=c.k_scales.clone())
             near_c.k_scales.view(-1)[:n][away] = 1e3
             check_attention(q, near_c, lens, t, out, lse)
+
+
+@pytest.mark.parametrize("kk", [0, 2])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scale_of_any_finite_size(kk, dtype):
+    # the scale times its unit is past fp32's range, the scores are not (nor is a query's product with codes, up to 2^28,
+    # times a key's scale: those lie below 2^96)
+    c = make_cache(5, 1, 16, 64, kk, 2, 3)
+    t, lens = torch.arange(5, dtype=torch.int32, device="cuda")[None], i32([70])
+    q = rand((1, 128), 8, dtype)
+    for scale, keys in ((1e37, 2.0 ** -123), (2e36, 2.0 ** -121), (1e-28, 2.0 ** 93), (-1e34, 2.0 ** -113)):
+        c2 = c._replace(k_scales=c.k_scales * keys)
+        out, lse = esb.esb_cache_attention(q, c2, lens, t, scale=scale, out=torch.empty_like(q, dtype=FL), want_lse=True)
+        check_attention(q, c2, lens, t, out, lse, scale=float(torch.tensor(scale)))
+    # no query, no score, whatever the scale
+    zero = torch.zeros_like(q)
+    out, lse = esb.esb_cache_attention(zero, c, lens, t, scale=3e38, want_lse=True)
+    check_attention(zero, c, lens, t, out, lse, scale=1.0)
