@@ -1037,10 +1037,16 @@ def _turn(rot: Optional[Rotation], positions, tokens: int) -> tuple[esb_rotation
     return rot.c(), _vector(positions, "positions", tokens, torch.int64)
 
 
-def _on_current(t: torch.Tensor):
-    """A launch goes to the current device: memory of another would be read across."""
-    if _current_device is not None and torch.cuda.is_initialized() and t.get_device() != _current_device():
-        raise ValueError("tensors must be on the current device")
+def _on_current(rot: Optional[Rotation], positions: Optional[torch.Tensor], *tensors: Optional[torch.Tensor]):
+    """A launch goes to the current device: memory of another would be read across.  Positions count with a rotation."""
+    if _current_device is None or not torch.cuda.is_initialized():
+        return
+    here = _current_device()
+    if rot is not None and (rot.table.get_device() != here or (positions is not None and positions.get_device() != here)):
+        raise ValueError("a rotation's tensors must be on the current device")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("tensors must be on the current device")
 
 
 def _head_count(t: torch.Tensor, name: str, head_dim: int) -> int:
@@ -1113,8 +1119,8 @@ def esb_headnorm(q: Optional[torch.Tensor], k: Optional[torch.Tensor], head_dim:
             kr = empty((tokens, cols // head_dim), dtype=f32, device=k.device)
             rp = kr.data_ptr()
         kp = esb_heads(k.data_ptr(), ld, ky.data_ptr(), ldy, wp, rp, cols // head_dim)
+    _on_current(rotation, positions, q, k, q_weight, k_weight, qy, ky)
     rot, pos = _turn(rotation, positions, tokens)
-    _on_current(x0)
     a = esb_head_norm((qp or esb_heads(), kp or esb_heads()), pos, rot, head_dim, xt, wt or 0, eps)
     _check(lib().esb_headnorm(tokens, ctypes.byref(a), _stream(stream)), "esb_headnorm")
     return HeadNorm(None if q is None else qy, None if k is None else ky, qr, kr)
@@ -1186,8 +1192,8 @@ def esb_headnorm_backward(gq: Optional[torch.Tensor], gk: Optional[torch.Tensor]
             dkw = sums[1]
             dp = sums.data_ptr() + 4 * head_dim
         kp = esb_heads_grad(gk.data_ptr(), ldg, k.data_ptr(), ld, k_rstd.data_ptr(), wp, dk.data_ptr(), ldd, dp, heads)
+    _on_current(rotation, positions, gq, gk, q, k, q_weight, k_weight, q_rstd, k_rstd, dq, dk, workspace)
     rot, pos = _turn(rotation, positions, tokens)
-    _on_current(x0)
     a = esb_head_norm_grad((qp or esb_heads_grad(), kp or esb_heads_grad()), pos, rot, head_dim, xt, wt or 0)
     wp, nb = None, 0
     if sums is not None:
@@ -1274,7 +1280,7 @@ def esb_cache_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: to
         qt, vp = t, vq.data_ptr()
     if rotation is not None:
         r, pos = _turn(rotation, positions, tokens)
-    _on_current(k)
+    _on_current(rotation, positions, k, v, slots, kq, vq, *cache[:4])
     a = esb_append(k.data_ptr(), v.data_ptr(), ldk, ldv, _vector(slots, "slots", tokens, torch.int64), pos,
                    None if r is None else ctypes.addressof(r), kp, vp, ldkq, ldvq, xt, qt, rule, rounding)
     _check(lib().esb_cache_append(tokens, ctypes.byref(c), ctypes.byref(a), _stream(stream)), "esb_cache_append")
@@ -1316,7 +1322,7 @@ def esb_cache_attention(q: torch.Tensor, cache: KvCache, lens: torch.Tensor, pag
             raise ValueError("out must have the shape of q")
     lse = empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
     r = None if rotation is None else rotation.c()
-    _on_current(q)
+    _on_current(rotation, None, q, out, lens, pages, starts, workspace, *cache[:4])
     a = esb_attention(q.data_ptr(), ldq, out.data_ptr(), ldo, None if lse is None else lse.data_ptr(), sp, lp, pages.data_ptr(),
                       pages.stride(0) if seqs > 1 else held[1], None if r is None else ctypes.addressof(r), seqs, held[1], heads,
                       window, qt, ot, c.head_dim ** -0.5 if scale is None else scale)
