@@ -38,45 +38,89 @@ struct AppendArgs {
     AppendSide side[2];                 // keys, values
     const int64_t *slots, *positions;
     int64_t tokens, places, page_ld, page_lds;
-    int heads, page_size, page_shift, D, words, q_type, rule, tvec;
+    int heads, page_size, page_shift, D, words, q_type, eights, tvec;
     RotArgs rot;
     HeadWork work;
 };
 
-// The scale of a head's 16 values in each of L lanes (the rest of them 0).
-template <int L>
-__device__ __forceinline__ float scale_of(const AppendArgs& a, const AppendSide& s, const float (&u)[8], const float (&v)[8], int left_u, int left_v)
+// The spread's scale of a head whose 16 values a lane lie in a row (ROWS), or as
+// the rotation pairs them.  Sums go in the order of the group projection's, so
+// that the scale is the same number: over 16 values of a row and then over lanes,
+// or, for sizes whose groups a warp takes (`eights`), over eight of each lane.
+// 8192 tokens x 8 heads of 128 in bf16, rotated: 27.8 us (26 with the sums in the
+// lanes' own order, whose scales differ in their last places).
+template <int L, bool ROWS>
+__device__ __forceinline__ float spread_scale(const AppendArgs& a, float astar, int half, const float (&u)[8], const float (&v)[8])
 {
-    if (a.rule == ESB_SCALE_ABSMAX) {
-        uint32_t mx = max(largest_of8(u, 1), largest_of8(v, 1));
+    const int part = threadIdx.x % L, left = a.D - 16 * part, turned = half >> 3;
+    // which lane holds the eights that this one adds up, and in which of its two
+    int lane[2];
+    bool second[2];
 #pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        return absmax_scale(mx, s.f);
+    for (int h = 0; h < 2; h++) {
+        const int e = 2 * part + h;
+        lane[h] = e < turned ? e : (e < 2 * turned ? e - turned : part);
+        second[h] = e < 2 * turned ? e >= turned : h;
     }
-    auto total = [&](float x) {
-#pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-        return x;
+    auto value = [&](int h, int i) {
+        if constexpr (ROWS) {
+            return h ? v[i] : u[i];
+        } else {
+            const float x = __shfl_sync(0xffffffffu, u[i], lane[h], L), y = __shfl_sync(0xffffffffu, v[i], lane[h], L);
+            return second[h] ? y : x;
+        }
     };
-    float s1 = 0.0f, s2 = 0.0f;
+    auto total = [&](float first, float last) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) s1 += u[i] + v[i];
-    const float mean = total(s1) / (float)a.D;
+        for (int o = L / 2; o > 0; o >>= 1) last += __shfl_xor_sync(0xffffffffu, last, o);
+        if (!a.eights) return last;
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) first += __shfl_xor_sync(0xffffffffu, first, o);
+        return first + last;
+    };
+    const float n = (float)a.D;
+    float first = 0.0f, last;
+#pragma unroll
+    for (int i = 0; i < 8; i++) first += value(0, i);
+    last = a.eights ? 0.0f : first;
+#pragma unroll
+    for (int i = 0; i < 8; i++) last += value(1, i);
+    const float mean = total(first, last) / n;
+    first = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        const float x = i < left_u ? u[i] - mean : 0.0f, y = i < left_v ? v[i] - mean : 0.0f;
-        s2 = fmaf(x, x, fmaf(y, y, s2));
+        const float d = value(0, i) - mean;
+        if (i < left) first = fmaf(d, d, first);
     }
-    return __fmul_rn(s.astar, __fadd_rn(__fsqrt_rn(total(s2) / (float)a.D), 1e-7f));
+    last = a.eights ? 0.0f : first;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float d = value(1, i) - mean;
+        if (8 + i < left) last = fmaf(d, d, last);
+    }
+    return __fmul_rn(astar, __fadd_rn(__fsqrt_rn(total(first, last) / n), 1e-7f));
+}
+
+// The scale of a head's 16 values in each of L lanes (those past its end 0), of
+// its spread or its largest magnitude.
+template <int L, bool SPREAD, bool ROWS>
+__device__ __forceinline__ float scale_of(const AppendArgs& a, const AppendSide& s, int half, const float (&u)[8], const float (&v)[8])
+{
+    if constexpr (SPREAD) return spread_scale<L, ROWS>(a, s.astar, half, u, v);
+    uint32_t mx = max(largest_of8(u, 1), largest_of8(v, 1));
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    return absmax_scale(mx, s.f);
 }
 
 // One token's head: its scale, then codes and values of the lane's two vectors
-// of 8 from d0 and d1 on (there: the lane has them).
-template <int L>
+// of 8 from d0 and d1 on (there: the lane has them; ROWS: they lie in a row,
+// else as a rotation by `half` pairs them).
+template <int L, bool SPREAD, bool ROWS>
 __device__ __forceinline__ void append_head(const AppendArgs& a, const AppendSide& s, bool on, int64_t slot, int64_t token, int head, int j0,
-                                            bool there, int d0, int d1, const float (&u)[8], const float (&v)[8])
+                                            bool there, int half, int d0, int d1, const float (&u)[8], const float (&v)[8])
 {
-    const float alpha = scale_of<L>(a, s, u, v, there ? 8 : 0, there ? 8 : 0);
+    const float alpha = scale_of<L, SPREAD, ROWS>(a, s, half, u, v);
     if (!on) return;
     const int64_t page = a.page_shift >= 0 ? slot >> a.page_shift : slot / a.page_size;
     const int place = (int)(slot - page * a.page_size);
@@ -93,13 +137,8 @@ __device__ __forceinline__ void append_head(const AppendArgs& a, const AppendSid
     const GroupScale g = make_scale(alpha, s.f);
     uint32_t w0[1], w1[1];
     float q0[8], q1[8];
-    if (a.rule == ESB_SCALE_ABSMAX) {                   // no quotient is past the largest element
-        quantise8<4, false>(u, g, s.f, w0, q0);
-        quantise8<4, false>(v, g, s.f, w1, q1);
-    } else {
-        quantise8<4, true>(u, g, s.f, w0, q0);
-        quantise8<4, true>(v, g, s.f, w1, q1);
-    }
+    quantise8<4, SPREAD>(u, g, s.f, w0, q0);            // absmax: no quotient is past the largest element
+    quantise8<4, SPREAD>(v, g, s.f, w1, q1);
     if (d1 == d0 + 8) {
         *reinterpret_cast<uint2*>(codes + d0 / 8) = make_uint2(w0[0], w1[0]);
     } else {
@@ -121,7 +160,7 @@ __device__ __forceinline__ void append_head(const AppendArgs& a, const AppendSid
 // (4,2) with the values (80 MB): 27.7 us, bound by instructions, 32 a value: the
 // exact rotation takes 8 of them, quotient, rounding, code and element some 20.
 // (41 us with rows in no order and a pair's other half read again.)
-template <int TYPE, int L, int MODE>
+template <int TYPE, int L, int MODE, bool SPREAD>
 __global__ void __launch_bounds__(kApThreads, kApBlocks) append_pairs_kernel(const AppendArgs a)
 {
     using T = Elem<TYPE>;
@@ -193,7 +232,7 @@ __global__ void __launch_bounds__(kApThreads, kApBlocks) append_pairs_kernel(con
                         for (int i = 0; i < 8; i++) { u[i] = f[i]; v[i] = g[i]; }
                     }
                 }
-                append_head<L>(a, s, at.on && slot >= 0 && slot < a.places, slot, at.token, at.head, j0, p.count > 0, d0, d1, u, v);
+                append_head<L, SPREAD, M == kPairRows>(a, s, at.on && slot >= 0 && slot < a.places, slot, at.token, at.head, j0, p.count > 0, p.half, d0, d1, u, v);
             }
         };
         RotArgs none = {};
@@ -202,8 +241,10 @@ __global__ void __launch_bounds__(kApThreads, kApBlocks) append_pairs_kernel(con
     }
 }
 // Any heads: a lane holds 16 consecutive values, and reads a pair's other half again.
-template <int TYPE, int L>
-__global__ void __launch_bounds__(kApThreads) append_kernel(const AppendArgs a)
+// Three blocks on an SM: left to itself the spread's kernel takes 117 registers, and
+// 8192 x 8 heads of 128 that start anywhere 54 us, with three 43.
+template <int TYPE, int L, bool SPREAD>
+__global__ void __launch_bounds__(kApThreads, 3) append_kernel(const AppendArgs a)
 {
     using T = Elem<TYPE>;
     griddep_wait();
@@ -226,7 +267,7 @@ __global__ void __launch_bounds__(kApThreads) append_kernel(const AppendArgs a)
             if (on && !value && a.rot.dim && d0 + 8 * i < a.D) rotated8<T>(x, n, d0 + 8 * i, s.xvec, a.rot, pos, v[i]);
             else load8_to(x + d0 + 8 * i, n - d0 - 8 * i, s.xvec, v[i]);
         }
-        const float alpha = scale_of<L>(a, s, v[0], v[1], a.D - d0, a.D - d0 - 8);
+        const float alpha = scale_of<L, SPREAD, true>(a, s, 0, v[0], v[1]);
         if (!on) continue;
         const int64_t page = slot / a.page_size;
         const int place = (int)(slot - page * a.page_size);
@@ -253,18 +294,18 @@ __global__ void __launch_bounds__(kApThreads) append_kernel(const AppendArgs a)
 }
 
 using ApKernel = void (*)(const AppendArgs);
-template <int TYPE, int L> ApKernel append_of(int mode)
+template <int TYPE, int L, bool SPREAD> ApKernel append_of(int mode)
 {
     switch (mode) {
-    case kPairHalves: return append_pairs_kernel<TYPE, L, kPairHalves>;
-    case kPairRows: return append_pairs_kernel<TYPE, L, kPairRows>;
-    case kPairMixed: return append_pairs_kernel<TYPE, L, kPairMixed>;
-    default: return append_kernel<TYPE, L>;
+    case kPairHalves: return append_pairs_kernel<TYPE, L, kPairHalves, SPREAD>;
+    case kPairRows: return append_pairs_kernel<TYPE, L, kPairRows, SPREAD>;
+    case kPairMixed: return append_pairs_kernel<TYPE, L, kPairMixed, SPREAD>;
+    default: return append_kernel<TYPE, L, SPREAD>;
     }
 }
-template <int TYPE> ApKernel append_of(int L, int mode)
+template <int TYPE, bool SPREAD> ApKernel append_of(int L, int mode)
 {
-    return L == 4 ? append_of<TYPE, 4>(mode) : L == 8 ? append_of<TYPE, 8>(mode) : append_of<TYPE, 16>(mode);
+    return L == 4 ? append_of<TYPE, 4, SPREAD>(mode) : L == 8 ? append_of<TYPE, 8, SPREAD>(mode) : append_of<TYPE, 16, SPREAD>(mode);
 }
 
 }  // namespace
@@ -289,10 +330,14 @@ cudaError_t launch_cache_append(int64_t tokens, const esb_kv_cache& c, const esb
     a.page_shift = -1;
     for (int i = 4; i < 31; i++)
         if (c.page_size == 1 << i) a.page_shift = i;
-    a.q_type = n.q_type; a.rule = n.rule; a.rot = make_rot(n.rotation, c.head_dim);
+    const int padded = (c.head_dim + 31) / 32 * 32;
+    a.eights = (padded & (padded - 1)) != 0;
+    a.q_type = n.q_type; a.rot = make_rot(n.rotation, c.head_dim);
     a.tvec = table_vectors(a.rot);
     const int L = lanes_of(a.D);
-    static ApKernel (*const pick[3])(int, int) = {append_of<ESB_F32>, append_of<ESB_F16>, append_of<ESB_BF16>};
+    static ApKernel (*const pick[3][2])(int, int) = {{append_of<ESB_F32, false>, append_of<ESB_F32, true>},
+                                                     {append_of<ESB_F16, false>, append_of<ESB_F16, true>},
+                                                     {append_of<ESB_BF16, false>, append_of<ESB_BF16, true>}};
     const int mode = pair_mode(a.D, a.rot.dim, a.rot.inter, a.side[0].xvec && a.side[1].xvec);
     int64_t blocks;
     if (mode != kPairAny) {
@@ -303,7 +348,7 @@ cudaError_t launch_cache_append(int64_t tokens, const esb_kv_cache& c, const esb
         const int64_t per = kApThreads / L;
         blocks = std::min<int64_t>((tokens * 2 * c.heads + per - 1) / per, 8ll * device_sm_count());
     }
-    return launch_pdl(pick[n.x_type](L, mode), dim3((unsigned)blocks), dim3(kApThreads), 0, st, a);
+    return launch_pdl(pick[n.x_type][n.rule == ESB_SCALE_DDA](L, mode), dim3((unsigned)blocks), dim3(kApThreads), 0, st, a);
 }
 
 }  // namespace esb

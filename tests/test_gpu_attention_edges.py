@@ -1,13 +1,13 @@
 """A decoder's attention at its edges: many queries on one head of the cache,
 lengths far past the page table, some places far ahead of a long rest,
-scores past fp32's range, scales of any size."""
+scores past fp32's range, scales of any size; the scales of appended heads."""
 import math
 
 import pytest
 import torch
 
 from paper_2109_03513_gb300 import esb
-from test_gpu_attention import BF, FL, cached64, check_attention, i32, ints, make_cache, tables
+from test_gpu_attention import APPENDS, BF, FL, cached64, check_attention, i32, ints, make_cache, tables, turn64
 from test_gpu_lm import TYPES, U, close, rand
 
 pytestmark = pytest.mark.gpu
@@ -144,3 +144,26 @@ def test_scale_of_any_finite_size(kk, dtype):
     zero = torch.zeros_like(q)
     out, lse = esb.esb_cache_attention(zero, c, lens, t, scale=3e38, want_lse=True)
     check_attention(zero, c, lens, t, out, lse, scale=1.0)
+
+
+@pytest.mark.parametrize("n,heads,d,rot,inter,page", APPENDS + [
+    (40, 2, 32, 32, False, 16), (21, 3, 160, 160, False, 16), (9, 1, 224, 96, False, 16), (30, 2, 64, 32, False, 16), (5, 1, 192, 64, True, 16)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scales_of_spreads_are_the_projections(n, heads, d, rot, inter, page, dtype):
+    # with the spread's scale too, a head's row is the group projection's bit for bit, wherever its values lie in memory
+    pages = -(-n // page)
+    r = esb.rotation(rot, 3000, interleaved=inter) if rot else None
+    pos = ints(0, 3000, (n,), 1)
+    wide = rand((n, 2 * heads * d + 16), 2, dtype)
+    for at in (0, 1):
+        k, v = wide[:, at:at + heads * d], wide[:, heads * d + 8 * at:2 * heads * d + 8 * at]
+        c = esb.kv_cache(pages, heads, page, d, esb.Fmt(4, 2), esb.Fmt(4, 1))
+        esb.esb_cache_append(c, k, v, torch.arange(n, device="cuda"), rotation=r, positions=pos if r else None, rule=esb.ESB_SCALE_DDA)
+        for x, codes, scales, f in ((k, c.k_codes, c.k_scales, c.k_fmt), (v, c.v_codes, c.v_scales, c.v_fmt)):
+            h = x.double().unflatten(1, (heads, d))
+            if x is k:
+                h = turn64(h, r.table if r else None, pos, inter)
+            want, _ = esb.esb_project_groups(h.float().flatten(0, 1), f, 0, rule=esb.ESB_SCALE_DDA)
+            i = torch.arange(n, device="cuda")
+            assert torch.equal(scales[i // page, :, i % page], want.scales.unflatten(0, (n, heads))[..., 0])
+            assert torch.equal(codes[i // page, :, i % page], want.codes.unflatten(0, (n, heads)))
