@@ -95,19 +95,21 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
 // plane's remainder is before that is.
 constexpr float kWeightUp = 128.0f, kLowUp = 2048.0f;
 
+__device__ __forceinline__ void mma16_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
 // The instruction's sums are truncated, not rounded: where queries and weights
 // have 22 bits, a place's products are summed on their own and added in fp32.
 __device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b0)[2], const uint32_t (&b1)[2])
 {
-    float x[4];
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0[1]), "r"(b1[1]), "f"(0.0f));
+    float x[4], y[4];
+    mma16_zero(x, a0, a1, a2, a3, b0[1], b1[1]);
+    mma16_zero(y, a0, a1, a2, a3, b0[0], b1[0]);
 #pragma unroll
-    for (int i = 0; i < 4; i++) x[i] *= 1.0f / kLowUp;
-    mma16(x, a0, a1, a2, a3, b0[0], b1[0]);
-#pragma unroll
-    for (int i = 0; i < 4; i++) d[i] += x[i];
+    for (int i = 0; i < 4; i++) d[i] = fmaf(x[i], 1.0f / kLowUp, d[i]) + y[i];
 }
 __device__ __forceinline__ void mma16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const uint32_t (&b0)[1], const uint32_t (&b1)[1])
 {
