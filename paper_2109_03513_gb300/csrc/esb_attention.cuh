@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kAtThreads, Shape<DP, NT, NP>::kSm) attention_
     int b = 0, head = 0, tile = 0;
     {
         // each thread sums a run of sequences
-        const int run = (a.seqs + kAtThreads - 1) / kAtThreads;
+        const int run = run_of(a.seqs, kAtThreads);
         int64_t w = 0;
 #pragma unroll 1
         for (int i = 0; i < run; i++) w += work_of<Sh>(a, i, run, kAtThreads, sh);

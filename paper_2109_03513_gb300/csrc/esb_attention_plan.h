@@ -41,4 +41,7 @@ ESB_HOST_DEVICE int end_place(const Tile& t, int first, int blocks, int block)
     return end < t.hi ? end : t.hi;
 }
 
+// Sequences (at least one) that each of a block's threads counts, in a run.
+ESB_HOST_DEVICE int run_of(int seqs, int threads) { return (seqs - 1) / threads + 1; }
+
 }  // namespace esb

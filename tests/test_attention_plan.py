@@ -17,6 +17,7 @@ extern "C" void tile(int64_t p0, int64_t p1, int seen, int window, int stage, in
     out[0] = t.lo; out[1] = t.hi; out[2] = t.blocks;
 }
 extern "C" int first(int lo, int hi, int first, int warp, int warps, int stage) { return esb::first_place({lo, hi, 0}, first, warp, warps, stage); }
+extern "C" int run(int seqs, int threads) { return esb::run_of(seqs, threads); }
 extern "C" int end(int lo, int hi, int first, int blocks, int block) { return esb::end_place({lo, hi, 0}, first, blocks, block); }
 """
 MOST = (1 << 31) - 1
@@ -65,3 +66,9 @@ def test_places_of_a_tile(shim, stage, held):
                         stages = -(-(end - place) // block) if end > place else 0
                         if stages:                                           # all of its stages begin in the table
                             assert 0 <= place and place + (stages - 1) * block < min(held, end)
+
+
+def test_runs_hold_every_sequence(shim):
+    for seqs in (1, 2, 127, 128, 129, 1 << 20, MOST - 128, MOST - 127, MOST - 126, MOST):
+        run = shim.run(seqs, 128)
+        assert 128 * run >= seqs > 128 * (run - 1)
