@@ -892,8 +892,9 @@ esb_status esb_cache_append(int64_t tokens, const esb_kv_cache* cache, const esb
  *            past them, and on pages outside 0 .. pages - 1, are not seen
  *   lse      [device] tokens x q_heads: log sum exp(scale q.k), or NULL
  * A query that sees no place has out 0 and lse -inf.  A place whose score lies
- * below fp32's range (or is -inf) weighs nothing, as if it were not seen.  A NaN among what a query
- * sees makes its numbers NaN; what it does not see has no effect, whatever it is.
+ * below fp32's range (or is -inf) weighs nothing, as if it were not seen.  A score
+ * above it, or a NaN, among what a query sees makes its numbers NaN; what it does
+ * not see has no effect, whatever it is.
  * Products are of fp16 numbers, sums fp32: codes take part as they are; queries
  * and weights (probabilities times a value's scale) with 11 significant bits
  * where queries are bf16, else with 22, but no finer than a fixed step: a query's

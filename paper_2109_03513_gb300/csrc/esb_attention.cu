@@ -14,6 +14,12 @@ int eights_of(int64_t tokens, int64_t seqs, int group, int most)
     const int64_t rows = (tokens + seqs - 1) / seqs * group;
     return rows <= 8 || most == 1 ? 1 : (rows <= 16 || most == 2 ? 2 : 4);
 }
+// Planes of queries and weights, 11 bits each.  One for bf16 queries: it puts outputs
+// 4e-4 of their size off, a quarter of what rounding them to bf16 does (1.7e-3, root mean
+// squares over 4 x 131072 places and 24 x 10000), and bf16 outputs 1.1e-3 from those of
+// fp32 arithmetic: some differ in their last place.  Two planes leave 4e-5 of that,
+// but take 171 us for 4 x 131072 places (134 with one), 55 for a draft of four tokens
+// (45), 975 for a prompt's part (614): they are for queries of more bits.
 int planes(int q_type) { return q_type == ESB_BF16 ? 1 : 2; }
 
 // High bytes of the fp16 numbers of codes 0..7 of a 4-bit set.

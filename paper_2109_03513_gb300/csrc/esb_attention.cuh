@@ -26,12 +26,13 @@
 // tile; parts of tiles go to the workspace, and a second kernel joins them in
 // their order.
 //
-// 4 x 131072 places, 8 heads of 128, 4 queries each (570 MB): 137 us, 4.2 TB/s,
-// 62% of the copy rate.  More than half of the instructions go to the pipe of
-// integer and permute work, which does 64 lanes a clock and is some three quarters
-// busy.  A prompt's 512 tokens over 4096 places, four of them (129 GFLOP):
-// 630 us, 205 TFLOP/s; its tiles' sums leave two warps a scheduler, which wait for
-// fixed latencies.  One sequence of 2048 places: 12 us, two kernels' starts,
+// 4 x 131072 places, 8 heads of 128, 4 queries each (570 MB): 134 us, 4.25 TB/s,
+// 63% of the copy rate.  More than half of the instructions go to the pipe of
+// integer and permute work, which does 64 lanes a clock and is 65% busy (a launch by
+// itself, its starts among it); after it warps wait for fixed latencies and one
+// another.  A prompt's 512 tokens over 4096 places, four of them (129 GFLOP):
+// 614 us, 210 TFLOP/s; its tiles' sums leave two warps a scheduler, which wait for
+// fixed latencies.  One sequence of 2048 places: 11 us, two kernels' starts,
 // look-ups and loads one after the other.
 #pragma once
 
@@ -213,7 +214,9 @@ template <int DP, int NT, int NP> struct Shape {
     static constexpr int kStages = DP == 256 ? (NT == 1 ? 3 : 4) : NT == 1 ? 3 : 6;
     static constexpr bool kQueryRegs = NT * NP * kSteps <= 16;   // else queries are read from shared memory for every stage
     // Blocks on an SM.  Tiles of 16 rows: 49 us for 24 x 10000 places, 55 with three blocks, whose registers spill;
-    // heads of 64: 37 us for 48 windows of 1000, 39.5 with three; of 128: 137 us for 4 x 131072 places, 148 with four.
+    // heads of 64: 37 us for 48 windows of 1000, 39.5 with three; of 128: 137 us for 4 x 131072 places, 148 with four
+    // (measured then; 45, 35 and 134 us now).  One plane each but for the windows: two planes of heads of 128 spill 88 bytes
+    // at three blocks, and were not measured with two.
     static constexpr int kSm = NT > 1 || DP == 256 ? 2 : DP == 64 ? 4 : 3;
     static constexpr int kQueryBytes = NT * NP * kSteps * 32 * 8;
     static constexpr int kRing = kAtWarps * kStages * kParts * Stage<DP>::kBytes, kMerge = kAtWarps * R * DP * 4;

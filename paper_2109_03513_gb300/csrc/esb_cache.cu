@@ -157,9 +157,11 @@ __device__ __forceinline__ void append_head(const AppendArgs& a, const AppendSid
 // Heads of whole vectors: a lane holds 8 pairs of a key as the rotation pairs
 // them, or 16 of a value's numbers, the next head's ahead; a warp keeps a
 // token's cos and sin for several heads.  8192 tokens x 8 heads of 128 in bf16 to
-// (4,2) with the values (80 MB): 27.7 us, bound by instructions, 32 a value: the
-// exact rotation takes 8 of them, quotient, rounding, code and element some 20.
-// (41 us with rows in no order and a pair's other half read again.)
+// (4,2) with the values (80 MB): 27.2 us, bound by latency: four warps a scheduler,
+// which issues in 54% of the cycles, wait for fixed latencies (1.9 cycles an
+// instruction) and loads (1.2); no pipe is busier than 36%.  32 instructions a
+// value: the exact rotation takes 8 of them, quotient, rounding, code and element
+// some 20.  (41 us with rows in no order and a pair's other half read again.)
 template <int TYPE, int L, int MODE, bool SPREAD>
 __global__ void __launch_bounds__(kApThreads, kApBlocks) append_pairs_kernel(const AppendArgs a)
 {

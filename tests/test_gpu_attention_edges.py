@@ -128,6 +128,23 @@ def test_scores_past_the_least_fp32_number_weigh_nothing(d, dtype):
             check_attention(q, near_c, lens, t, out, lse)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scores_past_the_largest_fp32_number_are_nan(dtype):
+    group, page, d, n = 2, 16, 64, 300
+    c = make_cache(19, 1, page, d, 2, 2, 3)
+    k = torch.ones((n, d), device="cuda")
+    k[::2] = -1.0
+    esb.esb_cache_append(c, k, rand((n, d), 5), torch.arange(n, device="cuda"))
+    t = torch.arange(19, dtype=torch.int32, device="cuda")[None]
+    q = rand((1, group * d), 8, dtype).abs() + 0.25
+    for place, seen in ((1, True), (149, True), (299, True), (150, False)):
+        c2 = c._replace(k_scales=c.k_scales.clone())
+        c2.k_scales.view(-1)[place] = float("inf")
+        out, lse = esb.esb_cache_attention(q, c2, i32([n]), t, want_lse=True)
+        assert (torch.isnan(out).all() and torch.isnan(lse).all()) if seen else (torch.isfinite(out).all() and torch.isfinite(lse).all())
+    assert torch.isfinite(esb.esb_cache_attention(q, c2, i32([150]), t)[0]).all()    # and one that is not seen
+
+
 @pytest.mark.parametrize("kk", [0, 2])
 @pytest.mark.parametrize("dtype", TYPES)
 def test_scale_of_any_finite_size(kk, dtype):
